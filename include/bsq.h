@@ -553,6 +553,163 @@ bsq_status bsq_train_grad(const bsq_config *cfg, const bsq_train_hparams *hp, co
 bsq_status bsq_train_adam(const bsq_config *cfg, const bsq_train_hparams *hp, int32_t step, float *theta,
                           const float *grad, float *m, float *v, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a shared projection (Section
+ * III-F's LoRA term with a choice of adapter per token), and their gradients.
+ * bsq_gemv and bsq_gemm add one adapter of rank 1..16 for all tokens; here
+ * every token of a batch names its own, or none:
+ *   t[m] = A_a x[m],   y[m] = y0[m] + s_a B_a t[m],   a = ids[m],
+ * for a group of projections that read the same x (y0: their outputs, e.g. of
+ * bsq_gemm without an adapter). With dy the gradient of y,
+ *   u[m] = s_a B_a^T dy[m],  dx[m] = dx0[m] + sum over the group of A_a^T u[m],
+ *   dA_a = sum_m u[m] x[m]^T,  dB_a = s_a sum_m dy[m] t[m]^T
+ * over the tokens with a = ids[m]. Sums are fp32 in a fixed order; t and u
+ * enter their second product as bf16 parts that add up to them, two for bf16
+ * results (2^-16 of a value is lost), three for fp32 ones (2^-24).
+ * ------------------------------------------------------------------------ */
+#define BSQ_MAX_ADAPTERS 1024
+#define BSQ_MAX_ADAPTER_RANK 128
+
+/* The adapters of one projection, device pointers: A bf16 [n][rank][d_in], B
+ * bf16 [n][d_out][rank] with one rank for the group (rank 1..128); scale fp32
+ * [n] or NULL for ones; ranks int32 [n], each adapter's own rank (clamped to
+ * 0..rank), or NULL where all have the full one. What A, B and t hold past
+ * an adapter's rank is not used (it may be NaN); dA and dB are 0 there. */
+typedef struct {
+    const uint16_t *A;
+    const uint16_t *B;
+    const float *scale;
+    const int32_t *ranks;
+    int64_t d_out;
+} bsq_adapter_pool;
+
+/* A batch's tokens sorted by adapter: made once per batch by
+ * bsq_adapters_plan, read by every layer's calls. `ids` is the array that it
+ * was made from (device int32 [M]), `buf` the device buffer (16-byte aligned,
+ * bsq_adapters_plan_bytes) that it wrote. */
+typedef struct {
+    const int32_t *ids;
+    void *buf;
+    int64_t M;
+    int32_t n;
+} bsq_adapter_plan;
+
+/* 1 <= M <= 2^24 tokens, 1 <= n <= BSQ_MAX_ADAPTERS (host only) */
+bsq_status bsq_adapters_plan_bytes(int64_t M, int32_t n, size_t *bytes);
+
+/* Write the plan of ids[0 .. M) into plan->buf. A negative id means no
+ * adapter; one of n or more too, and ORs BSQ_DEVERR_BAD_SET into *err (device
+ * int32 or NULL). */
+bsq_status bsq_adapters_plan(const bsq_adapter_plan *plan, size_t buf_bytes, int32_t *err, void *stream);
+
+/* Device workspace of bsq_adapters_apply (back = 0) or bsq_adapters_grad
+ * (back = 1), for a group of n_proj projections (host only). */
+bsq_status bsq_adapters_workspace_bytes(int32_t back, int64_t M, int32_t n, int32_t n_proj, int32_t rank,
+                                        int64_t d_in, const int64_t *d_out, size_t *bytes);
+
+/* y = y0 + s B (A x) of every token, for n_proj (1..8) projections.
+ *   pools  host array [n_proj]
+ *   X      device bf16 [M][ldx], ldx >= d_in
+ *   y0, y  host arrays [n_proj] of device [M][ldy0], [M][ldy] of y_dtype (bf16
+ *          or fp32), ld >= d_out; y0 (or an entry) NULL: zero; an entry of y may
+ *          be that of y0 with the same ld (in place: rows without an adapter
+ *          are then left as they are)
+ *   t      host array [n_proj] of device fp32 [M][rank] outputs (0 for a token
+ *          without an adapter), or NULL
+ *   ws     device workspace, 256-byte aligned, any contents
+ * Any d_in, d_out and ld from 1 on; rows that are 16-byte aligned multiples of
+ * 8 are read fastest. */
+bsq_status bsq_adapters_apply(const bsq_adapter_plan *plan, int32_t n_proj, const bsq_adapter_pool *pools,
+                              int32_t rank, int64_t d_in, const void *X, int64_t ldx, const void *const *y0,
+                              const int64_t *ldy0, void *const *y, const int64_t *ldy, int32_t y_dtype,
+                              float *const *t, void *ws, size_t ws_bytes, void *stream);
+
+/* The gradients.
+ *   t       host array [n_proj]: as bsq_adapters_apply wrote them
+ *   dy      host array [n_proj] of device bf16 [M][lddy]
+ *   dx0     device bf16 [M][lddx0] or NULL for zero
+ *   dx      device [M][lddx] of dx_dtype, or NULL (not wanted); may be dx0 (in
+ *           place, bf16 and the same ld)
+ *   dA, dB  host arrays [n_proj] of device fp32 [n][rank][d_in],
+ *           [n][d_out][rank], written whole (0 for an adapter without tokens);
+ *           accumulate = 1: added to */
+bsq_status bsq_adapters_grad(const bsq_adapter_plan *plan, int32_t n_proj, const bsq_adapter_pool *pools,
+                             int32_t rank, int64_t d_in, const void *X, int64_t ldx, float *const *t,
+                             const void *const *dy, const int64_t *lddy, const void *dx0, int64_t lddx0, void *dx,
+                             int64_t lddx, int32_t dx_dtype, float *const *dA, float *const *dB, int32_t accumulate,
+                             void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Softmax cross entropy of a large vocabulary from hidden states h_t and head
+ * weights v, in pieces of the vocabulary: the [T][N] logits are never kept.
+ *   z_tv = h_t . v,  lse_t = log sum_v exp(z_tv),  loss_t = lse_t - z_t,target
+ *   d_tv = g_t (exp(z_tv - lse_t) - [v = target_t]),  dH = d V,  dV = d^T H
+ * (perplexity of a compressed model; the loss of adapter training). Logits and
+ * sums are fp32; d enters its products in bf16 (2^-9 of each value, as every
+ * bf16 gradient). A token with a negative target has no loss: its loss, lse and
+ * row of dH are 0, and its hidden state is not used (it may be NaN). A target
+ * of N or more counts as negative and ORs BSQ_DEVERR_BAD_SET into *err.
+ * ------------------------------------------------------------------------ */
+
+/* Device workspace of bsq_xent_loss (grad = 0), bsq_xent_grad (1); host only. */
+bsq_status bsq_xent_workspace_bytes(int32_t grad, int64_t T, int64_t N, int64_t D, size_t *bytes);
+
+/*   H       device bf16 [T][ldh], ldh >= D
+ *   V       device bf16 [N][ldv], ldv >= D; D and ldv multiples of 8, 16-byte aligned
+ *   target  device int64 [T]
+ *   loss, lse  device fp32 [T]
+ *   err     device int32 or NULL
+ *   ws      device workspace, 256-byte aligned, any contents
+ * 0 <= T <= 2^20, 1 <= N < 2^31, 1 <= D <= 2^16. */
+bsq_status bsq_xent_loss(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                         const int64_t *target, float *loss, float *lse, int32_t *err, void *ws, size_t ws_bytes,
+                         void *stream);
+
+/*   lse     device fp32 [T], as bsq_xent_loss wrote it
+ *   g       device fp32 [T], the gradient of each token's loss (e.g. 1 over the
+ *           number of tokens for their mean); not read where there is no loss
+ *   dH      device bf16 [T][lddh]
+ *   dV      device [N][lddv] of dv_dtype (bf16 or fp32), or NULL (a frozen head);
+ *           accumulate = 1: added to */
+bsq_status bsq_xent_grad(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                         const int64_t *target, const float *lse, const float *g, void *dH, int64_t lddh, void *dV,
+                         int64_t lddv, int32_t dv_dtype, int32_t accumulate, int32_t *err, void *ws,
+                         size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * The global norm of many gradient tensors, and their clipping:
+ *   norm = sqrt(sum g^2),  coef = min(1, max_norm / (norm + 1e-6)),  out = coef g
+ * with the squares summed in fp64 in a fixed order.
+ * ------------------------------------------------------------------------ */
+
+/* The tensors of a training program, prepared once: bsq_clip_prepare fills
+ * `chunks`; `table` is a device buffer (256-byte aligned) of
+ * bsq_clip_table_bytes. */
+typedef struct {
+    void *table;
+    int64_t count;
+    int64_t chunks;
+} bsq_clip_plan;
+
+/* sizes: host array [count] of elements (0 allowed); host only */
+bsq_status bsq_clip_table_bytes(int64_t count, const int64_t *sizes, size_t *bytes);
+
+/* Write the table of `count` tensors (kernels on `stream`).
+ *   src     host array of device pointers; dst: likewise, or NULL (in place)
+ *   dtypes  host array of bsq_dtype (of a tensor and its output)
+ *   plan    host struct: table and count are read, chunks is written */
+bsq_status bsq_clip_prepare(bsq_clip_plan *plan, size_t table_bytes, const void *const *src, void *const *dst,
+                            const int64_t *sizes, const int32_t *dtypes, void *stream);
+
+/* stats (device fp32 [2]): norm and coef. A norm that is not finite gives coef
+ * = 1 and ORs BSQ_DEVERR_NONFINITE into *err (device int32 or NULL). Calls that
+ * share a plan must not overlap. */
+bsq_status bsq_grad_norm(const bsq_clip_plan *plan, float max_norm, float *stats, int32_t *err, void *stream);
+
+/* bsq_grad_norm, then out = coef g for every tensor (in place nothing is
+ * written where coef is 1). */
+bsq_status bsq_grad_clip(const bsq_clip_plan *plan, float max_norm, float *stats, int32_t *err, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

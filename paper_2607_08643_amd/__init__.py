@@ -14,4 +14,7 @@ from ._binding import (  # noqa: F401
     bsq_gemm, bsq_gemv, bsq_gemv_noalloc, bsq_layer, bsq_layer_sizes, bsq_lora, bsq_sizes, bsq_version, bsq_workspace_bytes,
     TrainHyper, bsq_train_adam, bsq_train_grad, bsq_train_hparams, bsq_train_param_count, bsq_train_workspace_bytes,
     layer_empty, lib, status_str,
+    AdapterPlan, AdapterPool, GradPlan, bsq_adapter_plan, bsq_adapter_pool, bsq_adapters_apply, bsq_adapters_grad,
+    bsq_adapters_plan, bsq_adapters_plan_bytes, bsq_adapters_workspace_bytes, bsq_clip_plan, bsq_grad_clip, bsq_grad_norm,
+    bsq_xent_grad, bsq_xent_loss, bsq_xent_workspace_bytes,
 )

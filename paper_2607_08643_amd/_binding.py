@@ -22,6 +22,8 @@ MAX_STAGES = 4
 PITCH_ALIGN = 16
 MAX_LORA_RANK = 16
 MAX_GROUP = 8
+MAX_ADAPTERS = 1024
+MAX_ADAPTER_RANK = 128
 GEMV_NOALLOC_SCRATCH_BYTES = 8 << 20
 
 BSQ_OK, BSQ_ERR_ARG, BSQ_ERR_SHAPE, BSQ_ERR_DTYPE, BSQ_ERR_ALIGN = 0, 1, 2, 3, 4
@@ -78,7 +80,10 @@ EXPORTS = ("bsq_version", "bsq_status_str", "bsq_config_check", "bsq_layer_sizes
            "bsq_codec_bytes", "bsq_codec_prepare", "bsq_encode", "bsq_decode", "bsq_gemv", "bsq_gemv_prepare",
            "bsq_gemv_run", "bsq_gemm", "bsq_encode_with_set", "bsq_coupled_select",
            "bsq_debug_set_wait_limit", "bsq_decode_stage", "bsq_gemv_noalloc", "bsq_train_param_count",
-           "bsq_train_workspace_bytes", "bsq_train_grad", "bsq_train_adam")
+           "bsq_train_workspace_bytes", "bsq_train_grad", "bsq_train_adam", "bsq_adapters_plan_bytes",
+           "bsq_adapters_plan", "bsq_adapters_workspace_bytes", "bsq_adapters_apply", "bsq_adapters_grad",
+           "bsq_xent_workspace_bytes", "bsq_xent_loss", "bsq_xent_grad", "bsq_clip_table_bytes", "bsq_clip_prepare",
+           "bsq_grad_norm", "bsq_grad_clip")
 
 # struct layouts above follow this version of include/bsq.h
 ABI_VERSION = 8
@@ -119,6 +124,18 @@ def lib():
     L.bsq_train_workspace_bytes.argtypes = [P, I64, ct.POINTER(SZ)]
     L.bsq_train_grad.argtypes = [P, P, P, I32, I64, P, I64, P, P, P, P, P, SZ, P]
     L.bsq_train_adam.argtypes = [P, P, I32, P, P, P, P, P]
+    L.bsq_adapters_plan_bytes.argtypes = [I64, I32, ct.POINTER(SZ)]
+    L.bsq_adapters_plan.argtypes = [P, SZ, P, P]
+    L.bsq_adapters_workspace_bytes.argtypes = [I32, I64, I32, I32, I32, I64, P, ct.POINTER(SZ)]
+    L.bsq_adapters_apply.argtypes = [P, I32, P, I32, I64, P, I64, P, P, P, P, I32, P, P, SZ, P]
+    L.bsq_adapters_grad.argtypes = [P, I32, P, I32, I64, P, I64, P, P, P, P, I64, P, I64, I32, P, P, I32, P, SZ, P]
+    L.bsq_xent_workspace_bytes.argtypes = [I32, I64, I64, I64, ct.POINTER(SZ)]
+    L.bsq_xent_loss.argtypes = [P, I64, P, I64, I64, I64, I64, P, P, P, P, P, SZ, P]
+    L.bsq_xent_grad.argtypes = [P, I64, P, I64, I64, I64, I64, P, P, P, P, I64, P, I64, I32, I32, P, P, SZ, P]
+    L.bsq_clip_table_bytes.argtypes = [I64, P, ct.POINTER(SZ)]
+    L.bsq_clip_prepare.argtypes = [P, SZ, P, P, P, P, P]
+    L.bsq_grad_norm.argtypes = [P, ct.c_float, P, P, P]
+    L.bsq_grad_clip.argtypes = [P, ct.c_float, P, P, P]
     for f in EXPORTS[2:]:
         getattr(L, f).restype = I32
     if L.bsq_version() != ABI_VERSION:
@@ -650,3 +667,380 @@ def bsq_train_adam(cfg: Config, hp: TrainHyper, step: int, theta, grad, m, v, st
     c, h = cfg.c(), hp.c()
     _check(lib().bsq_train_adam(ct.byref(c), ct.byref(h), step, _ptr(theta), _ptr(grad), _ptr(m), _ptr(v),
                                 _stream(stream)), "bsq_train_adam")
+
+
+# ---------------------------------------------------------------- shared by the operators below
+def _device_of(tensors, what):
+    """The one GPU that all tensors (None skipped) lie on."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{what}: tensors must be on the GPU")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError(f"{what}: tensors on {dev} and {t.device}")
+    return dev
+
+
+def _need(t, dtype, shape, what):
+    """t has this dtype and shape and is contiguous."""
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: must be contiguous")
+    return t
+
+
+def _row_stride(t, what):
+    """Elements between the rows of a matrix whose rows are contiguous."""
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: rows must be contiguous")
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap")
+    return ld
+
+
+def _matrix(t, dtype, shape, what):
+    """A matrix of this dtype and shape with contiguous rows; its row stride."""
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    return _row_stride(t, what)
+
+
+class _Launch:
+    """The device and stream of a call: what it allocates belongs to that
+    stream (so that a buffer it frees is reused in that stream's order)."""
+
+    def __init__(self, dev, stream):
+        self.dev, self.stream = dev, stream
+
+    def __enter__(self):
+        self.ctx = None
+        if self.stream is not None:
+            self.ctx = torch.cuda.stream(self.stream)
+        elif self.dev.index is not None and self.dev.index != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(self.dev)
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return ct.c_void_p((self.stream or torch.cuda.current_stream()).cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+        return False
+
+
+# ---------------------------------------------------------------- adapters of many requests
+class bsq_adapter_pool(ct.Structure):
+    _fields_ = [("A", ct.c_void_p), ("B", ct.c_void_p), ("scale", ct.c_void_p), ("ranks", ct.c_void_p),
+                ("d_out", ct.c_int64)]
+
+
+class bsq_adapter_plan(ct.Structure):
+    _fields_ = [("ids", ct.c_void_p), ("buf", ct.c_void_p), ("M", ct.c_int64), ("n", ct.c_int32)]
+
+
+class AdapterPool:
+    """The adapters of one projection: A [n, rank, d_in] and B [n, d_out, rank]
+    (bf16), scale fp32 [n] (None: ones), ranks int32 [n] (None: all full)."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None,
+                 ranks: torch.Tensor | None = None):
+        if A.dim() != 3 or B.dim() != 3:
+            raise ValueError("A must be [n, rank, d_in] and B [n, d_out, rank]")
+        n, rank, d_in = A.shape
+        _need(A, torch.bfloat16, (n, rank, d_in), "A")
+        _need(B, torch.bfloat16, (n, B.shape[1], rank), "B")
+        if scale is not None:
+            _need(scale, torch.float32, (n,), "scale")
+        if ranks is not None:
+            _need(ranks, torch.int32, (n,), "ranks")
+        self.device = _device_of((A, B, scale, ranks), "AdapterPool")
+        self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
+        self.n, self.rank, self.d_in, self.d_out = n, rank, d_in, B.shape[1]
+
+    def c(self) -> bsq_adapter_pool:
+        return bsq_adapter_pool(self.A.data_ptr(), self.B.data_ptr(),
+                                None if self.scale is None else self.scale.data_ptr(),
+                                None if self.ranks is None else self.ranks.data_ptr(), self.d_out)
+
+
+class AdapterPlan:
+    """A batch's tokens sorted by adapter (bsq_adapters_plan), for every
+    layer's calls on that batch."""
+
+    def __init__(self, ids: torch.Tensor, n: int, buf: torch.Tensor):
+        self.ids, self.n, self.buf, self.M = ids, n, buf, ids.numel()
+
+    def c(self) -> bsq_adapter_plan:
+        return bsq_adapter_plan(self.ids.data_ptr(), self.buf.data_ptr(), self.M, self.n)
+
+
+def bsq_adapters_plan_bytes(M: int, n: int) -> int:
+    out = ct.c_size_t(0)
+    _check(lib().bsq_adapters_plan_bytes(M, n, ct.byref(out)), "bsq_adapters_plan_bytes")
+    return out.value
+
+
+def bsq_adapters_plan(ids: torch.Tensor, n: int, buf: torch.Tensor | None = None, err: torch.Tensor | None = None,
+                      stream=None) -> AdapterPlan:
+    """The plan of a batch whose token m has adapter ids[m] of n (int32 [M];
+    negative: none). ids must keep its values while the plan is used."""
+    dev = _device_of((ids, buf, err), "bsq_adapters_plan")
+    _need(ids, torch.int32, (ids.numel(),), "ids")
+    need = bsq_adapters_plan_bytes(ids.numel(), n)
+    with _Launch(dev, stream) as st:
+        if buf is None:
+            buf = torch.empty(need, dtype=torch.uint8, device=dev)
+        plan = AdapterPlan(ids, n, buf)
+        c = plan.c()
+        _check(lib().bsq_adapters_plan(ct.byref(c), buf.numel() * buf.element_size(), _ptr(err), st), "bsq_adapters_plan")
+    return plan
+
+
+def bsq_adapters_workspace_bytes(back: bool, M: int, n: int, rank: int, d_in: int, d_out) -> int:
+    out = ct.c_size_t(0)
+    dims = (ct.c_int64 * len(d_out))(*d_out)
+    _check(lib().bsq_adapters_workspace_bytes(int(back), M, n, len(d_out), rank, d_in, dims, ct.byref(out)),
+           "bsq_adapters_workspace_bytes")
+    return out.value
+
+
+def _adapter_group(plan, pools, X, what):
+    if not 1 <= len(pools) <= MAX_GROUP:
+        raise ValueError(f"{what}: 1..{MAX_GROUP} projections")
+    n, rank, d_in = pools[0].n, pools[0].rank, pools[0].d_in
+    if any((p.n, p.rank, p.d_in) != (n, rank, d_in) for p in pools):
+        raise ValueError(f"{what}: the pools of a group share n, rank and d_in")
+    if plan.n != n:
+        raise ValueError(f"{what}: the plan is for {plan.n} adapters, the pools hold {n}")
+    ldx = _matrix(X, torch.bfloat16, (plan.M, d_in), "X")
+    dims = [p.d_out for p in pools]
+    return rank, d_in, ldx, (bsq_adapter_pool * len(pools))(*[p.c() for p in pools]), dims
+
+
+def _pointers(tensors):
+    return (ct.c_void_p * len(tensors))(*[None if t is None else t.data_ptr() for t in tensors])
+
+
+def _strides(values):
+    return (ct.c_int64 * len(values))(*values)
+
+
+def bsq_adapters_apply(plan: AdapterPlan, pools, X: torch.Tensor, base, out=None, keep: bool = False,
+                       y_dtype=torch.bfloat16, ws: torch.Tensor | None = None, stream=None):
+    """y = base + s B (A x) of every token for each projection of a group
+    (bsq_adapters_apply). base: a list of [M, d_out] (bf16 or fp32, which y
+    takes too), or None for zero (y of y_dtype); out: where y goes, e.g. base
+    itself (in place). Returns (list of y, list of t or None): keep asks for t =
+    A x (fp32 [M, rank]), which the gradients take. One AdapterPool instead of a
+    list: single tensors instead of lists."""
+    what = "bsq_adapters_apply"
+    single = isinstance(pools, AdapterPool)
+    if single:
+        pools, base, out = [pools], None if base is None else [base], None if out is None else [out]
+    rank, d_in, ldx, arr, dims = _adapter_group(plan, pools, X, what)
+    M, np_ = plan.M, len(pools)
+    if base is not None:
+        if len(base) != np_:
+            raise ValueError(f"{what}: one base per projection")
+        y_dtype = base[0].dtype
+        ldb = [_matrix(b, y_dtype, (M, d), "base") for b, d in zip(base, dims)]
+    dev = _device_of([plan.buf, X, ws] + [p.A for p in pools] + list(base or []) + list(out or []), what)
+    code = _dtype_code(y_dtype)
+    need = bsq_adapters_workspace_bytes(False, M, plan.n, rank, d_in, dims)
+    with _Launch(dev, stream) as st:
+        if out is None:
+            out = [torch.empty((M, d), dtype=y_dtype, device=dev) for d in dims]
+        ldy = [_matrix(y, y_dtype, (M, d), "out") for y, d in zip(out, dims)]
+        if len(out) != np_:
+            raise ValueError(f"{what}: one output per projection")
+        t = [torch.empty((M, rank), dtype=torch.float32, device=dev) for _ in dims] if keep else None
+        ws = ws if ws is not None else _empty_aligned(need, dev)
+        c = plan.c()
+        _check(lib().bsq_adapters_apply(ct.byref(c), np_, arr, rank, d_in, _ptr(X), ldx,
+                                        None if base is None else _pointers(base),
+                                        None if base is None else _strides(ldb), _pointers(out), _strides(ldy), code,
+                                        None if t is None else _pointers(t), _ptr(ws), ws.numel(), st), what)
+    if single:
+        return out[0], None if t is None else t[0]
+    return out, t
+
+
+def bsq_adapters_grad(plan: AdapterPlan, pools, X: torch.Tensor, t, dy, base: torch.Tensor | None = None,
+                      want_dx: bool = True, dx: torch.Tensor | None = None, dx_dtype=torch.bfloat16, grads=None,
+                      accumulate: bool = False, ws: torch.Tensor | None = None, stream=None):
+    """The gradients of bsq_adapters_apply: (dx or None, list of dA, list of
+    dB). t: as kept by the forward call; dy: list of [M, d_out] (bf16); base:
+    what else reaches x (bf16 [M, d_in], or None for zero); dx: where that goes,
+    e.g. base itself. grads: (list of dA, list of dB) to write, or with
+    accumulate to add to (fp32, shaped as A and B)."""
+    what = "bsq_adapters_grad"
+    single = isinstance(pools, AdapterPool)
+    if single:
+        pools, t, dy = [pools], [t], [dy]
+        grads = None if grads is None else ([grads[0]], [grads[1]])
+    rank, d_in, ldx, arr, dims = _adapter_group(plan, pools, X, what)
+    M, n, np_ = plan.M, plan.n, len(pools)
+    if len(t) != np_ or len(dy) != np_:
+        raise ValueError(f"{what}: one t and one dy per projection")
+    for q in t:
+        _need(q, torch.float32, (M, rank), "t")
+    lddy = [_matrix(q, torch.bfloat16, (M, d), "dy") for q, d in zip(dy, dims)]
+    if accumulate and grads is None:
+        raise ValueError(f"{what}: accumulate needs grads")
+    ldb = 0 if base is None else _matrix(base, torch.bfloat16, (M, d_in), "base")
+    more = [] if grads is None else list(grads[0]) + list(grads[1])
+    dev = _device_of([plan.buf, X, base, dx, ws] + [p.A for p in pools] + list(t) + list(dy) + more, what)
+    need = bsq_adapters_workspace_bytes(True, M, n, rank, d_in, dims)
+    with _Launch(dev, stream) as st:
+        if grads is None:
+            grads = ([torch.empty((n, rank, d_in), dtype=torch.float32, device=dev) for _ in dims],
+                     [torch.empty((n, d, rank), dtype=torch.float32, device=dev) for d in dims])
+        dA, dB = list(grads[0]), list(grads[1])
+        if len(dA) != np_ or len(dB) != np_:
+            raise ValueError(f"{what}: one dA and one dB per projection")
+        for q, w, d in zip(dA, dB, dims):
+            _need(q, torch.float32, (n, rank, d_in), "dA")
+            _need(w, torch.float32, (n, d, rank), "dB")
+        if want_dx and dx is None:
+            dx = torch.empty((M, d_in), dtype=dx_dtype, device=dev)
+        if not want_dx:
+            dx = None
+        lddx = 0 if dx is None else _matrix(dx, dx.dtype, (M, d_in), "dx")
+        ws = ws if ws is not None else _empty_aligned(need, dev)
+        c = plan.c()
+        _check(lib().bsq_adapters_grad(ct.byref(c), np_, arr, rank, d_in, _ptr(X), ldx, _pointers(t), _pointers(dy),
+                                       _strides(lddy), _ptr(base), ldb, _ptr(dx), lddx,
+                                       BSQ_BF16 if dx is None else _dtype_code(dx.dtype), _pointers(dA), _pointers(dB),
+                                       int(accumulate), _ptr(ws), ws.numel(), st), what)
+    return (dx, dA[0], dB[0]) if single else (dx, dA, dB)
+
+
+# ---------------------------------------------------------------- cross entropy
+def bsq_xent_workspace_bytes(grad: bool, T: int, N: int, D: int) -> int:
+    out = ct.c_size_t(0)
+    _check(lib().bsq_xent_workspace_bytes(int(grad), T, N, D, ct.byref(out)), "bsq_xent_workspace_bytes")
+    return out.value
+
+
+def _xent_shapes(H, V, target):
+    T, D = H.shape
+    ldh = _matrix(H, torch.bfloat16, (T, D), "H")
+    ldv = _matrix(V, torch.bfloat16, (V.shape[0], D), "V")
+    _need(target, torch.int64, (T,), "target")
+    return T, V.shape[0], D, ldh, ldv
+
+
+def bsq_xent_loss(H: torch.Tensor, V: torch.Tensor, target: torch.Tensor, loss=None, lse=None, err=None,
+                  ws: torch.Tensor | None = None, stream=None):
+    """Per-token softmax cross entropy of hidden states H [T, D] under the head
+    V [N, D] (bf16) and targets int64 [T] (negative: no loss), without keeping
+    the logits: (loss, lse), fp32 [T]."""
+    T, N, D, ldh, ldv = _xent_shapes(H, V, target)
+    dev = _device_of((H, V, target, loss, lse, err, ws), "bsq_xent_loss")
+    need = bsq_xent_workspace_bytes(False, T, N, D)
+    with _Launch(dev, stream) as st:
+        loss = torch.empty(T, dtype=torch.float32, device=dev) if loss is None else _need(loss, torch.float32, (T,), "loss")
+        lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else _need(lse, torch.float32, (T,), "lse")
+        ws = ws if ws is not None else _empty_aligned(need, dev)
+        _check(lib().bsq_xent_loss(_ptr(H), ldh, _ptr(V), ldv, T, N, D, _ptr(target), _ptr(loss), _ptr(lse), _ptr(err),
+                                   _ptr(ws), ws.numel(), st), "bsq_xent_loss")
+    return loss, lse
+
+
+def bsq_xent_grad(H: torch.Tensor, V: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, g: torch.Tensor,
+                  head: bool = True, dH=None, dV=None, accumulate: bool = False, err=None,
+                  ws: torch.Tensor | None = None, stream=None):
+    """Gradients of sum(g * loss): (dH [T, D] bf16, dV [N, D] or None where head
+    is False). lse: as returned by bsq_xent_loss; g: fp32 [T]. dV: where the
+    head's gradient goes (bf16 or fp32; by default a new bf16 tensor), or with
+    accumulate what it is added to."""
+    T, N, D, ldh, ldv = _xent_shapes(H, V, target)
+    _need(lse, torch.float32, (T,), "lse")
+    _need(g, torch.float32, (T,), "g")
+    if accumulate and (dV is None or not head):
+        raise ValueError("bsq_xent_grad: accumulate needs dV")
+    dev = _device_of((H, V, target, lse, g, dH, dV, err, ws), "bsq_xent_grad")
+    need = bsq_xent_workspace_bytes(True, T, N, D)
+    with _Launch(dev, stream) as st:
+        if dH is None:
+            dH = torch.empty((T, D), dtype=torch.bfloat16, device=dev)
+        lddh = _matrix(dH, torch.bfloat16, (T, D), "dH")
+        if not head:
+            dV = None
+        elif dV is None:
+            dV = torch.empty((N, D), dtype=torch.bfloat16, device=dev)
+        lddv = 0 if dV is None else _matrix(dV, dV.dtype, (N, D), "dV")
+        ws = ws if ws is not None else _empty_aligned(need, dev)
+        _check(lib().bsq_xent_grad(_ptr(H), ldh, _ptr(V), ldv, T, N, D, _ptr(target), _ptr(lse), _ptr(g), _ptr(dH), lddh,
+                                   _ptr(dV), lddv, BSQ_BF16 if dV is None else _dtype_code(dV.dtype), int(accumulate),
+                                   _ptr(err), _ptr(ws), ws.numel(), st), "bsq_xent_grad")
+    return dH, dV
+
+
+# ---------------------------------------------------------------- gradient norm and clipping
+class bsq_clip_plan(ct.Structure):
+    _fields_ = [("table", ct.c_void_p), ("count", ct.c_int64), ("chunks", ct.c_int64)]
+
+
+class GradPlan:
+    """The gradients of a training program (fp32 or bf16 tensors, contiguous),
+    prepared once for bsq_grad_norm and bsq_grad_clip; outs: where the clipped
+    ones go (None: in place). Holds the tensors."""
+
+    def __init__(self, tensors, outs=None, stream=None):
+        tensors = list(tensors)
+        outs = None if outs is None else list(outs)
+        if not tensors:
+            raise ValueError("GradPlan: no tensors")
+        if outs is not None and len(outs) != len(tensors):
+            raise ValueError("GradPlan: one output per tensor")
+        for i, t in enumerate(tensors):
+            if not t.is_contiguous():
+                raise ValueError("GradPlan: tensors must be contiguous")
+            if outs is not None:
+                _need(outs[i], t.dtype, t.shape, "output")
+        dev = _device_of(tensors + (outs or []), "GradPlan")
+        count = len(tensors)
+        sizes = _strides([t.numel() for t in tensors])
+        dtypes = (ct.c_int32 * count)(*[_dtype_code(t.dtype) for t in tensors])
+        need = ct.c_size_t(0)
+        _check(lib().bsq_clip_table_bytes(count, sizes, ct.byref(need)), "bsq_clip_table_bytes")
+        self.tensors, self.outs, self.device = tensors, outs, dev
+        with _Launch(dev, stream) as st:
+            self.table = _empty_aligned(need.value, dev)
+            self._c = bsq_clip_plan(self.table.data_ptr(), count, 0)
+            _check(lib().bsq_clip_prepare(ct.byref(self._c), self.table.numel(), _pointers(tensors),
+                                          None if outs is None else _pointers(outs), sizes, dtypes, st),
+                   "bsq_clip_prepare")
+
+
+def _grad_call(fn, name, plan, max_norm, stats, err, stream):
+    _device_of((plan.table, stats, err), name)
+    with _Launch(plan.device, stream) as st:
+        stats = torch.empty(2, dtype=torch.float32, device=plan.device) if stats is None else _need(
+            stats, torch.float32, (2,), "stats")
+        _check(fn(ct.byref(plan._c), max_norm, _ptr(stats), _ptr(err), st), name)
+    return stats
+
+
+def bsq_grad_norm(plan: GradPlan, max_norm: float, stats=None, err=None, stream=None) -> torch.Tensor:
+    """fp32 [2] on the GPU: the global norm of the plan's tensors and the
+    coefficient min(1, max_norm / (norm + 1e-6))."""
+    return _grad_call(lib().bsq_grad_norm, "bsq_grad_norm", plan, max_norm, stats, err, stream)
+
+
+def bsq_grad_clip(plan: GradPlan, max_norm: float, stats=None, err=None, stream=None) -> torch.Tensor:
+    """bsq_grad_norm, and the tensors times the coefficient (in place, or in the
+    plan's outputs)."""
+    return _grad_call(lib().bsq_grad_clip, "bsq_grad_clip", plan, max_norm, stats, err, stream)

@@ -620,4 +620,327 @@ bsq_status bsq_train_adam(const bsq_config *cfg, const bsq_train_hparams *hp, in
     return from_hip(launch_train_adam(*cfg, *hp, step, theta, grad, m, v, static_cast<hipStream_t>(stream)));
 }
 
+
+// ---------------------------------------------------------------------------
+// Adapters of many requests.
+// ---------------------------------------------------------------------------
+namespace {
+constexpr int64_t MAX_TOKENS = int64_t(1) << 24;
+constexpr int64_t MAX_WIDTH = int64_t(1) << 24;  // of a projection, either way
+
+bsq_status check_batch(int64_t M, int32_t n)
+{
+    if (M < 1 || n < 1) return BSQ_ERR_SHAPE;
+    if (M > MAX_TOKENS || n > BSQ_MAX_ADAPTERS) return BSQ_ERR_UNSUPPORTED;
+    return BSQ_OK;
+}
+
+bsq_status check_adapter_dims(int32_t n_proj, int32_t rank, int64_t d_in)
+{
+    if (n_proj < 1 || n_proj > BSQ_MAX_GROUP || rank < 1 || rank > BSQ_MAX_ADAPTER_RANK) return BSQ_ERR_ARG;
+    if (d_in < 1) return BSQ_ERR_SHAPE;
+    if (d_in > MAX_WIDTH) return BSQ_ERR_UNSUPPORTED;
+    return BSQ_OK;
+}
+
+// What apply and grad have in common; ws_bytes is checked against the need.
+bsq_status check_adapters(bool back, const bsq_adapter_plan *plan, int32_t n_proj, const bsq_adapter_pool *pools,
+                          int32_t rank, int64_t d_in, const void *X, int64_t ldx, const void *ws, size_t ws_bytes)
+{
+    if (!plan || !plan->buf || !pools || !X || !ws) return BSQ_ERR_ARG;
+    bsq_status s = check_batch(plan->M, plan->n);
+    if (s != BSQ_OK) return s;
+    if ((s = check_adapter_dims(n_proj, rank, d_in)) != BSQ_OK) return s;
+    if (ldx < d_in) return BSQ_ERR_SHAPE;
+    if (!aligned(plan->buf, 16) || !aligned(X, 2) || !aligned(ws, 256)) return BSQ_ERR_ALIGN;
+    int64_t d_out[BSQ_MAX_GROUP];
+    for (int i = 0; i < n_proj; ++i) {
+        const bsq_adapter_pool &p = pools[i];
+        if (!p.A || !p.B) return BSQ_ERR_ARG;
+        if (p.d_out < 1) return BSQ_ERR_SHAPE;
+        if (p.d_out > MAX_WIDTH) return BSQ_ERR_UNSUPPORTED;
+        if (!aligned(p.A, 2) || !aligned(p.B, 2) || !aligned(p.scale, 4) || !aligned(p.ranks, 4)) return BSQ_ERR_ALIGN;
+        d_out[i] = p.d_out;
+    }
+    if (ws_bytes < adapters_ws_bytes(back, plan->M, plan->n, n_proj, rank, d_in, d_out)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    return BSQ_OK;
+}
+}  // namespace
+
+bsq_status bsq_adapters_plan_bytes(int64_t M, int32_t n, size_t *bytes)
+{
+    if (!bytes) return BSQ_ERR_ARG;
+    const bsq_status s = check_batch(M, n);
+    if (s != BSQ_OK) return s;
+    *bytes = adapters_plan_bytes(M, n);
+    return BSQ_OK;
+}
+
+bsq_status bsq_adapters_plan(const bsq_adapter_plan *plan, size_t buf_bytes, int32_t *err, void *stream)
+{
+    if (!plan || !plan->ids || !plan->buf) return BSQ_ERR_ARG;
+    const bsq_status s = check_batch(plan->M, plan->n);
+    if (s != BSQ_OK) return s;
+    if (!aligned(plan->ids, 4) || !aligned(plan->buf, 16) || !aligned(err, 4)) return BSQ_ERR_ALIGN;
+    if (buf_bytes < adapters_plan_bytes(plan->M, plan->n)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    return from_hip(launch_adapters_plan(plan->ids, plan->M, plan->n, plan->buf, err, static_cast<hipStream_t>(stream)));
+}
+
+bsq_status bsq_adapters_workspace_bytes(int32_t back, int64_t M, int32_t n, int32_t n_proj, int32_t rank,
+                                        int64_t d_in, const int64_t *d_out, size_t *bytes)
+{
+    if (!bytes || !d_out || (back != 0 && back != 1)) return BSQ_ERR_ARG;
+    bsq_status s = check_batch(M, n);
+    if (s != BSQ_OK) return s;
+    if ((s = check_adapter_dims(n_proj, rank, d_in)) != BSQ_OK) return s;
+    for (int i = 0; i < n_proj; ++i) {
+        if (d_out[i] < 1) return BSQ_ERR_SHAPE;
+        if (d_out[i] > MAX_WIDTH) return BSQ_ERR_UNSUPPORTED;
+    }
+    *bytes = adapters_ws_bytes(back != 0, M, n, n_proj, rank, d_in, d_out);
+    return BSQ_OK;
+}
+
+bsq_status bsq_adapters_apply(const bsq_adapter_plan *plan, int32_t n_proj, const bsq_adapter_pool *pools,
+                              int32_t rank, int64_t d_in, const void *X, int64_t ldx, const void *const *y0,
+                              const int64_t *ldy0, void *const *y, const int64_t *ldy, int32_t y_dtype,
+                              float *const *t, void *ws, size_t ws_bytes, void *stream)
+{
+    if (y_dtype != BSQ_F32 && y_dtype != BSQ_BF16) return BSQ_ERR_DTYPE;
+    const bsq_status s = check_adapters(false, plan, n_proj, pools, rank, d_in, X, ldx, ws, ws_bytes);
+    if (s != BSQ_OK) return s;
+    if (!y || !ldy || (y0 && !ldy0)) return BSQ_ERR_ARG;
+    const size_t es = y_dtype == BSQ_F32 ? 4 : 2;
+    for (int i = 0; i < n_proj; ++i) {
+        if (!y[i] || (t && !t[i])) return BSQ_ERR_ARG;
+        if (ldy[i] < pools[i].d_out || (y0 && y0[i] && ldy0[i] < pools[i].d_out)) return BSQ_ERR_SHAPE;
+        if (y0 && y0[i] == y[i] && ldy0[i] != ldy[i]) return BSQ_ERR_ARG;
+        if (!aligned(y[i], es) || (y0 && !aligned(y0[i], es)) || (t && !aligned(t[i], 4))) return BSQ_ERR_ALIGN;
+    }
+    AdaptersCall c{};
+    c.plan = plan;
+    c.pools = pools;
+    c.np = n_proj;
+    c.rank = rank;
+    c.d_in = d_in;
+    c.X = X;
+    c.ldx = ldx;
+    c.y0 = y0;
+    c.ldy0 = ldy0;
+    c.y = y;
+    c.ldy = ldy;
+    c.y_dtype = y_dtype;
+    c.t = t;
+    c.ws = ws;
+    return from_hip(launch_adapters(c, static_cast<hipStream_t>(stream)));
+}
+
+bsq_status bsq_adapters_grad(const bsq_adapter_plan *plan, int32_t n_proj, const bsq_adapter_pool *pools,
+                             int32_t rank, int64_t d_in, const void *X, int64_t ldx, float *const *t,
+                             const void *const *dy, const int64_t *lddy, const void *dx0, int64_t lddx0, void *dx,
+                             int64_t lddx, int32_t dx_dtype, float *const *dA, float *const *dB, int32_t accumulate,
+                             void *ws, size_t ws_bytes, void *stream)
+{
+    if (dx && dx_dtype != BSQ_F32 && dx_dtype != BSQ_BF16) return BSQ_ERR_DTYPE;
+    const bsq_status s = check_adapters(true, plan, n_proj, pools, rank, d_in, X, ldx, ws, ws_bytes);
+    if (s != BSQ_OK) return s;
+    if (!t || !dy || !lddy || !dA || !dB || (accumulate != 0 && accumulate != 1)) return BSQ_ERR_ARG;
+    for (int i = 0; i < n_proj; ++i) {
+        if (!t[i] || !dy[i] || !dA[i] || !dB[i]) return BSQ_ERR_ARG;
+        if (lddy[i] < pools[i].d_out) return BSQ_ERR_SHAPE;
+        if (!aligned(t[i], 4) || !aligned(dy[i], 2) || !aligned(dA[i], 4) || !aligned(dB[i], 4)) return BSQ_ERR_ALIGN;
+    }
+    if (dx) {
+        if (lddx < d_in || (dx0 && lddx0 < d_in)) return BSQ_ERR_SHAPE;
+        if (dx0 == dx && (lddx0 != lddx || dx_dtype != BSQ_BF16)) return BSQ_ERR_ARG;
+        if (!aligned(dx, dx_dtype == BSQ_F32 ? 4 : 2) || !aligned(dx0, 2)) return BSQ_ERR_ALIGN;
+    }
+    AdaptersCall c{};
+    c.plan = plan;
+    c.pools = pools;
+    c.np = n_proj;
+    c.rank = rank;
+    c.d_in = d_in;
+    c.X = X;
+    c.ldx = ldx;
+    c.t = t;
+    c.dy = dy;
+    c.lddy = lddy;
+    c.dx0 = dx ? dx0 : nullptr;
+    c.lddx0 = lddx0;
+    c.dx = dx;
+    c.lddx = lddx;
+    c.dx_dtype = dx_dtype;
+    c.dA = dA;
+    c.dB = dB;
+    c.y_dtype = BSQ_BF16;
+    c.accumulate = accumulate;
+    c.ws = ws;
+    return from_hip(launch_adapters(c, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// Cross entropy.
+// ---------------------------------------------------------------------------
+namespace {
+bsq_status check_xent_dims(int64_t T, int64_t N, int64_t D)
+{
+    if (T < 0 || N < 1 || D < 1 || D % 8 != 0) return BSQ_ERR_SHAPE;
+    if (T > (int64_t(1) << 20) || N >= (int64_t(1) << 31) || D > (int64_t(1) << 16)) return BSQ_ERR_UNSUPPORTED;
+    return BSQ_OK;
+}
+
+bsq_status check_xent(bool grad, const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N,
+                      int64_t D, const int64_t *target, const int32_t *err, const void *ws, size_t ws_bytes)
+{
+    const bsq_status s = check_xent_dims(T, N, D);
+    if (s != BSQ_OK) return s;
+    if (!V || !ws || (T > 0 && (!H || !target))) return BSQ_ERR_ARG;
+    if (ldh < D || ldv < D || ldv % 8 != 0) return BSQ_ERR_SHAPE;
+    if (!aligned(H, 2) || !aligned(V, 16) || !aligned(target, 8) || !aligned(err, 4) || !aligned(ws, 256)) return BSQ_ERR_ALIGN;
+    if (ws_bytes < xent_ws_bytes(grad, T, N, D)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    return BSQ_OK;
+}
+}  // namespace
+
+bsq_status bsq_xent_workspace_bytes(int32_t grad, int64_t T, int64_t N, int64_t D, size_t *bytes)
+{
+    if (!bytes || (grad != 0 && grad != 1)) return BSQ_ERR_ARG;
+    const bsq_status s = check_xent_dims(T, N, D);
+    if (s != BSQ_OK) return s;
+    *bytes = xent_ws_bytes(grad != 0, T, N, D);
+    return BSQ_OK;
+}
+
+bsq_status bsq_xent_loss(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                         const int64_t *target, float *loss, float *lse, int32_t *err, void *ws, size_t ws_bytes,
+                         void *stream)
+{
+    const bsq_status s = check_xent(false, H, ldh, V, ldv, T, N, D, target, err, ws, ws_bytes);
+    if (s != BSQ_OK) return s;
+    if (T == 0) return BSQ_OK;
+    if (!loss || !lse) return BSQ_ERR_ARG;
+    if (!aligned(loss, 4) || !aligned(lse, 4)) return BSQ_ERR_ALIGN;
+    XentCall c{};
+    c.H = H;
+    c.ldh = ldh;
+    c.V = V;
+    c.ldv = ldv;
+    c.T = T;
+    c.N = N;
+    c.D = D;
+    c.target = target;
+    c.loss = loss;
+    c.lse = lse;
+    c.err = err;
+    c.ws = ws;
+    return from_hip(launch_xent_loss(c, static_cast<hipStream_t>(stream)));
+}
+
+bsq_status bsq_xent_grad(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                         const int64_t *target, const float *lse, const float *g, void *dH, int64_t lddh, void *dV,
+                         int64_t lddv, int32_t dv_dtype, int32_t accumulate, int32_t *err, void *ws,
+                         size_t ws_bytes, void *stream)
+{
+    if (dV && dv_dtype != BSQ_F32 && dv_dtype != BSQ_BF16) return BSQ_ERR_DTYPE;
+    const bsq_status s = check_xent(true, H, ldh, V, ldv, T, N, D, target, err, ws, ws_bytes);
+    if (s != BSQ_OK) return s;
+    if (accumulate != 0 && accumulate != 1) return BSQ_ERR_ARG;
+    if (T > 0 && (!lse || !g || !dH)) return BSQ_ERR_ARG;
+    if (T > 0 && lddh < D) return BSQ_ERR_SHAPE;
+    if (dV && lddv < D) return BSQ_ERR_SHAPE;
+    if (!aligned(lse, 4) || !aligned(g, 4) || !aligned(dH, 2) || !aligned(dV, dv_dtype == BSQ_F32 ? 4 : 2)) return BSQ_ERR_ALIGN;
+    XentCall c{};
+    c.H = H;
+    c.ldh = ldh;
+    c.V = V;
+    c.ldv = ldv;
+    c.T = T;
+    c.N = N;
+    c.D = D;
+    c.target = target;
+    c.lse_in = lse;
+    c.g = g;
+    c.dH = dH;
+    c.lddh = lddh;
+    c.dV = dV;
+    c.lddv = lddv;
+    c.dv_dtype = dv_dtype;
+    c.accumulate = accumulate;
+    c.err = err;
+    c.ws = ws;
+    return from_hip(launch_xent_grad(c, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// Gradient norm and clipping.
+// ---------------------------------------------------------------------------
+namespace {
+// chunks of all tensors
+bsq_status check_clip_sizes(int64_t count, const int64_t *sizes, int64_t *chunks)
+{
+    if (!sizes || count < 1) return BSQ_ERR_ARG;
+    if (count > (int64_t(1) << 24)) return BSQ_ERR_UNSUPPORTED;
+    *chunks = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (sizes[i] < 0) return BSQ_ERR_SHAPE;
+        if (sizes[i] > (int64_t(1) << 42)) return BSQ_ERR_UNSUPPORTED;
+        *chunks += clip_chunks(sizes[i]);
+    }
+    return *chunks > INT32_MAX ? BSQ_ERR_UNSUPPORTED : BSQ_OK;
+}
+
+bsq_status check_clip(const bsq_clip_plan *p, float max_norm, const float *stats, const int32_t *err)
+{
+    if (!p || !p->table || !stats || p->count < 1 || p->chunks < 0 || p->chunks > INT32_MAX) return BSQ_ERR_ARG;
+    if (!(max_norm >= 0.0f)) return BSQ_ERR_ARG;  // (infinity clips nothing)
+    if (!aligned(p->table, 256) || !aligned(stats, 4) || !aligned(err, 4)) return BSQ_ERR_ALIGN;
+    return BSQ_OK;
+}
+}  // namespace
+
+bsq_status bsq_clip_table_bytes(int64_t count, const int64_t *sizes, size_t *bytes)
+{
+    if (!bytes) return BSQ_ERR_ARG;
+    int64_t chunks = 0;
+    const bsq_status s = check_clip_sizes(count, sizes, &chunks);
+    if (s != BSQ_OK) return s;
+    *bytes = clip_table_bytes(count, chunks);
+    return BSQ_OK;
+}
+
+bsq_status bsq_clip_prepare(bsq_clip_plan *plan, size_t table_bytes, const void *const *src, void *const *dst,
+                            const int64_t *sizes, const int32_t *dtypes, void *stream)
+{
+    if (!plan || !plan->table || !src || !dtypes) return BSQ_ERR_ARG;
+    int64_t chunks = 0;
+    const bsq_status s = check_clip_sizes(plan->count, sizes, &chunks);
+    if (s != BSQ_OK) return s;
+    if (!aligned(plan->table, 256)) return BSQ_ERR_ALIGN;
+    for (int64_t i = 0; i < plan->count; ++i) {
+        if (dtypes[i] != BSQ_F32 && dtypes[i] != BSQ_BF16) return BSQ_ERR_DTYPE;
+        if (sizes[i] > 0 && (!src[i] || (dst && !dst[i]))) return BSQ_ERR_ARG;
+        const size_t es = dtypes[i] == BSQ_F32 ? 4 : 2;
+        if (!aligned(src[i], es) || (dst && !aligned(dst[i], es))) return BSQ_ERR_ALIGN;
+    }
+    if (table_bytes < clip_table_bytes(plan->count, chunks)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    plan->chunks = chunks;
+    return from_hip(launch_clip_prepare(plan->count, src, dst, sizes, dtypes, chunks, plan->table,
+                                        static_cast<hipStream_t>(stream)));
+}
+
+bsq_status bsq_grad_norm(const bsq_clip_plan *plan, float max_norm, float *stats, int32_t *err, void *stream)
+{
+    const bsq_status s = check_clip(plan, max_norm, stats, err);
+    if (s != BSQ_OK) return s;
+    return from_hip(launch_clip(*plan, false, max_norm, stats, err, static_cast<hipStream_t>(stream)));
+}
+
+bsq_status bsq_grad_clip(const bsq_clip_plan *plan, float max_norm, float *stats, int32_t *err, void *stream)
+{
+    const bsq_status s = check_clip(plan, max_norm, stats, err);
+    if (s != BSQ_OK) return s;
+    return from_hip(launch_clip(*plan, true, max_norm, stats, err, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

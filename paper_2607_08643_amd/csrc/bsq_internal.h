@@ -277,6 +277,62 @@ hipError_t launch_train_grad(const bsq_config &cfg, const bsq_train_hparams &hp,
 hipError_t launch_train_adam(const bsq_config &cfg, const bsq_train_hparams &hp, int step, float *theta,
                              const float *grad, float *m, float *v, hipStream_t st);
 
+// Adapters of many requests (adapters.hip): tokens of a tile of the plan,
+// sizes, and the two launches; `dy` set: the gradients.
+struct AdaptersCall {
+    const bsq_adapter_plan *plan;
+    const bsq_adapter_pool *pools;
+    int np, rank;
+    int64_t d_in;
+    const void *X;
+    int64_t ldx;
+    const void *const *y0;   // forward: bases (or NULL) and outputs
+    const int64_t *ldy0;
+    void *const *y;
+    const int64_t *ldy;
+    int y_dtype;
+    float *const *t;         // forward: written (or NULL); backward: read
+    const void *const *dy;   // backward
+    const int64_t *lddy;
+    const void *dx0;
+    int64_t lddx0;
+    void *dx;
+    int64_t lddx;
+    int dx_dtype;
+    float *const *dA, *const *dB;
+    int accumulate;
+    void *ws;
+};
+int64_t adapters_tile(int64_t M);
+size_t adapters_plan_bytes(int64_t M, int64_t n);
+size_t adapters_ws_bytes(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_in, const int64_t *d_out);
+hipError_t launch_adapters_plan(const int32_t *ids, int64_t M, int64_t n, void *buf, int32_t *err, hipStream_t st);
+hipError_t launch_adapters(const AdaptersCall &c, hipStream_t st);
+
+// Cross entropy of a large vocabulary (xent.hip).
+struct XentCall {
+    const void *H, *V;
+    int64_t ldh, ldv, T, N, D;
+    const int64_t *target;
+    float *loss, *lse;       // loss: written
+    const float *lse_in, *g; // gradient: read
+    void *dH, *dV;           // gradient: written; dV may be NULL
+    int64_t lddh, lddv;
+    int dv_dtype, accumulate;
+    int32_t *err;
+    void *ws;
+};
+size_t xent_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D);
+hipError_t launch_xent_loss(const XentCall &c, hipStream_t st);
+hipError_t launch_xent_grad(const XentCall &c, hipStream_t st);
+
+// Global gradient norm and clipping (clip.hip).
+int64_t clip_chunks(int64_t n);
+size_t clip_table_bytes(int64_t count, int64_t chunks);
+hipError_t launch_clip_prepare(int64_t count, const void *const *src, void *const *dst, const int64_t *sizes,
+                               const int32_t *dtypes, int64_t chunks, void *table, hipStream_t st);
+hipError_t launch_clip(const bsq_clip_plan &p, bool scale, float max_norm, float *stats, int32_t *err, hipStream_t st);
+
 // Polls a finishing workgroup makes for another workgroup's partial result
 // before it gives up (reports BSQ_DEVERR_TIMEOUT and poisons the workspace).
 // Workgroups run in dispatch order, so the wait is never expected to give

@@ -1,0 +1,674 @@
+// Softmax cross entropy of a large vocabulary from hidden states H [T][D] and
+// head weights V [N][D], and its gradient, without keeping the T x N logits:
+//   z = H V^T,  lse = log sum exp(z),  loss = lse - z_target,
+//   d = g (exp(z - lse) - onehot),  dH = d V,  dV = d^T H.
+//
+// loss: one matrix product whose tiles are reduced where they are made: per
+// token and tile the largest logit and the sum of exponentials against it, and
+// the target's logit; a second launch joins a token's tiles. 2 T N D
+// operations, D-deep; V is read once.
+//
+// gradient: the vocabulary in pieces of `vp` words. Per piece the logits are
+// made again and leave the tile as d in bf16 (the workspace holds one piece);
+// two further products read them: dV's rows of the piece, and the piece's
+// contribution to dH, added in fp32 over the pieces in order.
+//
+// Tokens without a loss are taken out first: the rows that have one are copied
+// next to each other (padded with zeros to whole tiles and to a multiple of
+// 64 inputs), and every product runs over those alone.
+#include <algorithm>
+#include <atomic>
+
+#include "gemm_common.h"
+
+namespace bsq {
+namespace {
+
+constexpr int XT = 256;
+constexpr int VBLK = 256;              // words of a logits tile
+constexpr int64_t ROW_PAD = 256;       // token rows are padded to this
+constexpr float LOG2E = 1.4426950408889634f;
+
+enum { EPI_STATS, EPI_PROB, EPI_DV, EPI_DH };
+
+struct XArgs {
+    // header words: 0: tokens with a loss
+    int32_t *hdr, *rows, *pos;    // rows [Tp]: token of a compact row; pos [T]: compact row of a token or -1
+    const uint16_t *H, *V;
+    int64_t ldh, ldv, T, N, D, Tp, Dp;
+    const int64_t *target;
+    const float *lse_in, *g_in;
+    int32_t *err;
+    uint16_t *Hc;                 // [Tp][Dp]
+    int32_t *tgt;                 // [Tp] compact targets
+    float *lse, *g;               // [Tp] compact
+    float2 *stat;                 // [word tiles][Tp]: largest logit, sum of exp against it
+    float *ztgt;                  // [Tp]
+    float *loss_out, *lse_out;
+    // a piece of the vocabulary: words [v0, v0 + vp)
+    int64_t v0, vp, dsp;          // dsp: row length of dS
+    uint16_t *dS;                 // [Tp][dsp]
+    float *dHp;                   // [hsplit][Tp][Dp]
+    int hsplit, first;
+    uint16_t *dH;
+    void *dV;
+    int64_t lddh, lddv;
+    int dv_bf16, dv_vec, dh_vec, accumulate;
+};
+
+// ---------------------------------------------------------------------------
+// The rows that have a loss, in order (one block), then their copies.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(1024) void xent_rows_kernel(const XArgs a)
+{
+    __shared__ int s_w[16];
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    int base = 0;
+    bool bad = false;
+    for (int64_t m0 = 0; m0 < a.T; m0 += 1024) {
+        const int64_t m = m0 + t;
+        const int64_t y = m < a.T ? a.target[m] : -1;
+        const bool live = y >= 0 && y < a.N;
+        bad |= y >= a.N;
+        const uint64_t bal = __ballot(live);
+        if (lane == 0) s_w[w] = __popcll(bal);
+        __syncthreads();
+        int at = base + __popcll(bal & ((uint64_t(1) << lane) - 1)), all = 0;
+        for (int k = 0; k < 16; ++k) {
+            at += (k < w) ? s_w[k] : 0;
+            all += s_w[k];
+        }
+        if (m < a.T) a.pos[m] = live ? at : -1;
+        if (live) a.rows[at] = int32_t(m);
+        base += all;
+        __syncthreads();
+    }
+    if (t == 0) a.hdr[0] = base;
+    if (bad && a.err) atomicOr(a.err, BSQ_DEVERR_BAD_SET);
+}
+
+// One block per compact row: its hidden state padded with zeros, and its
+// target, lse and g.
+__global__ __launch_bounds__(XT) void xent_pack_kernel(const XArgs a)
+{
+    const int64_t i = blockIdx.x;
+    const int live = a.hdr[0];
+    const bool in = i < live;
+    const int64_t m = in ? a.rows[i] : 0;
+    const uint16_t *src = a.H + m * a.ldh;
+    uint16_t *dst = a.Hc + i * a.Dp;
+    const bool vec = ((reinterpret_cast<uintptr_t>(a.H) | uintptr_t(2 * a.ldh)) & 15) == 0;
+    for (int64_t c = 8 * threadIdx.x; c < a.Dp; c += 8 * XT) {
+        u32x4_t v = u32x4_t{0u, 0u, 0u, 0u};
+        if (in && c < a.D) {  // (D is a multiple of 8)
+            if (vec) v = *reinterpret_cast<const u32x4_t *>(src + c);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e >> 1] |= uint32_t(src[c + e]) << (16 * (e & 1));
+        }
+        *reinterpret_cast<u32x4_t *>(dst + c) = v;
+    }
+    if (threadIdx.x == 0) {
+        a.tgt[i] = in ? int32_t(a.target[m]) : -1;
+        if (a.g) {
+            a.g[i] = in ? a.g_in[m] : 0.0f;
+            a.lse[i] = in ? a.lse_in[m] : 0.0f;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The products. Out[left][right] = sum_k L[left][k] R[right][k]; WM x WN
+// waves, a wave owns MF groups of 16 right rows (tokens; dV: words) and NF
+// groups of 16 left rows (words; dV, dH: inputs). Steps of 32 deep reach a ring
+// of NS LDS slots by DMA, NS steps ahead; the fragments of step u + 1 are read
+// while the products of step u issue.
+//
+// An operand lies in memory either with k contiguous (logits: H, V; dH: d) or
+// with k as its row (dH: V; dV: d and H), and is staged as it lies:
+//   k contiguous: slot rows of 32 k (64 bytes, four 16-byte chunks); chunk c of
+//     row r lies at c ^ key, key = (r / 4) % 4 (left operand of the logits, whose
+//     fragments take rows in runs of four: (r / 4 NF) % 4), so that the 16 rows
+//     of a fragment read fall on all banks;
+//   k as row: slot rows of one k (256 columns, 32-byte groups of 16); group q of
+//     row k lies at q ^ (k % 4 + 4 (k / 8 % 2)), and fragments are read
+//     transposed, four k of 16 columns at a time.
+// ---------------------------------------------------------------------------
+template <int MF, int NF, int WM, int WN>
+struct XShape {
+    static constexpr int NW = WM * WN;
+    static constexpr int RU = MF * WM, LU = NF * WN;
+    static constexpr int BR = 16 * RU, BL = 16 * LU;
+    static constexpr int SLOT = (RU + LU) * 1024;
+    static constexpr int NS_FIT = GEMM_LDS_BYTES / SLOT;
+    static constexpr int NS = NS_FIT < 8 ? NS_FIT : 8;
+    static constexpr int NI = RU + LU;
+    static constexpr int PMAX = (NI + NW - 1) / NW, PMIN = NI / NW;
+    static constexpr size_t LDS = size_t(NS) * SLOT;
+    static_assert(NS >= 3, "two steps in flight beside the one being read");
+    static_assert((NS - 1) * PMAX <= 63, "wait count fits vmcnt");
+    static_assert(WM * BL * 8 <= int(LDS) && WN * BR * 8 <= int(LDS), "statistics fit the ring");
+};
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+template <int EPI, int MF, int NF, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(WM * WN / 4, WM * WN / 4)))
+void xent_gemm(const XArgs a)
+{
+    using G = XShape<MF, NF, WM, WN>;
+    constexpr bool LOGITS = EPI == EPI_STATS || EPI == EPI_PROB;
+    constexpr bool LK = LOGITS;              // left operand k contiguous
+    constexpr bool RK = EPI != EPI_DV;       // right operand k contiguous
+    constexpr int LSH = (NF == 4) ? 4 : (NF == 2 ? 3 : 2);  // log2(4 NF)
+    extern __shared__ __attribute__((aligned(16))) uint4 s_mem4[];
+    uint8_t *s_mem = reinterpret_cast<uint8_t *>(s_mem4);
+    const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int live = a.hdr[0];
+
+    // Tiles: right tiles x left tiles (x splits of k for dH); every XCD takes a
+    // run of them that walks up to 8 right tiles before the next left one.
+    const int64_t rrows = (EPI == EPI_DV) ? a.vp : live;
+    const int64_t lrows = LOGITS ? a.vp : a.D;
+    const int rt = int((rrows + G::BR - 1) / G::BR), lt = int((lrows + G::BL - 1) / G::BL);
+    const int splits = (EPI == EPI_DH) ? a.hsplit : 1;
+    const int total = rt * lt * splits;
+    if (int(blockIdx.x) >= total) return;
+    const int xcd = blockIdx.x & 7, per = total >> 3, rem = total & 7;
+    int lg = xcd * per + (xcd < rem ? xcd : rem) + int(blockIdx.x >> 3);
+    const int z = lg / (rt * lt);
+    lg -= z * (rt * lt);
+    const int band = lg / (8 * lt);
+    lg -= band * 8 * lt;
+    const int bh = (rt - 8 * band < 8) ? rt - 8 * band : 8;
+    const int by = 8 * band + lg % bh, bx = lg / bh;
+
+    // k: steps of 32, an even number; valid up to kmax
+    const int64_t kmax = LOGITS ? a.D : (EPI == EPI_DV ? live : (a.N - a.v0 < a.vp ? a.N - a.v0 : a.vp));
+    const int pairs = int((kmax + 63) / 64);
+    const int kb = 2 * int(int64_t(pairs) * z / splits), ke = 2 * int(int64_t(pairs) * (z + 1) / splits);
+    const int ku = ke - kb;
+
+    const uint16_t *L = LOGITS ? a.V + a.v0 * a.ldv : (EPI == EPI_DV ? a.Hc : a.V + a.v0 * a.ldv);
+    const int64_t ldl = LOGITS ? a.ldv : (EPI == EPI_DV ? a.Dp : a.ldv);
+    const uint16_t *R = LOGITS ? a.Hc : a.dS;
+    const int64_t ldr = LOGITS ? a.Dp : a.dsp;
+    // rows (columns, k as row) that exist: those past them are read from the last
+    const int64_t lend = LOGITS ? (a.N - a.v0) : a.D;
+
+    // DMA: unit v of a step is one instruction of the wave, 16 bytes a lane.
+    const uint16_t *src[G::PMAX];
+    int kof[G::PMAX];      // k (contiguous: of the lane's chunk; as row: of its row) within the step
+    bool kc[G::PMAX];
+    int64_t ld_[G::PMAX];
+#pragma unroll
+    for (int r = 0; r < G::PMAX; ++r) {
+        const int v0 = wave + G::NW * r, v = (v0 < G::NI) ? v0 : G::NI - 1;
+        const bool right = v < G::RU;
+        const int u = right ? v : v - G::RU;
+        kc[r] = right ? RK : LK;
+        ld_[r] = right ? ldr : ldl;
+        if (kc[r]) {
+            const int row = 16 * u + (lane >> 2);
+            const int key = right ? (row >> 2) & 3 : (row >> LSH) & 3;
+            kof[r] = 8 * ((lane & 3) ^ key);
+            int64_t at = (right ? int64_t(by) * G::BR : int64_t(bx) * G::BL) + row;
+            if (!right && at >= lend) at = lend - 1;
+            src[r] = (right ? R : L) + at * ld_[r];
+        } else {
+            const int units = right ? G::RU : G::LU;   // 32-byte groups of a row
+            const int byte = u * 1024 + lane * 16, k = byte / (32 * units);
+            const int grp = ((byte - k * 32 * units) >> 5) ^ ((k & 3) | (((k >> 3) & 1) << 2));
+            int64_t col = (right ? int64_t(by) * G::BR : int64_t(bx) * G::BL) + 16 * grp + 8 * (lane & 1);
+            if (!right && col >= lend) col = 0;
+            kof[r] = k;
+            src[r] = (right ? R : L) + col;
+        }
+    }
+    const bool full = wave < G::NI % G::NW || G::PMAX == G::PMIN;
+    // The padded k of one operand are zero (H past D, d past the tokens and
+    // words); the other's are read from where it has values.
+    const int64_t lkmax = LOGITS ? a.D : (EPI == EPI_DV ? a.Tp : kmax);
+    auto dma = [&](int u, int slot) {
+        const int64_t k0 = 32 * int64_t(kb + (u < ku ? u : ku - 1));  // past the end: a reload that nothing reads
+#pragma unroll
+        for (int r = 0; r < G::PMAX; ++r) {
+            if (r >= G::PMIN && !full) continue;
+            const int v0 = wave + G::NW * r;
+            int64_t k = k0 + kof[r];
+            if (v0 >= G::RU && k >= lkmax) k = kc[r] ? 0 : lkmax - 1;
+            const uint16_t *p = src[r] + (kc[r] ? k : k * ld_[r]);
+            __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4 *>(p),
+                                             reinterpret_cast<uint4 *>(s_mem + slot * G::SLOT + (v0 << 10)), 16, 0, 0);
+        }
+    };
+
+    f32x4_t acc[MF][NF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+    if (ku > 0) {
+#pragma unroll
+        for (int c = 0; c < G::NS; ++c) dma(c, c);
+        bf16x8_t rf[2][MF], lf[2][NF];
+        // the lane's bytes of its first fragment
+        const int kr = 8 * g + (r16 >> 2), key = (r16 >> 2) | ((g & 1) << 2);
+        auto frag_k = [&](int base) { return *reinterpret_cast<const bf16x8_t *>(s_mem + base); };
+        auto frag_tr = [&](int slot_base, int units, int grp) {
+            const uint8_t *p = s_mem + slot_base + kr * 32 * units + ((grp ^ key) << 5) + ((r16 & 3) << 3);
+            const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)p);
+            const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(p + 4 * 32 * units));
+            return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        const int lrow = LOGITS ? wn * NF * 16 + (r16 >> 2) * (4 * NF) + (r16 & 3) : 0;
+        const int lbase = G::RU * 1024 + lrow * 64 + ((g ^ (r16 >> 2)) << 4);
+        const int rbase = (wm * MF * 16 + r16) * 64 + ((g ^ (r16 >> 2)) << 4);
+        auto frags = [&](int p, int slot) {
+            const int sb = slot * G::SLOT;
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                if constexpr (LK) lf[p][j] = frag_k(sb + lbase + j * 256);
+                else lf[p][j] = frag_tr(sb + G::RU * 1024, G::LU, wn * NF + j);
+            }
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                if constexpr (RK) rf[p][i] = frag_k(sb + rbase + i * 1024);
+                else rf[p][i] = frag_tr(sb, G::RU, wm * MF + i);
+            }
+        };
+        auto products = [&](int p) {
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lf[p][j], rf[p][i], acc[i][j], 0, 0, 0);
+        };
+        if (full) wait_vm<(G::NS - 1) * G::PMAX>();
+        else wait_vm<(G::NS - 1) * G::PMIN>();
+        lds_barrier();
+        frags(0, 0);
+        int slot = 0;
+        // step u: its fragments are in registers once the barrier's LDS wait is
+        // over, for every wave, so its slot takes step u + NS
+        auto step = [&](int u, int p) {
+            if (full) wait_vm<(G::NS - 2) * G::PMAX>();
+            else wait_vm<(G::NS - 2) * G::PMIN>();
+            lds_barrier();
+            dma(u + G::NS, slot);
+            slot = (slot + 1 == G::NS) ? 0 : slot + 1;
+            frags(1 - p, slot);
+            products(p);
+        };
+        for (int u = 0; u < ku; u += 2) {
+            step(u, 0);
+            step(u + 1, 1);
+        }
+        wait_vm<0>();  // the reloads land before the ring is used again or the block ends
+    }
+
+    const int64_t rbeg = int64_t(by) * G::BR + 16 * (wm * MF) + r16;  // right row of group i: + 16 i
+    if constexpr (EPI == EPI_STATS) {
+        // per token: the largest of the tile's logits, the sum against it
+        lds_barrier();
+        float *s_max = reinterpret_cast<float *>(s_mem), *s_sum = s_max + WN * G::BR;
+        const int64_t w0 = a.v0 + int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * NF * g;
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int64_t row = rbeg + 16 * i;
+            const int tg = (row < a.Tp) ? a.tgt[row] : -1;
+            float m = -__builtin_inff();
+            bool nan = false;
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t w = w0 + 4 * j + r;
+                    if (w >= a.N) continue;
+                    const float z = acc[i][j][r];
+                    if (w == tg) a.ztgt[row] = z;
+                    nan |= !(z == z);
+                    m = z > m ? z : m;
+                }
+            float s = 0.0f;
+            // against a finite value: a lane whose words are all -inf (or absent) adds 0
+            const float ref = (m == -__builtin_inff()) ? 0.0f : m;
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (w0 + 4 * j + r < a.N) s += __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * LOG2E);
+            if (nan) s = __builtin_nanf("");
+            // join the four lanes of the token
+#pragma unroll
+            for (int d = 16; d < 64; d <<= 1) {
+                const float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d);
+                const float mm = m2 > m ? m2 : m;
+                const float rr = (mm == -__builtin_inff()) ? 0.0f : mm;
+                s = s * __builtin_amdgcn_exp2f((m - rr) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - rr) * LOG2E);
+                m = mm;
+            }
+            if (g == 0) {
+                s_max[wn * G::BR + 16 * (wm * MF + i) + r16] = m;
+                s_sum[wn * G::BR + 16 * (wm * MF + i) + r16] = s;
+            }
+        }
+        __syncthreads();
+        for (int q = t; q < G::BR; q += 64 * G::NW) {
+            float m = s_max[q], s = s_sum[q];
+#pragma unroll
+            for (int w = 1; w < WN; ++w) {
+                const float m2 = s_max[w * G::BR + q], s2 = s_sum[w * G::BR + q];
+                const float mm = m2 > m ? m2 : m;
+                const float rr = (mm == -__builtin_inff()) ? 0.0f : mm;
+                s = s * __builtin_amdgcn_exp2f((m - rr) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - rr) * LOG2E);
+                m = mm;
+            }
+            const int64_t row = int64_t(by) * G::BR + q;
+            if (row < live) a.stat[int64_t(bx) * a.Tp + row] = make_float2(m, s);
+        }
+    } else if constexpr (EPI == EPI_PROB) {
+        // d = g (exp(z - lse) - onehot) in bf16; 0 for padded tokens and words
+        const int64_t w0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * NF * g;
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int64_t row = rbeg + 16 * i;
+            const bool in = row < live;
+            const int64_t tg = int64_t(a.tgt[row]) - a.v0;
+            const float lse = a.lse[row] , gg = a.g[row];
+            float v[4 * NF];
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t w = w0 + 4 * j + r;
+                    float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * LOG2E);
+                    if (w == tg) p -= 1.0f;
+                    v[4 * j + r] = (in && a.v0 + w < a.N) ? gg * p : 0.0f;
+                }
+            u32x4_t *q = reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w0);
+#pragma unroll
+            for (int h = 0; h < NF / 2; ++h)
+                q[h] = u32x4_t{pack_bf16x2(v[8 * h], v[8 * h + 1]), pack_bf16x2(v[8 * h + 2], v[8 * h + 3]),
+                               pack_bf16x2(v[8 * h + 4], v[8 * h + 5]), pack_bf16x2(v[8 * h + 6], v[8 * h + 7])};
+        }
+    } else if constexpr (EPI == EPI_DH) {
+        // fp32 sums over the pieces, each split its own
+        float *o = a.dHp + int64_t(z) * a.Tp * a.Dp;
+        const int64_t c0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * g;
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int64_t row = rbeg + 16 * i;
+            if (row >= live) continue;
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                const int64_t c = c0 + 16 * j;
+                if (c >= a.D) continue;  // (D is a multiple of 8)
+                f32x4_t *q = reinterpret_cast<f32x4_t *>(o + row * a.Dp + c);
+                *q = a.first ? acc[i][j] : *q + acc[i][j];
+            }
+        }
+    } else {
+        const int64_t c0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * g;
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int64_t w = a.v0 + rbeg + 16 * i;
+            if (w >= a.N || rbeg + 16 * i >= a.vp) continue;
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                const int64_t c = c0 + 16 * j;
+                if (c >= a.D) continue;
+                f32x4_t v = acc[i][j];
+                if (a.dv_bf16) {
+                    uint16_t *q = static_cast<uint16_t *>(a.dV) + w * a.lddv + c;
+                    if (a.dv_vec) {
+                        uint2 *q2 = reinterpret_cast<uint2 *>(q);
+                        if (a.accumulate) {
+                            const uint2 o = *q2;
+                            v += f32x4_t{__uint_as_float(o.x << 16), __uint_as_float(o.x & 0xffff0000u),
+                                         __uint_as_float(o.y << 16), __uint_as_float(o.y & 0xffff0000u)};
+                        }
+                        *q2 = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            q[r] = f32_to_bf16(a.accumulate ? bf16_to_f32(q[r]) + v[r] : v[r]);
+                    }
+                } else {
+                    float *q = static_cast<float *>(a.dV) + w * a.lddv + c;
+                    if (a.dv_vec) {
+                        f32x4_t *q4 = reinterpret_cast<f32x4_t *>(q);
+                        *q4 = a.accumulate ? *q4 + v : v;
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) q[r] = a.accumulate ? q[r] + v[r] : v[r];
+                    }
+                }
+            }
+        }
+    }
+}
+
+// A token's tiles joined: 16 tokens a block, 16 threads each over the tiles.
+__global__ __launch_bounds__(XT) void xent_join_kernel(const XArgs a, int tiles)
+{
+    __shared__ float s_m[16][17], s_s[16][17];
+    const int tok = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int64_t m = int64_t(blockIdx.x) * 16 + tok;
+    const int row = m < a.T ? a.pos[m] : -1;
+    float mx = -__builtin_inff(), s = 0.0f;
+    if (row >= 0) {
+        for (int q = part; q < tiles; q += 16) {
+            const float2 v = a.stat[int64_t(q) * a.Tp + row];
+            const float mm = v.x > mx ? v.x : mx;
+            const float rr = (mm == -__builtin_inff()) ? 0.0f : mm;
+            s = s * __builtin_amdgcn_exp2f((mx - rr) * LOG2E) + v.y * __builtin_amdgcn_exp2f((v.x - rr) * LOG2E);
+            mx = mm;
+        }
+    }
+    s_m[part][tok] = mx;
+    s_s[part][tok] = s;
+    __syncthreads();
+    if (part != 0 || m >= a.T) return;
+    for (int q = 1; q < 16; ++q) {
+        const float m2 = s_m[q][tok], s2 = s_s[q][tok];
+        const float mm = m2 > mx ? m2 : mx;
+        const float rr = (mm == -__builtin_inff()) ? 0.0f : mm;
+        s = s * __builtin_amdgcn_exp2f((mx - rr) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - rr) * LOG2E);
+        mx = mm;
+    }
+    const float lse = mx + logf(s);
+    a.lse_out[m] = row >= 0 ? lse : 0.0f;
+    a.loss_out[m] = row >= 0 ? lse - a.ztgt[row] : 0.0f;
+}
+
+// dH rows from the sums (0 for tokens without a loss). One block per token.
+__global__ __launch_bounds__(XT) void xent_dh_kernel(const XArgs a)
+{
+    const int64_t m = blockIdx.x;
+    const int row = a.pos[m];
+    for (int64_t c = 4 * threadIdx.x; c < a.D; c += 4 * XT) {
+        f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (row >= 0) {
+            const float *q = a.dHp + int64_t(row) * a.Dp + c;
+            for (int z = 0; z < a.hsplit; ++z) v += *reinterpret_cast<const f32x4_t *>(q + int64_t(z) * a.Tp * a.Dp);
+        }
+        uint16_t *o = a.dH + m * a.lddh + c;
+        if (a.dh_vec) *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        else
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = f32_to_bf16(v[r]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+constexpr int64_t PIECE_BYTES = int64_t(256) << 20;  // of d
+
+struct XLayout {
+    int64_t Tp, Dp, tiles, vp;
+    int hsplit;
+    size_t rows, pos, tgt, lse, g, ztgt, hc, stat, ds, dhp, total;
+};
+
+XLayout xent_layout(bool grad, int64_t T, int64_t N, int64_t D)
+{
+    XLayout l{};
+    l.Tp = std::max<int64_t>(1, (T + ROW_PAD - 1) / ROW_PAD) * ROW_PAD;
+    l.Dp = (D + 63) / 64 * 64;
+    l.tiles = (N + VBLK - 1) / VBLK;
+    size_t at = 256;
+    auto take = [&](size_t bytes) {
+        const size_t p = at;
+        at += align256(bytes);
+        return p;
+    };
+    l.rows = take(size_t(l.Tp) * 4);
+    l.pos = take(size_t(std::max<int64_t>(T, 1)) * 4);
+    l.tgt = take(size_t(l.Tp) * 4);
+    l.hc = take(size_t(l.Tp) * size_t(l.Dp) * 2);
+    if (!grad) {
+        l.ztgt = take(size_t(l.Tp) * 4);
+        l.stat = take(size_t(l.tiles) * size_t(l.Tp) * 8);
+    } else {
+        l.lse = take(size_t(l.Tp) * 4);
+        l.g = take(size_t(l.Tp) * 4);
+        const int64_t most = std::max<int64_t>(1, PIECE_BYTES / (l.Tp * 2 * VBLK));
+        const int64_t pieces = (l.tiles + most - 1) / most;
+        l.vp = (l.tiles + pieces - 1) / pieces * VBLK;
+        l.ds = take(size_t(l.Tp) * size_t(l.vp) * 2);
+        // splits of dH's depth: until its launch fills the compute units
+        const int64_t blocks = (l.Tp / 256) * ((D + 255) / 256);
+        l.hsplit = int(std::clamp<int64_t>(256 / blocks, 1, std::max<int64_t>(1, std::min<int64_t>(l.vp / 512, 32))));
+        l.dhp = take(size_t(l.hsplit) * size_t(l.Tp) * size_t(l.Dp) * 4);
+    }
+    l.total = at;
+    return l;
+}
+
+template <int EPI, int MF, int NF, int WM, int WN>
+hipError_t launch_gemm_shape(const XArgs &a, int64_t right, int64_t left, int splits, hipStream_t st)
+{
+    using G = XShape<MF, NF, WM, WN>;
+    static std::atomic<bool> lds_set{false};  // the ring exceeds the default dynamic LDS limit
+    if (!lds_set.load(std::memory_order_relaxed)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&xent_gemm<EPI, MF, NF, WM, WN>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, int(G::LDS));
+        if (e != hipSuccess) return e;
+        lds_set.store(true, std::memory_order_relaxed);
+    }
+    const int64_t blocks = (right + G::BR - 1) / G::BR * ((left + G::BL - 1) / G::BL) * splits;
+    if (blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL((xent_gemm<EPI, MF, NF, WM, WN>), dim3(unsigned(blocks)), dim3(64 * G::NW), G::LDS, st, a);
+    return hipGetLastError();
+}
+
+// Token tiles by the number of tokens. d's rows are read 64 deep by dV, so its
+// tiles have 64 or more.
+template <int EPI>
+hipError_t launch_tokens(const XArgs &a, int64_t left, int splits, hipStream_t st)
+{
+    if constexpr (EPI == EPI_STATS) {
+        if (a.T <= 16) return launch_gemm_shape<EPI, 1, 4, 1, 4>(a, a.T, left, splits, st);
+        if (a.T <= 32) return launch_gemm_shape<EPI, 1, 4, 2, 4>(a, a.T, left, splits, st);
+    }
+    if (a.T <= 64) return launch_gemm_shape<EPI, 2, 4, 2, 4>(a, a.T, left, splits, st);
+    if (a.T <= 128) return launch_gemm_shape<EPI, 4, 4, 2, 4>(a, a.T, left, splits, st);
+    return launch_gemm_shape<EPI, 8, 4, 2, 4>(a, a.T, left, splits, st);
+}
+
+XArgs xent_args(const XentCall &c, const XLayout &l)
+{
+    char *ws = static_cast<char *>(c.ws);
+    XArgs a{};
+    a.hdr = reinterpret_cast<int32_t *>(ws);
+    a.rows = reinterpret_cast<int32_t *>(ws + l.rows);
+    a.pos = reinterpret_cast<int32_t *>(ws + l.pos);
+    a.tgt = reinterpret_cast<int32_t *>(ws + l.tgt);
+    a.Hc = reinterpret_cast<uint16_t *>(ws + l.hc);
+    a.H = static_cast<const uint16_t *>(c.H);
+    a.V = static_cast<const uint16_t *>(c.V);
+    a.ldh = c.ldh;
+    a.ldv = c.ldv;
+    a.T = c.T;
+    a.N = c.N;
+    a.D = c.D;
+    a.Tp = l.Tp;
+    a.Dp = l.Dp;
+    a.target = c.target;
+    a.err = c.err;
+    return a;
+}
+
+hipError_t launch_rows(const XArgs &a, hipStream_t st)
+{
+    hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(xent_pack_kernel, dim3(unsigned(a.Tp)), dim3(XT), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t xent_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D) { return xent_layout(grad, T, N, D).total; }
+
+hipError_t launch_xent_loss(const XentCall &c, hipStream_t st)
+{
+    const XLayout l = xent_layout(false, c.T, c.N, c.D);
+    XArgs a = xent_args(c, l);
+    a.ztgt = reinterpret_cast<float *>(static_cast<char *>(c.ws) + l.ztgt);
+    a.stat = reinterpret_cast<float2 *>(static_cast<char *>(c.ws) + l.stat);
+    a.loss_out = c.loss;
+    a.lse_out = c.lse;
+    a.v0 = 0;
+    a.vp = l.tiles * VBLK;
+    hipError_t e = launch_rows(a, st);
+    if (e != hipSuccess) return e;
+    if ((e = launch_tokens<EPI_STATS>(a, a.vp, 1, st)) != hipSuccess) return e;
+    hipLaunchKernelGGL(xent_join_kernel, dim3(unsigned((c.T + 15) / 16)), dim3(XT), 0, st, a, int(l.tiles));
+    return hipGetLastError();
+}
+
+hipError_t launch_xent_grad(const XentCall &c, hipStream_t st)
+{
+    const XLayout l = xent_layout(true, c.T, c.N, c.D);
+    XArgs a = xent_args(c, l);
+    char *ws = static_cast<char *>(c.ws);
+    a.lse_in = c.lse_in;
+    a.g_in = c.g;
+    a.lse = reinterpret_cast<float *>(ws + l.lse);
+    a.g = reinterpret_cast<float *>(ws + l.g);
+    a.dS = reinterpret_cast<uint16_t *>(ws + l.ds);
+    a.dsp = l.vp;
+    a.dHp = reinterpret_cast<float *>(ws + l.dhp);
+    a.hsplit = l.hsplit;
+    a.dH = static_cast<uint16_t *>(c.dH);
+    a.lddh = c.lddh;
+    a.dh_vec = (reinterpret_cast<uintptr_t>(c.dH) | uintptr_t(2 * c.lddh)) % 8 == 0;
+    a.dV = c.dV;
+    a.lddv = c.lddv;
+    a.dv_bf16 = c.dv_dtype == BSQ_BF16;
+    const int64_t vb = a.dv_bf16 ? 8 : 16;
+    a.dv_vec = (reinterpret_cast<uintptr_t>(c.dV) | uintptr_t(vb / 4 * c.lddv)) % vb == 0;
+    a.accumulate = c.accumulate;
+    hipError_t e = launch_rows(a, st);
+    for (int64_t v0 = 0; e == hipSuccess && v0 < c.N; v0 += l.vp) {
+        a.v0 = v0;
+        a.vp = std::min(l.vp, (c.N - v0 + VBLK - 1) / VBLK * VBLK);
+        a.first = v0 == 0;
+        if ((e = launch_tokens<EPI_PROB>(a, a.vp, 1, st)) != hipSuccess) break;
+        if ((e = launch_tokens<EPI_DH>(a, c.D, l.hsplit, st)) != hipSuccess) break;
+        if (c.dV) e = launch_gemm_shape<EPI_DV, 8, 4, 2, 4>(a, a.vp, c.D, 1, st);
+    }
+    if (e != hipSuccess || c.T == 0) return e;
+    hipLaunchKernelGGL(xent_dh_kernel, dim3(unsigned(c.T)), dim3(XT), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace bsq
