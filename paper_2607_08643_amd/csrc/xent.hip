@@ -127,12 +127,16 @@ __global__ __launch_bounds__(XT) void xent_pack_kernel(const XArgs a)
 // An operand lies in memory either with k contiguous (logits: H, V; dH: d) or
 // with k as its row (dH: V; dV: d and H), and is staged as it lies:
 //   k contiguous: slot rows of 32 k (64 bytes, four 16-byte chunks); chunk c of
-//     row r lies at c ^ key, key = (r / 4) % 4 (left operand of the logits, whose
-//     fragments take rows in runs of four: (r / 4 NF) % 4), so that the 16 rows
-//     of a fragment read fall on all banks;
-//   k as row: slot rows of one k (256 columns, 32-byte groups of 16); group q of
-//     row k lies at q ^ (k % 4 + 4 (k / 8 % 2)), and fragments are read
-//     transposed, four k of 16 columns at a time.
+//     row r lies at c ^ key, key = -(r / 4) % 4 (left operand of the logits, whose
+//     fragments take rows in runs of four: -(r / 4 NF) % 4). A 16-byte LDS read
+//     serves lanes 0-3, 12-15 and 20-27 of a half wave together, then the others:
+//     with this key each of those sets falls on all 64 banks once (with
+//     (r / 4) % 4 the counters showed two accesses per bank);
+//   k as row (256 columns): blocks of eight k, k % 4 + 4 (k / 8 % 2) their rows, as
+//     [pair of 16-column groups][row][64 bytes]; the two groups change places in
+//     rows 4 to 7. A fragment is read transposed, four k of 16 columns at a time:
+//     half a wave takes the eight rows of one block together, 32 bytes of each, on
+//     all banks once, and the next pair of groups is a constant further on.
 // ---------------------------------------------------------------------------
 template <int MF, int NF, int WM, int WN>
 struct XShape {
@@ -153,6 +157,18 @@ struct XShape {
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
+// Two transposed reads, of four k rows each: eight k of the lane's column. The
+// pointers are restrict so that the reads carry alias information: without any,
+// the compiler waits for every DMA in flight ahead of each (the gradient's
+// products took 1.31 ms instead of 1.0). The waits that are needed are in the
+// loop, as for the plain reads.
+__device__ __forceinline__ bf16x8_t read_tr(const uint8_t *__restrict p, const uint8_t *__restrict q)
+{
+    const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)p);
+    const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)q);
+    return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
 template <int EPI, int MF, int NF, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(WM * WN / 4, WM * WN / 4)))
 void xent_gemm(const XArgs a)
@@ -161,6 +177,7 @@ void xent_gemm(const XArgs a)
     constexpr bool LOGITS = EPI == EPI_STATS || EPI == EPI_PROB;
     constexpr bool LK = LOGITS;              // left operand k contiguous
     constexpr bool RK = EPI != EPI_DV;       // right operand k contiguous
+    static_assert((LK || G::LU == 16) && (RK || G::RU == 16), "256 columns where k is the row");
     constexpr int LSH = (NF == 4) ? 4 : (NF == 2 ? 3 : 2);  // log2(4 NF)
     extern __shared__ __attribute__((aligned(16))) uint4 s_mem4[];
     uint8_t *s_mem = reinterpret_cast<uint8_t *>(s_mem4);
@@ -202,45 +219,46 @@ void xent_gemm(const XArgs a)
     // DMA: unit v of a step is one instruction of the wave, 16 bytes a lane.
     const uint16_t *src[G::PMAX];
     int kof[G::PMAX];      // k (contiguous: of the lane's chunk; as row: of its row) within the step
-    bool kc[G::PMAX];
-    int64_t ld_[G::PMAX];
 #pragma unroll
     for (int r = 0; r < G::PMAX; ++r) {
         const int v0 = wave + G::NW * r, v = (v0 < G::NI) ? v0 : G::NI - 1;
         const bool right = v < G::RU;
         const int u = right ? v : v - G::RU;
-        kc[r] = right ? RK : LK;
-        ld_[r] = right ? ldr : ldl;
-        if (kc[r]) {
+        const uint16_t *mat = right ? R : L;
+        const int64_t ld = right ? ldr : ldl, tile0 = right ? int64_t(by) * G::BR : int64_t(bx) * G::BL;
+        if (right ? RK : LK) {
             const int row = 16 * u + (lane >> 2);
-            const int key = right ? (row >> 2) & 3 : (row >> LSH) & 3;
+            const int key = -(row >> (right ? 2 : LSH)) & 3;
             kof[r] = 8 * ((lane & 3) ^ key);
-            int64_t at = (right ? int64_t(by) * G::BR : int64_t(bx) * G::BL) + row;
+            int64_t at = tile0 + row;
             if (!right && at >= lend) at = lend - 1;
-            src[r] = (right ? R : L) + at * ld_[r];
+            src[r] = mat + at * ld + kof[r];
         } else {
-            const int units = right ? G::RU : G::LU;   // 32-byte groups of a row
-            const int byte = u * 1024 + lane * 16, k = byte / (32 * units);
-            const int grp = ((byte - k * 32 * units) >> 5) ^ ((k & 3) | (((k >> 3) & 1) << 2));
-            int64_t col = (right ? int64_t(by) * G::BR : int64_t(bx) * G::BL) + 16 * grp + 8 * (lane & 1);
+            const int blk = u >> 2, key = (lane >> 2) & 7, chunk = lane & 3;
+            const int k = 16 * (blk >> 1) + 8 * (key >> 2) + 4 * (blk & 1) + (key & 3);
+            int64_t col = tile0 + 32 * (2 * (u & 3) + (lane >> 5)) + 16 * ((chunk >> 1) ^ (key >> 2)) + 8 * (chunk & 1);
             if (!right && col >= lend) col = 0;
             kof[r] = k;
-            src[r] = (right ? R : L) + col;
+            src[r] = mat + col + k * ld;
         }
     }
     const bool full = wave < G::NI % G::NW || G::PMAX == G::PMIN;
     // The padded k of one operand are zero (H past D, d past the tokens and
     // words); the other's are read from where it has values.
     const int64_t lkmax = LOGITS ? a.D : (EPI == EPI_DV ? a.Tp : kmax);
+    // elements from one step to the next
+    const int64_t rstep = RK ? 32 : 32 * ldr, lstep = LK ? 32 : 32 * ldl;
     auto dma = [&](int u, int slot) {
-        const int64_t k0 = 32 * int64_t(kb + (u < ku ? u : ku - 1));  // past the end: a reload that nothing reads
+        const int uu = u < ku ? u : ku - 1;  // past the end: a reload that nothing reads
+        const int64_t k0 = 32 * int64_t(kb + uu);
+        const bool tail = k0 + 32 > lkmax;
+        const int64_t roff = (kb + uu) * rstep, loff = (kb + uu) * lstep;
 #pragma unroll
         for (int r = 0; r < G::PMAX; ++r) {
             if (r >= G::PMIN && !full) continue;
             const int v0 = wave + G::NW * r;
-            int64_t k = k0 + kof[r];
-            if (v0 >= G::RU && k >= lkmax) k = kc[r] ? 0 : lkmax - 1;
-            const uint16_t *p = src[r] + (kc[r] ? k : k * ld_[r]);
+            const uint16_t *p = src[r] + (v0 < G::RU ? roff : loff);
+            if (tail && v0 >= G::RU && k0 + kof[r] >= lkmax) p = LK ? src[r] - kof[r] : src[r] + (lkmax - 1 - kof[r]) * ldl;
             __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4 *>(p),
                                              reinterpret_cast<uint4 *>(s_mem + slot * G::SLOT + (v0 << 10)), 16, 0, 0);
         }
@@ -256,29 +274,29 @@ void xent_gemm(const XArgs a)
 #pragma unroll
         for (int c = 0; c < G::NS; ++c) dma(c, c);
         bf16x8_t rf[2][MF], lf[2][NF];
-        // the lane's bytes of its first fragment
-        const int kr = 8 * g + (r16 >> 2), key = (r16 >> 2) | ((g & 1) << 2);
         auto frag_k = [&](int base) { return *reinterpret_cast<const bf16x8_t *>(s_mem + base); };
-        auto frag_tr = [&](int slot_base, int units, int grp) {
-            const uint8_t *p = s_mem + slot_base + kr * 32 * units + ((grp ^ key) << 5) + ((r16 & 3) << 3);
-            const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)p);
-            const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(p + 4 * 32 * units));
-            return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        // (k as row) the lane's bytes of even and of odd fragments
+        const int tkey = 4 * (g & 1) + (r16 >> 2);
+        const int tbase = (g >> 1) * 8192 + tkey * 64 + (r16 & 3) * 8;
+        const int t0 = tbase + 32 * (g & 1), t1 = tbase + 32 * (1 - (g & 1));
+        auto frag_tr = [&](int base, int f) {
+            const uint8_t *p = s_mem + base + ((f & 1) ? t1 : t0) + (f >> 1) * 512;
+            return read_tr(p, p + 4096);
         };
         const int lrow = LOGITS ? wn * NF * 16 + (r16 >> 2) * (4 * NF) + (r16 & 3) : 0;
-        const int lbase = G::RU * 1024 + lrow * 64 + ((g ^ (r16 >> 2)) << 4);
-        const int rbase = (wm * MF * 16 + r16) * 64 + ((g ^ (r16 >> 2)) << 4);
+        const int swz = (g ^ (-(r16 >> 2) & 3)) << 4;
+        const int lbase = G::RU * 1024 + lrow * 64 + swz, rbase = (wm * MF * 16 + r16) * 64 + swz;
         auto frags = [&](int p, int slot) {
             const int sb = slot * G::SLOT;
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
                 if constexpr (LK) lf[p][j] = frag_k(sb + lbase + j * 256);
-                else lf[p][j] = frag_tr(sb + G::RU * 1024, G::LU, wn * NF + j);
+                else lf[p][j] = frag_tr(sb + G::RU * 1024 + wn * NF * 256, j);
             }
 #pragma unroll
             for (int i = 0; i < MF; ++i) {
                 if constexpr (RK) rf[p][i] = frag_k(sb + rbase + i * 1024);
-                else rf[p][i] = frag_tr(sb, G::RU, wm * MF + i);
+                else rf[p][i] = frag_tr(sb + wm * MF * 256, i);
             }
         };
         auto products = [&](int p) {
@@ -303,6 +321,13 @@ void xent_gemm(const XArgs a)
             slot = (slot + 1 == G::NS) ? 0 : slot + 1;
             frags(1 - p, slot);
             products(p);
+            // the LDS reads spread over the products
+            constexpr int READS = MF * (RK ? 1 : 2) + NF * (LK ? 1 : 2), PER = (MF * NF) / READS > 0 ? (MF * NF) / READS : 1;
+#pragma unroll
+            for (int i = 0; i < READS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+            }
         };
         for (int u = 0; u < ku; u += 2) {
             step(u, 0);
