@@ -18,6 +18,7 @@
 // 64 inputs), and every product runs over those alone.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "gemm_common.h"
 
@@ -248,17 +249,17 @@ void xent_gemm(const XArgs a)
     const int64_t lkmax = LOGITS ? a.D : (EPI == EPI_DV ? a.Tp : kmax);
     // elements from one step to the next
     const int64_t rstep = RK ? 32 : 32 * ldr, lstep = LK ? 32 : 32 * ldl;
-    auto dma = [&](int u, int slot) {
-        const int uu = u < ku ? u : ku - 1;  // past the end: a reload that nothing reads
-        const int64_t k0 = 32 * int64_t(kb + uu);
-        const bool tail = k0 + 32 > lkmax;
-        const int64_t roff = (kb + uu) * rstep, loff = (kb + uu) * lstep;
+    // `ends`: the step may reach past lkmax (its last two do)
+    auto dma = [&](int u, int slot, bool ends) {
+        const int64_t roff = (kb + u) * rstep, loff = (kb + u) * lstep;
+        const bool past = ends && 32 * int64_t(kb + u) + 32 > lkmax;
 #pragma unroll
         for (int r = 0; r < G::PMAX; ++r) {
             if (r >= G::PMIN && !full) continue;
             const int v0 = wave + G::NW * r;
             const uint16_t *p = src[r] + (v0 < G::RU ? roff : loff);
-            if (tail && v0 >= G::RU && k0 + kof[r] >= lkmax) p = LK ? src[r] - kof[r] : src[r] + (lkmax - 1 - kof[r]) * ldl;
+            if (past && v0 >= G::RU && 32 * int64_t(kb + u) + kof[r] >= lkmax)
+                p = LK ? src[r] - kof[r] : src[r] + (lkmax - 1 - kof[r]) * ldl;
             __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4 *>(p),
                                              reinterpret_cast<uint4 *>(s_mem + slot * G::SLOT + (v0 << 10)), 16, 0, 0);
         }
@@ -271,8 +272,7 @@ void xent_gemm(const XArgs a)
         for (int j = 0; j < NF; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
     if (ku > 0) {
-#pragma unroll
-        for (int c = 0; c < G::NS; ++c) dma(c, c);
+        for (int c = 0; c < G::NS && c < ku; ++c) dma(c, c, true);
         bf16x8_t rf[2][MF], lf[2][NF];
         auto frag_k = [&](int base) { return *reinterpret_cast<const bf16x8_t *>(s_mem + base); };
         // (k as row) the lane's bytes of even and of odd fragments
@@ -286,54 +286,69 @@ void xent_gemm(const XArgs a)
         const int lrow = LOGITS ? wn * NF * 16 + (r16 >> 2) * (4 * NF) + (r16 & 3) : 0;
         const int swz = (g ^ (-(r16 >> 2) & 3)) << 4;
         const int lbase = G::RU * 1024 + lrow * 64 + swz, rbase = (wm * MF * 16 + r16) * 64 + swz;
-        auto frags = [&](int p, int slot) {
+        auto read_l = [&](int p, int slot, int j) {
             const int sb = slot * G::SLOT;
+            if constexpr (LK) lf[p][j] = frag_k(sb + lbase + j * 256);
+            else lf[p][j] = frag_tr(sb + G::RU * 1024 + wn * NF * 256, j);
+        };
+        auto read_r = [&](int p, int slot, int i) {
+            const int sb = slot * G::SLOT;
+            if constexpr (RK) rf[p][i] = frag_k(sb + rbase + i * 1024);
+            else rf[p][i] = frag_tr(sb + wm * MF * 256, i);
+        };
+        auto wait_steps = [&](auto n) {  // until at most n steps of DMAs are in flight
+            constexpr int N = decltype(n)::value;
+            if (full) wait_vm<N * G::PMAX>();
+            else wait_vm<N * G::PMIN>();
+        };
+        if (ku >= G::NS) wait_steps(std::integral_constant<int, G::NS - 1>{});
+        else wait_vm<0>();
+        lds_barrier();
 #pragma unroll
-            for (int j = 0; j < NF; ++j) {
-                if constexpr (LK) lf[p][j] = frag_k(sb + lbase + j * 256);
-                else lf[p][j] = frag_tr(sb + G::RU * 1024 + wn * NF * 256, j);
-            }
+        for (int j = 0; j < NF; ++j) read_l(0, 0, j);
+#pragma unroll
+        for (int i = 0; i < MF; ++i) read_r(0, 0, i);
+        int slot = 0;
+        // step u: its fragments are in registers once the barrier's LDS wait is
+        // over, for every wave, so its slot takes step u + NS. A row of products
+        // at a time: the reads of step u + 1 go with the first rows, so that they
+        // are over by the last, the DMAs with the last ones.
+        constexpr int READS = MF + NF, HALF = MF > 1 ? MF / 2 : 1, PER = (READS + HALF - 1) / HALF;
+        auto step = [&](int u, int p, auto inside) {
+            // inside: neither this step's DMAs nor those before are the last
+            constexpr bool IN = decltype(inside)::value;
+            const bool more = IN || u + G::NS < ku;
+            if (more) wait_steps(std::integral_constant<int, G::NS - 2>{});
+            else wait_vm<0>();
+            lds_barrier();
+            const int next = (slot + 1 == G::NS) ? 0 : slot + 1;
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < MF; ++i) {
-                if constexpr (RK) rf[p][i] = frag_k(sb + rbase + i * 1024);
-                else rf[p][i] = frag_tr(sb + wm * MF * 256, i);
-            }
-        };
-        auto products = [&](int p) {
 #pragma unroll
-            for (int i = 0; i < MF; ++i)
+                for (int q = 0; q < PER; ++q) {
+                    const int k = i * PER + q;
+                    if (i >= HALF || k >= READS) continue;
+                    if (k < NF) read_l(1 - p, next, k);
+                    else read_r(1 - p, next, k - NF);
+                }
+                if (i == MF - 1 - (MF > 1) && more) dma(u + G::NS, slot, !IN);
 #pragma unroll
                 for (int j = 0; j < NF; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lf[p][j], rf[p][i], acc[i][j], 0, 0, 0);
-        };
-        if (full) wait_vm<(G::NS - 1) * G::PMAX>();
-        else wait_vm<(G::NS - 1) * G::PMIN>();
-        lds_barrier();
-        frags(0, 0);
-        int slot = 0;
-        // step u: its fragments are in registers once the barrier's LDS wait is
-        // over, for every wave, so its slot takes step u + NS
-        auto step = [&](int u, int p) {
-            if (full) wait_vm<(G::NS - 2) * G::PMAX>();
-            else wait_vm<(G::NS - 2) * G::PMIN>();
-            lds_barrier();
-            dma(u + G::NS, slot);
-            slot = (slot + 1 == G::NS) ? 0 : slot + 1;
-            frags(1 - p, slot);
-            products(p);
-            // the LDS reads spread over the products
-            constexpr int READS = MF * (RK ? 1 : 2) + NF * (LK ? 1 : 2), PER = (MF * NF) / READS > 0 ? (MF * NF) / READS : 1;
-#pragma unroll
-            for (int i = 0; i < READS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            slot = next;
         };
-        for (int u = 0; u < ku; u += 2) {
-            step(u, 0);
-            step(u + 1, 1);
+        int u = 0;
+        for (; u + 1 + G::NS < ku - 2; u += 2) {
+            step(u, 0, std::true_type{});
+            step(u + 1, 1, std::true_type{});
         }
-        wait_vm<0>();  // the reloads land before the ring is used again or the block ends
+        for (; u < ku; u += 2) {
+            step(u, 0, std::false_type{});
+            step(u + 1, 1, std::false_type{});
+        }
     }
 
     const int64_t rbeg = int64_t(by) * G::BR + 16 * (wm * MF) + r16;  // right row of group i: + 16 i
