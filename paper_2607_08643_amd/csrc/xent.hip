@@ -18,6 +18,7 @@
 // 64 inputs), and every product runs over those alone.
 #include <algorithm>
 #include <atomic>
+#include <numeric>
 #include <type_traits>
 
 #include "gemm_common.h"
@@ -58,50 +59,84 @@ struct XArgs {
 };
 
 // ---------------------------------------------------------------------------
-// The rows that have a loss, in order (one block), then their copies.
+// The rows that have a loss, in order, and their copies. Up to ROWS_ONE tokens
+// every block of the copy finds its rows itself; beyond that one block lists
+// them first.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(1024) void xent_rows_kernel(const XArgs a)
+constexpr int XR = 1024;
+constexpr int64_t ROWS_ONE = XR;
+
+// Of XR tokens from m0 on: is the thread's one with a loss, and how many are
+// before it; `all` are added up. (Two barriers.)
+__device__ __forceinline__ bool count_rows(const XArgs &a, int64_t m0, int &before, int &all, bool &bad, int *s_w)
 {
-    __shared__ int s_w[16];
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-    int base = 0;
-    bool bad = false;
-    for (int64_t m0 = 0; m0 < a.T; m0 += 1024) {
-        const int64_t m = m0 + t;
-        const int64_t y = m < a.T ? a.target[m] : -1;
-        const bool live = y >= 0 && y < a.N;
-        bad |= y >= a.N;
-        const uint64_t bal = __ballot(live);
-        if (lane == 0) s_w[w] = __popcll(bal);
-        __syncthreads();
-        int at = base + __popcll(bal & ((uint64_t(1) << lane) - 1)), all = 0;
-        for (int k = 0; k < 16; ++k) {
-            at += (k < w) ? s_w[k] : 0;
-            all += s_w[k];
-        }
-        if (m < a.T) a.pos[m] = live ? at : -1;
-        if (live) a.rows[at] = int32_t(m);
-        base += all;
-        __syncthreads();
+    const int64_t m = m0 + t;
+    const int64_t y = m < a.T ? a.target[m] : -1;
+    const bool live = y >= 0 && y < a.N;
+    bad = y >= a.N;
+    const uint64_t bal = __ballot(live);
+    if (lane == 0) s_w[w] = __popcll(bal);
+    __syncthreads();
+    before = __popcll(bal & ((uint64_t(1) << lane) - 1));
+    all = 0;
+#pragma unroll
+    for (int k = 0; k < XR / 64; ++k) {
+        before += (k < w) ? s_w[k] : 0;
+        all += s_w[k];
     }
-    if (t == 0) a.hdr[0] = base;
-    if (bad && a.err) atomicOr(a.err, BSQ_DEVERR_BAD_SET);
+    __syncthreads();
+    return live;
 }
 
-// One block per compact row: its hidden state padded with zeros, and its
-// target, lse and g.
-__global__ __launch_bounds__(XT) void xent_pack_kernel(const XArgs a)
+__global__ __launch_bounds__(XR) void xent_rows_kernel(const XArgs a)
 {
-    const int64_t i = blockIdx.x;
-    const int live = a.hdr[0];
-    const bool in = i < live;
-    const int64_t m = in ? a.rows[i] : 0;
-    const uint16_t *src = a.H + m * a.ldh;
+    __shared__ int s_w[XR / 64];
+    int base = 0;
+    for (int64_t m0 = 0; m0 < a.T; m0 += XR) {
+        const int64_t m = m0 + threadIdx.x;
+        int before, all;
+        bool bad;
+        const bool live = count_rows(a, m0, before, all, bad, s_w);
+        if (m < a.T) a.pos[m] = live ? base + before : -1;
+        if (live) a.rows[base + before] = int32_t(m);
+        if (bad && a.err) atomicOr(a.err, BSQ_DEVERR_BAD_SET);
+        base += all;
+    }
+    if (threadIdx.x == 0) a.hdr[0] = base;
+}
+
+// Four compact rows a block, 256 threads each: the hidden state padded with
+// zeros, the target, lse and g.
+template <bool ONE>
+__global__ __launch_bounds__(XR) void xent_pack_kernel(const XArgs a)
+{
+    __shared__ int s_w[XR / 64], s_row[XR / XT];
+    const int t = threadIdx.x, sub = t / XT, tt = t % XT;
+    const int64_t first = int64_t(blockIdx.x) * (XR / XT), i = first + sub;
+    int64_t m = -1;
+    if constexpr (ONE) {
+        if (t < XR / XT) s_row[t] = -1;
+        int before, all;
+        bool bad;
+        const bool live = count_rows(a, 0, before, all, bad, s_w);
+        if (live && before >= first && before < first + XR / XT) s_row[before - first] = t;
+        if (blockIdx.x == 0) {
+            if (t < a.T) a.pos[t] = live ? before : -1;
+            if (bad && a.err) atomicOr(a.err, BSQ_DEVERR_BAD_SET);
+            if (t == 0) a.hdr[0] = all;
+        }
+        __syncthreads();
+        m = s_row[sub];
+    } else {
+        m = (i < a.hdr[0]) ? a.rows[i] : -1;
+    }
+    const uint16_t *src = a.H + (m < 0 ? 0 : m) * a.ldh;
     uint16_t *dst = a.Hc + i * a.Dp;
     const bool vec = ((reinterpret_cast<uintptr_t>(a.H) | uintptr_t(2 * a.ldh)) & 15) == 0;
-    for (int64_t c = 8 * threadIdx.x; c < a.Dp; c += 8 * XT) {
+    for (int64_t c = 8 * tt; c < a.Dp; c += 8 * XT) {
         u32x4_t v = u32x4_t{0u, 0u, 0u, 0u};
-        if (in && c < a.D) {  // (D is a multiple of 8)
+        if (m >= 0 && c < a.D) {  // (D is a multiple of 8)
             if (vec) v = *reinterpret_cast<const u32x4_t *>(src + c);
             else
 #pragma unroll
@@ -109,11 +144,11 @@ __global__ __launch_bounds__(XT) void xent_pack_kernel(const XArgs a)
         }
         *reinterpret_cast<u32x4_t *>(dst + c) = v;
     }
-    if (threadIdx.x == 0) {
-        a.tgt[i] = in ? int32_t(a.target[m]) : -1;
+    if (tt == 0) {
+        a.tgt[i] = m >= 0 ? int32_t(a.target[m]) : -1;
         if (a.g) {
-            a.g[i] = in ? a.g_in[m] : 0.0f;
-            a.lse[i] = in ? a.lse_in[m] : 0.0f;
+            a.g[i] = m >= 0 ? a.g_in[m] : 0.0f;
+            a.lse[i] = m >= 0 ? a.lse_in[m] : 0.0f;
         }
     }
 }
@@ -168,6 +203,16 @@ __device__ __forceinline__ bf16x8_t read_tr(const uint8_t *__restrict p, const u
     const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)p);
     const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)q);
     return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Largest value and sum of exponentials against it, joined with another pair.
+// (A pair of no values is -inf and 0.)
+__device__ __forceinline__ void join_stats(float &m, float &s, float m2, float s2)
+{
+    const float mm = m2 > m ? m2 : m;
+    const float ref = (mm == -__builtin_inff()) ? 0.0f : mm;
+    s = s * __builtin_amdgcn_exp2f((m - ref) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - ref) * LOG2E);
+    m = mm;
 }
 
 template <int EPI, int MF, int NF, int WM, int WN>
@@ -385,13 +430,7 @@ void xent_gemm(const XArgs a)
             if (nan) s = __builtin_nanf("");
             // join the four lanes of the token
 #pragma unroll
-            for (int d = 16; d < 64; d <<= 1) {
-                const float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d);
-                const float mm = m2 > m ? m2 : m;
-                const float rr = (mm == -__builtin_inff()) ? 0.0f : mm;
-                s = s * __builtin_amdgcn_exp2f((m - rr) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - rr) * LOG2E);
-                m = mm;
-            }
+            for (int d = 16; d < 64; d <<= 1) join_stats(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
             if (g == 0) {
                 s_max[wn * G::BR + 16 * (wm * MF + i) + r16] = m;
                 s_sum[wn * G::BR + 16 * (wm * MF + i) + r16] = s;
@@ -401,13 +440,7 @@ void xent_gemm(const XArgs a)
         for (int q = t; q < G::BR; q += 64 * G::NW) {
             float m = s_max[q], s = s_sum[q];
 #pragma unroll
-            for (int w = 1; w < WN; ++w) {
-                const float m2 = s_max[w * G::BR + q], s2 = s_sum[w * G::BR + q];
-                const float mm = m2 > m ? m2 : m;
-                const float rr = (mm == -__builtin_inff()) ? 0.0f : mm;
-                s = s * __builtin_amdgcn_exp2f((m - rr) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - rr) * LOG2E);
-                m = mm;
-            }
+            for (int w = 1; w < WN; ++w) join_stats(m, s, s_max[w * G::BR + q], s_sum[w * G::BR + q]);
             const int64_t row = int64_t(by) * G::BR + q;
             if (row < live) a.stat[int64_t(bx) * a.Tp + row] = make_float2(m, s);
         }
@@ -493,34 +526,36 @@ void xent_gemm(const XArgs a)
     }
 }
 
-// A token's tiles joined: 16 tokens a block, 16 threads each over the tiles.
+// A token's tiles joined: TOK tokens a block, XT / TOK threads each over the
+// tiles, their pairs then joined in order. (One block of 16 threads a token took
+// 22 us for 594 tiles, with any number of tokens.)
+template <int TOK>
 __global__ __launch_bounds__(XT) void xent_join_kernel(const XArgs a, int tiles)
 {
-    __shared__ float s_m[16][17], s_s[16][17];
-    const int tok = threadIdx.x & 15, part = threadIdx.x >> 4;
-    const int64_t m = int64_t(blockIdx.x) * 16 + tok;
+    constexpr int PARTS = XT / TOK;
+    __shared__ float s_m[PARTS][TOK + 1], s_s[PARTS][TOK + 1];
+    const int tok = threadIdx.x % TOK, part = threadIdx.x / TOK;
+    const int64_t m = int64_t(blockIdx.x) * TOK + tok;
     const int row = m < a.T ? a.pos[m] : -1;
     float mx = -__builtin_inff(), s = 0.0f;
-    if (row >= 0) {
-        for (int q = part; q < tiles; q += 16) {
+    if (row >= 0)
+#pragma unroll 4
+        for (int q = part; q < tiles; q += PARTS) {
             const float2 v = a.stat[int64_t(q) * a.Tp + row];
-            const float mm = v.x > mx ? v.x : mx;
-            const float rr = (mm == -__builtin_inff()) ? 0.0f : mm;
-            s = s * __builtin_amdgcn_exp2f((mx - rr) * LOG2E) + v.y * __builtin_amdgcn_exp2f((v.x - rr) * LOG2E);
-            mx = mm;
+            join_stats(mx, s, v.x, v.y);
         }
-    }
     s_m[part][tok] = mx;
     s_s[part][tok] = s;
-    __syncthreads();
-    if (part != 0 || m >= a.T) return;
-    for (int q = 1; q < 16; ++q) {
-        const float m2 = s_m[q][tok], s2 = s_s[q][tok];
-        const float mm = m2 > mx ? m2 : mx;
-        const float rr = (mm == -__builtin_inff()) ? 0.0f : mm;
-        s = s * __builtin_amdgcn_exp2f((mx - rr) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - rr) * LOG2E);
-        mx = mm;
+#pragma unroll
+    for (int h = PARTS / 2; h > 0; h >>= 1) {
+        __syncthreads();
+        if (part < h) {
+            join_stats(mx, s, s_m[part + h][tok], s_s[part + h][tok]);
+            s_m[part][tok] = mx;
+            s_s[part][tok] = s;
+        }
     }
+    if (part != 0 || m >= a.T) return;
     const float lse = mx + logf(s);
     a.lse_out[m] = row >= 0 ? lse : 0.0f;
     a.loss_out[m] = row >= 0 ? lse - a.ztgt[row] : 0.0f;
@@ -578,9 +613,12 @@ XLayout xent_layout(bool grad, int64_t T, int64_t N, int64_t D)
     } else {
         l.lse = take(size_t(l.Tp) * 4);
         l.g = take(size_t(l.Tp) * 4);
-        const int64_t most = std::max<int64_t>(1, PIECE_BYTES / (l.Tp * 2 * VBLK));
-        const int64_t pieces = (l.tiles + most - 1) / most;
-        l.vp = (l.tiles + pieces - 1) / pieces * VBLK;
+        // words of a piece: as many as fit, in whole rounds of tiles over the 256
+        // compute units where that leaves one round or more
+        int64_t most = std::max<int64_t>(1, PIECE_BYTES / (l.Tp * 2 * VBLK));
+        const int64_t rt = l.Tp / 256, round = 256 / std::gcd<int64_t>(256, rt);
+        if (most >= round) most = most / round * round;
+        l.vp = std::min(most, l.tiles) * VBLK;
         l.ds = take(size_t(l.Tp) * size_t(l.vp) * 2);
         // splits of dH's depth: until its launch fills the compute units
         const int64_t blocks = (l.Tp / 256) * ((D + 255) / 256);
@@ -645,12 +683,18 @@ XArgs xent_args(const XentCall &c, const XLayout &l)
     return a;
 }
 
-hipError_t launch_rows(const XArgs &a, hipStream_t st)
+// `rows`: the compact rows that the call's tiles read (a multiple of 16)
+hipError_t launch_rows(const XArgs &a, int64_t rows, hipStream_t st)
 {
-    hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, st, a);
+    const dim3 grid(unsigned(rows / (XR / XT)));
+    if (a.T <= ROWS_ONE) {
+        hipLaunchKernelGGL((xent_pack_kernel<true>), grid, dim3(XR), 0, st, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(XR), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(xent_pack_kernel, dim3(unsigned(a.Tp)), dim3(XT), 0, st, a);
+    hipLaunchKernelGGL((xent_pack_kernel<false>), grid, dim3(XR), 0, st, a);
     return hipGetLastError();
 }
 
@@ -668,10 +712,12 @@ hipError_t launch_xent_loss(const XentCall &c, hipStream_t st)
     a.lse_out = c.lse;
     a.v0 = 0;
     a.vp = l.tiles * VBLK;
-    hipError_t e = launch_rows(a, st);
+    hipError_t e = launch_rows(a, c.T <= 16 ? 16 : (c.T <= 32 ? 32 : a.Tp), st);
     if (e != hipSuccess) return e;
     if ((e = launch_tokens<EPI_STATS>(a, a.vp, 1, st)) != hipSuccess) return e;
-    hipLaunchKernelGGL(xent_join_kernel, dim3(unsigned((c.T + 15) / 16)), dim3(XT), 0, st, a, int(l.tiles));
+    // few tokens: a block each; else eight, whose pairs lie next to each other
+    if (c.T < 512) hipLaunchKernelGGL((xent_join_kernel<1>), dim3(unsigned(c.T)), dim3(XT), 0, st, a, int(l.tiles));
+    else hipLaunchKernelGGL((xent_join_kernel<8>), dim3(unsigned((c.T + 7) / 8)), dim3(XT), 0, st, a, int(l.tiles));
     return hipGetLastError();
 }
 
@@ -697,7 +743,7 @@ hipError_t launch_xent_grad(const XentCall &c, hipStream_t st)
     const int64_t vb = a.dv_bf16 ? 8 : 16;
     a.dv_vec = (reinterpret_cast<uintptr_t>(c.dV) | uintptr_t(vb / 4 * c.lddv)) % vb == 0;
     a.accumulate = c.accumulate;
-    hipError_t e = launch_rows(a, st);
+    hipError_t e = launch_rows(a, a.Tp, st);
     for (int64_t v0 = 0; e == hipSuccess && v0 < c.N; v0 += l.vp) {
         a.v0 = v0;
         a.vp = std::min(l.vp, (c.N - v0 + VBLK - 1) / VBLK * VBLK);
