@@ -568,6 +568,7 @@ bsq_status bsq_train_adam(const bsq_config *cfg, const bsq_train_hparams *hp, in
  * results (2^-16 of a value is lost), three for fp32 ones (2^-24).
  * ------------------------------------------------------------------------ */
 #define BSQ_MAX_ADAPTERS 1024
+#define BSQ_ADAPTERS_DIRECT 256
 #define BSQ_MAX_ADAPTER_RANK 128
 
 /* The adapters of one projection, device pointers: A bf16 [n][rank][d_in], B
@@ -585,8 +586,10 @@ typedef struct {
 
 /* A batch's tokens sorted by adapter: made once per batch by
  * bsq_adapters_plan, read by every layer's calls. `ids` is the array that it
- * was made from (device int32 [M]), `buf` the device buffer (16-byte aligned,
- * bsq_adapters_plan_bytes) that it wrote. */
+ * was made from (device int32 [M], unchanged while the plan is used), `buf` the
+ * device buffer (16-byte aligned, bsq_adapters_plan_bytes) that it wrote. Up to
+ * BSQ_ADAPTERS_DIRECT tokens no buffer is needed (NULL): the calls group the
+ * tokens themselves. */
 typedef struct {
     const int32_t *ids;
     void *buf;
@@ -594,12 +597,14 @@ typedef struct {
     int32_t n;
 } bsq_adapter_plan;
 
-/* 1 <= M <= 2^24 tokens, 1 <= n <= BSQ_MAX_ADAPTERS (host only) */
+/* 1 <= M <= 2^24 tokens, 1 <= n <= BSQ_MAX_ADAPTERS (host only); 0 bytes up
+ * to BSQ_ADAPTERS_DIRECT tokens */
 bsq_status bsq_adapters_plan_bytes(int64_t M, int32_t n, size_t *bytes);
 
 /* Write the plan of ids[0 .. M) into plan->buf. A negative id means no
  * adapter; one of n or more too, and ORs BSQ_DEVERR_BAD_SET into *err (device
- * int32 or NULL). */
+ * int32 or NULL). (Up to BSQ_ADAPTERS_DIRECT tokens the ids are checked where
+ * err is given, and nothing else is done.) */
 bsq_status bsq_adapters_plan(const bsq_adapter_plan *plan, size_t buf_bytes, int32_t *err, void *stream);
 
 /* Device workspace of bsq_adapters_apply (back = 0) or bsq_adapters_grad

@@ -9,6 +9,7 @@ the Python function allocates them with torch unless `out=` / `ws=` are given
 from __future__ import annotations
 
 import ctypes as ct
+import functools
 import math
 import os
 from dataclasses import dataclass, field
@@ -689,31 +690,35 @@ def _need(t, dtype, shape, what):
     """t has this dtype and shape and is contiguous."""
     if t.dtype != dtype:
         raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: must be contiguous")
     return t
 
 
-def _row_stride(t, what):
-    """Elements between the rows of a matrix whose rows are contiguous."""
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+def _matrix(t, dtype, shape, what):
+    """A matrix of this dtype and shape whose rows are contiguous; the elements
+    from one row to the next."""
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    rows, cols = shape
+    ld, one = t.stride()
+    if cols > 1 and one != 1:
         raise ValueError(f"{what}: rows must be contiguous")
-    ld = t.stride(0) if rows > 1 else cols
+    if rows < 2:
+        return cols
     if ld < cols:
         raise ValueError(f"{what}: rows overlap")
     return ld
 
 
-def _matrix(t, dtype, shape, what):
-    """A matrix of this dtype and shape with contiguous rows; its row stride."""
-    if t.dtype != dtype:
-        raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
-    return _row_stride(t, what)
+def _workspace(need, dev):
+    """A device buffer of `need` bytes, 256-byte aligned."""
+    t = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    return t if t.data_ptr() % 256 == 0 else _empty_aligned(need, dev)
 
 
 class _Launch:
@@ -758,15 +763,16 @@ class AdapterPool:
         if A.dim() != 3 or B.dim() != 3:
             raise ValueError("A must be [n, rank, d_in] and B [n, d_out, rank]")
         n, rank, d_in = A.shape
+        d_out = B.shape[1]
         _need(A, torch.bfloat16, (n, rank, d_in), "A")
-        _need(B, torch.bfloat16, (n, B.shape[1], rank), "B")
+        _need(B, torch.bfloat16, (n, d_out, rank), "B")
         if scale is not None:
             _need(scale, torch.float32, (n,), "scale")
         if ranks is not None:
             _need(ranks, torch.int32, (n,), "ranks")
         self.device = _device_of((A, B, scale, ranks), "AdapterPool")
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
-        self.n, self.rank, self.d_in, self.d_out = n, rank, d_in, B.shape[1]
+        self.n, self.rank, self.d_in, self.d_out = n, rank, d_in, d_out
 
     def c(self) -> bsq_adapter_pool:
         return bsq_adapter_pool(self.A.data_ptr(), self.B.data_ptr(),
@@ -776,15 +782,17 @@ class AdapterPool:
 
 class AdapterPlan:
     """A batch's tokens sorted by adapter (bsq_adapters_plan), for every
-    layer's calls on that batch."""
+    layer's calls on that batch. buf: None for batches that need none."""
 
-    def __init__(self, ids: torch.Tensor, n: int, buf: torch.Tensor):
-        self.ids, self.n, self.buf, self.M = ids, n, buf, ids.numel()
+    def __init__(self, ids: torch.Tensor, n: int, buf: torch.Tensor | None):
+        self.ids, self.n, self.buf, self.M = ids, n, buf, ids.shape[0]
+        self._c = bsq_adapter_plan(ids.data_ptr(), None if buf is None else buf.data_ptr(), self.M, n)
 
     def c(self) -> bsq_adapter_plan:
-        return bsq_adapter_plan(self.ids.data_ptr(), self.buf.data_ptr(), self.M, self.n)
+        return self._c
 
 
+@functools.lru_cache(maxsize=1024)
 def bsq_adapters_plan_bytes(M: int, n: int) -> int:
     out = ct.c_size_t(0)
     _check(lib().bsq_adapters_plan_bytes(M, n, ct.byref(out)), "bsq_adapters_plan_bytes")
@@ -797,17 +805,22 @@ def bsq_adapters_plan(ids: torch.Tensor, n: int, buf: torch.Tensor | None = None
     negative: none). ids must keep its values while the plan is used."""
     dev = _device_of((ids, buf, err), "bsq_adapters_plan")
     _need(ids, torch.int32, (ids.numel(),), "ids")
-    need = bsq_adapters_plan_bytes(ids.numel(), n)
+    need = bsq_adapters_plan_bytes(ids.shape[0], n)
     with _Launch(dev, stream) as st:
-        if buf is None:
+        if buf is None and need:
             buf = torch.empty(need, dtype=torch.uint8, device=dev)
         plan = AdapterPlan(ids, n, buf)
-        c = plan.c()
-        _check(lib().bsq_adapters_plan(ct.byref(c), buf.numel() * buf.element_size(), _ptr(err), st), "bsq_adapters_plan")
+        _check(lib().bsq_adapters_plan(ct.byref(plan._c), 0 if buf is None else buf.numel() * buf.element_size(), _ptr(err),
+                                       st), "bsq_adapters_plan")
     return plan
 
 
 def bsq_adapters_workspace_bytes(back: bool, M: int, n: int, rank: int, d_in: int, d_out) -> int:
+    return _adapters_workspace(bool(back), M, n, rank, d_in, tuple(d_out))
+
+
+@functools.lru_cache(maxsize=1024)
+def _adapters_workspace(back, M, n, rank, d_in, d_out):
     out = ct.c_size_t(0)
     dims = (ct.c_int64 * len(d_out))(*d_out)
     _check(lib().bsq_adapters_workspace_bytes(int(back), M, n, len(d_out), rank, d_in, dims, ct.byref(out)),
@@ -855,7 +868,7 @@ def bsq_adapters_apply(plan: AdapterPlan, pools, X: torch.Tensor, base, out=None
             raise ValueError(f"{what}: one base per projection")
         y_dtype = base[0].dtype
         ldb = [_matrix(b, y_dtype, (M, d), "base") for b, d in zip(base, dims)]
-    dev = _device_of([plan.buf, X, ws] + [p.A for p in pools] + list(base or []) + list(out or []), what)
+    dev = _device_of([plan.ids, X, ws] + [p.A for p in pools] + list(base or []) + list(out or []), what)
     code = _dtype_code(y_dtype)
     need = bsq_adapters_workspace_bytes(False, M, plan.n, rank, d_in, dims)
     with _Launch(dev, stream) as st:
@@ -865,9 +878,8 @@ def bsq_adapters_apply(plan: AdapterPlan, pools, X: torch.Tensor, base, out=None
         if len(out) != np_:
             raise ValueError(f"{what}: one output per projection")
         t = [torch.empty((M, rank), dtype=torch.float32, device=dev) for _ in dims] if keep else None
-        ws = ws if ws is not None else _empty_aligned(need, dev)
-        c = plan.c()
-        _check(lib().bsq_adapters_apply(ct.byref(c), np_, arr, rank, d_in, _ptr(X), ldx,
+        ws = ws if ws is not None else _workspace(need, dev)
+        _check(lib().bsq_adapters_apply(ct.byref(plan._c), np_, arr, rank, d_in, _ptr(X), ldx,
                                         None if base is None else _pointers(base),
                                         None if base is None else _strides(ldb), _pointers(out), _strides(ldy), code,
                                         None if t is None else _pointers(t), _ptr(ws), ws.numel(), st), what)
@@ -900,7 +912,7 @@ def bsq_adapters_grad(plan: AdapterPlan, pools, X: torch.Tensor, t, dy, base: to
         raise ValueError(f"{what}: accumulate needs grads")
     ldb = 0 if base is None else _matrix(base, torch.bfloat16, (M, d_in), "base")
     more = [] if grads is None else list(grads[0]) + list(grads[1])
-    dev = _device_of([plan.buf, X, base, dx, ws] + [p.A for p in pools] + list(t) + list(dy) + more, what)
+    dev = _device_of([plan.ids, X, base, dx, ws] + [p.A for p in pools] + list(t) + list(dy) + more, what)
     need = bsq_adapters_workspace_bytes(True, M, n, rank, d_in, dims)
     with _Launch(dev, stream) as st:
         if grads is None:
@@ -917,9 +929,8 @@ def bsq_adapters_grad(plan: AdapterPlan, pools, X: torch.Tensor, t, dy, base: to
         if not want_dx:
             dx = None
         lddx = 0 if dx is None else _matrix(dx, dx.dtype, (M, d_in), "dx")
-        ws = ws if ws is not None else _empty_aligned(need, dev)
-        c = plan.c()
-        _check(lib().bsq_adapters_grad(ct.byref(c), np_, arr, rank, d_in, _ptr(X), ldx, _pointers(t), _pointers(dy),
+        ws = ws if ws is not None else _workspace(need, dev)
+        _check(lib().bsq_adapters_grad(ct.byref(plan._c), np_, arr, rank, d_in, _ptr(X), ldx, _pointers(t), _pointers(dy),
                                        _strides(lddy), _ptr(base), ldb, _ptr(dx), lddx,
                                        BSQ_BF16 if dx is None else _dtype_code(dx.dtype), _pointers(dA), _pointers(dB),
                                        int(accumulate), _ptr(ws), ws.numel(), st), what)
@@ -927,6 +938,7 @@ def bsq_adapters_grad(plan: AdapterPlan, pools, X: torch.Tensor, t, dy, base: to
 
 
 # ---------------------------------------------------------------- cross entropy
+@functools.lru_cache(maxsize=1024)
 def bsq_xent_workspace_bytes(grad: bool, T: int, N: int, D: int) -> int:
     out = ct.c_size_t(0)
     _check(lib().bsq_xent_workspace_bytes(int(grad), T, N, D, ct.byref(out)), "bsq_xent_workspace_bytes")
@@ -952,7 +964,7 @@ def bsq_xent_loss(H: torch.Tensor, V: torch.Tensor, target: torch.Tensor, loss=N
     with _Launch(dev, stream) as st:
         loss = torch.empty(T, dtype=torch.float32, device=dev) if loss is None else _need(loss, torch.float32, (T,), "loss")
         lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else _need(lse, torch.float32, (T,), "lse")
-        ws = ws if ws is not None else _empty_aligned(need, dev)
+        ws = ws if ws is not None else _workspace(need, dev)
         _check(lib().bsq_xent_loss(_ptr(H), ldh, _ptr(V), ldv, T, N, D, _ptr(target), _ptr(loss), _ptr(lse), _ptr(err),
                                    _ptr(ws), ws.numel(), st), "bsq_xent_loss")
     return loss, lse
@@ -981,7 +993,7 @@ def bsq_xent_grad(H: torch.Tensor, V: torch.Tensor, target: torch.Tensor, lse: t
         elif dV is None:
             dV = torch.empty((N, D), dtype=torch.bfloat16, device=dev)
         lddv = 0 if dV is None else _matrix(dV, dV.dtype, (N, D), "dV")
-        ws = ws if ws is not None else _empty_aligned(need, dev)
+        ws = ws if ws is not None else _workspace(need, dev)
         _check(lib().bsq_xent_grad(_ptr(H), ldh, _ptr(V), ldv, T, N, D, _ptr(target), _ptr(lse), _ptr(g), _ptr(dH), lddh,
                                    _ptr(dV), lddv, BSQ_BF16 if dV is None else _dtype_code(dV.dtype), int(accumulate),
                                    _ptr(err), _ptr(ws), ws.numel(), st), "bsq_xent_grad")
@@ -1018,7 +1030,7 @@ class GradPlan:
         _check(lib().bsq_clip_table_bytes(count, sizes, ct.byref(need)), "bsq_clip_table_bytes")
         self.tensors, self.outs, self.device = tensors, outs, dev
         with _Launch(dev, stream) as st:
-            self.table = _empty_aligned(need.value, dev)
+            self.table = _workspace(need.value, dev)
             self._c = bsq_clip_plan(self.table.data_ptr(), count, 0)
             _check(lib().bsq_clip_prepare(ct.byref(self._c), self.table.numel(), _pointers(tensors),
                                           None if outs is None else _pointers(outs), sizes, dtypes, st),

@@ -8,12 +8,14 @@
 // cut into tiles of one adapter. Every product is then a small dense one on
 // the matrix cores, whatever the mixture of adapters:
 //
-//   shrink   a tile's t (or u): the long dimension is split over blocks and
-//            waves, whose fp32 partial sums go to the workspace;
-//   expand   sums those in order and adds s B t to a tile's rows of y (A^T u
-//            to those of dx);
-//   outer    dA and dB of a run of one adapter's tokens (a "piece"), whose
-//            partial results are added in order where there are several.
+//   shrink   a tile's t: d_in is split over blocks and waves, whose fp32 partial
+//            sums go to the workspace;
+//   expand   sums those in order and adds s B t to a tile's rows of y;
+//   dy       of a run of one adapter's tokens (a "piece"), dB and the partial
+//            sums of u from one reading of dy;
+//   da, dx   dA of a piece, and A^T u added to a tile's rows of dx.
+//
+// Partial results of an adapter's several pieces are added in order.
 //
 // t and u are held in fp32 and enter the next product as bf16 parts: the value
 // rounded, then what remains, rounded. For bf16 results two parts (2^-16 of the
@@ -27,6 +29,10 @@ namespace bsq {
 namespace {
 
 constexpr int AT = 256;  // threads of a block: 4 waves
+
+// Up to this many tokens a forward call groups them itself, every block from the
+// ids: a plan's launch (5 us) would be a third of a decode step's time.
+constexpr int64_t DIRECT_TOKENS = BSQ_ADAPTERS_DIRECT;
 constexpr int PLAN_WAVES = 16;
 
 struct PlanLayout {
@@ -41,7 +47,7 @@ constexpr int PLAN_HDR = 16;
 PlanLayout plan_layout(int64_t M, int64_t n)
 {
     PlanLayout l{};
-    l.tile = adapters_tile(M);
+    l.tile = (M <= 1024) ? 16 : 64;
     l.piece = std::max<int64_t>(256, (M / 16 + 63) / 64 * 64);
     l.max_tiles = std::min(M, M / l.tile + n + 1);
     l.max_pieces = std::min(M, M / l.piece + n);
@@ -177,7 +183,9 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void adapters_plan_kernel(const Pl
 }
 
 // ---------------------------------------------------------------------------
-// Shared by the products.
+// Shared by the products. A rank is cut into blocks of 16; the blocks of all
+// projections of a group are numbered through (block v: ranks 16 (v % rb) .. of
+// projection v / rb).
 // ---------------------------------------------------------------------------
 struct Proj {
     const uint16_t *A, *B;   // [n][rank][d_in], [n][d_out][rank]
@@ -191,17 +199,18 @@ struct Proj {
 };
 
 struct AdArgs {
-    const int32_t *plan;
+    const int32_t *plan;      // (or NULL: the tokens are grouped from ids)
+    const int32_t *ids;
     PlanLayout l;
     Proj p[BSQ_MAX_GROUP];
     const uint16_t *X;
     const uint16_t *dx0;
     void *dx;
     int64_t M, d_in, ldx, lddx0, lddx;
-    int n, np, rank, rp, ksplit;
-    int y_bf16, dx_bf16, accumulate;
-    float *part;      // [ksplit][np][M][rp]: partial t or u, places in plan order
-    uint16_t *hl;     // [2 np][M][3][rp]: s t (then u) as three bf16 parts
+    int n, np, rank, rb, nv, ksplit, ecols;
+    int accumulate;
+    float *part;      // forward [ksplit][nv][M][16], backward [chunks][nv][M][16]: partial t or u
+    uint16_t *hl;     // [nv][M][3][16]: u as three bf16 parts
     float *slots;     // partial dB and dA
     int64_t slot_floats;
 };
@@ -217,6 +226,8 @@ __device__ __forceinline__ int rank_of(const Proj &p, int a, int rank)
 
 typedef u32x4_t frag_t;
 
+__device__ __forceinline__ frag_t zero_frag() { return frag_t{0u, 0u, 0u, 0u}; }
+
 __device__ __forceinline__ bf16x8_t as_bf16(frag_t v) { return __builtin_bit_cast(bf16x8_t, v); }
 
 __device__ __forceinline__ f32x4_t mfma(frag_t l, frag_t r, f32x4_t c)
@@ -230,9 +241,9 @@ template <bool VEC>
 __device__ __forceinline__ frag_t load8(const uint16_t *p, int64_t valid)
 {
     if constexpr (VEC) {
-        return valid > 0 ? *reinterpret_cast<const frag_t *>(p) : frag_t{0u, 0u, 0u, 0u};
+        return valid > 0 ? *reinterpret_cast<const frag_t *>(p) : zero_frag();
     } else {
-        frag_t v = frag_t{0u, 0u, 0u, 0u};
+        frag_t v = zero_frag();
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (e < valid) v[e >> 1] |= uint32_t(p[e]) << (16 * (e & 1));
@@ -243,7 +254,7 @@ __device__ __forceinline__ frag_t load8(const uint16_t *p, int64_t valid)
 // Eight values stride apart, those from `valid` on as zero.
 __device__ __forceinline__ frag_t load8_strided(const uint16_t *p, int64_t stride, int64_t valid)
 {
-    frag_t v = frag_t{0u, 0u, 0u, 0u};
+    frag_t v = zero_frag();
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (e < valid) v[e >> 1] |= uint32_t(p[e * stride]) << (16 * (e & 1));
@@ -267,317 +278,318 @@ __device__ __forceinline__ void split3(const float (&x)[8], frag_t (&part)[3])
     }
 }
 
+// A tile as a wave sees it: the lane's token (that of a place past the tile's
+// end is its last), its place in t's partial sums, and whether it is the tile's.
+struct TileView {
+    int adapter, count;
+    int64_t token, place;
+    bool live;
+};
+
+// DIRECT (up to DIRECT_TOKENS tokens): block b is the tile whose first token is
+// b, the k-th of its adapter with k a multiple of 16; every wave finds the tile
+// from the ids. Places are tokens. False: there is no such tile.
+template <bool DIRECT, int TG>
+__device__ __forceinline__ bool tile_view(const AdArgs &a, bool with_none, int (*s_tok)[16], TileView &v)
+{
+    const int t = threadIdx.x, lane = t & 63, r16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int b = blockIdx.x;
+    if constexpr (DIRECT) {
+        constexpr int W = int(DIRECT_TOKENS / 64);
+        int id[W];
+        const int raw = a.ids[b];
+        const int mine = (raw >= 0 && raw < a.n) ? raw : -1;
+        if (mine < 0 && !with_none) return false;
+        int before = 0, all = 0, at[W];
+        bool same[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) id[w] = (64 * w + lane < a.M) ? a.ids[64 * w + lane] : -2;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const int one = (id[w] >= a.n || (id[w] < 0 && 64 * w + lane < a.M)) ? -1 : id[w];
+            same[w] = one == mine && 64 * w + lane < a.M;
+            const uint64_t mask = __ballot(same[w]);
+            at[w] = all + __popcll(mask & ((uint64_t(1) << lane) - 1));
+            if ((b >> 6) == w) before = all + __popcll(mask & ((uint64_t(1) << (b & 63)) - 1));
+            all += __popcll(mask);
+        }
+        if (before & 15) return false;
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (same[w] && at[w] >= before && at[w] < before + 16) s_tok[wave][at[w] - before] = 64 * w + lane;
+        v.adapter = mine;
+        v.count = (all - before < 16) ? all - before : 16;
+        v.live = r16 < v.count;
+        __builtin_amdgcn_wave_barrier();
+        v.token = v.place = s_tok[wave][v.live ? r16 : v.count - 1];
+        return true;
+    } else {
+        if (b >= a.plan[with_none ? 1 : 0]) return false;
+        const int4 tile = reinterpret_cast<const int4 *>(a.plan + a.l.tiles)[b];
+        const int tok = (TG == 1 ? 0 : 16 * wave) + r16;
+        v.adapter = tile.x;
+        v.count = tile.z;
+        v.live = tok < tile.z;
+        v.place = tile.y + (v.live ? tok : tile.z - 1);
+        v.token = a.plan[a.l.order + v.place];
+        return true;
+    }
+}
+
 // ---------------------------------------------------------------------------
-// shrink: part[z][p][place][r] = sum over the block's share of the long
-// dimension of W[r][k] S[token][k]; forward S = x and W = A (k contiguous),
-// backward S = dy and W = B^T (STRIDED: k apart by the rank).
-// 16-token tiles: the four waves share the tile and split k. 64-token tiles: a
-// wave per 16 tokens.
+// shrink: part[z][v][place][r] = sum over the block's share of d_in of A[r] x,
+// for VB rank blocks v at a time. 16-token tiles: the four waves share the tile
+// and split d_in. 64-token tiles: a wave per 16 tokens.
 // ---------------------------------------------------------------------------
-template <int RB, bool BACK, bool VEC, int TG>
+template <int VB, bool VEC, int TG, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
 {
-    constexpr int U = (RB >= 4) ? 2 : 4;  // 32-deep steps whose loads are in flight together
-    if (int(blockIdx.x) >= a.plan[0]) return;
-    const int4 tile = reinterpret_cast<const int4 *>(a.plan + a.l.tiles)[blockIdx.x];
-    const Proj &p = a.p[blockIdx.z];
+    constexpr int U = (VB >= 3) ? 4 : 8;  // 32-deep steps whose loads are in flight together
+    __shared__ int s_tok[4][16];
+    __shared__ f32x4_t s_acc[TG == 1 ? 4 : 1][VB][64];
+    TileView tv;
+    if (!tile_view<DIRECT, TG>(a, false, s_tok, tv)) return;
     const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int64_t K = BACK ? p.d_out : a.d_in;
-    const int64_t lds = BACK ? p.ldb : a.ldx;
-    const uint16_t *S = BACK ? static_cast<const uint16_t *>(p.base) : a.X;
-    const int ad = tile.x, re = rank_of(p, ad, a.rank);
-    const uint16_t *W = BACK ? p.B + int64_t(ad) * K * a.rank : p.A + int64_t(ad) * a.rank * K;
+    if (TG != 1 && 16 * wave >= tv.count) return;
+    const int64_t K = a.d_in;
+    const int v0 = int(blockIdx.z) * VB;
     // this wave's range of k, whole steps of 32
     const int64_t nshare = int64_t(a.ksplit) * (TG == 1 ? 4 : 1);
     const int64_t share = int64_t(blockIdx.y) * (TG == 1 ? 4 : 1) + (TG == 1 ? wave : 0);
     const int64_t steps = (K + 31) / 32;
     const int64_t s0 = steps * share / nshare, s1 = steps * (share + 1) / nshare;
-    const int tok = (TG == 1 ? 0 : 16 * wave) + r16;
-    if (TG != 1 && 16 * wave >= tile.z) return;
-    const int place = tile.y + (tok < tile.z ? tok : tile.z - 1);
-    const uint16_t *srow = S + int64_t(a.plan[a.l.order + place]) * lds;
-    f32x4_t acc[RB];
+    const uint16_t *xrow = a.X + tv.token * a.ldx;
+    const uint16_t *arow[VB];
+    bool ain[VB];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) acc[b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int b = 0; b < VB; ++b) {
+        const int v = v0 + b < a.nv ? v0 + b : a.nv - 1, pi = v / a.rb, r = 16 * (v - pi * a.rb) + r16;
+        const Proj &p = a.p[pi];
+        ain[b] = r < rank_of(p, tv.adapter, a.rank);
+        arow[b] = p.A + (int64_t(tv.adapter) * a.rank + (ain[b] ? r : 0)) * K;
+    }
+    f32x4_t acc[VB];
+#pragma unroll
+    for (int b = 0; b < VB; ++b) acc[b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     for (int64_t s = s0; s < s1; s += U) {
-        frag_t x[U], w[U][RB];
+        frag_t x[U], w[U][VB];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t k = 32 * (s + u) + 8 * g, left = (s + u < s1) ? K - k : 0;
-            x[u] = load8<VEC>(srow + k, left);
+            x[u] = load8<VEC>(xrow + k, left);
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int r = 16 * b + r16;
-                const int64_t valid = r < re ? left : 0;
-                if constexpr (BACK) w[u][b] = load8_strided(W + k * a.rank + r, a.rank, valid);
-                else w[u][b] = load8<VEC>(W + r * K + k, valid);
-            }
+            for (int b = 0; b < VB; ++b) w[u][b] = load8<VEC>(arow[b] + k, ain[b] ? left : 0);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int b = 0; b < RB; ++b) acc[b] = mfma(w[u][b], x[u], acc[b]);
+            for (int b = 0; b < VB; ++b) acc[b] = mfma(w[u][b], x[u], acc[b]);
     }
-    // lane: ranks 16 b + 4 g .. + 3 of token r16
+    // lane: ranks 4 g .. + 3 of a block, of token r16
+    float *part = a.part + (int64_t(blockIdx.y) * a.nv * a.M + tv.place) * 16 + 4 * g;
     if constexpr (TG == 1) {
-        __shared__ f32x4_t s_acc[4][RB][64];
 #pragma unroll
-        for (int b = 0; b < RB; ++b) s_acc[wave][b][lane] = acc[b];
+        for (int b = 0; b < VB; ++b) s_acc[wave][b][lane] = acc[b];
         __syncthreads();
-        for (int b = wave; b < RB; b += 4) {
+        for (int b = wave; b < VB; b += 4) {
             f32x4_t v = s_acc[0][b][lane];
 #pragma unroll
             for (int q = 1; q < 4; ++q) v += s_acc[q][b][lane];
-            if (tok < tile.z)
-                *reinterpret_cast<f32x4_t *>(a.part + ((int64_t(blockIdx.y) * a.np + blockIdx.z) * a.M + place) * a.rp +
-                                             16 * b + 4 * g) = v;
+            if (tv.live && v0 + b < a.nv) *reinterpret_cast<f32x4_t *>(part + int64_t(v0 + b) * a.M * 16) = v;
         }
     } else {
-        if (tok < tile.z)
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
-                *reinterpret_cast<f32x4_t *>(a.part + ((int64_t(blockIdx.y) * a.np + blockIdx.z) * a.M + place) * a.rp +
-                                             16 * b + 4 * g) = acc[b];
+        for (int b = 0; b < VB; ++b)
+            if (tv.live && v0 + b < a.nv) *reinterpret_cast<f32x4_t *>(part + int64_t(v0 + b) * a.M * 16) = acc[b];
     }
 }
 
-// Sum over the splits, in order, of eight partial values from rank r on.
-__device__ __forceinline__ void part_sum(const AdArgs &a, int p, int place, int r, float (&v)[8])
+// Sum over `splits` partial sums, in order, of eight values of block v from
+// rank r (0 or 8) on.
+__device__ __forceinline__ void part_sum(const AdArgs &a, int splits, int v, int64_t place, int r, float (&out)[8])
 {
-    const float *q = a.part + (int64_t(p) * a.M + place) * a.rp + r;
-    const int64_t step = int64_t(a.np) * a.M * a.rp;
+    const float *q = a.part + (int64_t(v) * a.M + place) * 16 + r;
+    const int64_t step = int64_t(a.nv) * a.M * 16;
     f32x4_t x = *reinterpret_cast<const f32x4_t *>(q), y = *reinterpret_cast<const f32x4_t *>(q + 4);
-    for (int z = 1; z < a.ksplit; ++z) {
+#pragma unroll 8
+    for (int z = 1; z < splits; ++z) {
         x += *reinterpret_cast<const f32x4_t *>(q + z * step);
         y += *reinterpret_cast<const f32x4_t *>(q + z * step + 4);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        v[e] = x[e];
-        v[4 + e] = y[e];
+        out[e] = x[e];
+        out[4 + e] = y[e];
     }
 }
 
 // ---------------------------------------------------------------------------
-// expand: y = y0 + s B t (or dx = dx0 + sum over projections of A^T u).
-// A block: a tile and 256 columns; a wave: 16 tokens (64-token tiles) over
-// all of them, or 64 columns of all 16. A lane's accumulators are 16
-// consecutive columns of one token (W's rows interleave in runs of four), so
-// y is read and written in whole 16-byte words.
+// Rows of 64 columns of a tile, read and written: lane (g, r16) has columns c +
+// 16 g .. + 15 of its token. WHOLE words where VEC and all 16 exist.
 // ---------------------------------------------------------------------------
-constexpr int EXP_COLS = 256;
+template <bool F32>
+struct Row16 {
+    u32x4_t w[F32 ? 4 : 2];
+};
 
-template <int RB, bool BACK, bool VEC, int TG, bool F32>
+template <bool F32, bool VEC>
+__device__ __forceinline__ Row16<F32> load_row(const void *p, int64_t nc)
+{
+    Row16<F32> v;
+#pragma unroll
+    for (int q = 0; q < (F32 ? 4 : 2); ++q) v.w[q] = zero_frag();
+    if (VEC && nc >= 16) {
+#pragma unroll
+        for (int q = 0; q < (F32 ? 4 : 2); ++q) v.w[q] = static_cast<const u32x4_t *>(p)[q];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (e < nc) {
+                if constexpr (F32) v.w[e >> 2][e & 3] = static_cast<const uint32_t *>(p)[e];
+                else v.w[e >> 3][(e >> 1) & 3] |= uint32_t(static_cast<const uint16_t *>(p)[e]) << (16 * (e & 1));
+            }
+    }
+    return v;
+}
+
+template <bool F32>
+__device__ __forceinline__ float row_value(const Row16<F32> &v, int e)
+{
+    if constexpr (F32) return __uint_as_float(v.w[e >> 2][e & 3]);
+    const uint32_t w = v.w[e >> 3][(e >> 1) & 3];
+    return __uint_as_float((e & 1) ? w & 0xffff0000u : w << 16);
+}
+
+template <bool F32, bool VEC>
+__device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[16])
+{
+    if (VEC && nc >= 16) {
+        if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                static_cast<f32x4_t *>(p)[j] = f32x4_t{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+        } else {
+            u32x4_t w[2];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e >> 2][e & 3] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) static_cast<u32x4_t *>(p)[q] = w[q];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (e < nc) {
+                if constexpr (F32) static_cast<float *>(p)[e] = v[e];
+                else static_cast<uint16_t *>(p)[e] = f32_to_bf16(v[e]);
+            }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// expand: y = y0 + s B t. A block: a tile and a.ecols columns; a wave: 16 tokens
+// (64-token tiles) over all of them, or every fourth 64 columns of all 16. t is
+// summed once; then per 64 columns the wave has y0 and B of the next ones in
+// flight. B's rows interleave in runs of four, so that a lane's sums are 16
+// consecutive columns of its token.
+// ---------------------------------------------------------------------------
+template <int RB, bool VEC, int TG, bool F32, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
 {
-    if (int(blockIdx.x) >= a.plan[1]) return;
-    const int4 tile = reinterpret_cast<const int4 *>(a.plan + a.l.tiles)[blockIdx.x];
+    __shared__ int s_tok[4][16];
+    TileView tv;
+    if (!tile_view<DIRECT, TG>(a, true, s_tok, tv)) return;
     const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const Proj &pz = a.p[BACK ? 0 : blockIdx.z];
-    const int64_t C = BACK ? a.d_in : pz.d_out;
-    const int64_t c0 = int64_t(blockIdx.y) * EXP_COLS + (TG == 1 ? 64 * wave : 0);
-    const int64_t c1 = (TG == 1) ? c0 + 64 : c0 + EXP_COLS;
-    const int tok = (TG == 1 ? 0 : 16 * wave) + r16;
-    if (TG != 1 && 16 * wave >= tile.z) return;
-    if (c0 >= C) return;
-    const void *base = BACK ? static_cast<const void *>(a.dx0) : pz.base;
-    void *out = BACK ? a.dx : pz.y;
-    const int64_t ldb = BACK ? a.lddx0 : pz.ldb, ldo = BACK ? a.lddx : pz.ldy;
-    constexpr bool out_bf16 = !F32, base_bf16 = BACK || !F32;
-    const bool live = tok < tile.z;
-    const int place = tile.y + (live ? tok : tile.z - 1);
-    const int64_t m = a.plan[a.l.order + place];
-    const int ad = tile.x;
-    if (ad < 0 && base == out) {
-        // unchanged rows; t of a token without an adapter is still written below
-        if (BACK || !pz.t || blockIdx.y != 0) return;
+    const Proj &p = a.p[blockIdx.z];
+    const int64_t C = p.d_out;
+    const int64_t cb = int64_t(blockIdx.y) * a.ecols;
+    if (cb >= C || (TG != 1 && 16 * wave >= tv.count)) return;
+    const int64_t c0 = cb + (TG == 1 ? 64 * wave : 0), cstep = (TG == 1) ? 256 : 64;
+    const int64_t c1 = (cb + a.ecols < C) ? cb + a.ecols : C;
+    const int ad = tv.adapter;
+    const bool keep = p.t && blockIdx.y == 0 && (TG != 1 || wave == 0) && tv.live;
+    // rows without an adapter stay as they are in place
+    if (ad < 0 && p.base == p.y && !keep) return;
+    const int re = ad >= 0 ? rank_of(p, ad, a.rank) : 0;
+    constexpr int64_t ES = F32 ? 4 : 2;
+    const char *base = static_cast<const char *>(p.base) + tv.token * p.ldb * ES;
+    char *out = static_cast<char *>(p.y) + tv.token * p.ldy * ES;
+    const uint16_t *B = p.B + int64_t(ad < 0 ? 0 : ad) * C * a.rank;
+    const int r0 = 8 * (g & 1);  // the lane's ranks of a block
+    auto load_b = [&](int64_t c, frag_t (&w)[RB][4]) {
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t cc = c + (r16 >> 2) * 16 + 4 * j + (r16 & 3);
+                const int left = cc < C ? re - 16 * b - r0 : 0;
+                w[b][j] = load8<VEC>(B + cc * a.rank + 16 * b + r0, left);
+                // ranks past the adapter's own hold anything
+                if (VEC && p.ranks && left < 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e >= left) w[b][j][e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+            }
+    };
+    auto load_y = [&](int64_t c) {
+        const int64_t col = c + 16 * g;
+        return load_row<F32, VEC>(base + col * ES, (p.base && tv.live && c < c1) ? C - col : 0);
+    };
+    frag_t w[RB][4];
+    Row16<F32> y0 = load_y(c0);
+    load_b(c0, w);
+    // t in parts: the first and the second share a product (lanes g < 2 the
+    // first), the third, for 32-bit results, has its own
+    frag_t tf[RB], tf3[F32 ? RB : 1];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (ad >= 0) part_sum(a, a.ksplit, int(blockIdx.z) * RB + b, tv.place, r0, v);
+        if (keep && g < 2)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (16 * b + r0 + e < a.rank) p.t[tv.token * a.rank + 16 * b + r0 + e] = v[e];
+        const float sc = ad >= 0 ? scale_of(p, ad) : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= sc;
+        frag_t part[3];
+        split3(v, part);
+        tf[b] = (g < 2) ? part[0] : part[1];
+        if (F32) tf3[b] = (g < 2) ? part[2] : zero_frag();
     }
-    // t or u of the lane's token in two parts: lanes g < 2 the first
-    const int P0 = BACK ? 0 : int(blockIdx.z), P1 = BACK ? a.np : P0 + 1;
-    for (int64_t c = c0; c < c1 && c < C; c += 64) {
+    if (ad < 0 && p.base == p.y) return;
+    for (int64_t c = c0; c < c1; c += cstep) {
         f32x4_t acc[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int pi = P0; pi < P1; ++pi) {
-            const Proj &p = a.p[pi];
-            const int re = ad >= 0 ? rank_of(p, ad, a.rank) : 0;
-            const float sc = ad >= 0 ? scale_of(p, ad) : 0.0f;
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int r0 = 16 * b + 8 * (g & 1);  // the lane's ranks r0 .. + 7
-                // the first part and the second share a product, the third (F32) has its own
-                frag_t tf = frag_t{0u, 0u, 0u, 0u}, tf3 = tf;
-                if constexpr (BACK) {
-                    if (ad >= 0) {
-                        const uint16_t *q = a.hl + (int64_t(a.np + pi) * a.M + place) * 3 * a.rp + r0;
-                        tf = *reinterpret_cast<const frag_t *>(q + (g >> 1) * a.rp);
-                        if (F32 && g < 2) tf3 = *reinterpret_cast<const frag_t *>(q + 2 * a.rp);
-                    }
-                } else {
-                    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                    if (ad >= 0) part_sum(a, pi, place, r0, v);
-                    if (p.t && blockIdx.y == 0 && c == 0 && live && g < 2)
+        for (int b = 0; b < RB; ++b)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (r0 + e < a.rank) p.t[m * a.rank + r0 + e] = v[e];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] *= sc;
-                    frag_t part[3];
-                    split3(v, part);
-                    tf = (g < 2) ? part[0] : part[1];
-                    if (F32 && g < 2) tf3 = part[2];
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int64_t cc = c + (r16 >> 2) * 16 + 4 * j + (r16 & 3);
-                    const int64_t row = cc < C ? cc : C - 1;
-                    frag_t w;
-                    if constexpr (BACK) {
-                        w = load8_strided(p.A + (int64_t(ad < 0 ? 0 : ad) * a.rank + r0) * C + row, C, re - r0);
-                    } else {
-                        w = load8<VEC>(p.B + (int64_t(ad < 0 ? 0 : ad) * C + row) * a.rank + r0,
-                                       VEC && r0 < re ? 8 : re - r0);
-                        // ranks past the adapter's own hold anything
-                        if (VEC && p.ranks && re - r0 < 8)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (e >= re - r0) w[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
-                    }
-                    if (F32) acc[j] = mfma(w, tf3, acc[j]);
-                    acc[j] = mfma(w, tf, acc[j]);
-                }
+            for (int j = 0; j < 4; ++j) {
+                if (F32) acc[j] = mfma(w[b][j], tf3[b], acc[j]);
+                acc[j] = mfma(w[b][j], tf[b], acc[j]);
             }
-        }
-        // lane: columns c + 16 g .. + 15 of its token
-        if (!live) continue;
-        const int64_t col = c + 16 * g;
-        if (col >= C) continue;
-        const int64_t nc = C - col < 16 ? C - col : 16;
         float v[16];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[4 * j + r] = acc[j][r];
-        const bool whole = VEC && nc == 16;
-        if (base) {
-            if (base_bf16) {
-                const uint16_t *q = static_cast<const uint16_t *>(base) + m * ldb + col;
-                if (whole) {
-                    const frag_t w[2] = {reinterpret_cast<const frag_t *>(q)[0], reinterpret_cast<const frag_t *>(q)[1]};
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        v[2 * e] += __uint_as_float(w[e >> 2][e & 3] << 16);
-                        v[2 * e + 1] += __uint_as_float(w[e >> 2][e & 3] & 0xffff0000u);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (e < nc) v[e] += bf16_to_f32(q[e]);
-                }
-            } else {
-                const float *q = static_cast<const float *>(base) + m * ldb + col;
-                if (whole) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const f32x4_t w = reinterpret_cast<const f32x4_t *>(q)[j];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) v[4 * j + r] += w[r];
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (e < nc) v[e] += q[e];
-                }
-            }
+        for (int e = 0; e < 16; ++e) v[e] = row_value<F32>(y0, e) + acc[e >> 2][e & 3];
+        const int64_t col = c + 16 * g;
+        if (c + cstep < c1) {
+            y0 = load_y(c + cstep);
+            load_b(c + cstep, w);
         }
-        if (out_bf16) {
-            uint16_t *q = static_cast<uint16_t *>(out) + m * ldo + col;
-            if (whole) {
-                frag_t w[2];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e >> 2][e & 3] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-                reinterpret_cast<frag_t *>(q)[0] = w[0];
-                reinterpret_cast<frag_t *>(q)[1] = w[1];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (e < nc) q[e] = f32_to_bf16(v[e]);
-            }
-        } else {
-            float *q = static_cast<float *>(out) + m * ldo + col;
-            if (whole) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    reinterpret_cast<f32x4_t *>(q)[j] = f32x4_t{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (e < nc) q[e] = v[e];
-            }
-        }
+        if (tv.live && col < C) store_row<F32, VEC>(out + col * ES, C - col, v);
     }
 }
 
 // ---------------------------------------------------------------------------
-// Backward: s t and u in three bf16 parts, in plan order, zero past an adapter's
-// rank. One thread per eight ranks of a token; z: projection.
+// Transposed reads of LDS tiles of 16-bit values: eight rows (k) of the lane's
+// column, two reads of four.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(AT) void adapters_parts(const AdArgs a)
-{
-    const int groups = a.rp / 8;
-    const int64_t i = int64_t(blockIdx.x) * AT + threadIdx.x;
-    const int64_t place = i / groups;
-    const int r0 = int(i - place * groups) * 8;
-    const int32_t *seg = a.plan + a.l.seg;
-    if (place >= seg[a.n]) return;
-    // its adapter: the last whose first place is not past it
-    int lo = 0, hi = a.n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (seg[mid] <= place) lo = mid;
-        else hi = mid;
-    }
-    const int ad = lo, pi = blockIdx.z;
-    const Proj &p = a.p[pi];
-    const int re = rank_of(p, ad, a.rank);
-    const float sc = scale_of(p, ad);
-    const int64_t m = a.plan[a.l.order + place];
-    float v[8];
-    frag_t part[3];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {  // s t, then u
-        if (h == 1) part_sum(a, pi, int(place), r0, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = (r0 + e < re) ? sc * (h == 0 ? p.t[m * a.rank + r0 + e] : v[e]) : 0.0f;
-        split3(v, part);
-        uint16_t *q = a.hl + (int64_t(h * a.np + pi) * a.M + place) * 3 * a.rp + r0;
-#pragma unroll
-        for (int k = 0; k < 3; ++k) *reinterpret_cast<frag_t *>(q + k * a.rp) = part[k];
-    }
-}
-
-// ---------------------------------------------------------------------------
-// outer: of a piece's tokens, G[c][r] = sum_m S[m][c] Q[m][r]: dB (S = dy, Q =
-// s t) or dA transposed (S = x, Q = u). A wave owns 64 columns. Per step of 32
-// tokens it stages its 32 x 64 of S in LDS and the block stages Q's three parts;
-// both are read transposed, as operands with the tokens along the product's
-// depth. blockIdx.z: 2 projection + (1 for dA).
-//
-// LDS rows of S: 64 columns, 128 bytes, in 32-byte groups; group q of row k
-// lies at q ^ key(k), so that the eight rows that half a wave reads together
-// fall on different banks.
-// ---------------------------------------------------------------------------
-constexpr int OUT_COLS = 256;
-
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
-// 8 tokens (rows k0 .. k0 + 7 of 16-column groups) of the lane's column: two
-// transposed reads of four rows. p: the lane's own 8 bytes of the first row
-// group (row 8 g + r16 / 4, columns 4 (r16 % 4) ..), four: bytes of four rows.
 __device__ __forceinline__ frag_t read_tr(const uint8_t *p, int four)
 {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -586,63 +598,221 @@ __device__ __forceinline__ frag_t read_tr(const uint8_t *p, int four)
     return frag_t{a[0], a[1], b[0], b[1]};
 }
 
-template <int RB, bool VEC>
-__global__ __launch_bounds__(AT) void adapters_outer(const AdArgs a)
+// ---------------------------------------------------------------------------
+// dx: dx = dx0 + sum over the projections of A^T u. A block: a tile and 256
+// columns; a wave: 16 tokens (or 64 of the columns). Per rank block the 16 x 256
+// of A are staged in LDS (two blocks of eight ranks, [pair of 16-column
+// groups][rank][64 bytes], the groups swapped in ranks 8 to 15: the rows that
+// half a wave reads together fall on all banks once) and read transposed. The
+// columns are permuted on the way in so that a lane's sums are 16 consecutive
+// ones.
+// ---------------------------------------------------------------------------
+template <bool VEC, int TG, bool F32>
+__global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 {
+    constexpr int NC = (TG == 1) ? 1 : 4;  // 64-column groups of a wave
+    __shared__ __attribute__((aligned(16))) uint8_t s_a[2][8192];
+    TileView tv;
+    if (!tile_view<false, TG>(a, true, nullptr, tv)) return;
+    const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int64_t C = a.d_in, cb = int64_t(blockIdx.y) * 256;
+    const int ad = tv.adapter;
+    if (ad < 0 && a.dx0 == a.dx) return;
+    const int64_t c0 = cb + (TG == 1 ? 64 * wave : 0);
+    // (a wave without tokens helps to stage)
+    const bool idle = TG != 1 && 16 * wave >= tv.count;
+    Row16<false> x0[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int64_t col = c0 + 64 * c + 16 * g;
+        x0[c] = load_row<false, VEC>(a.dx0 + tv.token * a.lddx0 + col, (a.dx0 && tv.live) ? C - col : 0);
+    }
+    f32x4_t acc[NC][4];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[c][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    if (ad >= 0) {
+        frag_t st[2];
+        auto fetch = [&](int v) {
+            const int pi = v / a.rb, b = v - pi * a.rb;
+            const Proj &p = a.p[pi];
+            const int re = rank_of(p, ad, a.rank);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int w = t + AT * q, r = 16 * b + (w >> 5);
+                const int64_t col = cb + 8 * (w & 31);
+                st[q] = load8<VEC>(p.A + (int64_t(ad) * a.rank + r) * C + col, r < re ? C - col : 0);
+            }
+        };
+        fetch(0);
+        const int key = 4 * (g & 1) + (r16 >> 2);
+        const int t0 = key * 64 + 8 * (r16 & 3) + 32 * (g & 1), t1 = t0 ^ 32;
+        for (int v = 0; v < a.nv; ++v) {
+            uint8_t *sa = s_a[v & 1];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                // rank k, columns 8 cc ..: quads (i, j) and (i, j + 1) of 64-column group cc / 8
+                const int w = t + AT * q, k = w >> 5, cc = w & 31, kk = 4 * (k >> 3) + (k & 3);
+                const int i = (cc & 7) >> 1, f = 4 * (cc >> 3) + 2 * (cc & 1);
+                uint8_t *d = sa + ((k >> 2) & 1) * 4096 + (f >> 1) * 512 + kk * 64 + 8 * i;
+                const int swap = 32 * (kk >> 2);
+                *reinterpret_cast<uint2 *>(d + swap) = make_uint2(st[q][0], st[q][1]);
+                *reinterpret_cast<uint2 *>(d + (32 - swap)) = make_uint2(st[q][2], st[q][3]);
+            }
+            __syncthreads();  // (the buffer of v is written again at v + 2, past v + 1's barrier)
+            if (v + 1 < a.nv) fetch(v + 1);
+            if (idle) continue;
+            const uint16_t *q = a.hl + (int64_t(v) * a.M + tv.place) * 48 + 8 * (g & 1);
+            const frag_t uf = *reinterpret_cast<const frag_t *>(q + 16 * (g >> 1));
+            const frag_t u3 = (F32 && g < 2) ? *reinterpret_cast<const frag_t *>(q + 32) : zero_frag();
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int f = 4 * c + j;
+                    const frag_t w = read_tr(sa + (TG == 1 ? wave * 1024 : 0) + ((f & 1) ? t1 : t0) + (f >> 1) * 512, 4096);
+                    if (F32) acc[c][j] = mfma(w, u3, acc[c][j]);
+                    acc[c][j] = mfma(w, uf, acc[c][j]);
+                }
+        }
+    }
+    if (!tv.live) return;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int64_t col = c0 + 64 * c + 16 * g;
+        if (col >= C) continue;
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = row_value<false>(x0[c], e) + acc[c][e >> 2][e & 3];
+        store_row<F32, VEC>(static_cast<char *>(a.dx) + (tv.token * a.lddx + col) * (F32 ? 4 : 2), C - col, v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// dy pass: of a piece's tokens, dB[c][r] = sum_m dy[m][c] (s t)[m][r] and the
+// partial u[m][r] = sum over the block's 256 columns of dy[m][c] B[c][r], from
+// one reading of dy. A wave owns 64 columns. Per step of 32 tokens it stages its
+// 32 x 64 of dy in LDS and the block stages s t in three parts. For dB both are
+// read transposed (tokens along the depth); for u dy is read as it lies, and the
+// wave's 64 x rank of B^T stay in registers for the whole piece.
+//
+// LDS rows of dy: 64 columns, 128 bytes, in 32-byte groups; group q of row k
+// lies at q ^ key(k), so that the eight rows that half a wave reads together
+// fall on different banks.
+// ---------------------------------------------------------------------------
+constexpr int OUT_COLS = 256;
+
+__device__ __forceinline__ int out_key(int k) { return ((k >> 1) & 1) | (((k >> 3) & 1) << 1); }
+
+// The wave's 32 rows x 64 columns from k0 of the piece on: lane -> row lane / 8
+// (+ 8 i), columns c + 8 (lane % 8) ..
+template <bool VEC>
+__device__ __forceinline__ void out_fetch(const uint16_t *S, int64_t ld, const int32_t *order, int k0, int count, int64_t c,
+                                          int64_t C, frag_t (&sv)[4])
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t col = c + 8 * (lane & 7);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = k0 + 8 * i + (lane >> 3);
+        const bool in = k < count;
+        sv[i] = load8<VEC>(S + int64_t(order[in ? k : 0]) * ld + col, in ? C - col : 0);
+    }
+}
+
+__device__ __forceinline__ void out_stage(uint8_t *ss, const frag_t (&sv)[4])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = 8 * i + (lane >> 3);
+        *reinterpret_cast<frag_t *>(ss + k * 128 + ((((lane & 7) >> 1) ^ out_key(k)) << 5) + ((lane & 1) << 4)) = sv[i];
+    }
+}
+
+// Where a piece's result goes: the gradient itself (an adapter's only piece), or
+// its slot.
+struct OutPlace {
+    float *to;
+    bool add;
+};
+
+__device__ __forceinline__ OutPlace out_place(const AdArgs &a, const int4 &piece, int pi, bool is_a)
+{
+    const Proj &p = a.p[pi];
+    if (piece.w < 0) return {(is_a ? p.dA : p.dB) + int64_t(piece.x) * a.rank * (is_a ? a.d_in : p.d_out), a.accumulate != 0};
+    float *o = a.slots + int64_t(piece.w) * a.slot_floats + (is_a ? int64_t(a.rank) * p.d_out : 0);
+    for (int q = 0; q < pi; ++q) o += int64_t(a.rank) * (a.p[q].d_out + a.d_in);
+    return {o, false};
+}
+
+template <int RB, bool VEC>
+__global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
+{
+    constexpr int RP = 16 * RB;
     __shared__ __attribute__((aligned(16))) uint8_t s_s[4][32 * 128];
-    __shared__ __attribute__((aligned(16))) uint8_t s_q[32 * 3 * RB * 32];  // [32][3][16 RB] bf16
+    __shared__ __attribute__((aligned(16))) uint8_t s_q[32 * 96 * RB];   // [32][3][RP] bf16
+    __shared__ __attribute__((aligned(16))) float s_u[4][32][RP + 4];
     if (int(blockIdx.x) >= a.plan[2]) return;
     const int4 piece = reinterpret_cast<const int4 *>(a.plan + a.l.pieces)[blockIdx.x];
-    const int pi = int(blockIdx.z) >> 1, is_a = int(blockIdx.z) & 1;
+    const int pi = blockIdx.z;
     const Proj &p = a.p[pi];
-    const int64_t C = is_a ? a.d_in : p.d_out;
-    const int64_t cb = int64_t(blockIdx.y) * OUT_COLS;
+    const int64_t C = p.d_out, cb = int64_t(blockIdx.y) * OUT_COLS;
     if (cb >= C) return;
     const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t c0 = cb + 64 * wave;
-    const uint16_t *S = is_a ? a.X : static_cast<const uint16_t *>(p.base);
-    const int64_t lds = is_a ? a.ldx : p.ldb;
-    const uint16_t *Q = a.hl + (int64_t(is_a ? a.np + pi : pi) * a.M + piece.y) * 3 * a.rp;
+    const uint16_t *S = static_cast<const uint16_t *>(p.base);
     const int32_t *order = a.plan + a.l.order + piece.y;
+    const int re = rank_of(p, piece.x, a.rank);
+    const float sc = scale_of(p, piece.x);
+    // B^T of the wave's columns: rank 16 b + r16, columns c0 + 32 h + 8 g ..
+    frag_t bt[2][RB];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            const int64_t c = c0 + 32 * h + 8 * g;
+            const int r = 16 * b + r16;
+            bt[h][b] = load8_strided(p.B + (int64_t(piece.x) * C + c) * a.rank + r, a.rank, r < re ? C - c : 0);
+        }
     f32x4_t acc[4][RB];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int b = 0; b < RB; ++b) acc[i][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     uint8_t *ss = s_s[wave];
-    // staging: lane -> row lane / 8 (+ 8 i), columns 8 (lane % 8) ..
-    const int64_t sc = c0 + 8 * (lane & 7);
-    constexpr int QW = 6 * RB, QV = (32 * QW + AT - 1) / AT;  // 16-byte words of a row of Q, and per thread
-    frag_t sv[4], qv[QV];
+    // s t: eight ranks of a row a thread
+    constexpr int QV = (64 * RB + AT - 1) / AT;
+    frag_t sv[4];
+    float qv[QV][8];
     auto fetch = [&](int k0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = k0 + 8 * i + (lane >> 3);
-            const bool in = k < piece.z;
-            const int64_t m = order[in ? k : 0];
-            sv[i] = load8<VEC>(S + m * lds + sc, in ? C - sc : 0);
-        }
+        out_fetch<VEC>(S, p.ldb, order, k0, piece.z, c0, C, sv);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
-            const int w = t + AT * q, row = w / QW;
+            const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
             const bool in = row < 32 && k0 + row < piece.z;
-            qv[q] = in ? reinterpret_cast<const frag_t *>(Q + int64_t(k0) * 3 * a.rp)[w] : frag_t{0u, 0u, 0u, 0u};
+            const float *tr = p.t + int64_t(order[in ? k0 + row : 0]) * a.rank + r;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) qv[q][e] = (in && r + e < re) ? sc * tr[e] : 0.0f;
         }
     };
     fetch(0);
-    // the lane's row in a transposed read: 8 g + r16 / 4 (+ 4)
-    const int kr = 8 * g + (r16 >> 2), key = ((kr >> 1) & 1) | (((kr >> 3) & 1) << 1);
+    const int kr = 8 * g + (r16 >> 2), key = out_key(kr);  // the lane's row in a transposed read
     for (int k0 = 0; k0 < piece.z; k0 += 32) {
         __syncthreads();  // the last step's reads are over
+        out_stage(ss, sv);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = 8 * i + (lane >> 3), kk = ((k >> 1) & 1) | (((k >> 3) & 1) << 1);
-            *reinterpret_cast<frag_t *>(ss + k * 128 + ((((lane & 7) >> 1) ^ kk) << 5) + ((lane & 1) << 4)) = sv[i];
+        for (int q = 0; q < QV; ++q) {
+            const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
+            if (row >= 32) continue;
+            frag_t part[3];
+            split3(qv[q], part);
+#pragma unroll
+            for (int h = 0; h < 3; ++h) *reinterpret_cast<frag_t *>(s_q + row * 96 * RB + h * 32 * RB + 2 * r) = part[h];
         }
-#pragma unroll
-        for (int q = 0; q < QV; ++q)
-            if (t + AT * q < 32 * QW) reinterpret_cast<frag_t *>(s_q)[t + AT * q] = qv[q];
         __syncthreads();
         if (k0 + 32 < piece.z) fetch(k0 + 32);
         frag_t sf[4];
@@ -657,33 +827,153 @@ __global__ __launch_bounds__(AT) void adapters_outer(const AdArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[i][b] = mfma(sf[i], qf, acc[i][b]);
             }
+        // u of 32 tokens over the wave's columns
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int row = 16 * m + r16;
+            frag_t rf[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                rf[h] = *reinterpret_cast<const frag_t *>(ss + row * 128 + (((2 * h + (g >> 1)) ^ out_key(row)) << 5) + ((g & 1) << 4));
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                f32x4_t u = mfma(bt[0][b], rf[0], f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
+                u = mfma(bt[1][b], rf[1], u);
+                *reinterpret_cast<f32x4_t *>(&s_u[wave][row][16 * b + 4 * g]) = u;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 2 * RB; ++q) {
+            const int w = t + AT * q, row = w / RP, r = w - row * RP;
+            if (k0 + row >= piece.z) continue;
+            const float u = (s_u[0][row][r] + s_u[1][row][r]) + (s_u[2][row][r] + s_u[3][row][r]);
+            a.part[((int64_t(blockIdx.y) * a.nv + pi * RB + (r >> 4)) * a.M + piece.y + k0 + row) * 16 + (r & 15)] = u;
+        }
     }
     // lane: columns c0 + 16 i + 4 g .. + 3 at rank 16 b + r16
-    const int64_t R = a.rank;
-    float *out;
-    bool add = false;
-    if (piece.w < 0) {
-        out = is_a ? p.dA : p.dB;
-        out += int64_t(piece.x) * R * C;
-        add = a.accumulate;
-    } else {
-        out = a.slots + int64_t(piece.w) * a.slot_floats;
-        for (int q = 0; q < pi; ++q) out += R * (a.p[q].d_out + a.d_in);
-        out += is_a ? R * p.d_out : 0;
-    }
+    const OutPlace o = out_place(a, piece, pi, false);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
-            const int64_t r = 16 * b + r16, c = c0 + 16 * i + 4 * g;
-            if (r >= R) continue;
+            const int r = 16 * b + r16;
+            const int64_t c = c0 + 16 * i + 4 * g;
+            if (r >= a.rank) continue;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (c + e >= C) break;
-                float *q = is_a ? out + r * C + c + e : out + (c + e) * R + r;
-                *q = add ? *q + acc[i][b][e] : acc[i][b][e];
+                float *q = o.to + (c + e) * a.rank + r;
+                *q = o.add ? *q + acc[i][b][e] : acc[i][b][e];
             }
         }
+}
+
+// u = s times the partial sums in order, in three bf16 parts, zero past an
+// adapter's rank. One thread per eight ranks of a token; z: projection.
+__global__ __launch_bounds__(AT) void adapters_parts(const AdArgs a)
+{
+    const int groups = 2 * a.rb;
+    const int64_t i = int64_t(blockIdx.x) * AT + threadIdx.x;
+    const int64_t place = i / groups;
+    const int r = int(i - place * groups) * 8;
+    const int32_t *seg = a.plan + a.l.seg;
+    if (place >= seg[a.n]) return;
+    // its adapter: the last whose first place is not past it
+    int lo = 0, hi = a.n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (seg[mid] <= place) lo = mid;
+        else hi = mid;
+    }
+    const int pi = blockIdx.z, v = pi * a.rb + (r >> 4);
+    const Proj &p = a.p[pi];
+    const int re = rank_of(p, lo, a.rank);
+    const float sc = scale_of(p, lo);
+    float x[8];
+    part_sum(a, int((p.d_out + OUT_COLS - 1) / OUT_COLS), v, place, r & 8, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (r + e < re) ? sc * x[e] : 0.0f;
+    frag_t part[3];
+    split3(x, part);
+    uint16_t *q = a.hl + (int64_t(v) * a.M + place) * 48 + (r & 8);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<frag_t *>(q + 16 * k) = part[k];
+}
+
+// ---------------------------------------------------------------------------
+// dA: of a piece's tokens, dA[r][c] = sum_m u[m][r] x[m][c], for VB rank blocks
+// of the group from one reading of x; staged and read as dB's operands.
+// ---------------------------------------------------------------------------
+template <int VB, bool VEC>
+__global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t s_s[4][32 * 128];
+    __shared__ __attribute__((aligned(16))) uint8_t s_q[VB][32 * 96];  // [32][3][16] bf16 each
+    if (int(blockIdx.x) >= a.plan[2]) return;
+    const int4 piece = reinterpret_cast<const int4 *>(a.plan + a.l.pieces)[blockIdx.x];
+    const int64_t C = a.d_in, cb = int64_t(blockIdx.y) * OUT_COLS;
+    const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int64_t c0 = cb + 64 * wave;
+    const int v0 = int(blockIdx.z) * VB;
+    const int32_t *order = a.plan + a.l.order + piece.y;
+    f32x4_t acc[4][VB];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int b = 0; b < VB; ++b) acc[i][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    uint8_t *ss = s_s[wave];
+    constexpr int QW = 192 * VB, QV = (QW + AT - 1) / AT;  // 16-byte words of u's parts
+    frag_t sv[4], qv[QV];
+    auto fetch = [&](int k0) {
+        out_fetch<VEC>(a.X, a.ldx, order, k0, piece.z, c0, C, sv);
+#pragma unroll
+        for (int q = 0; q < QV; ++q) {
+            const int w = t + AT * q, b = w / 192, x = w - 192 * b, row = x / 6;
+            const bool in = w < QW && v0 + b < a.nv && k0 + row < piece.z;
+            qv[q] = in ? reinterpret_cast<const frag_t *>(a.hl + (int64_t(v0 + b) * a.M + piece.y + k0) * 48)[x] : zero_frag();
+        }
+    };
+    fetch(0);
+    const int kr = 8 * g + (r16 >> 2), key = out_key(kr);
+    for (int k0 = 0; k0 < piece.z; k0 += 32) {
+        __syncthreads();  // the last step's reads are over
+        out_stage(ss, sv);
+#pragma unroll
+        for (int q = 0; q < QV; ++q)
+            if (t + AT * q < QW) reinterpret_cast<frag_t *>(s_q)[t + AT * q] = qv[q];
+        __syncthreads();
+        if (k0 + 32 < piece.z) fetch(k0 + 32);
+        frag_t sf[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sf[i] = read_tr(ss + kr * 128 + ((i ^ key) << 5) + ((r16 & 3) << 3), 4 * 128);
+#pragma unroll
+        for (int b = 0; b < VB; ++b)
+#pragma unroll
+            for (int h = 0; h < 3; ++h) {
+                const frag_t qf = read_tr(s_q[b] + kr * 96 + h * 32 + ((r16 & 3) << 3), 4 * 96);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][b] = mfma(sf[i], qf, acc[i][b]);
+            }
+    }
+#pragma unroll
+    for (int b = 0; b < VB; ++b) {
+        const int v = v0 + b;
+        if (v >= a.nv) break;
+        const int pi = v / a.rb, r = 16 * (v - pi * a.rb) + r16;
+        if (r >= a.rank) continue;
+        const OutPlace o = out_place(a, piece, pi, true);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t c = c0 + 16 * i + 4 * g;
+            float *q = o.to + int64_t(r) * C + c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < C) q[e] = o.add ? q[e] + acc[i][b][e] : acc[i][b][e];
+        }
+    }
 }
 
 // Adapters of several pieces: their sum in order; of none: zero. One block per
@@ -719,53 +1009,84 @@ __global__ __launch_bounds__(AT) void adapters_pieces(const AdArgs a)
 // ---------------------------------------------------------------------------
 struct AdLayout {
     int ksplit;
-    size_t part, hl, slots, total;
+    size_t part, hl, slots, plan, total;
     int64_t slot_floats;
 };
 
-// Ranks of a row of t in the workspace: one, two, four or eight blocks of 16.
-int rank_pad(int rank) { return rank <= 16 ? 16 : (rank <= 32 ? 32 : (rank <= 64 ? 64 : 128)); }
+// Rank blocks of 16 of a projection: one, two, four or eight.
+int rank_blocks(int rank) { return rank <= 16 ? 1 : (rank <= 32 ? 2 : (rank <= 64 ? 4 : 8)); }
 
-// Splits of a shrink's long dimension (the longest of the group): until the
-// launch has about 2048 blocks, each wave keeping 128 or more of it.
-int shrink_splits(int64_t tiles, int np, int64_t K, bool split_waves)
+// Rank blocks that a launch over x takes at once, of nv.
+int blocks_at_once(int nv) { return nv <= 4 ? nv : (nv % 3 == 0 ? 3 : 4); }
+
+// Splits of d_in: until the launch has about 2048 blocks, each wave keeping
+// 128 or more of it.
+int shrink_splits(int64_t tiles, int groups, int64_t K, bool split_waves)
 {
     const int64_t most = std::max<int64_t>(1, K / (split_waves ? 512 : 128));
-    return int(std::clamp<int64_t>(2048 / std::max<int64_t>(1, tiles * np), 1, std::min<int64_t>(most, 8)));
+    return int(std::clamp<int64_t>(2048 / std::max<int64_t>(1, tiles * groups), 1, std::min<int64_t>(most, 8)));
 }
 
 AdLayout ad_layout(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_in, const int64_t *d_out)
 {
     const PlanLayout pl = plan_layout(M, n);
     AdLayout l{};
-    int64_t longest = back ? 0 : d_in;
+    const int nv = np * rank_blocks(rank), at_once = blocks_at_once(nv);
+    int64_t widest = 0;
     for (int i = 0; i < np; ++i) {
-        if (back) longest = std::max(longest, d_out[i]);
+        widest = std::max(widest, d_out[i]);
         l.slot_floats += int64_t(rank) * (d_in + d_out[i]);
     }
     l.slot_floats = (l.slot_floats + 3) / 4 * 4;
-    l.ksplit = shrink_splits(M / pl.tile + 1, np, longest, pl.tile == 16);
-    const size_t rp = size_t(rank_pad(rank));
-    l.part = 0;
-    l.hl = l.part + align256(size_t(l.ksplit) * np * size_t(M) * rp * 4);
-    l.slots = l.hl + (back ? align256(size_t(2 * np) * size_t(M) * 3 * rp * 2) : 0);
-    l.total = l.slots + (back ? align256(size_t(pl.max_slots) * size_t(l.slot_floats) * 4) : 0);
+    l.ksplit = shrink_splits(M / pl.tile + 1, (nv + at_once - 1) / at_once, d_in, pl.tile == 16);
+    const int64_t parts = back ? (widest + OUT_COLS - 1) / OUT_COLS : l.ksplit;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t p = at;
+        at += align256(bytes);
+        return p;
+    };
+    l.part = take(size_t(parts) * nv * size_t(M) * 16 * 4);
+    if (back) {
+        l.hl = take(size_t(nv) * size_t(M) * 48 * 2);
+        l.slots = take(size_t(pl.max_slots) * size_t(l.slot_floats) * 4);
+        if (M <= DIRECT_TOKENS) l.plan = take(size_t(pl.words) * 4);
+    }
+    l.total = at;
     return l;
 }
 
-template <bool VEC, int TG>
-hipError_t shrink_expand(const AdArgs &a, bool back, bool second, dim3 grid, hipStream_t st)
+bool al16(const void *p, int64_t row_bytes) { return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(row_bytes)) & 15) == 0; }
+
+template <bool VEC>
+hipError_t launch_shrink(const AdArgs &a, dim3 grid, int vb, bool direct, hipStream_t st)
 {
-#define BSQ_RB(RB)                                                                                                   \
-    case RB:                                                                                                         \
-        if (!second && back) hipLaunchKernelGGL((adapters_shrink<RB, true, VEC, TG>), grid, dim3(AT), 0, st, a);     \
-        else if (!second) hipLaunchKernelGGL((adapters_shrink<RB, false, VEC, TG>), grid, dim3(AT), 0, st, a);       \
-        else if (back && a.dx_bf16) hipLaunchKernelGGL((adapters_expand<RB, true, VEC, TG, false>), grid, dim3(AT), 0, st, a); \
-        else if (back) hipLaunchKernelGGL((adapters_expand<RB, true, VEC, TG, true>), grid, dim3(AT), 0, st, a);     \
-        else if (a.y_bf16) hipLaunchKernelGGL((adapters_expand<RB, false, VEC, TG, false>), grid, dim3(AT), 0, st, a); \
-        else hipLaunchKernelGGL((adapters_expand<RB, false, VEC, TG, true>), grid, dim3(AT), 0, st, a);              \
+#define BSQ_VB(N)                                                                                                        \
+    case N:                                                                                                              \
+        if (direct) hipLaunchKernelGGL((adapters_shrink<N, VEC, 1, true>), grid, dim3(AT), 0, st, a);                    \
+        else if (a.l.tile == 16) hipLaunchKernelGGL((adapters_shrink<N, VEC, 1, false>), grid, dim3(AT), 0, st, a);      \
+        else hipLaunchKernelGGL((adapters_shrink<N, VEC, 4, false>), grid, dim3(AT), 0, st, a);                          \
         break;
-    switch (a.rp / 16) {
+    switch (vb) {
+        BSQ_VB(1)
+        BSQ_VB(2)
+        BSQ_VB(3)
+        BSQ_VB(4)
+    }
+#undef BSQ_VB
+    return hipGetLastError();
+}
+
+template <bool VEC, bool F32>
+hipError_t launch_expand(const AdArgs &a, dim3 grid, bool direct, hipStream_t st)
+{
+#define BSQ_RB(N)                                                                                                        \
+    case N:                                                                                                              \
+        if (direct) hipLaunchKernelGGL((adapters_expand<N, VEC, 1, F32, true>), grid, dim3(AT), 0, st, a);               \
+        else if (a.l.tile == 16) hipLaunchKernelGGL((adapters_expand<N, VEC, 1, F32, false>), grid, dim3(AT), 0, st, a); \
+        else hipLaunchKernelGGL((adapters_expand<N, VEC, 4, F32, false>), grid, dim3(AT), 0, st, a);                     \
+        break;
+    switch (a.rb) {
         BSQ_RB(1)
         BSQ_RB(2)
         BSQ_RB(4)
@@ -775,33 +1096,41 @@ hipError_t shrink_expand(const AdArgs &a, bool back, bool second, dim3 grid, hip
     return hipGetLastError();
 }
 
-hipError_t shrink_expand(const AdArgs &a, bool back, bool second, bool vec, dim3 grid, hipStream_t st)
-{
-    const bool tg1 = a.l.tile == 16;
-    if (vec) return tg1 ? shrink_expand<true, 1>(a, back, second, grid, st) : shrink_expand<true, 4>(a, back, second, grid, st);
-    return tg1 ? shrink_expand<false, 1>(a, back, second, grid, st) : shrink_expand<false, 4>(a, back, second, grid, st);
-}
-
 template <bool VEC>
-hipError_t launch_outer(const AdArgs &a, dim3 grid, hipStream_t st)
+hipError_t launch_dy(const AdArgs &a, dim3 grid, hipStream_t st)
 {
-    const int rb = a.rp / 16;
-    if (rb == 1) hipLaunchKernelGGL((adapters_outer<1, VEC>), grid, dim3(AT), 0, st, a);
-    else if (rb == 2) hipLaunchKernelGGL((adapters_outer<2, VEC>), grid, dim3(AT), 0, st, a);
-    else if (rb == 4) hipLaunchKernelGGL((adapters_outer<4, VEC>), grid, dim3(AT), 0, st, a);
-    else hipLaunchKernelGGL((adapters_outer<8, VEC>), grid, dim3(AT), 0, st, a);
+    switch (a.rb) {
+    case 1: hipLaunchKernelGGL((adapters_dy<1, VEC>), grid, dim3(AT), 0, st, a); break;
+    case 2: hipLaunchKernelGGL((adapters_dy<2, VEC>), grid, dim3(AT), 0, st, a); break;
+    case 4: hipLaunchKernelGGL((adapters_dy<4, VEC>), grid, dim3(AT), 0, st, a); break;
+    default: hipLaunchKernelGGL((adapters_dy<8, VEC>), grid, dim3(AT), 0, st, a); break;
+    }
     return hipGetLastError();
 }
 
-bool al16(const void *p, int64_t row_bytes) { return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(row_bytes)) & 15) == 0; }
+template <bool VEC>
+hipError_t launch_da(const AdArgs &a, int vb, dim3 grid, hipStream_t st)
+{
+    switch (vb) {
+    case 1: hipLaunchKernelGGL((adapters_da<1, VEC>), grid, dim3(AT), 0, st, a); break;
+    case 2: hipLaunchKernelGGL((adapters_da<2, VEC>), grid, dim3(AT), 0, st, a); break;
+    case 3: hipLaunchKernelGGL((adapters_da<3, VEC>), grid, dim3(AT), 0, st, a); break;
+    default: hipLaunchKernelGGL((adapters_da<4, VEC>), grid, dim3(AT), 0, st, a); break;
+    }
+    return hipGetLastError();
+}
 
-}  // namespace
+template <bool VEC, bool F32>
+hipError_t launch_dx(const AdArgs &a, dim3 grid, hipStream_t st)
+{
+    if (a.l.tile == 16) hipLaunchKernelGGL((adapters_dx<VEC, 1, F32>), grid, dim3(AT), 0, st, a);
+    else hipLaunchKernelGGL((adapters_dx<VEC, 4, F32>), grid, dim3(AT), 0, st, a);
+    return hipGetLastError();
+}
 
-int64_t adapters_tile(int64_t M) { return M <= 1024 ? 16 : 64; }
+unsigned blocks(int64_t n, int64_t per) { return unsigned((n + per - 1) / per); }
 
-size_t adapters_plan_bytes(int64_t M, int64_t n) { return size_t(plan_layout(M, n).words) * 4; }
-
-hipError_t launch_adapters_plan(const int32_t *ids, int64_t M, int64_t n, void *buf, int32_t *err, hipStream_t st)
+hipError_t run_plan(const int32_t *ids, int64_t M, int64_t n, void *buf, int32_t *err, hipStream_t st)
 {
     PlanArgs a{};
     a.ids = ids;
@@ -821,6 +1150,86 @@ hipError_t launch_adapters_plan(const int32_t *ids, int64_t M, int64_t n, void *
     return hipGetLastError();
 }
 
+hipError_t run_forward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest, hipStream_t st)
+{
+    const bool direct = a.M <= DIRECT_TOKENS, f32 = c.y_dtype == BSQ_F32;
+    bool va = vx, vy = c.rank % 8 == 0;  // vector loads of x with A, of B with y
+    for (int i = 0; i < c.np; ++i) {
+        Proj &p = a.p[i];
+        p.base = c.y0 ? c.y0[i] : nullptr;
+        p.ldb = c.y0 ? c.ldy0[i] : 0;
+        p.y = c.y[i];
+        p.ldy = c.ldy[i];
+        va = va && al16(p.A, 2 * c.d_in);
+        vy = vy && al16(p.B, 0) && al16(p.base, (f32 ? 4 : 2) * p.ldb) && al16(p.y, (f32 ? 4 : 2) * p.ldy);
+    }
+    const unsigned tiles = unsigned(direct ? a.M : a.l.max_tiles);
+    const int vb = blocks_at_once(a.nv);
+    const dim3 sgrid(tiles, unsigned(a.ksplit), blocks(a.nv, vb));
+    hipError_t e = va ? launch_shrink<true>(a, sgrid, vb, direct, st) : launch_shrink<false>(a, sgrid, vb, direct, st);
+    if (e != hipSuccess) return e;
+    // columns of a block: t is summed once for all of them, but few tiles need
+    // many blocks to fill the compute units
+    const int64_t wide = (a.l.tile == 16) ? 1024 : 512;
+    a.ecols = (int64_t(tiles) * c.np * blocks(widest, wide) >= 2048) ? int(wide) : 256;
+    const dim3 egrid(tiles, blocks(widest, a.ecols), unsigned(c.np));
+    if (f32) return vy ? launch_expand<true, true>(a, egrid, direct, st) : launch_expand<false, true>(a, egrid, direct, st);
+    return vy ? launch_expand<true, false>(a, egrid, direct, st) : launch_expand<false, false>(a, egrid, direct, st);
+}
+
+hipError_t run_backward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest, hipStream_t st)
+{
+    bool vd = true, va = c.d_in % 8 == 0;
+    for (int i = 0; i < c.np; ++i) {
+        Proj &p = a.p[i];
+        p.base = c.dy[i];
+        p.ldb = c.lddy[i];
+        p.dA = c.dA[i];
+        p.dB = c.dB[i];
+        vd = vd && al16(p.base, 2 * p.ldb) && p.d_out % 8 == 0;
+        va = va && al16(p.A, 2 * c.d_in);
+    }
+    const dim3 dgrid(unsigned(a.l.max_pieces), blocks(widest, OUT_COLS), unsigned(c.np));
+    hipError_t e = vd ? launch_dy<true>(a, dgrid, st) : launch_dy<false>(a, dgrid, st);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(adapters_parts, dim3(blocks(a.M * 2 * a.rb, AT), 1, unsigned(c.np)), dim3(AT), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int vb = blocks_at_once(a.nv);
+    const dim3 agrid(unsigned(a.l.max_pieces), blocks(c.d_in, OUT_COLS), blocks(a.nv, vb));
+    if ((e = vx ? launch_da<true>(a, vb, agrid, st) : launch_da<false>(a, vb, agrid, st)) != hipSuccess) return e;
+    hipLaunchKernelGGL(adapters_pieces, dim3(blocks(int64_t(c.rank) * std::max(widest, c.d_in), 4 * AT), unsigned(a.n), unsigned(2 * c.np)),
+                       dim3(AT), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess || !c.dx) return e;
+    a.dx0 = static_cast<const uint16_t *>(c.dx0);
+    a.dx = c.dx;
+    a.lddx0 = c.lddx0;
+    a.lddx = c.lddx;
+    const bool f32 = c.dx_dtype == BSQ_F32;
+    const bool vec = va && al16(c.dx0, 2 * c.lddx0) && al16(c.dx, (f32 ? 4 : 2) * c.lddx);
+    const dim3 xgrid(unsigned(a.l.max_tiles), blocks(c.d_in, 256), 1);
+    if (f32) return vec ? launch_dx<true, true>(a, xgrid, st) : launch_dx<false, true>(a, xgrid, st);
+    return vec ? launch_dx<true, false>(a, xgrid, st) : launch_dx<false, false>(a, xgrid, st);
+}
+
+// Reports ids that are no adapter's (up to DIRECT_TOKENS tokens have no plan).
+__global__ __launch_bounds__(DIRECT_TOKENS) void adapters_check_kernel(const int32_t *ids, int64_t M, int n, int32_t *err)
+{
+    const int64_t m = threadIdx.x;
+    if (m < M && ids[m] >= n) atomicOr(err, BSQ_DEVERR_BAD_SET);
+}
+
+}  // namespace
+
+size_t adapters_plan_bytes(int64_t M, int64_t n) { return M <= DIRECT_TOKENS ? 0 : size_t(plan_layout(M, n).words) * 4; }
+
+hipError_t launch_adapters_plan(const int32_t *ids, int64_t M, int64_t n, void *buf, int32_t *err, hipStream_t st)
+{
+    if (M > DIRECT_TOKENS) return run_plan(ids, M, n, buf, err, st);
+    if (!err) return hipSuccess;
+    hipLaunchKernelGGL(adapters_check_kernel, dim3(1), dim3(DIRECT_TOKENS), 0, st, ids, M, int(n), err);
+    return hipGetLastError();
+}
+
 size_t adapters_ws_bytes(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_in, const int64_t *d_out)
 {
     return ad_layout(back, M, n, np, rank, d_in, d_out).total;
@@ -831,11 +1240,12 @@ hipError_t launch_adapters(const AdaptersCall &c, hipStream_t st)
     const bool back = c.dy != nullptr;
     AdArgs a{};
     a.plan = static_cast<const int32_t *>(c.plan->buf);
+    a.ids = c.plan->ids;
     a.M = c.plan->M;
     a.n = c.plan->n;
     a.l = plan_layout(a.M, a.n);
-    int64_t d_out[BSQ_MAX_GROUP], most = 0;
-    for (int i = 0; i < c.np; ++i) most = std::max(most, d_out[i] = c.pools[i].d_out);
+    int64_t d_out[BSQ_MAX_GROUP], widest = 0;
+    for (int i = 0; i < c.np; ++i) widest = std::max(widest, d_out[i] = c.pools[i].d_out);
     const AdLayout l = ad_layout(back, a.M, a.n, c.np, c.rank, c.d_in, d_out);
     char *ws = static_cast<char *>(c.ws);
     a.X = static_cast<const uint16_t *>(c.X);
@@ -843,17 +1253,14 @@ hipError_t launch_adapters(const AdaptersCall &c, hipStream_t st)
     a.d_in = c.d_in;
     a.np = c.np;
     a.rank = c.rank;
-    a.rp = rank_pad(c.rank);
+    a.rb = rank_blocks(c.rank);
+    a.nv = a.np * a.rb;
     a.ksplit = l.ksplit;
     a.part = reinterpret_cast<float *>(ws + l.part);
     a.hl = reinterpret_cast<uint16_t *>(ws + l.hl);
     a.slots = reinterpret_cast<float *>(ws + l.slots);
     a.slot_floats = l.slot_floats;
-    a.y_bf16 = c.y_dtype == BSQ_BF16;
     a.accumulate = c.accumulate;
-    const int64_t es = a.y_bf16 ? 2 : 4;
-    const bool vx = al16(c.X, 2 * c.ldx) && c.d_in % 8 == 0;
-    bool va = vx, vy = c.rank % 8 == 0, vd = true;  // vector loads of x with A, of y with B, of dy
     for (int i = 0; i < c.np; ++i) {
         const bsq_adapter_pool &q = c.pools[i];
         Proj &p = a.p[i];
@@ -863,42 +1270,15 @@ hipError_t launch_adapters(const AdaptersCall &c, hipStream_t st)
         p.ranks = q.ranks;
         p.d_out = q.d_out;
         p.t = c.t ? c.t[i] : nullptr;
-        va = va && al16(q.A, 2 * c.d_in);
-        if (back) {
-            p.base = c.dy[i];
-            p.ldb = c.lddy[i];
-            p.dA = c.dA[i];
-            p.dB = c.dB[i];
-            vd = vd && al16(p.base, 2 * p.ldb) && p.d_out % 8 == 0;
-        } else {
-            p.base = c.y0 ? c.y0[i] : nullptr;
-            p.ldb = c.y0 ? c.ldy0[i] : 0;
-            p.y = c.y[i];
-            p.ldy = c.ldy[i];
-            vy = vy && al16(q.B, 0) && al16(p.base, es * p.ldb) && al16(p.y, es * p.ldy);
-        }
     }
-    const dim3 sgrid(unsigned(a.l.max_tiles), unsigned(l.ksplit), unsigned(c.np));
-    hipError_t e = shrink_expand(a, back, false, back ? vd : va, sgrid, st);
-    if (e != hipSuccess) return e;
-    if (!back)
-        return shrink_expand(a, false, true, vy, dim3(unsigned(a.l.max_tiles), unsigned((most + EXP_COLS - 1) / EXP_COLS), unsigned(c.np)), st);
-    hipLaunchKernelGGL(adapters_parts, dim3(unsigned((a.M * (a.rp / 8) + AT - 1) / AT), 1, unsigned(c.np)), dim3(AT), 0, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int64_t widest = std::max(most, c.d_in);
-    const dim3 ogrid(unsigned(a.l.max_pieces), unsigned((widest + OUT_COLS - 1) / OUT_COLS), unsigned(2 * c.np));
-    e = (vx && vd) ? launch_outer<true>(a, ogrid, st) : launch_outer<false>(a, ogrid, st);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(adapters_pieces, dim3(unsigned((int64_t(c.rank) * widest + 4 * AT - 1) / (4 * AT)), unsigned(a.n), unsigned(2 * c.np)),
-                       dim3(AT), 0, st, a);
-    if ((e = hipGetLastError()) != hipSuccess || !c.dx) return e;
-    a.dx0 = static_cast<const uint16_t *>(c.dx0);
-    a.dx = c.dx;
-    a.lddx0 = c.lddx0;
-    a.lddx = c.lddx;
-    a.dx_bf16 = c.dx_dtype == BSQ_BF16;
-    const bool vdx = al16(c.dx0, 2 * c.lddx0) && al16(c.dx, (a.dx_bf16 ? 2 : 4) * c.lddx);
-    return shrink_expand(a, true, true, vdx, dim3(unsigned(a.l.max_tiles), unsigned((c.d_in + EXP_COLS - 1) / EXP_COLS), 1), st);
+    const bool vx = al16(c.X, 2 * c.ldx) && c.d_in % 8 == 0;
+    if (!back) return run_forward(c, a, vx, widest, st);
+    if (a.M <= DIRECT_TOKENS) {
+        const hipError_t e = run_plan(a.ids, a.M, a.n, ws + l.plan, nullptr, st);
+        if (e != hipSuccess) return e;
+        a.plan = reinterpret_cast<const int32_t *>(ws + l.plan);
+    }
+    return run_backward(c, a, vx, widest, st);
 }
 
 }  // namespace bsq

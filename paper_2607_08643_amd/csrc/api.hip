@@ -647,12 +647,13 @@ bsq_status check_adapter_dims(int32_t n_proj, int32_t rank, int64_t d_in)
 bsq_status check_adapters(bool back, const bsq_adapter_plan *plan, int32_t n_proj, const bsq_adapter_pool *pools,
                           int32_t rank, int64_t d_in, const void *X, int64_t ldx, const void *ws, size_t ws_bytes)
 {
-    if (!plan || !plan->buf || !pools || !X || !ws) return BSQ_ERR_ARG;
+    if (!plan || !plan->ids || !pools || !X || !ws) return BSQ_ERR_ARG;
     bsq_status s = check_batch(plan->M, plan->n);
     if (s != BSQ_OK) return s;
+    if (plan->M > BSQ_ADAPTERS_DIRECT && !plan->buf) return BSQ_ERR_ARG;
     if ((s = check_adapter_dims(n_proj, rank, d_in)) != BSQ_OK) return s;
     if (ldx < d_in) return BSQ_ERR_SHAPE;
-    if (!aligned(plan->buf, 16) || !aligned(X, 2) || !aligned(ws, 256)) return BSQ_ERR_ALIGN;
+    if (!aligned(plan->buf, 16) || !aligned(plan->ids, 4) || !aligned(X, 2) || !aligned(ws, 256)) return BSQ_ERR_ALIGN;
     int64_t d_out[BSQ_MAX_GROUP];
     for (int i = 0; i < n_proj; ++i) {
         const bsq_adapter_pool &p = pools[i];
@@ -678,9 +679,10 @@ bsq_status bsq_adapters_plan_bytes(int64_t M, int32_t n, size_t *bytes)
 
 bsq_status bsq_adapters_plan(const bsq_adapter_plan *plan, size_t buf_bytes, int32_t *err, void *stream)
 {
-    if (!plan || !plan->ids || !plan->buf) return BSQ_ERR_ARG;
+    if (!plan || !plan->ids) return BSQ_ERR_ARG;
     const bsq_status s = check_batch(plan->M, plan->n);
     if (s != BSQ_OK) return s;
+    if (plan->M > BSQ_ADAPTERS_DIRECT && !plan->buf) return BSQ_ERR_ARG;
     if (!aligned(plan->ids, 4) || !aligned(plan->buf, 16) || !aligned(err, 4)) return BSQ_ERR_ALIGN;
     if (buf_bytes < adapters_plan_bytes(plan->M, plan->n)) return BSQ_ERR_BUFFER_TOO_SMALL;
     return from_hip(launch_adapters_plan(plan->ids, plan->M, plan->n, plan->buf, err, static_cast<hipStream_t>(stream)));

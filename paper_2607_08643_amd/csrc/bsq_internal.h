@@ -277,8 +277,8 @@ hipError_t launch_train_grad(const bsq_config &cfg, const bsq_train_hparams &hp,
 hipError_t launch_train_adam(const bsq_config &cfg, const bsq_train_hparams &hp, int step, float *theta,
                              const float *grad, float *m, float *v, hipStream_t st);
 
-// Adapters of many requests (adapters.hip): tokens of a tile of the plan,
-// sizes, and the two launches; `dy` set: the gradients.
+// Adapters of many requests (adapters.hip): sizes and launches; `dy` set: the
+// gradients.
 struct AdaptersCall {
     const bsq_adapter_plan *plan;
     const bsq_adapter_pool *pools;
@@ -303,7 +303,6 @@ struct AdaptersCall {
     int accumulate;
     void *ws;
 };
-int64_t adapters_tile(int64_t M);
 size_t adapters_plan_bytes(int64_t M, int64_t n);
 size_t adapters_ws_bytes(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_in, const int64_t *d_out);
 hipError_t launch_adapters_plan(const int32_t *ids, int64_t M, int64_t n, void *buf, int32_t *err, hipStream_t st);

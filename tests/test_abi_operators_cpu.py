@@ -27,7 +27,7 @@ def _i64(*v):
 
 
 # ---------------------------------------------------------------- adapters
-def _plan(M=100, n=4, ids=FAKE, buf=FAKE):
+def _plan(M=1000, n=4, ids=FAKE, buf=FAKE):
     return B.bsq_adapter_plan(ids or None, buf or None, M, n)
 
 
@@ -37,8 +37,8 @@ def _pool(A=FAKE, Bp=FAKE, scale=0, ranks=0, d_out=64):
 
 def test_adapter_plan_sizes_and_refusals():
     Lib = bsq.lib()
-    sizes = [bsq.bsq_adapters_plan_bytes(M, n) for M, n in ((1, 1), (1000, 16), (1000, 1024), (1 << 24, 1024))]
-    assert sizes == sorted(sizes) and sizes[0] > 0
+    sizes = [bsq.bsq_adapters_plan_bytes(M, n) for M, n in ((1, 1), (256, 1024), (257, 1), (1000, 16), (1000, 1024), (1 << 24, 1024))]
+    assert sizes == sorted(sizes) and sizes[1] == 0 and sizes[2] > 0  # up to 256 tokens there is nothing to keep
     for M, n, status in ((0, 1, bsq.BSQ_ERR_SHAPE), (-1, 1, bsq.BSQ_ERR_SHAPE), (1, 0, bsq.BSQ_ERR_SHAPE),
                          ((1 << 24) + 1, 1, bsq.BSQ_ERR_UNSUPPORTED), (1, 1025, bsq.BSQ_ERR_UNSUPPORTED)):
         with pytest.raises(bsq.BsqError) as e:
@@ -55,7 +55,7 @@ def test_adapter_plan_sizes_and_refusals():
     assert plan(_plan(ids=FAKE + 2)) == bsq.BSQ_ERR_ALIGN
     assert plan(_plan(buf=FAKE + 8)) == bsq.BSQ_ERR_ALIGN
     assert plan(_plan(), err=FAKE + 1) == bsq.BSQ_ERR_ALIGN
-    assert plan(_plan(), nbytes=bsq.bsq_adapters_plan_bytes(100, 4) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
+    assert plan(_plan(), nbytes=bsq.bsq_adapters_plan_bytes(1000, 4) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
     assert Lib.bsq_adapters_plan_bytes(1, 1, None) == bsq.BSQ_ERR_ARG
 
 
@@ -85,6 +85,8 @@ def test_adapters_apply_rejects_before_launch():
         return Lib.bsq_adapters_apply(ct.byref(plan), n_proj, pools, rank, d_in, _p(X), ldx, _arr(y0), _i64(ldy0),
                                       _arr(y), _i64(ldy), dt, _arr(t) if t else None, _p(ws), ws_bytes, None)
     assert apply(plan=_plan(buf=0)) == bsq.BSQ_ERR_ARG
+    assert apply(plan=_plan(ids=0)) == bsq.BSQ_ERR_ARG
+    assert apply(plan=_plan(M=100, buf=0), ws_bytes=0) == bsq.BSQ_ERR_BUFFER_TOO_SMALL  # no buffer needed
     assert apply(plan=_plan(M=0)) == bsq.BSQ_ERR_SHAPE
     assert apply(n_proj=0) == bsq.BSQ_ERR_ARG
     assert apply(n_proj=9) == bsq.BSQ_ERR_ARG
@@ -109,7 +111,7 @@ def test_adapters_apply_rejects_before_launch():
     assert apply(t=FAKE + 2) == bsq.BSQ_ERR_ALIGN
     assert apply(ws=0) == bsq.BSQ_ERR_ARG
     assert apply(ws=FAKE + 128) == bsq.BSQ_ERR_ALIGN
-    assert apply(ws_bytes=bsq.bsq_adapters_workspace_bytes(False, 100, 4, 16, 256, [64]) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
+    assert apply(ws_bytes=bsq.bsq_adapters_workspace_bytes(False, 1000, 4, 16, 256, [64]) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
 
 
 def test_adapters_grad_rejects_before_launch():
@@ -139,7 +141,7 @@ def test_adapters_grad_rejects_before_launch():
     assert grad(dA=FAKE + 2) == bsq.BSQ_ERR_ALIGN
     assert grad(dB=FAKE + 2) == bsq.BSQ_ERR_ALIGN
     assert grad(rank=0) == bsq.BSQ_ERR_ARG
-    assert grad(ws_bytes=bsq.bsq_adapters_workspace_bytes(True, 100, 4, 16, 256, [64]) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
+    assert grad(ws_bytes=bsq.bsq_adapters_workspace_bytes(True, 1000, 4, 16, 256, [64]) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
     # nothing of dx is looked at where it is not wanted
     assert grad(dx=0, dt=9, lddx=0, ws=0) == bsq.BSQ_ERR_ARG
 

@@ -174,7 +174,7 @@ def test_apply_matches_formula(case, gpu):
         assert torch.equal(o[free], w[free])
 
 
-@pytest.mark.parametrize("M,n,kind", [(1, 1, "one"), (64, 3, "mixed"), (1000, 1024, "mixed"), (1025, 7, "runs"),
+@pytest.mark.parametrize("M,n,kind", [(257, 1, "one"), (300, 3, "mixed"), (1000, 1024, "mixed"), (1025, 7, "runs"),
                                       (5000, 40, "mixed"), (8192, 2, "none")])
 def test_plan_is_a_stable_sort(M, n, kind, gpu):
     say(f"adapters plan M={M} n={n} {kind}")
