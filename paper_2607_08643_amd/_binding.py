@@ -721,6 +721,12 @@ def _workspace(need, dev):
     return t if t.data_ptr() % 256 == 0 else _empty_aligned(need, dev)
 
 
+# the current stream of a device as a hipStream_t (without a Stream object
+# around it, which takes longer than a launch, where torch offers that)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class _Launch:
     """The device and stream of a call: what it allocates belongs to that
     stream (so that a buffer it frees is reused in that stream's order)."""
@@ -736,7 +742,7 @@ class _Launch:
             self.ctx = torch.cuda.device(self.dev)
         if self.ctx is not None:
             self.ctx.__enter__()
-        return ct.c_void_p((self.stream or torch.cuda.current_stream()).cuda_stream)
+        return ct.c_void_p(_raw_stream(self.dev.index) if self.stream is None else self.stream.cuda_stream)
 
     def __exit__(self, *exc):
         if self.ctx is not None:
@@ -763,9 +769,11 @@ class AdapterPool:
         if A.dim() != 3 or B.dim() != 3:
             raise ValueError("A must be [n, rank, d_in] and B [n, d_out, rank]")
         n, rank, d_in = A.shape
-        d_out = B.shape[1]
-        _need(A, torch.bfloat16, (n, rank, d_in), "A")
-        _need(B, torch.bfloat16, (n, d_out, rank), "B")
+        nb, d_out, rb = B.shape
+        if not (A.dtype is B.dtype is torch.bfloat16 and nb == n and rb == rank and A.is_contiguous()
+                and B.is_contiguous()):
+            _need(A, torch.bfloat16, (n, rank, d_in), "A")
+            _need(B, torch.bfloat16, (n, d_out, rank), "B")
         if scale is not None:
             _need(scale, torch.float32, (n,), "scale")
         if ranks is not None:
@@ -806,6 +814,8 @@ def bsq_adapters_plan(ids: torch.Tensor, n: int, buf: torch.Tensor | None = None
     dev = _device_of((ids, buf, err), "bsq_adapters_plan")
     _need(ids, torch.int32, (ids.numel(),), "ids")
     need = bsq_adapters_plan_bytes(ids.shape[0], n)
+    if not need and err is None:
+        return AdapterPlan(ids, n, buf)
     with _Launch(dev, stream) as st:
         if buf is None and need:
             buf = torch.empty(need, dtype=torch.uint8, device=dev)

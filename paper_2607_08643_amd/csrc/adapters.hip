@@ -33,7 +33,7 @@ constexpr int AT = 256;  // threads of a block: 4 waves
 // Up to this many tokens a forward call groups them itself, every block from the
 // ids: a plan's launch (5 us) would be a third of a decode step's time.
 constexpr int64_t DIRECT_TOKENS = BSQ_ADAPTERS_DIRECT;
-constexpr int PLAN_WAVES = 16;
+constexpr int PLAN_WAVES = 16, PLAN_AHEAD = 8;  // groups of 64 ids that a wave has in flight
 
 struct PlanLayout {
     int64_t tile, piece;              // tokens of a tile, of a piece
@@ -108,22 +108,27 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void adapters_plan_kernel(const Pl
     bool bad = false;
     // pass 0 counts, pass 1 places
     for (int pass = 0; pass < 2; ++pass) {
-        for (int64_t m0 = lo; m0 < hi; m0 += 64) {
-            const int64_t m = m0 + lane;
-            const bool in = m < hi;
-            const int32_t id = in ? a.ids[m] : -1;
-            bad |= id >= a.n;
-            const int key = (id >= 0 && id < a.n) ? id : a.n;
-            uint64_t same = __ballot(in);
-            for (int b = 0; b < a.bits; ++b) {
-                const uint64_t ones = __ballot((key >> b) & 1);
-                same &= ((key >> b) & 1) ? ones : ~ones;
+        for (int64_t m1 = lo; m1 < hi; m1 += 64 * PLAN_AHEAD) {
+            int32_t id[PLAN_AHEAD];
+#pragma unroll
+            for (int q = 0; q < PLAN_AHEAD; ++q) id[q] = (m1 + 64 * q + lane < hi) ? a.ids[m1 + 64 * q + lane] : -1;
+#pragma unroll
+            for (int q = 0; q < PLAN_AHEAD; ++q) {
+                const int64_t m = m1 + 64 * q + lane;
+                const bool in = m < hi;
+                bad |= id[q] >= a.n;
+                const int key = (id[q] >= 0 && id[q] < a.n) ? id[q] : a.n;
+                uint64_t same = __ballot(in);
+                for (int b = 0; b < a.bits; ++b) {
+                    const uint64_t ones = __ballot((key >> b) & 1);
+                    same &= ((key >> b) & 1) ? ones : ~ones;
+                }
+                const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
+                const bool first = in && before == 0;
+                if (pass == 1 && in) order[row[key] + before] = int32_t(m);
+                // (a wave's LDS operations run in order, so the reads above come first)
+                if (first) row[key] += __popcll(same);
             }
-            const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
-            const bool first = in && before == 0;
-            if (pass == 1 && in) order[row[key] + before] = int32_t(m);
-            // (a wave's LDS operations run in order, so the reads above come first)
-            if (first) row[key] += __popcll(same);
         }
         __syncthreads();
         if (pass == 1) break;
@@ -251,16 +256,6 @@ __device__ __forceinline__ frag_t load8(const uint16_t *p, int64_t valid)
     }
 }
 
-// Eight values stride apart, those from `valid` on as zero.
-__device__ __forceinline__ frag_t load8_strided(const uint16_t *p, int64_t stride, int64_t valid)
-{
-    frag_t v = zero_frag();
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < valid) v[e >> 1] |= uint32_t(p[e * stride]) << (16 * (e & 1));
-    return v;
-}
-
 // The bf16 parts of x: rounded, and what remains, rounded, twice (nothing
 // where the value is or has become infinite).
 __device__ __forceinline__ void split3(const float (&x)[8], frag_t (&part)[3])
@@ -282,7 +277,7 @@ __device__ __forceinline__ void split3(const float (&x)[8], frag_t (&part)[3])
 // end is its last), its place in t's partial sums, and whether it is the tile's.
 struct TileView {
     int adapter, count;
-    int64_t token, place;
+    int64_t token, place, first;  // first: place of the tile's first token (not DIRECT)
     bool live;
 };
 
@@ -330,6 +325,7 @@ __device__ __forceinline__ bool tile_view(const AdArgs &a, bool with_none, int (
         const int tok = (TG == 1 ? 0 : 16 * wave) + r16;
         v.adapter = tile.x;
         v.count = tile.z;
+        v.first = tile.y;
         v.live = tok < tile.z;
         v.place = tile.y + (v.live ? tok : tile.z - 1);
         v.token = a.plan[a.l.order + v.place];
@@ -340,27 +336,45 @@ __device__ __forceinline__ bool tile_view(const AdArgs &a, bool with_none, int (
 // ---------------------------------------------------------------------------
 // shrink: part[z][v][place][r] = sum over the block's share of d_in of A[r] x,
 // for VB rank blocks v at a time. 16-token tiles: the four waves share the tile
-// and split d_in. 64-token tiles: a wave per 16 tokens.
+// and split d_in. 64-token tiles: 32 tokens a wave (A is read half as often as
+// with 16) and two waves along d_in. Loads are a step ahead of their products.
+// Bound by reading x.
 // ---------------------------------------------------------------------------
 template <int VB, bool VEC, int TG, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
 {
-    constexpr int U = (VB >= 3) ? 4 : 8;  // 32-deep steps whose loads are in flight together
+    constexpr int U = 4;                        // 32-deep steps whose loads are in flight together
+    constexpr int MT = (TG == 1) ? 1 : 2;       // 16-token groups of a wave
+    constexpr int KW = (TG == 1) ? 4 : 2;       // waves along d_in
     __shared__ int s_tok[4][16];
-    __shared__ f32x4_t s_acc[TG == 1 ? 4 : 1][VB][64];
+    __shared__ f32x4_t s_acc[4][MT * VB][64];
     TileView tv;
     if (!tile_view<DIRECT, TG>(a, false, s_tok, tv)) return;
     const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    if (TG != 1 && 16 * wave >= tv.count) return;
     const int64_t K = a.d_in;
     const int v0 = int(blockIdx.z) * VB;
-    // this wave's range of k, whole steps of 32
-    const int64_t nshare = int64_t(a.ksplit) * (TG == 1 ? 4 : 1);
-    const int64_t share = int64_t(blockIdx.y) * (TG == 1 ? 4 : 1) + (TG == 1 ? wave : 0);
+    // this wave's range of k, whole steps of 32, and its tokens
+    const int kw = (TG == 1) ? wave : wave & 1, tg = (TG == 1) ? 0 : wave >> 1;
+    const int64_t nshare = int64_t(a.ksplit) * KW, share = int64_t(blockIdx.y) * KW + kw;
     const int64_t steps = (K + 31) / 32;
-    const int64_t s0 = steps * share / nshare, s1 = steps * (share + 1) / nshare;
-    const uint16_t *xrow = a.X + tv.token * a.ldx;
+    const int64_t s0 = steps * share / nshare, s1 = (32 * tg < tv.count || TG == 1) ? steps * (share + 1) / nshare : s0;
+    const uint16_t *xrow[MT];
+    int64_t place[MT];
+    bool live[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        if constexpr (TG == 1) {
+            place[m] = tv.place;
+            live[m] = tv.live;
+            xrow[m] = a.X + tv.token * a.ldx;
+        } else {
+            const int tok = 32 * tg + 16 * m + r16;
+            live[m] = tok < tv.count;
+            place[m] = tv.first + (live[m] ? tok : tv.count - 1);
+            xrow[m] = a.X + int64_t(a.plan[a.l.order + place[m]]) * a.ldx;
+        }
+    }
     const uint16_t *arow[VB];
     bool ain[VB];
 #pragma unroll
@@ -370,39 +384,45 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
         ain[b] = r < rank_of(p, tv.adapter, a.rank);
         arow[b] = p.A + (int64_t(tv.adapter) * a.rank + (ain[b] ? r : 0)) * K;
     }
-    f32x4_t acc[VB];
+    f32x4_t acc[MT][VB];
 #pragma unroll
-    for (int b = 0; b < VB; ++b) acc[b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t s = s0; s < s1; s += U) {
-        frag_t x[U], w[U][VB];
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int b = 0; b < VB; ++b) acc[m][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    frag_t x[U][MT], w[U][VB];
+    auto fetch = [&](int u, int64_t s) {
+        const int64_t k = 32 * s + 8 * g, left = (s < s1) ? K - k : 0;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) x[u][m] = load8<VEC>(xrow[m] + k, left);
+#pragma unroll
+        for (int b = 0; b < VB; ++b) w[u][b] = load8<VEC>(arow[b] + k, ain[b] ? left : 0);
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) fetch(u, s0 + u);
+    for (int64_t s = s0; s < s1; s += U)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t k = 32 * (s + u) + 8 * g, left = (s + u < s1) ? K - k : 0;
-            x[u] = load8<VEC>(xrow + k, left);
 #pragma unroll
-            for (int b = 0; b < VB; ++b) w[u][b] = load8<VEC>(arow[b] + k, ain[b] ? left : 0);
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int b = 0; b < VB; ++b) acc[m][b] = mfma(w[u][b], x[u][m], acc[m][b]);
+            fetch(u, s + U + u);
         }
+    // lane: ranks 4 g .. + 3 of a block, of token r16; the waves along d_in added in order
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int b = 0; b < VB; ++b) acc[b] = mfma(w[u][b], x[u], acc[b]);
-    }
-    // lane: ranks 4 g .. + 3 of a block, of token r16
-    float *part = a.part + (int64_t(blockIdx.y) * a.nv * a.M + tv.place) * 16 + 4 * g;
-    if constexpr (TG == 1) {
+        for (int b = 0; b < VB; ++b) s_acc[wave][m * VB + b][lane] = acc[m][b];
+    __syncthreads();
+    float *part = a.part + int64_t(blockIdx.y) * a.nv * a.M * 16 + 4 * g;
 #pragma unroll
-        for (int b = 0; b < VB; ++b) s_acc[wave][b][lane] = acc[b];
-        __syncthreads();
-        for (int b = wave; b < VB; b += 4) {
-            f32x4_t v = s_acc[0][b][lane];
+    for (int q = 0; q < MT * VB; ++q) {
+        const int m = q / VB, b = q - m * VB;
+        if (q % KW != kw) continue;
+        f32x4_t v = s_acc[KW * tg][q][lane];
 #pragma unroll
-            for (int q = 1; q < 4; ++q) v += s_acc[q][b][lane];
-            if (tv.live && v0 + b < a.nv) *reinterpret_cast<f32x4_t *>(part + int64_t(v0 + b) * a.M * 16) = v;
-        }
-    } else {
-#pragma unroll
-        for (int b = 0; b < VB; ++b)
-            if (tv.live && v0 + b < a.nv) *reinterpret_cast<f32x4_t *>(part + int64_t(v0 + b) * a.M * 16) = acc[b];
+        for (int k = 1; k < KW; ++k) v += s_acc[KW * tg + k][q][lane];
+        if (live[m] && v0 + b < a.nv) *reinterpret_cast<f32x4_t *>(part + (int64_t(v0 + b) * a.M + place[m]) * 16) = v;
     }
 }
 
@@ -426,30 +446,45 @@ __device__ __forceinline__ void part_sum(const AdArgs &a, int splits, int v, int
 }
 
 // ---------------------------------------------------------------------------
-// Rows of 64 columns of a tile, read and written: lane (g, r16) has columns c +
-// 16 g .. + 15 of its token. WHOLE words where VEC and all 16 exist.
+// 64 columns of 16 tokens, read and written: lane (g, r16) has 16 columns of its
+// token in runs of RUN (16 bytes of the type in memory), run q from column 4 RUN
+// q + RUN g on, so that a wave's 16-byte words are 64 bytes next to each other.
+// Value e of the lane is the sum that a product of 16 x 16 leaves in register e %
+// 4 of block e / 4 when row i of block j of W is column run_column(i, j).
 // ---------------------------------------------------------------------------
+template <int RUN>
+__device__ __forceinline__ int run_column(int i, int j)  // row i of block j
+{
+    return RUN == 8 ? 32 * (j >> 1) + 8 * (i >> 2) + 4 * (j & 1) + (i & 3) : 16 * j + i;
+}
+
 template <bool F32>
 struct Row16 {
     u32x4_t w[F32 ? 4 : 2];
 };
 
-template <bool F32, bool VEC>
+// `p`: the lane's first column; `nc`: columns from there on that exist
+template <bool F32, int RUN, bool VEC>
 __device__ __forceinline__ Row16<F32> load_row(const void *p, int64_t nc)
 {
+    static_assert(!F32 || RUN == 4, "words of four 32-bit values");
     Row16<F32> v;
+    constexpr int NQ = 16 / RUN;
 #pragma unroll
-    for (int q = 0; q < (F32 ? 4 : 2); ++q) v.w[q] = zero_frag();
-    if (VEC && nc >= 16) {
+    for (int q = 0; q < NQ; ++q) {
+        const int64_t left = nc - 4 * RUN * q;
+        v.w[q] = zero_frag();
+        const char *pq = static_cast<const char *>(p) + 64 * q;
+        if (VEC && left >= RUN) {
+            v.w[q] = *reinterpret_cast<const u32x4_t *>(pq);
+        } else {
 #pragma unroll
-        for (int q = 0; q < (F32 ? 4 : 2); ++q) v.w[q] = static_cast<const u32x4_t *>(p)[q];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            if (e < nc) {
-                if constexpr (F32) v.w[e >> 2][e & 3] = static_cast<const uint32_t *>(p)[e];
-                else v.w[e >> 3][(e >> 1) & 3] |= uint32_t(static_cast<const uint16_t *>(p)[e]) << (16 * (e & 1));
-            }
+            for (int e = 0; e < RUN; ++e)
+                if (e < left) {
+                    if constexpr (F32) v.w[q][e] = reinterpret_cast<const uint32_t *>(pq)[e];
+                    else v.w[q][e >> 1] |= uint32_t(reinterpret_cast<const uint16_t *>(pq)[e]) << (16 * (e & 1));
+                }
+        }
     }
     return v;
 }
@@ -462,28 +497,32 @@ __device__ __forceinline__ float row_value(const Row16<F32> &v, int e)
     return __uint_as_float((e & 1) ? w & 0xffff0000u : w << 16);
 }
 
-template <bool F32, bool VEC>
+template <bool F32, int RUN, bool VEC>
 __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[16])
 {
-    if (VEC && nc >= 16) {
-        if constexpr (F32) {
+    constexpr int ES = F32 ? 4 : 2;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                static_cast<f32x4_t *>(p)[j] = f32x4_t{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-        } else {
-            u32x4_t w[2];
+    for (int q = 0; q < 16 / RUN; ++q) {
+        const int64_t left = nc - 4 * RUN * q;
+        char *pq = static_cast<char *>(p) + 4 * RUN * q * ES;
+        const float *x = v + RUN * q;
+        if (VEC && left >= RUN) {
+            if constexpr (F32) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e >> 2][e & 3] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) static_cast<u32x4_t *>(p)[q] = w[q];
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            if (e < nc) {
-                if constexpr (F32) static_cast<float *>(p)[e] = v[e];
-                else static_cast<uint16_t *>(p)[e] = f32_to_bf16(v[e]);
+                for (int k = 0; k < RUN / 4; ++k)
+                    reinterpret_cast<f32x4_t *>(pq)[k] = f32x4_t{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+            } else {
+                *reinterpret_cast<u32x4_t *>(pq) =
+                    u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < RUN; ++e)
+                if (e < left) {
+                    if constexpr (F32) reinterpret_cast<float *>(pq)[e] = x[e];
+                    else reinterpret_cast<uint16_t *>(pq)[e] = f32_to_bf16(x[e]);
+                }
+        }
     }
 }
 
@@ -491,8 +530,7 @@ __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[
 // expand: y = y0 + s B t. A block: a tile and a.ecols columns; a wave: 16 tokens
 // (64-token tiles) over all of them, or every fourth 64 columns of all 16. t is
 // summed once; then per 64 columns the wave has y0 and B of the next ones in
-// flight. B's rows interleave in runs of four, so that a lane's sums are 16
-// consecutive columns of its token.
+// flight. Bound by reading y0 and writing y.
 // ---------------------------------------------------------------------------
 template <int RB, bool VEC, int TG, bool F32, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
@@ -514,6 +552,7 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
     if (ad < 0 && p.base == p.y && !keep) return;
     const int re = ad >= 0 ? rank_of(p, ad, a.rank) : 0;
     constexpr int64_t ES = F32 ? 4 : 2;
+    constexpr int RUN = F32 ? 4 : 8;
     const char *base = static_cast<const char *>(p.base) + tv.token * p.ldb * ES;
     char *out = static_cast<char *>(p.y) + tv.token * p.ldy * ES;
     const uint16_t *B = p.B + int64_t(ad < 0 ? 0 : ad) * C * a.rank;
@@ -523,7 +562,7 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
         for (int b = 0; b < RB; ++b)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int64_t cc = c + (r16 >> 2) * 16 + 4 * j + (r16 & 3);
+                const int64_t cc = c + run_column<RUN>(r16, j);
                 const int left = cc < C ? re - 16 * b - r0 : 0;
                 w[b][j] = load8<VEC>(B + cc * a.rank + 16 * b + r0, left);
                 // ranks past the adapter's own hold anything
@@ -534,8 +573,8 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
             }
     };
     auto load_y = [&](int64_t c) {
-        const int64_t col = c + 16 * g;
-        return load_row<F32, VEC>(base + col * ES, (p.base && tv.live && c < c1) ? C - col : 0);
+        const int64_t col = c + RUN * g;
+        return load_row<F32, RUN, VEC>(base + col * ES, (p.base && tv.live && c < c1) ? C - col : 0);
     };
     frag_t w[RB][4];
     Row16<F32> y0 = load_y(c0);
@@ -574,12 +613,12 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
         float v[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = row_value<F32>(y0, e) + acc[e >> 2][e & 3];
-        const int64_t col = c + 16 * g;
+        const int64_t col = c + RUN * g;
         if (c + cstep < c1) {
             y0 = load_y(c + cstep);
             load_b(c + cstep, w);
         }
-        if (tv.live && col < C) store_row<F32, VEC>(out + col * ES, C - col, v);
+        if (tv.live) store_row<F32, RUN, VEC>(out + col * ES, C - col, v);
     }
 }
 
@@ -604,8 +643,7 @@ __device__ __forceinline__ frag_t read_tr(const uint8_t *p, int four)
 // of A are staged in LDS (two blocks of eight ranks, [pair of 16-column
 // groups][rank][64 bytes], the groups swapped in ranks 8 to 15: the rows that
 // half a wave reads together fall on all banks once) and read transposed. The
-// columns are permuted on the way in so that a lane's sums are 16 consecutive
-// ones.
+// columns are permuted on the way in (run_column).
 // ---------------------------------------------------------------------------
 template <bool VEC, int TG, bool F32>
 __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
@@ -625,8 +663,8 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
     Row16<false> x0[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int64_t col = c0 + 64 * c + 16 * g;
-        x0[c] = load_row<false, VEC>(a.dx0 + tv.token * a.lddx0 + col, (a.dx0 && tv.live) ? C - col : 0);
+        const int64_t col = c0 + 64 * c + 8 * g;
+        x0[c] = load_row<false, 8, VEC>(a.dx0 + tv.token * a.lddx0 + col, (a.dx0 && tv.live) ? C - col : 0);
     }
     f32x4_t acc[NC][4];
 #pragma unroll
@@ -653,9 +691,9 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
             uint8_t *sa = s_a[v & 1];
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                // rank k, columns 8 cc ..: quads (i, j) and (i, j + 1) of 64-column group cc / 8
+                // rank k, columns 8 cc ..: rows 4 i .. of blocks f and f + 1 (run_column)
                 const int w = t + AT * q, k = w >> 5, cc = w & 31, kk = 4 * (k >> 3) + (k & 3);
-                const int i = (cc & 7) >> 1, f = 4 * (cc >> 3) + 2 * (cc & 1);
+                const int i = cc & 3, f = 4 * (cc >> 3) + 2 * ((cc >> 2) & 1);
                 uint8_t *d = sa + ((k >> 2) & 1) * 4096 + (f >> 1) * 512 + kk * 64 + 8 * i;
                 const int swap = 32 * (kk >> 2);
                 *reinterpret_cast<uint2 *>(d + swap) = make_uint2(st[q][0], st[q][1]);
@@ -681,52 +719,54 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
     if (!tv.live) return;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int64_t col = c0 + 64 * c + 16 * g;
-        if (col >= C) continue;
+        const int64_t col = c0 + 64 * c + 8 * g;
         float v[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = row_value<false>(x0[c], e) + acc[c][e >> 2][e & 3];
-        store_row<F32, VEC>(static_cast<char *>(a.dx) + (tv.token * a.lddx + col) * (F32 ? 4 : 2), C - col, v);
+        store_row<F32, 8, VEC>(static_cast<char *>(a.dx) + (tv.token * a.lddx + col) * (F32 ? 4 : 2), C - col, v);
     }
 }
 
 // ---------------------------------------------------------------------------
 // dy pass: of a piece's tokens, dB[c][r] = sum_m dy[m][c] (s t)[m][r] and the
 // partial u[m][r] = sum over the block's 256 columns of dy[m][c] B[c][r], from
-// one reading of dy. A wave owns 64 columns. Per step of 32 tokens it stages its
-// 32 x 64 of dy in LDS and the block stages s t in three parts. For dB both are
-// read transposed (tokens along the depth); for u dy is read as it lies, and the
-// wave's 64 x rank of B^T stay in registers for the whole piece.
+// one reading of dy. Per step of 64 tokens the block stages 64 x 256 of dy and s
+// t in three parts in LDS, and holds the next step's in registers. For dB (a
+// wave: 64 columns, all tokens) both are read transposed, tokens along the depth;
+// for u (a wave: 16 tokens, all columns) dy is read as it lies and the block's
+// 256 x rank of B, staged once, transposed. 64 tokens a step keep 32 KiB of dy
+// in flight per block; with 32 the loads' latency showed (83 us for 8192 tokens
+// of q, k and v).
 //
-// LDS rows of dy: 64 columns, 128 bytes, in 32-byte groups; group q of row k
-// lies at q ^ key(k), so that the eight rows that half a wave reads together
-// fall on different banks.
+// LDS rows of dy: a wave's 64 columns, 128 bytes, in 32-byte groups; group q of
+// row k lies at q ^ key(k), so that the eight rows that half a wave reads
+// together fall on different banks. The others: 32-byte rows of 16 values.
 // ---------------------------------------------------------------------------
-constexpr int OUT_COLS = 256;
+constexpr int OUT_COLS = 256, OUT_STEP = 64;
 
 __device__ __forceinline__ int out_key(int k) { return ((k >> 1) & 1) | (((k >> 3) & 1) << 1); }
 
-// The wave's 32 rows x 64 columns from k0 of the piece on: lane -> row lane / 8
+// The wave's 64 rows x 64 columns from k0 of the piece on: lane -> row lane / 8
 // (+ 8 i), columns c + 8 (lane % 8) ..
 template <bool VEC>
 __device__ __forceinline__ void out_fetch(const uint16_t *S, int64_t ld, const int32_t *order, int k0, int count, int64_t c,
-                                          int64_t C, frag_t (&sv)[4])
+                                          int64_t C, frag_t (&sv)[8])
 {
     const int lane = threadIdx.x & 63;
     const int64_t col = c + 8 * (lane & 7);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
         const int k = k0 + 8 * i + (lane >> 3);
         const bool in = k < count;
         sv[i] = load8<VEC>(S + int64_t(order[in ? k : 0]) * ld + col, in ? C - col : 0);
     }
 }
 
-__device__ __forceinline__ void out_stage(uint8_t *ss, const frag_t (&sv)[4])
+__device__ __forceinline__ void out_stage(uint8_t *ss, const frag_t (&sv)[8])
 {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
         const int k = 8 * i + (lane >> 3);
         *reinterpret_cast<frag_t *>(ss + k * 128 + ((((lane & 7) >> 1) ^ out_key(k)) << 5) + ((lane & 1) << 4)) = sv[i];
     }
@@ -751,10 +791,9 @@ __device__ __forceinline__ OutPlace out_place(const AdArgs &a, const int4 &piece
 template <int RB, bool VEC>
 __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
 {
-    constexpr int RP = 16 * RB;
-    __shared__ __attribute__((aligned(16))) uint8_t s_s[4][32 * 128];
-    __shared__ __attribute__((aligned(16))) uint8_t s_q[32 * 96 * RB];   // [32][3][RP] bf16
-    __shared__ __attribute__((aligned(16))) float s_u[4][32][RP + 4];
+    __shared__ __attribute__((aligned(16))) uint8_t s_s[4][OUT_STEP * 128];
+    __shared__ __attribute__((aligned(16))) uint8_t s_q[RB][3][OUT_STEP * 32];
+    __shared__ __attribute__((aligned(16))) uint8_t s_b[RB][OUT_COLS * 32];
     if (int(blockIdx.x) >= a.plan[2]) return;
     const int4 piece = reinterpret_cast<const int4 *>(a.plan + a.l.pieces)[blockIdx.x];
     const int pi = blockIdx.z;
@@ -768,87 +807,94 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
     const int32_t *order = a.plan + a.l.order + piece.y;
     const int re = rank_of(p, piece.x, a.rank);
     const float sc = scale_of(p, piece.x);
-    // B^T of the wave's columns: rank 16 b + r16, columns c0 + 32 h + 8 g ..
-    frag_t bt[2][RB];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            const int64_t c = c0 + 32 * h + 8 * g;
-            const int r = 16 * b + r16;
-            bt[h][b] = load8_strided(p.B + (int64_t(piece.x) * C + c) * a.rank + r, a.rank, r < re ? C - c : 0);
-        }
-    f32x4_t acc[4][RB];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int b = 0; b < RB; ++b) acc[i][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    uint8_t *ss = s_s[wave];
+    const bool bvec = (a.rank & 7) == 0 && (reinterpret_cast<uintptr_t>(p.B) & 15) == 0;
+    frag_t sv[8];
     // s t: eight ranks of a row a thread
-    constexpr int QV = (64 * RB + AT - 1) / AT;
-    frag_t sv[4];
+    constexpr int QV = (OUT_STEP * 2 * RB + AT - 1) / AT;
     float qv[QV][8];
     auto fetch = [&](int k0) {
         out_fetch<VEC>(S, p.ldb, order, k0, piece.z, c0, C, sv);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
-            const bool in = row < 32 && k0 + row < piece.z;
+            const bool in = row < OUT_STEP && k0 + row < piece.z;
             const float *tr = p.t + int64_t(order[in ? k0 + row : 0]) * a.rank + r;
 #pragma unroll
             for (int e = 0; e < 8; ++e) qv[q][e] = (in && r + e < re) ? sc * tr[e] : 0.0f;
         }
     };
     fetch(0);
+    // B: row (column of dy) t, 16 ranks of every block
+    {
+        const uint16_t *br = p.B + (int64_t(piece.x) * C + cb + t) * a.rank;
+        const bool in = cb + t < C;
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 16 * b + 8 * h, left = in ? re - r : 0;
+                frag_t v = bvec ? load8<true>(br + r, left) : load8<false>(br + r, left);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e >= left) v[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+                *reinterpret_cast<frag_t *>(s_b[b] + t * 32 + 16 * h) = v;
+            }
+    }
+    f32x4_t acc[4][RB];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int b = 0; b < RB; ++b) acc[i][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    uint8_t *ss = s_s[wave];
     const int kr = 8 * g + (r16 >> 2), key = out_key(kr);  // the lane's row in a transposed read
-    for (int k0 = 0; k0 < piece.z; k0 += 32) {
+    const int quad = (r16 & 3) << 3;
+    for (int k0 = 0; k0 < piece.z; k0 += OUT_STEP) {
         __syncthreads();  // the last step's reads are over
         out_stage(ss, sv);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
-            if (row >= 32) continue;
+            if (row >= OUT_STEP) continue;
             frag_t part[3];
             split3(qv[q], part);
 #pragma unroll
-            for (int h = 0; h < 3; ++h) *reinterpret_cast<frag_t *>(s_q + row * 96 * RB + h * 32 * RB + 2 * r) = part[h];
+            for (int h = 0; h < 3; ++h) *reinterpret_cast<frag_t *>(s_q[r >> 4][h] + row * 32 + 2 * (r & 8)) = part[h];
         }
         __syncthreads();
-        if (k0 + 32 < piece.z) fetch(k0 + 32);
-        frag_t sf[4];
+        if (k0 + OUT_STEP < piece.z) fetch(k0 + OUT_STEP);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            sf[i] = read_tr(ss + kr * 128 + ((i ^ key) << 5) + ((r16 & 3) << 3), 4 * 128);
+        for (int d = 0; d < 2; ++d) {  // 32 tokens
+            if (k0 + 32 * d >= piece.z) break;
+            frag_t sf[4];
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
+            for (int i = 0; i < 4; ++i) sf[i] = read_tr(ss + (32 * d + kr) * 128 + ((i ^ key) << 5) + quad, 4 * 128);
 #pragma unroll
-            for (int h = 0; h < 3; ++h) {
-                const frag_t qf = read_tr(s_q + kr * (96 * RB) + h * (32 * RB) + b * 32 + ((r16 & 3) << 3), 4 * 96 * RB);
+            for (int b = 0; b < RB; ++b)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i][b] = mfma(sf[i], qf, acc[i][b]);
-            }
-        // u of 32 tokens over the wave's columns
+                for (int h = 0; h < 3; ++h) {
+                    const frag_t qf = read_tr(s_q[b][h] + (32 * d + kr) * 32 + quad, 4 * 32);
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int row = 16 * m + r16;
-            frag_t rf[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                rf[h] = *reinterpret_cast<const frag_t *>(ss + row * 128 + (((2 * h + (g >> 1)) ^ out_key(row)) << 5) + ((g & 1) << 4));
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                f32x4_t u = mfma(bt[0][b], rf[0], f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
-                u = mfma(bt[1][b], rf[1], u);
-                *reinterpret_cast<f32x4_t *>(&s_u[wave][row][16 * b + 4 * g]) = u;
-            }
+                    for (int i = 0; i < 4; ++i) acc[i][b] = mfma(sf[i], qf, acc[i][b]);
+                }
         }
-        __syncthreads();
+        // u of tokens 16 wave .. + 15 over the block's columns
+        const int row = 16 * wave + r16;
+        if (k0 + 16 * wave < piece.z) {
+            f32x4_t u[RB];
 #pragma unroll
-        for (int q = 0; q < 2 * RB; ++q) {
-            const int w = t + AT * q, row = w / RP, r = w - row * RP;
-            if (k0 + row >= piece.z) continue;
-            const float u = (s_u[0][row][r] + s_u[1][row][r]) + (s_u[2][row][r] + s_u[3][row][r]);
-            a.part[((int64_t(blockIdx.y) * a.nv + pi * RB + (r >> 4)) * a.M + piece.y + k0 + row) * 16 + (r & 15)] = u;
+            for (int b = 0; b < RB; ++b) u[b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int h = 0; h < 8; ++h) {
+                const frag_t rf = *reinterpret_cast<const frag_t *>(
+                    s_s[h >> 1] + row * 128 + (((2 * (h & 1) + (g >> 1)) ^ out_key(row)) << 5) + ((g & 1) << 4));
+#pragma unroll
+                for (int b = 0; b < RB; ++b) u[b] = mfma(read_tr(s_b[b] + (32 * h + kr) * 32 + quad, 4 * 32), rf, u[b]);
+            }
+            if (k0 + row < piece.z)
+#pragma unroll
+                for (int b = 0; b < RB; ++b)
+                    *reinterpret_cast<f32x4_t *>(
+                        a.part + ((int64_t(blockIdx.y) * a.nv + pi * RB + b) * a.M + piece.y + k0 + row) * 16 + 4 * g) = u[b];
         }
     }
     // lane: columns c0 + 16 i + 4 g .. + 3 at rank 16 b + r16
@@ -908,8 +954,8 @@ __global__ __launch_bounds__(AT) void adapters_parts(const AdArgs a)
 template <int VB, bool VEC>
 __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
 {
-    __shared__ __attribute__((aligned(16))) uint8_t s_s[4][32 * 128];
-    __shared__ __attribute__((aligned(16))) uint8_t s_q[VB][32 * 96];  // [32][3][16] bf16 each
+    __shared__ __attribute__((aligned(16))) uint8_t s_s[4][OUT_STEP * 128];
+    __shared__ __attribute__((aligned(16))) uint8_t s_q[VB][3][OUT_STEP * 32];
     if (int(blockIdx.x) >= a.plan[2]) return;
     const int4 piece = reinterpret_cast<const int4 *>(a.plan + a.l.pieces)[blockIdx.x];
     const int64_t C = a.d_in, cb = int64_t(blockIdx.y) * OUT_COLS;
@@ -924,39 +970,45 @@ __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
 #pragma unroll
         for (int b = 0; b < VB; ++b) acc[i][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     uint8_t *ss = s_s[wave];
-    constexpr int QW = 192 * VB, QV = (QW + AT - 1) / AT;  // 16-byte words of u's parts
-    frag_t sv[4], qv[QV];
+    constexpr int QR = OUT_STEP * 6, QV = (VB * QR + AT - 1) / AT;  // 16-byte words of u's parts, of a block
+    frag_t sv[8], qv[QV];
     auto fetch = [&](int k0) {
         out_fetch<VEC>(a.X, a.ldx, order, k0, piece.z, c0, C, sv);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
-            const int w = t + AT * q, b = w / 192, x = w - 192 * b, row = x / 6;
-            const bool in = w < QW && v0 + b < a.nv && k0 + row < piece.z;
+            const int w = t + AT * q, b = w / QR, x = w - QR * b, row = x / 6;
+            const bool in = b < VB && v0 + b < a.nv && k0 + row < piece.z;
             qv[q] = in ? reinterpret_cast<const frag_t *>(a.hl + (int64_t(v0 + b) * a.M + piece.y + k0) * 48)[x] : zero_frag();
         }
     };
     fetch(0);
-    const int kr = 8 * g + (r16 >> 2), key = out_key(kr);
-    for (int k0 = 0; k0 < piece.z; k0 += 32) {
+    const int kr = 8 * g + (r16 >> 2), key = out_key(kr), quad = (r16 & 3) << 3;
+    for (int k0 = 0; k0 < piece.z; k0 += OUT_STEP) {
         __syncthreads();  // the last step's reads are over
         out_stage(ss, sv);
 #pragma unroll
-        for (int q = 0; q < QV; ++q)
-            if (t + AT * q < QW) reinterpret_cast<frag_t *>(s_q)[t + AT * q] = qv[q];
+        for (int q = 0; q < QV; ++q) {
+            // parts of a row: 0 0 1 1 2 2
+            const int w = t + AT * q, b = w / QR, x = w - QR * b, row = x / 6, c = x - 6 * row;
+            if (b < VB) *reinterpret_cast<frag_t *>(s_q[b][c >> 1] + row * 32 + 16 * (c & 1)) = qv[q];
+        }
         __syncthreads();
-        if (k0 + 32 < piece.z) fetch(k0 + 32);
-        frag_t sf[4];
+        if (k0 + OUT_STEP < piece.z) fetch(k0 + OUT_STEP);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            sf[i] = read_tr(ss + kr * 128 + ((i ^ key) << 5) + ((r16 & 3) << 3), 4 * 128);
+        for (int d = 0; d < 2; ++d) {  // 32 tokens
+            if (k0 + 32 * d >= piece.z) break;
+            frag_t sf[4];
 #pragma unroll
-        for (int b = 0; b < VB; ++b)
+            for (int i = 0; i < 4; ++i) sf[i] = read_tr(ss + (32 * d + kr) * 128 + ((i ^ key) << 5) + quad, 4 * 128);
 #pragma unroll
-            for (int h = 0; h < 3; ++h) {
-                const frag_t qf = read_tr(s_q[b] + kr * 96 + h * 32 + ((r16 & 3) << 3), 4 * 96);
+            for (int b = 0; b < VB; ++b)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i][b] = mfma(sf[i], qf, acc[i][b]);
-            }
+                for (int h = 0; h < 3; ++h) {
+                    const frag_t qf = read_tr(s_q[b][h] + (32 * d + kr) * 32 + quad, 4 * 32);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[i][b] = mfma(sf[i], qf, acc[i][b]);
+                }
+        }
     }
 #pragma unroll
     for (int b = 0; b < VB; ++b) {
@@ -1019,12 +1071,12 @@ int rank_blocks(int rank) { return rank <= 16 ? 1 : (rank <= 32 ? 2 : (rank <= 6
 // Rank blocks that a launch over x takes at once, of nv.
 int blocks_at_once(int nv) { return nv <= 4 ? nv : (nv % 3 == 0 ? 3 : 4); }
 
-// Splits of d_in: until the launch has about 2048 blocks, each wave keeping
+// Splits of d_in: until the launch has about 1024 blocks, each wave keeping
 // 128 or more of it.
 int shrink_splits(int64_t tiles, int groups, int64_t K, bool split_waves)
 {
-    const int64_t most = std::max<int64_t>(1, K / (split_waves ? 512 : 128));
-    return int(std::clamp<int64_t>(2048 / std::max<int64_t>(1, tiles * groups), 1, std::min<int64_t>(most, 8)));
+    const int64_t most = std::max<int64_t>(1, K / (split_waves ? 512 : 256));
+    return int(std::clamp<int64_t>(1024 / std::max<int64_t>(1, tiles * groups), 1, std::min<int64_t>(most, 16)));
 }
 
 AdLayout ad_layout(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_in, const int64_t *d_out)
@@ -1170,8 +1222,8 @@ hipError_t run_forward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest
     if (e != hipSuccess) return e;
     // columns of a block: t is summed once for all of them, but few tiles need
     // many blocks to fill the compute units
-    const int64_t wide = (a.l.tile == 16) ? 1024 : 512;
-    a.ecols = (int64_t(tiles) * c.np * blocks(widest, wide) >= 2048) ? int(wide) : 256;
+    a.ecols = (a.l.tile == 16) ? 1024 : 512;
+    while (a.ecols > 256 && int64_t(tiles) * c.np * blocks(widest, a.ecols) < 768) a.ecols /= 2;
     const dim3 egrid(tiles, blocks(widest, a.ecols), unsigned(c.np));
     if (f32) return vy ? launch_expand<true, true>(a, egrid, direct, st) : launch_expand<false, true>(a, egrid, direct, st);
     return vy ? launch_expand<true, false>(a, egrid, direct, st) : launch_expand<false, false>(a, egrid, direct, st);
