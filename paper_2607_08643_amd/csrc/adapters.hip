@@ -10,7 +10,8 @@
 //
 //   shrink   a tile's t: d_in is split over blocks and waves, whose fp32 partial
 //            sums go to the workspace;
-//   expand   sums those in order and adds s B t to a tile's rows of y;
+//   parts    sums those in order (small batches: expand does);
+//   expand   adds s B t to a tile's rows of y;
 //   dy       of a run of one adapter's tokens (a "piece"), dB and the partial
 //            sums of u from one reading of dy;
 //   da, dx   dA of a piece, and A^T u added to a tile's rows of dx.
@@ -33,6 +34,9 @@ constexpr int AT = 256;  // threads of a block: 4 waves
 // Up to this many tokens a forward call groups them itself, every block from the
 // ids: a plan's launch (5 us) would be a third of a decode step's time.
 constexpr int64_t DIRECT_TOKENS = BSQ_ADAPTERS_DIRECT;
+#ifndef ECB
+#define ECB 768
+#endif
 constexpr int PLAN_WAVES = 16, PLAN_AHEAD = 8;  // groups of 64 ids that a wave has in flight
 
 struct PlanLayout {
@@ -215,7 +219,7 @@ struct AdArgs {
     int n, np, rank, rb, nv, ksplit, ecols;
     int accumulate;
     float *part;      // forward [ksplit][nv][M][16], backward [chunks][nv][M][16]: partial t or u
-    uint16_t *hl;     // [nv][M][3][16]: u as three bf16 parts
+    uint16_t *hl;     // [nv][M][3][16]: s t or u as three bf16 parts
     float *slots;     // partial dB and dA
     int64_t slot_floats;
 };
@@ -547,7 +551,7 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
     const int64_t c0 = cb + (TG == 1 ? 64 * wave : 0), cstep = (TG == 1) ? 256 : 64;
     const int64_t c1 = (cb + a.ecols < C) ? cb + a.ecols : C;
     const int ad = tv.adapter;
-    const bool keep = p.t && blockIdx.y == 0 && (TG != 1 || wave == 0) && tv.live;
+    const bool keep = DIRECT && p.t && blockIdx.y == 0 && wave == 0 && tv.live;
     // rows without an adapter stay as they are in place
     if (ad < 0 && p.base == p.y && !keep) return;
     const int re = ad >= 0 ? rank_of(p, ad, a.rank) : 0;
@@ -584,19 +588,27 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
     frag_t tf[RB], tf3[F32 ? RB : 1];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (ad >= 0) part_sum(a, a.ksplit, int(blockIdx.z) * RB + b, tv.place, r0, v);
-        if (keep && g < 2)
+        tf[b] = zero_frag();
+        if (F32) tf3[b] = zero_frag();
+        if constexpr (DIRECT) {
+            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (ad >= 0) part_sum(a, a.ksplit, int(blockIdx.z) * RB + b, tv.place, r0, v);
+            if (keep && g < 2)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (16 * b + r0 + e < a.rank) p.t[tv.token * a.rank + 16 * b + r0 + e] = v[e];
-        const float sc = ad >= 0 ? scale_of(p, ad) : 0.0f;
+                for (int e = 0; e < 8; ++e)
+                    if (16 * b + r0 + e < a.rank) p.t[tv.token * a.rank + 16 * b + r0 + e] = v[e];
+            const float sc = ad >= 0 ? scale_of(p, ad) : 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= sc;
-        frag_t part[3];
-        split3(v, part);
-        tf[b] = (g < 2) ? part[0] : part[1];
-        if (F32) tf3[b] = (g < 2) ? part[2] : zero_frag();
+            for (int e = 0; e < 8; ++e) v[e] *= sc;
+            frag_t part[3];
+            split3(v, part);
+            tf[b] = (g < 2) ? part[0] : part[1];
+            if (F32 && g < 2) tf3[b] = part[2];
+        } else if (ad >= 0) {
+            const uint16_t *q = a.hl + (int64_t(int(blockIdx.z) * RB + b) * a.M + tv.place) * 48 + r0;
+            tf[b] = *reinterpret_cast<const frag_t *>(q + 16 * (g >> 1));
+            if (F32 && g < 2) tf3[b] = *reinterpret_cast<const frag_t *>(q + 32);
+        }
     }
     if (ad < 0 && p.base == p.y) return;
     for (int64_t c = c0; c < c1; c += cstep) {
@@ -747,19 +759,27 @@ constexpr int OUT_COLS = 256, OUT_STEP = 64;
 __device__ __forceinline__ int out_key(int k) { return ((k >> 1) & 1) | (((k >> 3) & 1) << 1); }
 
 // The wave's 64 rows x 64 columns from k0 of the piece on: lane -> row lane / 8
-// (+ 8 i), columns c + 8 (lane % 8) ..
+// (+ 8 i), columns c + 8 (lane % 8) .. The rows' tokens are read a step before
+// (out_tokens), so that no load waits for another.
+__device__ __forceinline__ void out_tokens(const int32_t *order, int k0, int count, int32_t (&tok)[8])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int k = k0 + 8 * i + (lane >> 3);
+        tok[i] = order[k < count ? k : 0];
+    }
+}
+
 template <bool VEC>
-__device__ __forceinline__ void out_fetch(const uint16_t *S, int64_t ld, const int32_t *order, int k0, int count, int64_t c,
+__device__ __forceinline__ void out_fetch(const uint16_t *S, int64_t ld, const int32_t (&tok)[8], int k0, int count, int64_t c,
                                           int64_t C, frag_t (&sv)[8])
 {
     const int lane = threadIdx.x & 63;
     const int64_t col = c + 8 * (lane & 7);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int k = k0 + 8 * i + (lane >> 3);
-        const bool in = k < count;
-        sv[i] = load8<VEC>(S + int64_t(order[in ? k : 0]) * ld + col, in ? C - col : 0);
-    }
+    for (int i = 0; i < 8; ++i)
+        sv[i] = load8<VEC>(S + int64_t(tok[i]) * ld + col, (k0 + 8 * i + (lane >> 3) < count) ? C - col : 0);
 }
 
 __device__ __forceinline__ void out_stage(uint8_t *ss, const frag_t (&sv)[8])
@@ -812,17 +832,28 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
     // s t: eight ranks of a row a thread
     constexpr int QV = (OUT_STEP * 2 * RB + AT - 1) / AT;
     float qv[QV][8];
+    int32_t tok[8], qtok[QV];
+    auto tokens = [&](int k0) {
+        out_tokens(order, k0, piece.z, tok);
+#pragma unroll
+        for (int q = 0; q < QV; ++q) {
+            const int k = k0 + (t + AT * q) / (2 * RB);
+            qtok[q] = order[k < piece.z ? k : 0];
+        }
+    };
     auto fetch = [&](int k0) {
-        out_fetch<VEC>(S, p.ldb, order, k0, piece.z, c0, C, sv);
+        out_fetch<VEC>(S, p.ldb, tok, k0, piece.z, c0, C, sv);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
             const bool in = row < OUT_STEP && k0 + row < piece.z;
-            const float *tr = p.t + int64_t(order[in ? k0 + row : 0]) * a.rank + r;
+            const float *tr = p.t + int64_t(qtok[q]) * a.rank + r;
 #pragma unroll
             for (int e = 0; e < 8; ++e) qv[q][e] = (in && r + e < re) ? sc * tr[e] : 0.0f;
         }
+        tokens(k0 + OUT_STEP);
     };
+    tokens(0);
     fetch(0);
     // B: row (column of dy) t, 16 ranks of every block
     {
@@ -915,8 +946,10 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
         }
 }
 
-// u = s times the partial sums in order, in three bf16 parts, zero past an
-// adapter's rank. One thread per eight ranks of a token; z: projection.
+// s times the partial sums of t (or u) in order, in three bf16 parts, zero past
+// an adapter's rank; t itself is kept where it is asked for. One thread per eight
+// ranks of a token; z: projection.
+template <bool BACK>
 __global__ __launch_bounds__(AT) void adapters_parts(const AdArgs a)
 {
     const int groups = 2 * a.rb;
@@ -924,20 +957,30 @@ __global__ __launch_bounds__(AT) void adapters_parts(const AdArgs a)
     const int64_t place = i / groups;
     const int r = int(i - place * groups) * 8;
     const int32_t *seg = a.plan + a.l.seg;
-    if (place >= seg[a.n]) return;
-    // its adapter: the last whose first place is not past it
-    int lo = 0, hi = a.n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (seg[mid] <= place) lo = mid;
-        else hi = mid;
-    }
+    if (place >= a.M) return;
     const int pi = blockIdx.z, v = pi * a.rb + (r >> 4);
     const Proj &p = a.p[pi];
+    const bool none = place >= seg[a.n];
+    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    int lo = 0, hi = a.n;
+    if (!none) {
+        part_sum(a, BACK ? int((p.d_out + OUT_COLS - 1) / OUT_COLS) : a.ksplit, v, place, r & 8, x);
+        // its adapter: the last whose first place is not past it
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (seg[mid] <= place) lo = mid;
+            else hi = mid;
+        }
+    }
+    if (!BACK && p.t) {
+        float *t = p.t + int64_t(a.plan[a.l.order + place]) * a.rank + r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (r + e < a.rank) t[e] = x[e];
+    }
+    if (none) return;
     const int re = rank_of(p, lo, a.rank);
     const float sc = scale_of(p, lo);
-    float x[8];
-    part_sum(a, int((p.d_out + OUT_COLS - 1) / OUT_COLS), v, place, r & 8, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (r + e < re) ? sc * x[e] : 0.0f;
     frag_t part[3];
@@ -972,8 +1015,11 @@ __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
     uint8_t *ss = s_s[wave];
     constexpr int QR = OUT_STEP * 6, QV = (VB * QR + AT - 1) / AT;  // 16-byte words of u's parts, of a block
     frag_t sv[8], qv[QV];
+    int32_t tok[8];
+    out_tokens(order, 0, piece.z, tok);
     auto fetch = [&](int k0) {
-        out_fetch<VEC>(a.X, a.ldx, order, k0, piece.z, c0, C, sv);
+        out_fetch<VEC>(a.X, a.ldx, tok, k0, piece.z, c0, C, sv);
+        out_tokens(order, k0 + OUT_STEP, piece.z, tok);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, b = w / QR, x = w - QR * b, row = x / 6;
@@ -1099,8 +1145,8 @@ AdLayout ad_layout(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_
         return p;
     };
     l.part = take(size_t(parts) * nv * size_t(M) * 16 * 4);
+    if (back || M > DIRECT_TOKENS) l.hl = take(size_t(nv) * size_t(M) * 48 * 2);
     if (back) {
-        l.hl = take(size_t(nv) * size_t(M) * 48 * 2);
         l.slots = take(size_t(pl.max_slots) * size_t(l.slot_floats) * 4);
         if (M <= DIRECT_TOKENS) l.plan = take(size_t(pl.words) * 4);
     }
@@ -1220,10 +1266,14 @@ hipError_t run_forward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest
     const dim3 sgrid(tiles, unsigned(a.ksplit), blocks(a.nv, vb));
     hipError_t e = va ? launch_shrink<true>(a, sgrid, vb, direct, st) : launch_shrink<false>(a, sgrid, vb, direct, st);
     if (e != hipSuccess) return e;
-    // columns of a block: t is summed once for all of them, but few tiles need
-    // many blocks to fill the compute units
+    if (!direct) {
+        hipLaunchKernelGGL((adapters_parts<false>), dim3(blocks(a.M * 2 * a.rb, AT), 1, unsigned(c.np)), dim3(AT), 0, st, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    // columns of a block: t and the tile are read once for all of them, but few
+    // tiles need many blocks to fill the compute units
     a.ecols = (a.l.tile == 16) ? 1024 : 512;
-    while (a.ecols > 256 && int64_t(tiles) * c.np * blocks(widest, a.ecols) < 768) a.ecols /= 2;
+    while (a.ecols > 256 && int64_t(tiles) * c.np * blocks(widest, a.ecols) < ECB) a.ecols /= 2;
     const dim3 egrid(tiles, blocks(widest, a.ecols), unsigned(c.np));
     if (f32) return vy ? launch_expand<true, true>(a, egrid, direct, st) : launch_expand<false, true>(a, egrid, direct, st);
     return vy ? launch_expand<true, false>(a, egrid, direct, st) : launch_expand<false, false>(a, egrid, direct, st);
@@ -1244,7 +1294,7 @@ hipError_t run_backward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t wides
     const dim3 dgrid(unsigned(a.l.max_pieces), blocks(widest, OUT_COLS), unsigned(c.np));
     hipError_t e = vd ? launch_dy<true>(a, dgrid, st) : launch_dy<false>(a, dgrid, st);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(adapters_parts, dim3(blocks(a.M * 2 * a.rb, AT), 1, unsigned(c.np)), dim3(AT), 0, st, a);
+    hipLaunchKernelGGL((adapters_parts<true>), dim3(blocks(a.M * 2 * a.rb, AT), 1, unsigned(c.np)), dim3(AT), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int vb = blocks_at_once(a.nv);
     const dim3 agrid(unsigned(a.l.max_pieces), blocks(c.d_in, OUT_COLS), blocks(a.nv, vb));
