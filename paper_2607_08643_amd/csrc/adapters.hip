@@ -34,9 +34,6 @@ constexpr int AT = 256;  // threads of a block: 4 waves
 // Up to this many tokens a forward call groups them itself, every block from the
 // ids: a plan's launch (5 us) would be a third of a decode step's time.
 constexpr int64_t DIRECT_TOKENS = BSQ_ADAPTERS_DIRECT;
-#ifndef ECB
-#define ECB 768
-#endif
 constexpr int PLAN_WAVES = 16, PLAN_AHEAD = 8;  // groups of 64 ids that a wave has in flight
 
 struct PlanLayout {
@@ -118,6 +115,7 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void adapters_plan_kernel(const Pl
             for (int q = 0; q < PLAN_AHEAD; ++q) id[q] = (m1 + 64 * q + lane < hi) ? a.ids[m1 + 64 * q + lane] : -1;
 #pragma unroll
             for (int q = 0; q < PLAN_AHEAD; ++q) {
+                if (m1 + 64 * q >= hi) break;
                 const int64_t m = m1 + 64 * q + lane;
                 const bool in = m < hi;
                 bad |= id[q] >= a.n;
@@ -244,20 +242,33 @@ __device__ __forceinline__ f32x4_t mfma(frag_t l, frag_t r, f32x4_t c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(l), as_bf16(r), c, 0, 0, 0);
 }
 
-// Eight values p[0 .. 8) of a row, those from `valid` on as zero. VEC: p is
-// 16-byte aligned and valid is 8 or more, or 0 or less.
+// A load under a condition is waited for where it stands. So loads are
+// unconditional, from where there is something to read, and what is not part of
+// the data is masked where it is used.
+//
+// Values k .. k + 7 of a row of n; those past its end are others of the row.
+// VEC: the row is 16-byte aligned, n and k multiples of 8.
 template <bool VEC>
-__device__ __forceinline__ frag_t load8(const uint16_t *p, int64_t valid)
+__device__ __forceinline__ frag_t raw8(const uint16_t *row, int64_t k, int64_t n)
+{
+    if constexpr (VEC) return *reinterpret_cast<const frag_t *>(row + (k < n ? k : 0));
+    frag_t v = zero_frag();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e >> 1] |= uint32_t(row[k + e < n ? k + e : n - 1]) << (16 * (e & 1));
+    return v;
+}
+
+// v's first `left` values, zeros behind them. VEC: all eight or none.
+template <bool VEC>
+__device__ __forceinline__ frag_t first8(frag_t v, int64_t left)
 {
     if constexpr (VEC) {
-        return valid > 0 ? *reinterpret_cast<const frag_t *>(p) : zero_frag();
-    } else {
-        frag_t v = zero_frag();
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < valid) v[e >> 1] |= uint32_t(p[e]) << (16 * (e & 1));
-        return v;
+        const uint32_t m = left > 0 ? ~0u : 0u;
+        return frag_t{v[0] & m, v[1] & m, v[2] & m, v[3] & m};
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] &= (left > 2 * e ? 0xffffu : 0u) | (left > 2 * e + 1 ? 0xffff0000u : 0u);
+    return v;
 }
 
 // The bf16 parts of x: rounded, and what remains, rounded, twice (nothing
@@ -303,11 +314,10 @@ __device__ __forceinline__ bool tile_view(const AdArgs &a, bool with_none, int (
         int before = 0, all = 0, at[W];
         bool same[W];
 #pragma unroll
-        for (int w = 0; w < W; ++w) id[w] = (64 * w + lane < a.M) ? a.ids[64 * w + lane] : -2;
+        for (int w = 0; w < W; ++w) id[w] = a.ids[64 * w + lane < a.M ? 64 * w + lane : 0];
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const int one = (id[w] >= a.n || (id[w] < 0 && 64 * w + lane < a.M)) ? -1 : id[w];
-            same[w] = one == mine && 64 * w + lane < a.M;
+            same[w] = ((id[w] >= 0 && id[w] < a.n) ? id[w] : -1) == mine && 64 * w + lane < a.M;
             const uint64_t mask = __ballot(same[w]);
             at[w] = all + __popcll(mask & ((uint64_t(1) << lane) - 1));
             if ((b >> 6) == w) before = all + __popcll(mask & ((uint64_t(1) << (b & 63)) - 1));
@@ -358,11 +368,11 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t K = a.d_in;
     const int v0 = int(blockIdx.z) * VB;
-    // this wave's range of k, whole steps of 32, and its tokens
+    // the block's range of k, whole steps of 32, that the waves along it take in
+    // turns of U, and the wave's tokens
     const int kw = (TG == 1) ? wave : wave & 1, tg = (TG == 1) ? 0 : wave >> 1;
-    const int64_t nshare = int64_t(a.ksplit) * KW, share = int64_t(blockIdx.y) * KW + kw;
-    const int64_t steps = (K + 31) / 32;
-    const int64_t s0 = steps * share / nshare, s1 = (32 * tg < tv.count || TG == 1) ? steps * (share + 1) / nshare : s0;
+    const int64_t steps = (K + 31) / 32, s0 = steps * blockIdx.y / a.ksplit;
+    const int64_t s1 = (32 * tg < tv.count || TG == 1) ? steps * (blockIdx.y + 1) / a.ksplit : s0;
     const uint16_t *xrow[MT];
     int64_t place[MT];
     bool live[MT];
@@ -379,14 +389,16 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
             xrow[m] = a.X + int64_t(a.plan[a.l.order + place[m]]) * a.ldx;
         }
     }
+    // ranks past the adapter's own read its first (rows of a product do not mix)
     const uint16_t *arow[VB];
-    bool ain[VB];
+    int rin[VB];  // of the lane's four results, those within the adapter's rank
 #pragma unroll
     for (int b = 0; b < VB; ++b) {
-        const int v = v0 + b < a.nv ? v0 + b : a.nv - 1, pi = v / a.rb, r = 16 * (v - pi * a.rb) + r16;
+        const int v = v0 + b < a.nv ? v0 + b : a.nv - 1, pi = v / a.rb, r0 = 16 * (v - pi * a.rb);
         const Proj &p = a.p[pi];
-        ain[b] = r < rank_of(p, tv.adapter, a.rank);
-        arow[b] = p.A + (int64_t(tv.adapter) * a.rank + (ain[b] ? r : 0)) * K;
+        const int re = rank_of(p, tv.adapter, a.rank);
+        rin[b] = re - r0 - 4 * g;
+        arow[b] = p.A + (int64_t(tv.adapter) * a.rank + (r0 + r16 < re ? r0 + r16 : 0)) * K;
     }
     f32x4_t acc[MT][VB];
 #pragma unroll
@@ -395,23 +407,28 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
         for (int b = 0; b < VB; ++b) acc[m][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     frag_t x[U][MT], w[U][VB];
     auto fetch = [&](int u, int64_t s) {
-        const int64_t k = 32 * s + 8 * g, left = (s < s1) ? K - k : 0;
+        const int64_t k = 32 * (s < s1 ? s : s0) + 8 * g;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) x[u][m] = load8<VEC>(xrow[m] + k, left);
+        for (int m = 0; m < MT; ++m) x[u][m] = raw8<VEC>(xrow[m], k, K);
 #pragma unroll
-        for (int b = 0; b < VB; ++b) w[u][b] = load8<VEC>(arow[b] + k, ain[b] ? left : 0);
+        for (int b = 0; b < VB; ++b) w[u][b] = raw8<VEC>(arow[b], k, K);
     };
+    if (s0 < s1) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) fetch(u, s0 + u);
-    for (int64_t s = s0; s < s1; s += U)
+        for (int u = 0; u < U; ++u) fetch(u, s0 + U * kw + u);
+        for (int64_t s = s0 + U * kw; s < s1; s += U * KW)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u) {
+                const int64_t left = (s + u < s1) ? K - 32 * (s + u) - 8 * g : 0;
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+                for (int m = 0; m < MT; ++m) {
+                    const frag_t xm = first8<VEC>(x[u][m], left);
 #pragma unroll
-                for (int b = 0; b < VB; ++b) acc[m][b] = mfma(w[u][b], x[u][m], acc[m][b]);
-            fetch(u, s + U + u);
-        }
+                    for (int b = 0; b < VB; ++b) acc[m][b] = mfma(w[u][b], xm, acc[m][b]);
+                }
+                fetch(u, s + U * KW + u);
+            }
+    }
     // lane: ranks 4 g .. + 3 of a block, of token r16; the waves along d_in added in order
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -426,6 +443,8 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
         f32x4_t v = s_acc[KW * tg][q][lane];
 #pragma unroll
         for (int k = 1; k < KW; ++k) v += s_acc[KW * tg + k][q][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < rin[b] ? v[e] : 0.0f;
         if (live[m] && v0 + b < a.nv) *reinterpret_cast<f32x4_t *>(part + (int64_t(v0 + b) * a.M + place[m]) * 16) = v;
     }
 }
@@ -467,28 +486,30 @@ struct Row16 {
     u32x4_t w[F32 ? 4 : 2];
 };
 
-// `p`: the lane's first column; `nc`: columns from there on that exist
+// `p`: the lane's first column; `nc`: columns from there on that exist; `whole`:
+// all of the wave's 64 do
 template <bool F32, int RUN, bool VEC>
-__device__ __forceinline__ Row16<F32> load_row(const void *p, int64_t nc)
+__device__ __forceinline__ Row16<F32> load_row(const void *p, int64_t nc, bool whole)
 {
     static_assert(!F32 || RUN == 4, "words of four 32-bit values");
     Row16<F32> v;
-    constexpr int NQ = 16 / RUN;
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
+    for (int q = 0; q < 16 / RUN; ++q) v.w[q] = zero_frag();
+    if (VEC && whole) {
+#pragma unroll
+        for (int q = 0; q < 16 / RUN; ++q) v.w[q] = *reinterpret_cast<const u32x4_t *>(static_cast<const char *>(p) + 64 * q);
+        return v;
+    }
+#pragma unroll
+    for (int q = 0; q < 16 / RUN; ++q) {
         const int64_t left = nc - 4 * RUN * q;
-        v.w[q] = zero_frag();
         const char *pq = static_cast<const char *>(p) + 64 * q;
-        if (VEC && left >= RUN) {
-            v.w[q] = *reinterpret_cast<const u32x4_t *>(pq);
-        } else {
 #pragma unroll
-            for (int e = 0; e < RUN; ++e)
-                if (e < left) {
-                    if constexpr (F32) v.w[q][e] = reinterpret_cast<const uint32_t *>(pq)[e];
-                    else v.w[q][e >> 1] |= uint32_t(reinterpret_cast<const uint16_t *>(pq)[e]) << (16 * (e & 1));
-                }
-        }
+        for (int e = 0; e < RUN; ++e)
+            if (e < left) {
+                if constexpr (F32) v.w[q][e] = reinterpret_cast<const uint32_t *>(pq)[e];
+                else v.w[q][e >> 1] |= uint32_t(reinterpret_cast<const uint16_t *>(pq)[e]) << (16 * (e & 1));
+            }
     }
     return v;
 }
@@ -561,24 +582,21 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
     char *out = static_cast<char *>(p.y) + tv.token * p.ldy * ES;
     const uint16_t *B = p.B + int64_t(ad < 0 ? 0 : ad) * C * a.rank;
     const int r0 = 8 * (g & 1);  // the lane's ranks of a block
+    // B: rows past d_out are its last (rows of a product do not mix), ranks past the
+    // adapter's own are masked before the product
+    const bool part_rank = p.ranks != nullptr || a.rank % 16 != 0;
     auto load_b = [&](int64_t c, frag_t (&w)[RB][4]) {
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
+        for (int j = 0; j < 4; ++j) {
+            const int64_t cc = c + run_column<RUN>(r16, j);
+            const uint16_t *row = B + (cc < C ? cc : C - 1) * a.rank;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t cc = c + run_column<RUN>(r16, j);
-                const int left = cc < C ? re - 16 * b - r0 : 0;
-                w[b][j] = load8<VEC>(B + cc * a.rank + 16 * b + r0, left);
-                // ranks past the adapter's own hold anything
-                if (VEC && p.ranks && left < 8)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e >= left) w[b][j][e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
-            }
+            for (int b = 0; b < RB; ++b) w[b][j] = raw8<VEC>(row, 16 * b + r0, a.rank);
+        }
     };
     auto load_y = [&](int64_t c) {
         const int64_t col = c + RUN * g;
-        return load_row<F32, RUN, VEC>(base + col * ES, (p.base && tv.live && c < c1) ? C - col : 0);
+        return load_row<F32, RUN, VEC>(base + col * ES, (p.base && tv.live) ? C - col : 0, p.base && c + 64 <= C);
     };
     frag_t w[RB][4];
     Row16<F32> y0 = load_y(c0);
@@ -615,6 +633,13 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
         f32x4_t acc[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (part_rank)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const frag_t m = first8<false>(frag_t{~0u, ~0u, ~0u, ~0u}, re - 16 * b - r0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[b][j] &= m;
+            }
 #pragma unroll
         for (int b = 0; b < RB; ++b)
 #pragma unroll
@@ -676,7 +701,8 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int64_t col = c0 + 64 * c + 8 * g;
-        x0[c] = load_row<false, 8, VEC>(a.dx0 + tv.token * a.lddx0 + col, (a.dx0 && tv.live) ? C - col : 0);
+        x0[c] = load_row<false, 8, VEC>(a.dx0 + tv.token * a.lddx0 + col, (a.dx0 && tv.live) ? C - col : 0,
+                                        a.dx0 && c0 + 64 * c + 64 <= C);
     }
     f32x4_t acc[NC][4];
 #pragma unroll
@@ -685,15 +711,15 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
         for (int j = 0; j < 4; ++j) acc[c][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     if (ad >= 0) {
         frag_t st[2];
+        int re = 0;  // ranks of the block in flight
         auto fetch = [&](int v) {
             const int pi = v / a.rb, b = v - pi * a.rb;
             const Proj &p = a.p[pi];
-            const int re = rank_of(p, ad, a.rank);
+            re = rank_of(p, ad, a.rank) - 16 * b;
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const int w = t + AT * q, r = 16 * b + (w >> 5);
-                const int64_t col = cb + 8 * (w & 31);
-                st[q] = load8<VEC>(p.A + (int64_t(ad) * a.rank + r) * C + col, r < re ? C - col : 0);
+                const int w = t + AT * q, r = w >> 5;
+                st[q] = raw8<VEC>(p.A + (int64_t(ad) * a.rank + 16 * b + (r < re ? r : 0)) * C, cb + 8 * (w & 31), C);
             }
         };
         fetch(0);
@@ -708,8 +734,9 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
                 const int i = cc & 3, f = 4 * (cc >> 3) + 2 * ((cc >> 2) & 1);
                 uint8_t *d = sa + ((k >> 2) & 1) * 4096 + (f >> 1) * 512 + kk * 64 + 8 * i;
                 const int swap = 32 * (kk >> 2);
-                *reinterpret_cast<uint2 *>(d + swap) = make_uint2(st[q][0], st[q][1]);
-                *reinterpret_cast<uint2 *>(d + (32 - swap)) = make_uint2(st[q][2], st[q][3]);
+                const frag_t x = first8<true>(st[q], k < re);  // (columns past d_in are not written)
+                *reinterpret_cast<uint2 *>(d + swap) = make_uint2(x[0], x[1]);
+                *reinterpret_cast<uint2 *>(d + (32 - swap)) = make_uint2(x[2], x[3]);
             }
             __syncthreads();  // (the buffer of v is written again at v + 2, past v + 1's barrier)
             if (v + 1 < a.nv) fetch(v + 1);
@@ -772,23 +799,24 @@ __device__ __forceinline__ void out_tokens(const int32_t *order, int k0, int cou
 }
 
 template <bool VEC>
-__device__ __forceinline__ void out_fetch(const uint16_t *S, int64_t ld, const int32_t (&tok)[8], int k0, int count, int64_t c,
-                                          int64_t C, frag_t (&sv)[8])
+__device__ __forceinline__ void out_fetch(const uint16_t *S, int64_t ld, const int32_t (&tok)[8], int64_t c, int64_t C,
+                                          frag_t (&sv)[8])
 {
     const int lane = threadIdx.x & 63;
-    const int64_t col = c + 8 * (lane & 7);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        sv[i] = load8<VEC>(S + int64_t(tok[i]) * ld + col, (k0 + 8 * i + (lane >> 3) < count) ? C - col : 0);
+    for (int i = 0; i < 8; ++i) sv[i] = raw8<VEC>(S + int64_t(tok[i]) * ld, c + 8 * (lane & 7), C);
 }
 
-__device__ __forceinline__ void out_stage(uint8_t *ss, const frag_t (&sv)[8])
+template <bool VEC>
+__device__ __forceinline__ void out_stage(uint8_t *ss, const frag_t (&sv)[8], int k0, int count, int64_t c, int64_t C)
 {
     const int lane = threadIdx.x & 63;
+    const int64_t left = C - c - 8 * (lane & 7);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int k = 8 * i + (lane >> 3);
-        *reinterpret_cast<frag_t *>(ss + k * 128 + ((((lane & 7) >> 1) ^ out_key(k)) << 5) + ((lane & 1) << 4)) = sv[i];
+        *reinterpret_cast<frag_t *>(ss + k * 128 + ((((lane & 7) >> 1) ^ out_key(k)) << 5) + ((lane & 1) << 4)) =
+            first8<VEC>(sv[i], k0 + k < count ? left : 0);
     }
 }
 
@@ -827,7 +855,6 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
     const int32_t *order = a.plan + a.l.order + piece.y;
     const int re = rank_of(p, piece.x, a.rank);
     const float sc = scale_of(p, piece.x);
-    const bool bvec = (a.rank & 7) == 0 && (reinterpret_cast<uintptr_t>(p.B) & 15) == 0;
     frag_t sv[8];
     // s t: eight ranks of a row a thread
     constexpr int QV = (OUT_STEP * 2 * RB + AT - 1) / AT;
@@ -842,14 +869,23 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
         }
     };
     auto fetch = [&](int k0) {
-        out_fetch<VEC>(S, p.ldb, tok, k0, piece.z, c0, C, sv);
+        out_fetch<VEC>(S, p.ldb, tok, c0, C, sv);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
-            const bool in = row < OUT_STEP && k0 + row < piece.z;
-            const float *tr = p.t + int64_t(qtok[q]) * a.rank + r;
+            const float *tr = p.t + int64_t(qtok[q]) * a.rank;
+            if constexpr (VEC) {  // (rank a multiple of 8, t 16-byte aligned)
+                const f32x4_t *t4 = reinterpret_cast<const f32x4_t *>(tr + (r < a.rank ? r : 0));
+                const f32x4_t u = t4[0], v = t4[1];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) qv[q][e] = (in && r + e < re) ? sc * tr[e] : 0.0f;
+                for (int e = 0; e < 4; ++e) {
+                    qv[q][e] = u[e];
+                    qv[q][4 + e] = v[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) qv[q][e] = tr[r + e < a.rank ? r + e : 0];
+            }
         }
         tokens(k0 + OUT_STEP);
     };
@@ -857,17 +893,14 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
     fetch(0);
     // B: row (column of dy) t, 16 ranks of every block
     {
-        const uint16_t *br = p.B + (int64_t(piece.x) * C + cb + t) * a.rank;
         const bool in = cb + t < C;
+        const uint16_t *br = p.B + (int64_t(piece.x) * C + (in ? cb + t : 0)) * a.rank;
 #pragma unroll
         for (int b = 0; b < RB; ++b)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int r = 16 * b + 8 * h, left = in ? re - r : 0;
-                frag_t v = bvec ? load8<true>(br + r, left) : load8<false>(br + r, left);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e >= left) v[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+                const int r = 16 * b + 8 * h;
+                const frag_t v = first8<false>(raw8<VEC>(br, r, a.rank), in ? re - r : 0);
                 *reinterpret_cast<frag_t *>(s_b[b] + t * 32 + 16 * h) = v;
             }
     }
@@ -881,13 +914,16 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
     const int quad = (r16 & 3) << 3;
     for (int k0 = 0; k0 < piece.z; k0 += OUT_STEP) {
         __syncthreads();  // the last step's reads are over
-        out_stage(ss, sv);
+        out_stage<VEC>(ss, sv, k0, piece.z, c0, C);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
             if (row >= OUT_STEP) continue;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (k0 + row < piece.z && r + e < re) ? sc * qv[q][e] : 0.0f;
             frag_t part[3];
-            split3(qv[q], part);
+            split3(x, part);
 #pragma unroll
             for (int h = 0; h < 3; ++h) *reinterpret_cast<frag_t *>(s_q[r >> 4][h] + row * 32 + 2 * (r & 8)) = part[h];
         }
@@ -1018,25 +1054,25 @@ __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
     int32_t tok[8];
     out_tokens(order, 0, piece.z, tok);
     auto fetch = [&](int k0) {
-        out_fetch<VEC>(a.X, a.ldx, tok, k0, piece.z, c0, C, sv);
+        out_fetch<VEC>(a.X, a.ldx, tok, c0, C, sv);
         out_tokens(order, k0 + OUT_STEP, piece.z, tok);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
-            const int w = t + AT * q, b = w / QR, x = w - QR * b, row = x / 6;
-            const bool in = b < VB && v0 + b < a.nv && k0 + row < piece.z;
-            qv[q] = in ? reinterpret_cast<const frag_t *>(a.hl + (int64_t(v0 + b) * a.M + piece.y + k0) * 48)[x] : zero_frag();
+            const int w = t + AT * q, b = w / QR, x = w - QR * b;
+            const int v = v0 + b < a.nv ? v0 + b : v0;
+            qv[q] = reinterpret_cast<const frag_t *>(a.hl + (int64_t(v) * a.M + piece.y + k0) * 48)[x / 6 < piece.z - k0 ? x : 0];
         }
     };
     fetch(0);
     const int kr = 8 * g + (r16 >> 2), key = out_key(kr), quad = (r16 & 3) << 3;
     for (int k0 = 0; k0 < piece.z; k0 += OUT_STEP) {
         __syncthreads();  // the last step's reads are over
-        out_stage(ss, sv);
+        out_stage<VEC>(ss, sv, k0, piece.z, c0, C);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             // parts of a row: 0 0 1 1 2 2
             const int w = t + AT * q, b = w / QR, x = w - QR * b, row = x / 6, c = x - 6 * row;
-            if (b < VB) *reinterpret_cast<frag_t *>(s_q[b][c >> 1] + row * 32 + 16 * (c & 1)) = qv[q];
+            if (b < VB) *reinterpret_cast<frag_t *>(s_q[b][c >> 1] + row * 32 + 16 * (c & 1)) = first8<true>(qv[q], k0 + row < piece.z);
         }
         __syncthreads();
         if (k0 + OUT_STEP < piece.z) fetch(k0 + OUT_STEP);
@@ -1272,8 +1308,8 @@ hipError_t run_forward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest
     }
     // columns of a block: t and the tile are read once for all of them, but few
     // tiles need many blocks to fill the compute units
-    a.ecols = (a.l.tile == 16) ? 1024 : 512;
-    while (a.ecols > 256 && int64_t(tiles) * c.np * blocks(widest, a.ecols) < ECB) a.ecols /= 2;
+    a.ecols = (a.l.tile == 16) ? 1024 : 256;
+    while (a.ecols > 256 && int64_t(tiles) * c.np * blocks(widest, a.ecols) < 768) a.ecols /= 2;
     const dim3 egrid(tiles, blocks(widest, a.ecols), unsigned(c.np));
     if (f32) return vy ? launch_expand<true, true>(a, egrid, direct, st) : launch_expand<false, true>(a, egrid, direct, st);
     return vy ? launch_expand<true, false>(a, egrid, direct, st) : launch_expand<false, false>(a, egrid, direct, st);
@@ -1281,14 +1317,15 @@ hipError_t run_forward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest
 
 hipError_t run_backward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest, hipStream_t st)
 {
-    bool vd = true, va = c.d_in % 8 == 0;
+    // vector loads of dy, t and B; of A with dx
+    bool vd = c.rank % 8 == 0, va = c.d_in % 8 == 0;
     for (int i = 0; i < c.np; ++i) {
         Proj &p = a.p[i];
         p.base = c.dy[i];
         p.ldb = c.lddy[i];
         p.dA = c.dA[i];
         p.dB = c.dB[i];
-        vd = vd && al16(p.base, 2 * p.ldb) && p.d_out % 8 == 0;
+        vd = vd && al16(p.base, 2 * p.ldb) && p.d_out % 8 == 0 && al16(p.t, 0) && al16(p.B, 0);
         va = va && al16(p.A, 2 * c.d_in);
     }
     const dim3 dgrid(unsigned(a.l.max_pieces), blocks(widest, OUT_COLS), unsigned(c.np));
