@@ -244,25 +244,62 @@ __device__ __forceinline__ f32x4_t mfma(frag_t l, frag_t r, f32x4_t c)
 
 // A load under a condition is waited for where it stands. So loads are
 // unconditional, from where there is something to read, and what is not part of
-// the data is masked where it is used.
-//
-// Values k .. k + 7 of a row of n; those past its end are others of the row.
-// VEC: the row is 16-byte aligned, n and k multiples of 8.
-template <bool VEC>
-__device__ __forceinline__ frag_t raw8(const uint16_t *row, int64_t k, int64_t n)
+// the data is masked where it is used. They are of 16 bytes at any alignment of
+// their elements (global memory takes that; element by element, odd row lengths
+// took several times as long).
+typedef u32x4_t any_u32x4_t __attribute__((aligned(2)));
+typedef f32x4_t any_f32x4_t __attribute__((aligned(4)));
+
+__device__ __forceinline__ frag_t load16(const void *p) { return *static_cast<const any_u32x4_t *>(p); }
+
+// v without its first s (0 to 7) values.
+__device__ __forceinline__ frag_t drop8(frag_t v, int s)
 {
-    if constexpr (VEC) return *reinterpret_cast<const frag_t *>(row + (k < n ? k : 0));
-    frag_t v = zero_frag();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e >> 1] |= uint32_t(row[k + e < n ? k + e : n - 1]) << (16 * (e & 1));
+    if (s & 4) v = frag_t{v[2], v[3], 0u, 0u};
+    if (s & 2) v = frag_t{v[1], v[2], v[3], 0u};
+    if (s & 1) v = frag_t{(v[0] >> 16) | (v[1] << 16), (v[1] >> 16) | (v[2] << 16), (v[2] >> 16) | (v[3] << 16), v[3] >> 16};
     return v;
 }
 
-// v's first `left` values, zeros behind them. VEC: all eight or none.
-template <bool VEC>
+// Values k .. k + 7 (k a multiple of 8) of n; those past the end are others of
+// them. EVEN: n is a multiple of 8.
+template <bool EVEN>
+__device__ __forceinline__ frag_t raw8(const uint16_t *p, int64_t k, int64_t n)
+{
+    if constexpr (EVEN) return load16(p + (k < n ? k : 0));
+    if (n >= 8) {
+        const int64_t from = k < n - 8 ? k : n - 8;
+        const frag_t v = load16(p + from);
+        return drop8(v, k < n ? int(k - from) : 0);
+    }
+    frag_t v = zero_frag();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e >> 1] |= uint32_t(p[k + e < n ? k + e : n - 1]) << (16 * (e & 1));
+    return v;
+}
+
+// Values from `start` on of an array of n, whatever they are past a row's end.
+// EVEN: rows of multiples of 8.
+template <bool EVEN>
+__device__ __forceinline__ frag_t flat8(const uint16_t *p, int64_t start, int64_t n)
+{
+    if constexpr (EVEN) return load16(p + start);
+    if (n >= 8) {
+        const int64_t from = start < n - 8 ? start : n - 8;
+        const frag_t v = load16(p + from);
+        return drop8(v, start < n ? int(start - from) : 0);
+    }
+    frag_t v = zero_frag();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e >> 1] |= uint32_t(p[start + e < n ? start + e : n - 1]) << (16 * (e & 1));
+    return v;
+}
+
+// v's first `left` values, zeros behind them. EVEN: all eight or none.
+template <bool EVEN>
 __device__ __forceinline__ frag_t first8(frag_t v, int64_t left)
 {
-    if constexpr (VEC) {
+    if constexpr (EVEN) {
         const uint32_t m = left > 0 ? ~0u : 0u;
         return frag_t{v[0] & m, v[1] & m, v[2] & m, v[3] & m};
     }
@@ -354,7 +391,7 @@ __device__ __forceinline__ bool tile_view(const AdArgs &a, bool with_none, int (
 // with 16) and two waves along d_in. Loads are a step ahead of their products.
 // Bound by reading x.
 // ---------------------------------------------------------------------------
-template <int VB, bool VEC, int TG, bool DIRECT>
+template <int VB, bool EVEN, int TG, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
 {
     constexpr int U = 4;                        // 32-deep steps whose loads are in flight together
@@ -409,9 +446,9 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
     auto fetch = [&](int u, int64_t s) {
         const int64_t k = 32 * (s < s1 ? s : s0) + 8 * g;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) x[u][m] = raw8<VEC>(xrow[m], k, K);
+        for (int m = 0; m < MT; ++m) x[u][m] = raw8<EVEN>(xrow[m], k, K);
 #pragma unroll
-        for (int b = 0; b < VB; ++b) w[u][b] = raw8<VEC>(arow[b], k, K);
+        for (int b = 0; b < VB; ++b) w[u][b] = raw8<EVEN>(arow[b], k, K);
     };
     if (s0 < s1) {
 #pragma unroll
@@ -422,7 +459,7 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
                 const int64_t left = (s + u < s1) ? K - 32 * (s + u) - 8 * g : 0;
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    const frag_t xm = first8<VEC>(x[u][m], left);
+                    const frag_t xm = first8<EVEN>(x[u][m], left);
 #pragma unroll
                     for (int b = 0; b < VB; ++b) acc[m][b] = mfma(w[u][b], xm, acc[m][b]);
                 }
@@ -488,22 +525,26 @@ struct Row16 {
 
 // `p`: the lane's first column; `nc`: columns from there on that exist; `whole`:
 // all of the wave's 64 do
-template <bool F32, int RUN, bool VEC>
+template <bool F32, int RUN>
 __device__ __forceinline__ Row16<F32> load_row(const void *p, int64_t nc, bool whole)
 {
     static_assert(!F32 || RUN == 4, "words of four 32-bit values");
     Row16<F32> v;
 #pragma unroll
     for (int q = 0; q < 16 / RUN; ++q) v.w[q] = zero_frag();
-    if (VEC && whole) {
+    if (whole) {
 #pragma unroll
-        for (int q = 0; q < 16 / RUN; ++q) v.w[q] = *reinterpret_cast<const u32x4_t *>(static_cast<const char *>(p) + 64 * q);
+        for (int q = 0; q < 16 / RUN; ++q) v.w[q] = load16(static_cast<const char *>(p) + 64 * q);
         return v;
     }
 #pragma unroll
     for (int q = 0; q < 16 / RUN; ++q) {
         const int64_t left = nc - 4 * RUN * q;
         const char *pq = static_cast<const char *>(p) + 64 * q;
+        if (left >= RUN) {
+            v.w[q] = load16(pq);
+            continue;
+        }
 #pragma unroll
         for (int e = 0; e < RUN; ++e)
             if (e < left) {
@@ -522,7 +563,7 @@ __device__ __forceinline__ float row_value(const Row16<F32> &v, int e)
     return __uint_as_float((e & 1) ? w & 0xffff0000u : w << 16);
 }
 
-template <bool F32, int RUN, bool VEC>
+template <bool F32, int RUN>
 __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[16])
 {
     constexpr int ES = F32 ? 4 : 2;
@@ -531,13 +572,13 @@ __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[
         const int64_t left = nc - 4 * RUN * q;
         char *pq = static_cast<char *>(p) + 4 * RUN * q * ES;
         const float *x = v + RUN * q;
-        if (VEC && left >= RUN) {
+        if (left >= RUN) {
             if constexpr (F32) {
 #pragma unroll
                 for (int k = 0; k < RUN / 4; ++k)
-                    reinterpret_cast<f32x4_t *>(pq)[k] = f32x4_t{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+                    reinterpret_cast<any_f32x4_t *>(pq)[k] = f32x4_t{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
             } else {
-                *reinterpret_cast<u32x4_t *>(pq) =
+                *reinterpret_cast<any_u32x4_t *>(pq) =
                     u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
             }
         } else {
@@ -557,7 +598,7 @@ __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[
 // summed once; then per 64 columns the wave has y0 and B of the next ones in
 // flight. Bound by reading y0 and writing y.
 // ---------------------------------------------------------------------------
-template <int RB, bool VEC, int TG, bool F32, bool DIRECT>
+template <int RB, bool EVEN, int TG, bool F32, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
 {
     __shared__ int s_tok[4][16];
@@ -589,14 +630,17 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int64_t cc = c + run_column<RUN>(r16, j);
-            const uint16_t *row = B + (cc < C ? cc : C - 1) * a.rank;
+            const int64_t row = (cc < C ? cc : C - 1) * a.rank;
 #pragma unroll
-            for (int b = 0; b < RB; ++b) w[b][j] = raw8<VEC>(row, 16 * b + r0, a.rank);
+            for (int b = 0; b < RB; ++b) {
+                const int r = 16 * b + r0 < a.rank ? 16 * b + r0 : 0;
+                w[b][j] = flat8<EVEN>(B, row + r, C * a.rank);
+            }
         }
     };
     auto load_y = [&](int64_t c) {
         const int64_t col = c + RUN * g;
-        return load_row<F32, RUN, VEC>(base + col * ES, (p.base && tv.live) ? C - col : 0, p.base && c + 64 <= C);
+        return load_row<F32, RUN>(base + col * ES, (p.base && tv.live) ? C - col : 0, p.base && c + 64 <= C);
     };
     frag_t w[RB][4];
     Row16<F32> y0 = load_y(c0);
@@ -655,7 +699,7 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
             y0 = load_y(c + cstep);
             load_b(c + cstep, w);
         }
-        if (tv.live) store_row<F32, RUN, VEC>(out + col * ES, C - col, v);
+        if (tv.live) store_row<F32, RUN>(out + col * ES, C - col, v);
     }
 }
 
@@ -682,7 +726,7 @@ __device__ __forceinline__ frag_t read_tr(const uint8_t *p, int four)
 // half a wave reads together fall on all banks once) and read transposed. The
 // columns are permuted on the way in (run_column).
 // ---------------------------------------------------------------------------
-template <bool VEC, int TG, bool F32>
+template <bool EVEN, int TG, bool F32>
 __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 {
     constexpr int NC = (TG == 1) ? 1 : 4;  // 64-column groups of a wave
@@ -701,7 +745,7 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int64_t col = c0 + 64 * c + 8 * g;
-        x0[c] = load_row<false, 8, VEC>(a.dx0 + tv.token * a.lddx0 + col, (a.dx0 && tv.live) ? C - col : 0,
+        x0[c] = load_row<false, 8>(a.dx0 + tv.token * a.lddx0 + col, (a.dx0 && tv.live) ? C - col : 0,
                                         a.dx0 && c0 + 64 * c + 64 <= C);
     }
     f32x4_t acc[NC][4];
@@ -719,7 +763,7 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const int w = t + AT * q, r = w >> 5;
-                st[q] = raw8<VEC>(p.A + (int64_t(ad) * a.rank + 16 * b + (r < re ? r : 0)) * C, cb + 8 * (w & 31), C);
+                st[q] = raw8<EVEN>(p.A + (int64_t(ad) * a.rank + 16 * b + (r < re ? r : 0)) * C, cb + 8 * (w & 31), C);
             }
         };
         fetch(0);
@@ -762,7 +806,7 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
         float v[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = row_value<false>(x0[c], e) + acc[c][e >> 2][e & 3];
-        store_row<F32, 8, VEC>(static_cast<char *>(a.dx) + (tv.token * a.lddx + col) * (F32 ? 4 : 2), C - col, v);
+        store_row<F32, 8>(static_cast<char *>(a.dx) + (tv.token * a.lddx + col) * (F32 ? 4 : 2), C - col, v);
     }
 }
 
@@ -798,16 +842,16 @@ __device__ __forceinline__ void out_tokens(const int32_t *order, int k0, int cou
     }
 }
 
-template <bool VEC>
+template <bool EVEN>
 __device__ __forceinline__ void out_fetch(const uint16_t *S, int64_t ld, const int32_t (&tok)[8], int64_t c, int64_t C,
                                           frag_t (&sv)[8])
 {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sv[i] = raw8<VEC>(S + int64_t(tok[i]) * ld, c + 8 * (lane & 7), C);
+    for (int i = 0; i < 8; ++i) sv[i] = raw8<EVEN>(S + int64_t(tok[i]) * ld, c + 8 * (lane & 7), C);
 }
 
-template <bool VEC>
+template <bool EVEN>
 __device__ __forceinline__ void out_stage(uint8_t *ss, const frag_t (&sv)[8], int k0, int count, int64_t c, int64_t C)
 {
     const int lane = threadIdx.x & 63;
@@ -816,7 +860,7 @@ __device__ __forceinline__ void out_stage(uint8_t *ss, const frag_t (&sv)[8], in
     for (int i = 0; i < 8; ++i) {
         const int k = 8 * i + (lane >> 3);
         *reinterpret_cast<frag_t *>(ss + k * 128 + ((((lane & 7) >> 1) ^ out_key(k)) << 5) + ((lane & 1) << 4)) =
-            first8<VEC>(sv[i], k0 + k < count ? left : 0);
+            first8<EVEN>(sv[i], k0 + k < count ? left : 0);
     }
 }
 
@@ -836,7 +880,7 @@ __device__ __forceinline__ OutPlace out_place(const AdArgs &a, const int4 &piece
     return {o, false};
 }
 
-template <int RB, bool VEC>
+template <int RB, bool EVEN>
 __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint8_t s_s[4][OUT_STEP * 128];
@@ -869,13 +913,13 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
         }
     };
     auto fetch = [&](int k0) {
-        out_fetch<VEC>(S, p.ldb, tok, c0, C, sv);
+        out_fetch<EVEN>(S, p.ldb, tok, c0, C, sv);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
             const float *tr = p.t + int64_t(qtok[q]) * a.rank;
-            if constexpr (VEC) {  // (rank a multiple of 8, t 16-byte aligned)
-                const f32x4_t *t4 = reinterpret_cast<const f32x4_t *>(tr + (r < a.rank ? r : 0));
+            if constexpr (EVEN) {  // (rank a multiple of 8)
+                const any_f32x4_t *t4 = reinterpret_cast<const any_f32x4_t *>(tr + (r < a.rank ? r : 0));
                 const f32x4_t u = t4[0], v = t4[1];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -900,7 +944,7 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int r = 16 * b + 8 * h;
-                const frag_t v = first8<false>(raw8<VEC>(br, r, a.rank), in ? re - r : 0);
+                const frag_t v = first8<false>(flat8<EVEN>(br, r < a.rank ? r : 0, (C - (in ? cb + t : 0)) * a.rank), in ? re - r : 0);
                 *reinterpret_cast<frag_t *>(s_b[b] + t * 32 + 16 * h) = v;
             }
     }
@@ -914,7 +958,7 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
     const int quad = (r16 & 3) << 3;
     for (int k0 = 0; k0 < piece.z; k0 += OUT_STEP) {
         __syncthreads();  // the last step's reads are over
-        out_stage<VEC>(ss, sv, k0, piece.z, c0, C);
+        out_stage<EVEN>(ss, sv, k0, piece.z, c0, C);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
@@ -1030,7 +1074,7 @@ __global__ __launch_bounds__(AT) void adapters_parts(const AdArgs a)
 // dA: of a piece's tokens, dA[r][c] = sum_m u[m][r] x[m][c], for VB rank blocks
 // of the group from one reading of x; staged and read as dB's operands.
 // ---------------------------------------------------------------------------
-template <int VB, bool VEC>
+template <int VB, bool EVEN>
 __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint8_t s_s[4][OUT_STEP * 128];
@@ -1054,7 +1098,7 @@ __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
     int32_t tok[8];
     out_tokens(order, 0, piece.z, tok);
     auto fetch = [&](int k0) {
-        out_fetch<VEC>(a.X, a.ldx, tok, c0, C, sv);
+        out_fetch<EVEN>(a.X, a.ldx, tok, c0, C, sv);
         out_tokens(order, k0 + OUT_STEP, piece.z, tok);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
@@ -1067,7 +1111,7 @@ __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
     const int kr = 8 * g + (r16 >> 2), key = out_key(kr), quad = (r16 & 3) << 3;
     for (int k0 = 0; k0 < piece.z; k0 += OUT_STEP) {
         __syncthreads();  // the last step's reads are over
-        out_stage<VEC>(ss, sv, k0, piece.z, c0, C);
+        out_stage<EVEN>(ss, sv, k0, piece.z, c0, C);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             // parts of a row: 0 0 1 1 2 2
@@ -1190,16 +1234,14 @@ AdLayout ad_layout(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_
     return l;
 }
 
-bool al16(const void *p, int64_t row_bytes) { return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(row_bytes)) & 15) == 0; }
-
-template <bool VEC>
+template <bool EVEN>
 hipError_t launch_shrink(const AdArgs &a, dim3 grid, int vb, bool direct, hipStream_t st)
 {
 #define BSQ_VB(N)                                                                                                        \
     case N:                                                                                                              \
-        if (direct) hipLaunchKernelGGL((adapters_shrink<N, VEC, 1, true>), grid, dim3(AT), 0, st, a);                    \
-        else if (a.l.tile == 16) hipLaunchKernelGGL((adapters_shrink<N, VEC, 1, false>), grid, dim3(AT), 0, st, a);      \
-        else hipLaunchKernelGGL((adapters_shrink<N, VEC, 4, false>), grid, dim3(AT), 0, st, a);                          \
+        if (direct) hipLaunchKernelGGL((adapters_shrink<N, EVEN, 1, true>), grid, dim3(AT), 0, st, a);                    \
+        else if (a.l.tile == 16) hipLaunchKernelGGL((adapters_shrink<N, EVEN, 1, false>), grid, dim3(AT), 0, st, a);      \
+        else hipLaunchKernelGGL((adapters_shrink<N, EVEN, 4, false>), grid, dim3(AT), 0, st, a);                          \
         break;
     switch (vb) {
         BSQ_VB(1)
@@ -1211,14 +1253,14 @@ hipError_t launch_shrink(const AdArgs &a, dim3 grid, int vb, bool direct, hipStr
     return hipGetLastError();
 }
 
-template <bool VEC, bool F32>
+template <bool EVEN, bool F32>
 hipError_t launch_expand(const AdArgs &a, dim3 grid, bool direct, hipStream_t st)
 {
 #define BSQ_RB(N)                                                                                                        \
     case N:                                                                                                              \
-        if (direct) hipLaunchKernelGGL((adapters_expand<N, VEC, 1, F32, true>), grid, dim3(AT), 0, st, a);               \
-        else if (a.l.tile == 16) hipLaunchKernelGGL((adapters_expand<N, VEC, 1, F32, false>), grid, dim3(AT), 0, st, a); \
-        else hipLaunchKernelGGL((adapters_expand<N, VEC, 4, F32, false>), grid, dim3(AT), 0, st, a);                     \
+        if (direct) hipLaunchKernelGGL((adapters_expand<N, EVEN, 1, F32, true>), grid, dim3(AT), 0, st, a);               \
+        else if (a.l.tile == 16) hipLaunchKernelGGL((adapters_expand<N, EVEN, 1, F32, false>), grid, dim3(AT), 0, st, a); \
+        else hipLaunchKernelGGL((adapters_expand<N, EVEN, 4, F32, false>), grid, dim3(AT), 0, st, a);                     \
         break;
     switch (a.rb) {
         BSQ_RB(1)
@@ -1230,35 +1272,35 @@ hipError_t launch_expand(const AdArgs &a, dim3 grid, bool direct, hipStream_t st
     return hipGetLastError();
 }
 
-template <bool VEC>
+template <bool EVEN>
 hipError_t launch_dy(const AdArgs &a, dim3 grid, hipStream_t st)
 {
     switch (a.rb) {
-    case 1: hipLaunchKernelGGL((adapters_dy<1, VEC>), grid, dim3(AT), 0, st, a); break;
-    case 2: hipLaunchKernelGGL((adapters_dy<2, VEC>), grid, dim3(AT), 0, st, a); break;
-    case 4: hipLaunchKernelGGL((adapters_dy<4, VEC>), grid, dim3(AT), 0, st, a); break;
-    default: hipLaunchKernelGGL((adapters_dy<8, VEC>), grid, dim3(AT), 0, st, a); break;
+    case 1: hipLaunchKernelGGL((adapters_dy<1, EVEN>), grid, dim3(AT), 0, st, a); break;
+    case 2: hipLaunchKernelGGL((adapters_dy<2, EVEN>), grid, dim3(AT), 0, st, a); break;
+    case 4: hipLaunchKernelGGL((adapters_dy<4, EVEN>), grid, dim3(AT), 0, st, a); break;
+    default: hipLaunchKernelGGL((adapters_dy<8, EVEN>), grid, dim3(AT), 0, st, a); break;
     }
     return hipGetLastError();
 }
 
-template <bool VEC>
+template <bool EVEN>
 hipError_t launch_da(const AdArgs &a, int vb, dim3 grid, hipStream_t st)
 {
     switch (vb) {
-    case 1: hipLaunchKernelGGL((adapters_da<1, VEC>), grid, dim3(AT), 0, st, a); break;
-    case 2: hipLaunchKernelGGL((adapters_da<2, VEC>), grid, dim3(AT), 0, st, a); break;
-    case 3: hipLaunchKernelGGL((adapters_da<3, VEC>), grid, dim3(AT), 0, st, a); break;
-    default: hipLaunchKernelGGL((adapters_da<4, VEC>), grid, dim3(AT), 0, st, a); break;
+    case 1: hipLaunchKernelGGL((adapters_da<1, EVEN>), grid, dim3(AT), 0, st, a); break;
+    case 2: hipLaunchKernelGGL((adapters_da<2, EVEN>), grid, dim3(AT), 0, st, a); break;
+    case 3: hipLaunchKernelGGL((adapters_da<3, EVEN>), grid, dim3(AT), 0, st, a); break;
+    default: hipLaunchKernelGGL((adapters_da<4, EVEN>), grid, dim3(AT), 0, st, a); break;
     }
     return hipGetLastError();
 }
 
-template <bool VEC, bool F32>
+template <bool EVEN, bool F32>
 hipError_t launch_dx(const AdArgs &a, dim3 grid, hipStream_t st)
 {
-    if (a.l.tile == 16) hipLaunchKernelGGL((adapters_dx<VEC, 1, F32>), grid, dim3(AT), 0, st, a);
-    else hipLaunchKernelGGL((adapters_dx<VEC, 4, F32>), grid, dim3(AT), 0, st, a);
+    if (a.l.tile == 16) hipLaunchKernelGGL((adapters_dx<EVEN, 1, F32>), grid, dim3(AT), 0, st, a);
+    else hipLaunchKernelGGL((adapters_dx<EVEN, 4, F32>), grid, dim3(AT), 0, st, a);
     return hipGetLastError();
 }
 
@@ -1284,23 +1326,21 @@ hipError_t run_plan(const int32_t *ids, int64_t M, int64_t n, void *buf, int32_t
     return hipGetLastError();
 }
 
-hipError_t run_forward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest, hipStream_t st)
+hipError_t run_forward(const AdaptersCall &c, AdArgs &a, int64_t widest, hipStream_t st)
 {
     const bool direct = a.M <= DIRECT_TOKENS, f32 = c.y_dtype == BSQ_F32;
-    bool va = vx, vy = c.rank % 8 == 0;  // vector loads of x with A, of B with y
     for (int i = 0; i < c.np; ++i) {
         Proj &p = a.p[i];
         p.base = c.y0 ? c.y0[i] : nullptr;
         p.ldb = c.y0 ? c.ldy0[i] : 0;
         p.y = c.y[i];
         p.ldy = c.ldy[i];
-        va = va && al16(p.A, 2 * c.d_in);
-        vy = vy && al16(p.B, 0) && al16(p.base, (f32 ? 4 : 2) * p.ldb) && al16(p.y, (f32 ? 4 : 2) * p.ldy);
     }
+    const bool even_in = c.d_in % 8 == 0, even_rank = c.rank % 8 == 0;
     const unsigned tiles = unsigned(direct ? a.M : a.l.max_tiles);
     const int vb = blocks_at_once(a.nv);
     const dim3 sgrid(tiles, unsigned(a.ksplit), blocks(a.nv, vb));
-    hipError_t e = va ? launch_shrink<true>(a, sgrid, vb, direct, st) : launch_shrink<false>(a, sgrid, vb, direct, st);
+    hipError_t e = even_in ? launch_shrink<true>(a, sgrid, vb, direct, st) : launch_shrink<false>(a, sgrid, vb, direct, st);
     if (e != hipSuccess) return e;
     if (!direct) {
         hipLaunchKernelGGL((adapters_parts<false>), dim3(blocks(a.M * 2 * a.rb, AT), 1, unsigned(c.np)), dim3(AT), 0, st, a);
@@ -1311,31 +1351,31 @@ hipError_t run_forward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest
     a.ecols = (a.l.tile == 16) ? 1024 : 256;
     while (a.ecols > 256 && int64_t(tiles) * c.np * blocks(widest, a.ecols) < 768) a.ecols /= 2;
     const dim3 egrid(tiles, blocks(widest, a.ecols), unsigned(c.np));
-    if (f32) return vy ? launch_expand<true, true>(a, egrid, direct, st) : launch_expand<false, true>(a, egrid, direct, st);
-    return vy ? launch_expand<true, false>(a, egrid, direct, st) : launch_expand<false, false>(a, egrid, direct, st);
+    if (f32) return even_rank ? launch_expand<true, true>(a, egrid, direct, st) : launch_expand<false, true>(a, egrid, direct, st);
+    return even_rank ? launch_expand<true, false>(a, egrid, direct, st) : launch_expand<false, false>(a, egrid, direct, st);
 }
 
-hipError_t run_backward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t widest, hipStream_t st)
+hipError_t run_backward(const AdaptersCall &c, AdArgs &a, int64_t widest, hipStream_t st)
 {
-    // vector loads of dy, t and B; of A with dx
-    bool vd = c.rank % 8 == 0, va = c.d_in % 8 == 0;
+    // rows of dy, t and B in whole words of eight; rows of x and A
+    bool even_dy = c.rank % 8 == 0;
+    const bool even_in = c.d_in % 8 == 0;
     for (int i = 0; i < c.np; ++i) {
         Proj &p = a.p[i];
         p.base = c.dy[i];
         p.ldb = c.lddy[i];
         p.dA = c.dA[i];
         p.dB = c.dB[i];
-        vd = vd && al16(p.base, 2 * p.ldb) && p.d_out % 8 == 0 && al16(p.t, 0) && al16(p.B, 0);
-        va = va && al16(p.A, 2 * c.d_in);
+        even_dy = even_dy && p.d_out % 8 == 0;
     }
     const dim3 dgrid(unsigned(a.l.max_pieces), blocks(widest, OUT_COLS), unsigned(c.np));
-    hipError_t e = vd ? launch_dy<true>(a, dgrid, st) : launch_dy<false>(a, dgrid, st);
+    hipError_t e = even_dy ? launch_dy<true>(a, dgrid, st) : launch_dy<false>(a, dgrid, st);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((adapters_parts<true>), dim3(blocks(a.M * 2 * a.rb, AT), 1, unsigned(c.np)), dim3(AT), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int vb = blocks_at_once(a.nv);
     const dim3 agrid(unsigned(a.l.max_pieces), blocks(c.d_in, OUT_COLS), blocks(a.nv, vb));
-    if ((e = vx ? launch_da<true>(a, vb, agrid, st) : launch_da<false>(a, vb, agrid, st)) != hipSuccess) return e;
+    if ((e = even_in ? launch_da<true>(a, vb, agrid, st) : launch_da<false>(a, vb, agrid, st)) != hipSuccess) return e;
     hipLaunchKernelGGL(adapters_pieces, dim3(blocks(int64_t(c.rank) * std::max(widest, c.d_in), 4 * AT), unsigned(a.n), unsigned(2 * c.np)),
                        dim3(AT), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess || !c.dx) return e;
@@ -1344,10 +1384,9 @@ hipError_t run_backward(const AdaptersCall &c, AdArgs &a, bool vx, int64_t wides
     a.lddx0 = c.lddx0;
     a.lddx = c.lddx;
     const bool f32 = c.dx_dtype == BSQ_F32;
-    const bool vec = va && al16(c.dx0, 2 * c.lddx0) && al16(c.dx, (f32 ? 4 : 2) * c.lddx);
     const dim3 xgrid(unsigned(a.l.max_tiles), blocks(c.d_in, 256), 1);
-    if (f32) return vec ? launch_dx<true, true>(a, xgrid, st) : launch_dx<false, true>(a, xgrid, st);
-    return vec ? launch_dx<true, false>(a, xgrid, st) : launch_dx<false, false>(a, xgrid, st);
+    if (f32) return even_in ? launch_dx<true, true>(a, xgrid, st) : launch_dx<false, true>(a, xgrid, st);
+    return even_in ? launch_dx<true, false>(a, xgrid, st) : launch_dx<false, false>(a, xgrid, st);
 }
 
 // Reports ids that are no adapter's (up to DIRECT_TOKENS tokens have no plan).
@@ -1410,14 +1449,13 @@ hipError_t launch_adapters(const AdaptersCall &c, hipStream_t st)
         p.d_out = q.d_out;
         p.t = c.t ? c.t[i] : nullptr;
     }
-    const bool vx = al16(c.X, 2 * c.ldx) && c.d_in % 8 == 0;
-    if (!back) return run_forward(c, a, vx, widest, st);
+    if (!back) return run_forward(c, a, widest, st);
     if (a.M <= DIRECT_TOKENS) {
         const hipError_t e = run_plan(a.ids, a.M, a.n, ws + l.plan, nullptr, st);
         if (e != hipSuccess) return e;
         a.plan = reinterpret_cast<const int32_t *>(ws + l.plan);
     }
-    return run_backward(c, a, vx, widest, st);
+    return run_backward(c, a, widest, st);
 }
 
 }  // namespace bsq
