@@ -622,7 +622,7 @@ bsq_status bsq_adapters_workspace_bytes(int32_t back, int64_t M, int32_t n, int3
  *   t      host array [n_proj] of device fp32 [M][rank] outputs (0 for a token
  *          without an adapter), or NULL
  *   ws     device workspace, 256-byte aligned, any contents
- * Any d_in and d_out from 1 to 2^24, any alignment of the elements; multiples of
+ * Any d_in and d_out from 1 to 2^22, any alignment of the elements; multiples of
  * 8 are read fastest. */
 bsq_status bsq_adapters_apply(const bsq_adapter_plan *plan, int32_t n_proj, const bsq_adapter_pool *pools,
                               int32_t rank, int64_t d_in, const void *X, int64_t ldx, const void *const *y0,

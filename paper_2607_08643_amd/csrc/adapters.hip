@@ -405,11 +405,12 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t K = a.d_in;
     const int v0 = int(blockIdx.z) * VB;
-    // the block's range of k, whole steps of 32, that the waves along it take in
-    // turns of U, and the wave's tokens
+    // the block's range of k, in whole turns of U steps of 32 for each wave along it,
+    // and the wave's tokens
     const int kw = (TG == 1) ? wave : wave & 1, tg = (TG == 1) ? 0 : wave >> 1;
-    const int64_t steps = (K + 31) / 32, s0 = steps * blockIdx.y / a.ksplit;
-    const int64_t s1 = (32 * tg < tv.count || TG == 1) ? steps * (blockIdx.y + 1) / a.ksplit : s0;
+    const int64_t steps = (K + 31) / 32, turns = (steps + U * KW - 1) / (U * KW);
+    const int64_t s0 = turns * blockIdx.y / a.ksplit * (U * KW), end = turns * (blockIdx.y + 1) / a.ksplit * (U * KW);
+    const int64_t s1 = (32 * tg < tv.count || TG == 1) ? (end < steps ? end : steps) : s0;
     const uint16_t *xrow[MT];
     int64_t place[MT];
     bool live[MT];
@@ -450,21 +451,27 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
 #pragma unroll
         for (int b = 0; b < VB; ++b) w[u][b] = raw8<EVEN>(arow[b], k, K);
     };
-    if (s0 < s1) {
+    auto product = [&](int u, int64_t s) {
+        const int64_t left = (s < s1) ? K - 32 * s - 8 * g : 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) fetch(u, s0 + U * kw + u);
-        for (int64_t s = s0 + U * kw; s < s1; s += U * KW)
+        for (int m = 0; m < MT; ++m) {
+            const frag_t xm = first8<EVEN>(x[u][m], left);
+#pragma unroll
+            for (int b = 0; b < VB; ++b) acc[m][b] = mfma(w[u][b], xm, acc[m][b]);
+        }
+    };
+    int64_t s = s0 + U * kw;
+    if (s < s1) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) fetch(u, s + u);
+        for (; s + U * KW < s1; s += U * KW)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int64_t left = (s + u < s1) ? K - 32 * (s + u) - 8 * g : 0;
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const frag_t xm = first8<EVEN>(x[u][m], left);
-#pragma unroll
-                    for (int b = 0; b < VB; ++b) acc[m][b] = mfma(w[u][b], xm, acc[m][b]);
-                }
+                product(u, s + u);
                 fetch(u, s + U * KW + u);
             }
+#pragma unroll
+        for (int u = 0; u < U; ++u) product(u, s + u);
     }
     // lane: ranks 4 g .. + 3 of a block, of token r16; the waves along d_in added in order
 #pragma unroll
@@ -601,6 +608,7 @@ __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[
 template <int RB, bool EVEN, int TG, bool F32, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
 {
+    constexpr int PF = (RB == 1) ? 2 : 1;  // 64-column groups in flight
     __shared__ int s_tok[4][16];
     TileView tv;
     if (!tile_view<DIRECT, TG>(a, true, s_tok, tv)) return;
@@ -642,9 +650,15 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
         const int64_t col = c + RUN * g;
         return load_row<F32, RUN>(base + col * ES, (p.base && tv.live) ? C - col : 0, p.base && c + 64 <= C);
     };
-    frag_t w[RB][4];
-    Row16<F32> y0 = load_y(c0);
-    load_b(c0, w);
+    frag_t w[PF][RB][4];
+    Row16<F32> y0[PF];
+    auto load = [&](int q, int64_t c) {  // (past the block's columns: its first again)
+        const int64_t cc = c < c1 ? c : c0;
+        y0[q] = load_y(cc);
+        load_b(cc, w[q]);
+    };
+#pragma unroll
+    for (int q = 0; q < PF; ++q) load(q, c0 + q * cstep);
     // t in parts: the first and the second share a product (lanes g < 2 the
     // first), the third, for 32-bit results, has its own
     frag_t tf[RB], tf3[F32 ? RB : 1];
@@ -673,34 +687,35 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
         }
     }
     if (ad < 0 && p.base == p.y) return;
-    for (int64_t c = c0; c < c1; c += cstep) {
-        f32x4_t acc[4];
+    for (int64_t cq = c0; cq < c1; cq += PF * cstep)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        if (part_rank)
+        for (int q = 0; q < PF; ++q) {
+            const int64_t c = cq + q * cstep;
+            if (c >= c1) break;
+            f32x4_t acc[4];
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const frag_t m = first8<false>(frag_t{~0u, ~0u, ~0u, ~0u}, re - 16 * b - r0);
+            for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            if (part_rank)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[b][j] &= m;
-            }
+                for (int b = 0; b < RB; ++b) {
+                    const frag_t m = first8<false>(frag_t{~0u, ~0u, ~0u, ~0u}, re - 16 * b - r0);
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
+                    for (int j = 0; j < 4; ++j) w[q][b][j] &= m;
+                }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (F32) acc[j] = mfma(w[b][j], tf3[b], acc[j]);
-                acc[j] = mfma(w[b][j], tf[b], acc[j]);
-            }
-        float v[16];
+            for (int b = 0; b < RB; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = row_value<F32>(y0, e) + acc[e >> 2][e & 3];
-        const int64_t col = c + RUN * g;
-        if (c + cstep < c1) {
-            y0 = load_y(c + cstep);
-            load_b(c + cstep, w);
+                for (int j = 0; j < 4; ++j) {
+                    if (F32) acc[j] = mfma(w[q][b][j], tf3[b], acc[j]);
+                    acc[j] = mfma(w[q][b][j], tf[b], acc[j]);
+                }
+            float v[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = row_value<F32>(y0[q], e) + acc[e >> 2][e & 3];
+            if (cq + PF * cstep < c1) load(q, c + PF * cstep);
+            const int64_t col = c + RUN * g;
+            if (tv.live) store_row<F32, RUN>(out + col * ES, C - col, v);
         }
-        if (tv.live) store_row<F32, RUN>(out + col * ES, C - col, v);
-    }
 }
 
 // ---------------------------------------------------------------------------
@@ -719,23 +734,26 @@ __device__ __forceinline__ frag_t read_tr(const uint8_t *p, int four)
 }
 
 // ---------------------------------------------------------------------------
-// dx: dx = dx0 + sum over the projections of A^T u. A block: a tile and 256
-// columns; a wave: 16 tokens (or 64 of the columns). Per rank block the 16 x 256
-// of A are staged in LDS (two blocks of eight ranks, [pair of 16-column
+// dx: dx = dx0 + sum over the projections of A^T u. A block: a tile and 128
+// columns, 16 tokens a wave (16-token tiles: 256, 64 a wave). Per rank block 16
+// rows of A are staged in LDS (two blocks of eight ranks, [pair of 16-column
 // groups][rank][64 bytes], the groups swapped in ranks 8 to 15: the rows that
 // half a wave reads together fall on all banks once) and read transposed. The
 // columns are permuted on the way in (run_column).
 // ---------------------------------------------------------------------------
+constexpr int DX_COLS = 128;
+
 template <bool EVEN, int TG, bool F32>
 __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 {
-    constexpr int NC = (TG == 1) ? 1 : 4;  // 64-column groups of a wave
-    __shared__ __attribute__((aligned(16))) uint8_t s_a[2][8192];
+    constexpr int BC = (TG == 1) ? 256 : DX_COLS, NC = (TG == 1) ? 1 : BC / 64;  // columns of a block, 64-column groups of a wave
+    constexpr int HALF = 16 * BC, SQ = BC / 128;                                 // bytes of eight ranks, 16-byte words a thread
+    __shared__ __attribute__((aligned(16))) uint8_t s_a[2][2 * HALF];
     TileView tv;
     if (!tile_view<false, TG>(a, true, nullptr, tv)) return;
     const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int64_t C = a.d_in, cb = int64_t(blockIdx.y) * 256;
+    const int64_t C = a.d_in, cb = int64_t(blockIdx.y) * BC;
     const int ad = tv.adapter;
     if (ad < 0 && a.dx0 == a.dx) return;
     const int64_t c0 = cb + (TG == 1 ? 64 * wave : 0);
@@ -754,16 +772,16 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[c][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     if (ad >= 0) {
-        frag_t st[2];
+        frag_t st[SQ];
         int re = 0;  // ranks of the block in flight
         auto fetch = [&](int v) {
             const int pi = v / a.rb, b = v - pi * a.rb;
             const Proj &p = a.p[pi];
             re = rank_of(p, ad, a.rank) - 16 * b;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int w = t + AT * q, r = w >> 5;
-                st[q] = raw8<EVEN>(p.A + (int64_t(ad) * a.rank + 16 * b + (r < re ? r : 0)) * C, cb + 8 * (w & 31), C);
+            for (int q = 0; q < SQ; ++q) {
+                const int w = t + AT * q, r = w / (BC / 8);
+                st[q] = raw8<EVEN>(p.A + (int64_t(ad) * a.rank + 16 * b + (r < re ? r : 0)) * C, cb + 8 * (w % (BC / 8)), C);
             }
         };
         fetch(0);
@@ -772,11 +790,11 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
         for (int v = 0; v < a.nv; ++v) {
             uint8_t *sa = s_a[v & 1];
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
+            for (int q = 0; q < SQ; ++q) {
                 // rank k, columns 8 cc ..: rows 4 i .. of blocks f and f + 1 (run_column)
-                const int w = t + AT * q, k = w >> 5, cc = w & 31, kk = 4 * (k >> 3) + (k & 3);
+                const int w = t + AT * q, k = w / (BC / 8), cc = w % (BC / 8), kk = 4 * (k >> 3) + (k & 3);
                 const int i = cc & 3, f = 4 * (cc >> 3) + 2 * ((cc >> 2) & 1);
-                uint8_t *d = sa + ((k >> 2) & 1) * 4096 + (f >> 1) * 512 + kk * 64 + 8 * i;
+                uint8_t *d = sa + ((k >> 2) & 1) * HALF + (f >> 1) * 512 + kk * 64 + 8 * i;
                 const int swap = 32 * (kk >> 2);
                 const frag_t x = first8<true>(st[q], k < re);  // (columns past d_in are not written)
                 *reinterpret_cast<uint2 *>(d + swap) = make_uint2(x[0], x[1]);
@@ -793,7 +811,7 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int f = 4 * c + j;
-                    const frag_t w = read_tr(sa + (TG == 1 ? wave * 1024 : 0) + ((f & 1) ? t1 : t0) + (f >> 1) * 512, 4096);
+                    const frag_t w = read_tr(sa + (TG == 1 ? wave * 1024 : 0) + ((f & 1) ? t1 : t0) + (f >> 1) * 512, HALF);
                     if (F32) acc[c][j] = mfma(w, u3, acc[c][j]);
                     acc[c][j] = mfma(w, uf, acc[c][j]);
                 }
@@ -814,7 +832,7 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 // dy pass: of a piece's tokens, dB[c][r] = sum_m dy[m][c] (s t)[m][r] and the
 // partial u[m][r] = sum over the block's 256 columns of dy[m][c] B[c][r], from
 // one reading of dy. Per step of 64 tokens the block stages 64 x 256 of dy and s
-// t in three parts in LDS, and holds the next step's in registers. For dB (a
+// t in three parts in LDS, and holds the next two steps' in registers. For dB (a
 // wave: 64 columns, all tokens) both are read transposed, tokens along the depth;
 // for u (a wave: 16 tokens, all columns) dy is read as it lies and the block's
 // 256 x rank of B, staged once, transposed. 64 tokens a step keep 32 KiB of dy
@@ -825,7 +843,7 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 // row k lies at q ^ key(k), so that the eight rows that half a wave reads
 // together fall on different banks. The others: 32-byte rows of 16 values.
 // ---------------------------------------------------------------------------
-constexpr int OUT_COLS = 256, OUT_STEP = 64;
+constexpr int OUT_COLS = 256, OUT_STEP = 64, OUT_AHEAD = 2;  // columns and tokens of a step, steps in flight
 
 __device__ __forceinline__ int out_key(int k) { return ((k >> 1) & 1) | (((k >> 3) & 1) << 1); }
 
@@ -883,6 +901,7 @@ __device__ __forceinline__ OutPlace out_place(const AdArgs &a, const int4 &piece
 template <int RB, bool EVEN>
 __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
 {
+    constexpr int PF = (RB <= 2) ? OUT_AHEAD : 1;  // steps in flight
     __shared__ __attribute__((aligned(16))) uint8_t s_s[4][OUT_STEP * 128];
     __shared__ __attribute__((aligned(16))) uint8_t s_q[RB][3][OUT_STEP * 32];
     __shared__ __attribute__((aligned(16))) uint8_t s_b[RB][OUT_COLS * 32];
@@ -899,42 +918,45 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
     const int32_t *order = a.plan + a.l.order + piece.y;
     const int re = rank_of(p, piece.x, a.rank);
     const float sc = scale_of(p, piece.x);
-    frag_t sv[8];
     // s t: eight ranks of a row a thread
     constexpr int QV = (OUT_STEP * 2 * RB + AT - 1) / AT;
-    float qv[QV][8];
-    int32_t tok[8], qtok[QV];
-    auto tokens = [&](int k0) {
-        out_tokens(order, k0, piece.z, tok);
+    frag_t sv[PF][8];
+    float qv[PF][QV][8];
+    int32_t tok[2][8], qtok[2][QV];
+    auto tokens = [&](int k0, int h) {
+        out_tokens(order, k0, piece.z, tok[h]);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int k = k0 + (t + AT * q) / (2 * RB);
-            qtok[q] = order[k < piece.z ? k : 0];
+            qtok[h][q] = order[k < piece.z ? k : 0];
         }
     };
-    auto fetch = [&](int k0) {
-        out_fetch<EVEN>(S, p.ldb, tok, c0, C, sv);
+    // (loads return in order: the next step's tokens go ahead of this one's rows)
+    auto fetch = [&](int k0, int i) {
+        const int h = i & 1;
+        tokens(k0 + OUT_STEP, 1 - h);
+        out_fetch<EVEN>(S, p.ldb, tok[h], c0, C, sv[i % PF]);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
-            const float *tr = p.t + int64_t(qtok[q]) * a.rank;
+            const float *tr = p.t + int64_t(qtok[h][q]) * a.rank;
             if constexpr (EVEN) {  // (rank a multiple of 8)
                 const any_f32x4_t *t4 = reinterpret_cast<const any_f32x4_t *>(tr + (r < a.rank ? r : 0));
                 const f32x4_t u = t4[0], v = t4[1];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    qv[q][e] = u[e];
-                    qv[q][4 + e] = v[e];
+                    qv[i % PF][q][e] = u[e];
+                    qv[i % PF][q][4 + e] = v[e];
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) qv[q][e] = tr[r + e < a.rank ? r + e : 0];
+                for (int e = 0; e < 8; ++e) qv[i % PF][q][e] = tr[r + e < a.rank ? r + e : 0];
             }
         }
-        tokens(k0 + OUT_STEP);
     };
-    tokens(0);
-    fetch(0);
+    tokens(0, 0);
+#pragma unroll
+    for (int i = 0; i < PF; ++i) fetch(i * OUT_STEP, i);
     // B: row (column of dy) t, 16 ranks of every block
     {
         const bool in = cb + t < C;
@@ -956,23 +978,23 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
     uint8_t *ss = s_s[wave];
     const int kr = 8 * g + (r16 >> 2), key = out_key(kr);  // the lane's row in a transposed read
     const int quad = (r16 & 3) << 3;
-    for (int k0 = 0; k0 < piece.z; k0 += OUT_STEP) {
+    auto step = [&](int k0, int cur) {
         __syncthreads();  // the last step's reads are over
-        out_stage<EVEN>(ss, sv, k0, piece.z, c0, C);
+        out_stage<EVEN>(ss, sv[cur % PF], k0, piece.z, c0, C);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, row = w / (2 * RB), r = 8 * (w - row * 2 * RB);
             if (row >= OUT_STEP) continue;
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (k0 + row < piece.z && r + e < re) ? sc * qv[q][e] : 0.0f;
+            for (int e = 0; e < 8; ++e) x[e] = (k0 + row < piece.z && r + e < re) ? sc * qv[cur % PF][q][e] : 0.0f;
             frag_t part[3];
             split3(x, part);
 #pragma unroll
             for (int h = 0; h < 3; ++h) *reinterpret_cast<frag_t *>(s_q[r >> 4][h] + row * 32 + 2 * (r & 8)) = part[h];
         }
         __syncthreads();
-        if (k0 + OUT_STEP < piece.z) fetch(k0 + OUT_STEP);
+        if (k0 + PF * OUT_STEP < piece.z) fetch(k0 + PF * OUT_STEP, cur + PF);
 #pragma unroll
         for (int d = 0; d < 2; ++d) {  // 32 tokens
             if (k0 + 32 * d >= piece.z) break;
@@ -1007,6 +1029,10 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
                     *reinterpret_cast<f32x4_t *>(
                         a.part + ((int64_t(blockIdx.y) * a.nv + pi * RB + b) * a.M + piece.y + k0 + row) * 16 + 4 * g) = u[b];
         }
+    };
+    for (int k0 = 0; k0 < piece.z; k0 += 2 * OUT_STEP) {
+        step(k0, 0);
+        if (k0 + OUT_STEP < piece.z) step(k0 + OUT_STEP, 1);
     }
     // lane: columns c0 + 16 i + 4 g .. + 3 at rank 16 b + r16
     const OutPlace o = out_place(a, piece, pi, false);
@@ -1077,6 +1103,7 @@ __global__ __launch_bounds__(AT) void adapters_parts(const AdArgs a)
 template <int VB, bool EVEN>
 __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
 {
+    constexpr int PF = OUT_AHEAD;  // steps in flight
     __shared__ __attribute__((aligned(16))) uint8_t s_s[4][OUT_STEP * 128];
     __shared__ __attribute__((aligned(16))) uint8_t s_q[VB][3][OUT_STEP * 32];
     if (int(blockIdx.x) >= a.plan[2]) return;
@@ -1094,32 +1121,33 @@ __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
         for (int b = 0; b < VB; ++b) acc[i][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     uint8_t *ss = s_s[wave];
     constexpr int QR = OUT_STEP * 6, QV = (VB * QR + AT - 1) / AT;  // 16-byte words of u's parts, of a block
-    frag_t sv[8], qv[QV];
-    int32_t tok[8];
-    out_tokens(order, 0, piece.z, tok);
-    auto fetch = [&](int k0) {
-        out_fetch<EVEN>(a.X, a.ldx, tok, c0, C, sv);
-        out_tokens(order, k0 + OUT_STEP, piece.z, tok);
+    frag_t sv[PF][8], qv[PF][QV];
+    int32_t tok[2][8];
+    out_tokens(order, 0, piece.z, tok[0]);
+    auto fetch = [&](int k0, int i) {
+        out_tokens(order, k0 + OUT_STEP, piece.z, tok[1 - (i & 1)]);
+        out_fetch<EVEN>(a.X, a.ldx, tok[i & 1], c0, C, sv[i % PF]);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             const int w = t + AT * q, b = w / QR, x = w - QR * b;
             const int v = v0 + b < a.nv ? v0 + b : v0;
-            qv[q] = reinterpret_cast<const frag_t *>(a.hl + (int64_t(v) * a.M + piece.y + k0) * 48)[x / 6 < piece.z - k0 ? x : 0];
+            qv[i % PF][q] = reinterpret_cast<const frag_t *>(a.hl + (int64_t(v) * a.M + piece.y) * 48)[k0 + x / 6 < piece.z ? 6 * k0 + x : 0];
         }
     };
-    fetch(0);
+#pragma unroll
+    for (int i = 0; i < PF; ++i) fetch(i * OUT_STEP, i);
     const int kr = 8 * g + (r16 >> 2), key = out_key(kr), quad = (r16 & 3) << 3;
-    for (int k0 = 0; k0 < piece.z; k0 += OUT_STEP) {
+    auto step = [&](int k0, int cur) {
         __syncthreads();  // the last step's reads are over
-        out_stage<EVEN>(ss, sv, k0, piece.z, c0, C);
+        out_stage<EVEN>(ss, sv[cur % PF], k0, piece.z, c0, C);
 #pragma unroll
         for (int q = 0; q < QV; ++q) {
             // parts of a row: 0 0 1 1 2 2
             const int w = t + AT * q, b = w / QR, x = w - QR * b, row = x / 6, c = x - 6 * row;
-            if (b < VB) *reinterpret_cast<frag_t *>(s_q[b][c >> 1] + row * 32 + 16 * (c & 1)) = first8<true>(qv[q], k0 + row < piece.z);
+            if (b < VB) *reinterpret_cast<frag_t *>(s_q[b][c >> 1] + row * 32 + 16 * (c & 1)) = first8<true>(qv[cur % PF][q], k0 + row < piece.z);
         }
         __syncthreads();
-        if (k0 + OUT_STEP < piece.z) fetch(k0 + OUT_STEP);
+        if (k0 + PF * OUT_STEP < piece.z) fetch(k0 + PF * OUT_STEP, cur + PF);
 #pragma unroll
         for (int d = 0; d < 2; ++d) {  // 32 tokens
             if (k0 + 32 * d >= piece.z) break;
@@ -1135,6 +1163,10 @@ __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
                     for (int i = 0; i < 4; ++i) acc[i][b] = mfma(sf[i], qf, acc[i][b]);
                 }
         }
+    };
+    for (int k0 = 0; k0 < piece.z; k0 += 2 * OUT_STEP) {
+        step(k0, 0);
+        if (k0 + OUT_STEP < piece.z) step(k0 + OUT_STEP, 1);
     }
 #pragma unroll
     for (int b = 0; b < VB; ++b) {
@@ -1197,12 +1229,11 @@ int rank_blocks(int rank) { return rank <= 16 ? 1 : (rank <= 32 ? 2 : (rank <= 6
 // Rank blocks that a launch over x takes at once, of nv.
 int blocks_at_once(int nv) { return nv <= 4 ? nv : (nv % 3 == 0 ? 3 : 4); }
 
-// Splits of d_in: until the launch has about 1024 blocks, each wave keeping
-// 128 or more of it.
-int shrink_splits(int64_t tiles, int groups, int64_t K, bool split_waves)
+// Splits of d_in: until the launch has about 1024 blocks, each wave with a turn
+// of 128 inputs (64-token tiles: two) or more.
+int shrink_splits(int64_t tiles, int groups, int64_t K)
 {
-    const int64_t most = std::max<int64_t>(1, K / (split_waves ? 512 : 256));
-    return int(std::clamp<int64_t>(1024 / std::max<int64_t>(1, tiles * groups), 1, std::min<int64_t>(most, 16)));
+    return int(std::clamp<int64_t>(1024 / std::max<int64_t>(1, tiles * groups), 1, std::clamp<int64_t>(K / 512, 1, 16)));
 }
 
 AdLayout ad_layout(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_in, const int64_t *d_out)
@@ -1216,7 +1247,7 @@ AdLayout ad_layout(bool back, int64_t M, int64_t n, int np, int rank, int64_t d_
         l.slot_floats += int64_t(rank) * (d_in + d_out[i]);
     }
     l.slot_floats = (l.slot_floats + 3) / 4 * 4;
-    l.ksplit = shrink_splits(M / pl.tile + 1, (nv + at_once - 1) / at_once, d_in, pl.tile == 16);
+    l.ksplit = shrink_splits(M / pl.tile + 1, (nv + at_once - 1) / at_once, d_in);
     const int64_t parts = back ? (widest + OUT_COLS - 1) / OUT_COLS : l.ksplit;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -1384,7 +1415,7 @@ hipError_t run_backward(const AdaptersCall &c, AdArgs &a, int64_t widest, hipStr
     a.lddx0 = c.lddx0;
     a.lddx = c.lddx;
     const bool f32 = c.dx_dtype == BSQ_F32;
-    const dim3 xgrid(unsigned(a.l.max_tiles), blocks(c.d_in, 256), 1);
+    const dim3 xgrid(unsigned(a.l.max_tiles), blocks(c.d_in, a.l.tile == 16 ? 256 : DX_COLS), 1);
     if (f32) return even_in ? launch_dx<true, true>(a, xgrid, st) : launch_dx<false, true>(a, xgrid, st);
     return even_in ? launch_dx<true, false>(a, xgrid, st) : launch_dx<false, false>(a, xgrid, st);
 }

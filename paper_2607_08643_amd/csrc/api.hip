@@ -626,7 +626,7 @@ bsq_status bsq_train_adam(const bsq_config *cfg, const bsq_train_hparams *hp, in
 // ---------------------------------------------------------------------------
 namespace {
 constexpr int64_t MAX_TOKENS = int64_t(1) << 24;
-constexpr int64_t MAX_WIDTH = int64_t(1) << 24;  // of a projection, either way
+constexpr int64_t MAX_WIDTH = int64_t(1) << 22;  // of a projection, either way (grid rows of 128 columns: 65535 at most)
 
 bsq_status check_batch(int64_t M, int32_t n)
 {

@@ -556,9 +556,9 @@ __global__ __launch_bounds__(XT) void xent_join_kernel(const XArgs a, int tiles)
         }
     }
     if (part != 0 || m >= a.T) return;
-    const float lse = mx + logf(s);
-    a.lse_out[m] = row >= 0 ? lse : 0.0f;
-    a.loss_out[m] = row >= 0 ? lse - a.ztgt[row] : 0.0f;
+    // (of the loss only the smaller terms are rounded: mx is often near z)
+    a.lse_out[m] = row >= 0 ? mx + logf(s) : 0.0f;
+    a.loss_out[m] = row >= 0 ? (mx - a.ztgt[row]) + logf(s) : 0.0f;
 }
 
 // dH rows from the sums (0 for tokens without a loss). One block per token.
