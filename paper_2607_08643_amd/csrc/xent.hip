@@ -30,6 +30,9 @@ constexpr int XT = 256;
 constexpr int VBLK = 256;              // words of a logits tile
 constexpr int64_t ROW_PAD = 256;       // token rows are padded to this
 constexpr float LOG2E = 1.4426950408889634f;
+// Up to this many tokens the tiles are chosen by those that have a loss (past it
+// 256-token tiles fill the compute units).
+constexpr int64_t HALF_TOKENS = 1024;
 
 enum { EPI_STATS, EPI_PROB, EPI_DV, EPI_DH };
 
@@ -215,9 +218,38 @@ __device__ __forceinline__ void join_stats(float &m, float &s, float m2, float s
     m = mm;
 }
 
+// Tiles of a product over `live` tokens, and splits of dH's depth: until the
+// launch fills the compute units.
+struct XTiles {
+    int rt, lt, splits;
+};
+
+template <int EPI, int BR, int BL>
+__device__ __forceinline__ XTiles xent_tiles(const XArgs &a, int live)
+{
+    const int64_t rrows = (EPI == EPI_DV) ? a.vp : live;
+    const int64_t lrows = (EPI == EPI_STATS || EPI == EPI_PROB) ? a.vp : a.D;
+    XTiles n{int((rrows + BR - 1) / BR), int((lrows + BL - 1) / BL), 1};
+    if (EPI == EPI_DH) {
+        const int fill = n.rt > 0 ? 256 / (n.rt * n.lt) : 1;
+        n.splits = fill < 1 ? 1 : (fill < a.hsplit ? fill : a.hsplit);
+    }
+    return n;
+}
+
+// Whether 128-token tiles finish before 256-token ones: rounds of tiles over the
+// 256 compute units, of 2/3 the time (512 tokens of 32003 words: 168 us in two
+// rounds, 129 in one; 301 tokens of which 180 have a loss: 98 in one, 122).
+template <int EPI>
+__device__ __forceinline__ bool xent_half_tiles(const XArgs &a, int live)
+{
+    const XTiles h = xent_tiles<EPI, 128, 256>(a, live), w = xent_tiles<EPI, 256, 256>(a, live);
+    const int rh = (h.rt * h.lt * h.splits + 255) / 256, rw = (w.rt * w.lt * w.splits + 255) / 256;
+    return 2 * rh * w.splits < 3 * rw * h.splits;
+}
+
 template <int EPI, int MF, int NF, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(WM * WN / 4, WM * WN / 4)))
-void xent_gemm(const XArgs a)
+__device__ __forceinline__ void xent_tile(const XArgs &a, int live)
 {
     using G = XShape<MF, NF, WM, WN>;
     constexpr bool LOGITS = EPI == EPI_STATS || EPI == EPI_PROB;
@@ -230,15 +262,11 @@ void xent_gemm(const XArgs a)
     const int t = threadIdx.x, lane = t & 63, g = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const int live = a.hdr[0];
 
     // Tiles: right tiles x left tiles (x splits of k for dH); every XCD takes a
     // run of them that walks up to 8 right tiles before the next left one.
-    const int64_t rrows = (EPI == EPI_DV) ? a.vp : live;
-    const int64_t lrows = LOGITS ? a.vp : a.D;
-    const int rt = int((rrows + G::BR - 1) / G::BR), lt = int((lrows + G::BL - 1) / G::BL);
-    const int splits = (EPI == EPI_DH) ? a.hsplit : 1;
-    const int total = rt * lt * splits;
+    const XTiles n = xent_tiles<EPI, G::BR, G::BL>(a, live);
+    const int rt = n.rt, lt = n.lt, splits = n.splits, total = rt * lt * splits;
     if (int(blockIdx.x) >= total) return;
     const int xcd = blockIdx.x & 7, per = total >> 3, rem = total & 7;
     int lg = xcd * per + (xcd < rem ? xcd : rem) + int(blockIdx.x >> 3);
@@ -526,6 +554,22 @@ void xent_gemm(const XArgs a)
     }
 }
 
+template <int EPI, int MF, int NF, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(WM * WN / 4, WM * WN / 4)))
+void xent_gemm(const XArgs a)
+{
+    xent_tile<EPI, MF, NF, WM, WN>(a, a.hdr[0]);
+}
+
+// The tiles by the tokens that have a loss, which only the GPU knows.
+template <int EPI>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void xent_gemm_live(const XArgs a)
+{
+    const int live = a.hdr[0];
+    if (xent_half_tiles<EPI>(a, live)) xent_tile<EPI, 4, 4, 2, 4>(a, live);
+    else xent_tile<EPI, 8, 4, 2, 4>(a, live);
+}
+
 // A token's tiles joined: TOK tokens a block, XT / TOK threads each over the
 // tiles, their pairs then joined in order. (One block of 16 threads a token took
 // 22 us for 594 tiles, with any number of tokens.)
@@ -565,12 +609,15 @@ __global__ __launch_bounds__(XT) void xent_join_kernel(const XArgs a, int tiles)
 __global__ __launch_bounds__(XT) void xent_dh_kernel(const XArgs a)
 {
     const int64_t m = blockIdx.x;
-    const int row = a.pos[m];
+    const int row = a.pos[m], live = a.hdr[0];
+    const bool half = a.T <= 128 || (a.T <= HALF_TOKENS && xent_half_tiles<EPI_DH>(a, live));
+    const int splits = half ? xent_tiles<EPI_DH, 128, 256>(a, live).splits : xent_tiles<EPI_DH, 256, 256>(a, live).splits;
     for (int64_t c = 4 * threadIdx.x; c < a.D; c += 4 * XT) {
         f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         if (row >= 0) {
             const float *q = a.dHp + int64_t(row) * a.Dp + c;
-            for (int z = 0; z < a.hsplit; ++z) v += *reinterpret_cast<const f32x4_t *>(q + int64_t(z) * a.Tp * a.Dp);
+#pragma unroll 8
+            for (int z = 0; z < splits; ++z) v += *reinterpret_cast<const f32x4_t *>(q + int64_t(z) * a.Tp * a.Dp);
         }
         uint16_t *o = a.dH + m * a.lddh + c;
         if (a.dh_vec) *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
@@ -629,21 +676,28 @@ XLayout xent_layout(bool grad, int64_t T, int64_t N, int64_t D)
     return l;
 }
 
+// KERNEL takes tiles of BR x BL at least.
+template <auto KERNEL, int BR, int BL, int THREADS, size_t LDS>
+hipError_t launch_gemm_tiles(const XArgs &a, int64_t right, int64_t left, int splits, hipStream_t st)
+{
+    static std::atomic<bool> lds_set{false};  // the ring exceeds the default dynamic LDS limit
+    if (!lds_set.load(std::memory_order_relaxed)) {
+        const hipError_t e =
+            hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, int(LDS));
+        if (e != hipSuccess) return e;
+        lds_set.store(true, std::memory_order_relaxed);
+    }
+    const int64_t blocks = (right + BR - 1) / BR * ((left + BL - 1) / BL) * splits;
+    if (blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL(KERNEL, dim3(unsigned(blocks)), dim3(THREADS), LDS, st, a);
+    return hipGetLastError();
+}
+
 template <int EPI, int MF, int NF, int WM, int WN>
 hipError_t launch_gemm_shape(const XArgs &a, int64_t right, int64_t left, int splits, hipStream_t st)
 {
     using G = XShape<MF, NF, WM, WN>;
-    static std::atomic<bool> lds_set{false};  // the ring exceeds the default dynamic LDS limit
-    if (!lds_set.load(std::memory_order_relaxed)) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&xent_gemm<EPI, MF, NF, WM, WN>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, int(G::LDS));
-        if (e != hipSuccess) return e;
-        lds_set.store(true, std::memory_order_relaxed);
-    }
-    const int64_t blocks = (right + G::BR - 1) / G::BR * ((left + G::BL - 1) / G::BL) * splits;
-    if (blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL((xent_gemm<EPI, MF, NF, WM, WN>), dim3(unsigned(blocks)), dim3(64 * G::NW), G::LDS, st, a);
-    return hipGetLastError();
+    return launch_gemm_tiles<&xent_gemm<EPI, MF, NF, WM, WN>, G::BR, G::BL, 64 * G::NW, G::LDS>(a, right, left, splits, st);
 }
 
 // Token tiles by the number of tokens. d's rows are read 64 deep by dV, so its
@@ -657,6 +711,10 @@ hipError_t launch_tokens(const XArgs &a, int64_t left, int splits, hipStream_t s
     }
     if (a.T <= 64) return launch_gemm_shape<EPI, 2, 4, 2, 4>(a, a.T, left, splits, st);
     if (a.T <= 128) return launch_gemm_shape<EPI, 4, 4, 2, 4>(a, a.T, left, splits, st);
+    using H = XShape<4, 4, 2, 4>;
+    using W = XShape<8, 4, 2, 4>;
+    if (a.T <= HALF_TOKENS)
+        return launch_gemm_tiles<&xent_gemm_live<EPI>, H::BR, H::BL, 512, (W::LDS > H::LDS ? W::LDS : H::LDS)>(a, a.T, left, splits, st);
     return launch_gemm_shape<EPI, 8, 4, 2, 4>(a, a.T, left, splits, st);
 }
 
