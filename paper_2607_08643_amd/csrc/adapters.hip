@@ -608,7 +608,7 @@ __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[
 template <int RB, bool EVEN, int TG, bool F32, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
 {
-    constexpr int PF = (RB == 1) ? 2 : 1;  // 64-column groups in flight
+    constexpr int PF = (RB == 1 && !DIRECT) ? 2 : 1;  // 64-column groups in flight (DIRECT: 17 us for 64 tokens, with two 20)
     __shared__ int s_tok[4][16];
     TileView tv;
     if (!tile_view<DIRECT, TG>(a, true, s_tok, tv)) return;
@@ -1378,8 +1378,9 @@ hipError_t run_forward(const AdaptersCall &c, AdArgs &a, int64_t widest, hipStre
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     // columns of a block: t and the tile are read once for all of them, but few
-    // tiles need many blocks to fill the compute units
-    a.ecols = (a.l.tile == 16) ? 1024 : 256;
+    // tiles need many blocks to fill the compute units (64 tokens of 24576 columns: 2048
+    // columns 14 us, 1024 17, 512 23)
+    a.ecols = (a.l.tile == 16) ? 2048 : 256;
     while (a.ecols > 256 && int64_t(tiles) * c.np * blocks(widest, a.ecols) < 768) a.ecols /= 2;
     const dim3 egrid(tiles, blocks(widest, a.ecols), unsigned(c.np));
     if (f32) return even_rank ? launch_expand<true, true>(a, egrid, direct, st) : launch_expand<false, true>(a, egrid, direct, st);
