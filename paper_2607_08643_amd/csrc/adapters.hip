@@ -426,7 +426,9 @@ __device__ __forceinline__ bool tile_view(const AdArgs &a, bool with_none, int (
 // for VB rank blocks v at a time. 16-token tiles: the four waves share the tile
 // and split d_in. 64-token tiles: 32 tokens a wave (A is read half as often as
 // with 16) and two waves along d_in. Loads are a step ahead of their products.
-// Bound by reading x.
+// Bound by reading x, whose 64-byte pieces of many rows come at 2.0 to 2.2 TB/s
+// (2000 tokens of 25600 inputs at rank 64: 52 us; 8192 of 4096 for three projections
+// of rank 16: 31 us).
 // ---------------------------------------------------------------------------
 template <int VB, bool EVEN, int TG, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
@@ -640,7 +642,9 @@ __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[
 // expand: y = y0 + s B t. A block: a tile and a.ecols columns; a wave: 16 tokens
 // (64-token tiles) over all of them, or every fourth 64 columns of all 16. t is
 // summed once; then per 64 columns the wave has y0 and B of the next ones in
-// flight. Bound by reading y0 and writing y.
+// flight. Bound by reading y0 and writing y (8192 tokens of 6144 columns at rank
+// 16: 54 us, 3.7 TB/s of both). Reading ahead past a block's last columns, to
+// spare the condition, made it 4 us slower.
 // ---------------------------------------------------------------------------
 template <int RB, bool EVEN, int TG, bool F32, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
@@ -776,7 +780,9 @@ __device__ __forceinline__ frag_t read_tr(const uint8_t *p, int four)
 // rows of A are staged in LDS (two blocks of eight ranks, [pair of 16-column
 // groups][rank][64 bytes], the groups swapped in ranks 8 to 15: the rows that
 // half a wave reads together fall on all banks once) and read transposed. The
-// columns are permuted on the way in (run_column).
+// columns are permuted on the way in (run_column). Bound by reading dx0 and
+// writing dx (8192 tokens of 4096 columns, three projections of rank 16: 43 us, 3.1
+// TB/s of both).
 // ---------------------------------------------------------------------------
 constexpr int DX_COLS = 128;
 
@@ -873,8 +879,8 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
 // wave: 64 columns, all tokens) both are read transposed, tokens along the depth;
 // for u (a wave: 16 tokens, all columns) dy is read as it lies and the block's
 // 256 x rank of B, staged once, transposed. 64 tokens a step keep 32 KiB of dy
-// in flight per block; with 32 the loads' latency showed (83 us for 8192 tokens
-// of q, k and v).
+// in flight per block (8192 tokens of 6144 columns at rank 16: 32 us, 3.1 TB/s of
+// dy); with 32 the loads' latency showed (83 us for 8192 tokens of q, k and v).
 //
 // LDS rows of dy: a wave's 64 columns, 128 bytes, in 32-byte groups; group q of
 // row k lies at q ^ key(k), so that the eight rows that half a wave reads
@@ -1135,7 +1141,10 @@ __global__ __launch_bounds__(AT) void adapters_parts(const AdArgs a)
 
 // ---------------------------------------------------------------------------
 // dA: of a piece's tokens, dA[r][c] = sum_m u[m][r] x[m][c], for VB rank blocks
-// of the group from one reading of x; staged and read as dB's operands.
+// of the group from one reading of x; staged and read as dB's operands. Bound by
+// the turn of a step, loads to LDS to products, with few waves beside each other
+// (8192 tokens of 4096 columns, three blocks: 41 us, 1.7 TB/s of x; pieces of M / 24
+// tokens for more blocks cost more in partial sums than they gain).
 // ---------------------------------------------------------------------------
 template <int VB, bool EVEN>
 __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)

@@ -13,6 +13,11 @@
 // two further products read them: dV's rows of the piece, and the piece's
 // contribution to dH, added in fp32 over the pieces in order.
 //
+// Bound by the matrix cores from some hundred tokens on: 4096 tokens of 151936
+// words, 4096 inputs: logits 4.4 ms (1.16 PFLOP/s), dH 3.8 (1.33), dV 4.3 (1.19);
+// the loss alone of 2000 tokens 2.2 ms (1.14). One token's loss is one reading of V:
+// 250 us, 5.0 TB/s.
+//
 // Tokens without a loss are taken out first: the rows that have one are copied
 // next to each other (padded with zeros to whole tiles and to a multiple of
 // 64 inputs), and every product runs over those alone.

@@ -192,6 +192,38 @@ def test_plan_is_a_stable_sort(M, n, kind, gpu):
     assert int(words[0]) == int(tiles[:n].sum()) and int(words[1]) == int(tiles.sum())
 
 
+@pytest.mark.parametrize("M,n,kind", [(300, 64, "mixed"), (8192, 64, "runs"), (8193, 65, "mixed"), (8256, 1024, "mixed"),
+                                      (20001, 5, "runs"), (70000, 1, "one")])
+def test_plan_lists_every_tile_and_piece(M, n, kind, gpu):
+    """Either side of 8192 tokens (up to which ids are read once) and of 64
+    adapters (up to which a wave writes an adapter's tiles): the whole plan."""
+    say(f"adapters plan M={M} n={n} {kind}")
+    ids = _ids(kind, M, n, 11)
+    plan = bsq.bsq_adapters_plan(ids.to(gpu), n)
+    torch.cuda.synchronize()
+    words = plan.buf.view(torch.int32).cpu().long()
+    key = torch.where(ids < 0, n, ids).long()
+    counts = torch.bincount(key, minlength=n + 1).tolist()
+    tile, piece = 16 if M <= 1024 else 64, max(256, (M // 16 + 63) // 64 * 64)
+    order = 16 + (2 * (n + 2) + 3) // 4 * 4
+    assert torch.equal(words[order:order + M], torch.sort(key, stable=True).indices)
+    tiles, pieces, first, slot = [], [], 0, 0
+    for a, c in enumerate(counts):
+        tiles += [[a if a < n else -1, first + q, min(tile, c - q), 0] for q in range(0, c, tile)]
+        if a < n:
+            many = c > piece
+            for q in range(0, c, piece):
+                pieces.append([a, first + q, min(piece, c - q), slot if many else -1])
+                slot += many
+        first += c
+    live = sum(t[0] >= 0 for t in tiles)
+    assert words[:3].tolist() == [live, len(tiles), len(pieces)]
+    at = order + (M + 3) // 4 * 4
+    assert words[at:at + 4 * len(tiles)].view(-1, 4).tolist() == tiles
+    at += 4 * min(M, M // tile + n + 1)
+    assert words[at:at + 4 * len(pieces)].view(-1, 4).tolist() == pieces
+
+
 def test_an_id_out_of_range_is_reported_and_means_none(gpu):
     b = Batch(gpu, 40, (64,), 128, 16, 4, _ids("mixed", 40, 4, 9))
     ids = b.ids.clone()
