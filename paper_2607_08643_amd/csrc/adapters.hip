@@ -24,6 +24,7 @@
 // product), for fp32 results three (2^-24).
 #include <algorithm>
 
+#include "adapter_rows.h"
 #include "gemm_common.h"
 
 namespace bsq {
@@ -475,7 +476,7 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
         const Proj &p = a.p[pi];
         const int re = rank_of(p, tv.adapter, a.rank);
         rin[b] = re - r0 - 4 * g;
-        arow[b] = p.A + (int64_t(tv.adapter) * a.rank + (r0 + r16 < re ? r0 + r16 : 0)) * K;
+        arow[b] = p.A + adapter_row(tv.adapter, a.rank, r0 + r16, re) * K;
     }
     f32x4_t acc[MT][VB];
 #pragma unroll
@@ -820,11 +821,12 @@ __global__ __launch_bounds__(AT) void adapters_dx(const AdArgs a)
         auto fetch = [&](int v) {
             const int pi = v / a.rb, b = v - pi * a.rb;
             const Proj &p = a.p[pi];
-            re = rank_of(p, ad, a.rank) - 16 * b;
+            const int own = rank_of(p, ad, a.rank);
+            re = own - 16 * b;
 #pragma unroll
             for (int q = 0; q < SQ; ++q) {
                 const int w = t + AT * q, r = w / (BC / 8);
-                st[q] = raw8<EVEN>(p.A + (int64_t(ad) * a.rank + 16 * b + (r < re ? r : 0)) * C, cb + 8 * (w % (BC / 8)), C);
+                st[q] = raw8<EVEN>(p.A + adapter_row(ad, a.rank, 16 * b + r, own) * C, cb + 8 * (w % (BC / 8)), C);
             }
         };
         fetch(0);
@@ -1268,9 +1270,6 @@ struct AdLayout {
     size_t part, hl, slots, plan, total;
     int64_t slot_floats;
 };
-
-// Rank blocks of 16 of a projection: one, two, four or eight.
-int rank_blocks(int rank) { return rank <= 16 ? 1 : (rank <= 32 ? 2 : (rank <= 64 ? 4 : 8)); }
 
 // Rank blocks that a launch over x takes at once, of nv.
 int blocks_at_once(int nv) { return nv <= 4 ? nv : (nv % 3 == 0 ? 3 : 4); }
