@@ -674,8 +674,9 @@ __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
     const uint16_t *B = p.B + int64_t(ad < 0 ? 0 : ad) * C * a.rank;
     const int r0 = 8 * (g & 1);  // the lane's ranks of a block
     // B: rows past d_out are its last (rows of a product do not mix), ranks past the
-    // adapter's own are masked before the product
-    const bool part_rank = p.ranks != nullptr || a.rank % 16 != 0;
+    // adapter's own are masked before the product (all of them where there is no
+    // adapter: 0 times an infinity would be no 0)
+    const bool part_rank = p.ranks != nullptr || a.rank % 16 != 0 || ad < 0;
     auto load_b = [&](int64_t c, frag_t (&w)[RB][4]) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

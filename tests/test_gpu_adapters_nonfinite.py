@@ -1,0 +1,50 @@
+"""Infinities and NaN in the weights of an adapter reach its own tokens and nothing
+else."""
+import pytest
+import torch
+
+import paper_2607_08643_amd as bsq
+from parity_bounds import say
+from test_gpu_adapters import Batch, _ids
+
+pytestmark = pytest.mark.gpu
+
+INF, NAN = float("inf"), float("nan")
+
+
+def _spoil(q, a, value):
+    """Adapter a's A and B hold `value` in places."""
+    q.A[a, 0, 0], q.A[a, -1, -1] = value, value
+    q.B[a, 0, 0], q.B[a, -1, -1] = value, -value
+
+
+@pytest.mark.parametrize("value", [INF, NAN])
+@pytest.mark.parametrize("y_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,d_in,rank", [(40, 264, 16), (300, 264, 32), (1500, 96, 16), (1500, 77, 128)])
+def test_a_spoiled_adapter_stays_alone(M, d_in, rank, y_dtype, value, gpu):
+    """Whatever an adapter holds, tokens without one keep y0 and dx0, and other
+    adapters' tokens and gradients their bits."""
+    say(f"spoiled adapter M={M} d_in={d_in} rank={rank} {y_dtype} {value}")
+    n = 3
+    b = Batch(gpu, M, (96, 33), d_in, rank, n, _ids("mixed", M, n, 2), y_dtype=y_dtype)
+    plan = bsq.bsq_adapters_plan(b.ids, n)
+    g = torch.Generator().manual_seed(5)
+    dy = [torch.randn((M, d), generator=g).bfloat16().to(gpu) for d in b.dims]
+    base = torch.randn((M, d_in), generator=g).bfloat16().to(gpu)
+    y, t = bsq.bsq_adapters_apply(plan, b.pools, b.X, b.base, keep=True)
+    bare, _ = bsq.bsq_adapters_apply(plan, b.pools, b.X, None, y_dtype=y_dtype)
+    dx, dA, dB = bsq.bsq_adapters_grad(plan, b.pools, b.X, t, dy, base=base)
+    free, other = b.ids < 0, b.ids > 0
+    assert free.any() and other.any()
+    for q in b.pools:
+        _spoil(q, 0, value)
+    y2, t2 = bsq.bsq_adapters_apply(plan, b.pools, b.X, b.base, keep=True)
+    bare2, _ = bsq.bsq_adapters_apply(plan, b.pools, b.X, None, y_dtype=y_dtype)
+    dx2, dA2, dB2 = bsq.bsq_adapters_grad(plan, b.pools, b.X, t, dy, base=base)
+    torch.cuda.synchronize()
+    for p in range(2):
+        assert torch.equal(y2[p][free], b.base[p][free]) and (bare2[p][free] == 0).all() and (t2[p][free] == 0).all()
+        assert torch.equal(y2[p][other], y[p][other]) and torch.equal(bare2[p][other], bare[p][other])
+        assert torch.equal(t2[p][other], t[p][other])
+        assert torch.equal(dA2[p][1:], dA[p][1:]) and torch.equal(dB2[p][1:], dB[p][1:])
+    assert torch.equal(dx2[free], base[free]) and torch.equal(dx2[other], dx[other])
