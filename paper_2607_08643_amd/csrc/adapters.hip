@@ -23,6 +23,7 @@
 // value is lost, and a rank block of 16 with its two parts fills one 32-deep
 // product), for fp32 results three (2^-24).
 #include <algorithm>
+#include <type_traits>
 
 #include "adapter_rows.h"
 #include "gemm_common.h"
@@ -491,14 +492,21 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
 #pragma unroll
         for (int b = 0; b < VB; ++b) w[u][b] = raw8<EVEN>(arow[b], k, K);
     };
-    auto product = [&](int u, int64_t s) {
+    // `last`: the wave's last turn, the only one that may reach past d_in or the
+    // block's steps. Both operands are masked there: what stands for the missing
+    // ones are values of the row, and 0 times an infinity is no 0.
+    auto product = [&](int u, int64_t s, auto last) {
+        constexpr bool LAST = decltype(last)::value;
         const int64_t left = (s < s1) ? K - 32 * s - 8 * g : 0;
+        frag_t xm[MT], wm[VB];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const frag_t xm = first8<EVEN>(x[u][m], left);
+        for (int m = 0; m < MT; ++m) xm[m] = LAST ? first8<EVEN>(x[u][m], left) : x[u][m];
 #pragma unroll
-            for (int b = 0; b < VB; ++b) acc[m][b] = mfma(w[u][b], xm, acc[m][b]);
-        }
+        for (int b = 0; b < VB; ++b) wm[b] = LAST ? first8<EVEN>(w[u][b], left) : w[u][b];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int b = 0; b < VB; ++b) acc[m][b] = mfma(wm[b], xm[m], acc[m][b]);
     };
     int64_t s = s0 + U * kw;
     if (s < s1) {
@@ -507,11 +515,11 @@ __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
         for (; s + U * KW < s1; s += U * KW)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                product(u, s + u);
+                product(u, s + u, std::false_type{});
                 fetch(u, s + U * KW + u);
             }
 #pragma unroll
-        for (int u = 0; u < U; ++u) product(u, s + u);
+        for (int u = 0; u < U; ++u) product(u, s + u, std::true_type{});
     }
     // lane: ranks 4 g .. + 3 of a block, of token r16; the waves along d_in added in order
 #pragma unroll

@@ -1,5 +1,6 @@
-"""Infinities and NaN in the weights of an adapter reach its own tokens and nothing
-else."""
+"""Infinities and NaN in the weights of adapters reach what the formulas say they
+reach, and nothing else: tokens without an adapter are the base alone, sums over
+d_in have no terms past its end."""
 import pytest
 import torch
 
@@ -48,3 +49,23 @@ def test_a_spoiled_adapter_stays_alone(M, d_in, rank, y_dtype, value, gpu):
         assert torch.equal(t2[p][other], t[p][other])
         assert torch.equal(dA2[p][1:], dA[p][1:]) and torch.equal(dB2[p][1:], dB[p][1:])
     assert torch.equal(dx2[free], base[free]) and torch.equal(dx2[other], dx[other])
+
+
+@pytest.mark.parametrize("M", [40, 300, 1500])
+@pytest.mark.parametrize("d_in", [8, 77, 264, 544, 1000])
+def test_no_terms_past_the_end_of_d_in(M, d_in, gpu):
+    """An infinite entry of A times x = 1 is an infinite t: nothing past d_in (where
+    x has no values) is multiplied with it."""
+    say(f"infinite A, M={M} d_in={d_in}")
+    b = Batch(gpu, M, (40,), d_in, 16, 2, _ids("one", M, 2, 2))
+    b.X[:, 0] = 1.0
+    b.X[:, d_in - 1] = 1.0
+    plan = bsq.bsq_adapters_plan(b.ids, 2)
+    _, t = bsq.bsq_adapters_apply(plan, b.pools, b.X, None, keep=True)
+    A = b.pools[0].A
+    A[1, 2, 0], A[1, 7, 0], A[1, 9, d_in - 1] = INF, -INF, -INF
+    _, u = bsq.bsq_adapters_apply(plan, b.pools, b.X, None, keep=True)
+    torch.cuda.synchronize()
+    want = t[0].clone()
+    want[:, 2], want[:, 7], want[:, 9] = INF, -INF, -INF
+    assert torch.equal(u[0], want)
