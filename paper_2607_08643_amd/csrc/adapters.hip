@@ -1088,7 +1088,8 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
         step(k0, 0);
         if (k0 + OUT_STEP < piece.z) step(k0 + OUT_STEP, 1);
     }
-    // lane: columns c0 + 16 i + 4 g .. + 3 at rank 16 b + r16
+    // lane: columns c0 + 16 i + 4 g .. + 3 at rank 16 b + r16; 0 past the adapter's
+    // rank, also where dy is not finite (its sum there is of 0 times an infinity)
     const OutPlace o = out_place(a, piece, pi, false);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -1101,7 +1102,8 @@ __global__ __launch_bounds__(AT) void adapters_dy(const AdArgs a)
             for (int e = 0; e < 4; ++e) {
                 if (c + e >= C) break;
                 float *q = o.to + (c + e) * a.rank + r;
-                *q = o.add ? *q + acc[i][b][e] : acc[i][b][e];
+                const float v = r < re ? acc[i][b][e] : 0.0f;
+                *q = o.add ? *q + v : v;
             }
         }
 }
@@ -1231,14 +1233,17 @@ __global__ __launch_bounds__(AT) void adapters_da(const AdArgs a)
         if (v >= a.nv) break;
         const int pi = v / a.rb, r = 16 * (v - pi * a.rb) + r16;
         if (r >= a.rank) continue;
+        const bool in = r < rank_of(a.p[pi], piece.x, a.rank);  // (as dB: 0 past the adapter's rank)
         const OutPlace o = out_place(a, piece, pi, true);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t c = c0 + 16 * i + 4 * g;
             float *q = o.to + int64_t(r) * C + c;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c + e < C) q[e] = o.add ? q[e] + acc[i][b][e] : acc[i][b][e];
+            for (int e = 0; e < 4; ++e) {
+                const float v = in ? acc[i][b][e] : 0.0f;
+                if (c + e < C) q[e] = o.add ? q[e] + v : v;
+            }
         }
     }
 }

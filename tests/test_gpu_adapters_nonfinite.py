@@ -1,6 +1,7 @@
-"""Infinities and NaN in the weights of adapters reach what the formulas say they
-reach, and nothing else: tokens without an adapter are the base alone, sums over
-d_in have no terms past its end."""
+"""Infinities and NaN in the weights or inputs of adapters reach what the formulas
+say they reach, and nothing else: tokens without an adapter are the base alone,
+sums over d_in have no terms past its end, gradients past an adapter's own rank
+are 0."""
 import pytest
 import torch
 
@@ -69,3 +70,35 @@ def test_no_terms_past_the_end_of_d_in(M, d_in, gpu):
     want = t[0].clone()
     want[:, 2], want[:, 7], want[:, 9] = INF, -INF, -INF
     assert torch.equal(u[0], want)
+
+
+@pytest.mark.parametrize("value", [INF, NAN])
+@pytest.mark.parametrize("M", [40, 300, 5000])
+def test_gradients_past_an_adapters_rank_are_zero(M, value, gpu):
+    """Also where x or dy are not finite (0 times an infinity is no 0)."""
+    say(f"gradients past the rank, M={M}, {value}")
+    n, rank, own = 2, 20, [5, 0]
+    b = Batch(gpu, M, (70,), 296, rank, n, _ids("mixed", M, n, 3), own)
+    plan = bsq.bsq_adapters_plan(b.ids, n)
+    _, t = bsq.bsq_adapters_apply(plan, b.pools, b.X, None, keep=True)
+    dy = torch.randn((M, 70), generator=torch.Generator().manual_seed(1)).bfloat16().to(gpu)
+    _, dA, dB = bsq.bsq_adapters_grad(plan, b.pools, b.X, t, [dy], want_dx=False)
+    m = [int(b.tokens(a)[-1]) for a in range(n)]
+    X2, dy2 = b.X.clone(), dy.clone()
+    for k in m:
+        X2[k, 3] = value
+    _, dA2, dB2 = bsq.bsq_adapters_grad(plan, b.pools, X2, t, [dy], want_dx=False)
+    for k in m:
+        dy2[k, 11] = value
+    before = ([torch.ones_like(dA[0])], [torch.ones_like(dB[0])])
+    _, _, dB3 = bsq.bsq_adapters_grad(plan, b.pools, b.X, t, [dy2], want_dx=False)
+    _, dA4, dB4 = bsq.bsq_adapters_grad(plan, b.pools, X2, t, [dy2], want_dx=False, grads=before, accumulate=True)
+    torch.cuda.synchronize()
+    for a, r in enumerate(own):
+        assert (dA2[0][a, r:] == 0).all() and (dB3[0][a, :, r:] == 0).all()
+        assert (dA4[0][a, r:] == 1).all() and (dB4[0][a, :, r:] == 1).all()
+    keep = torch.arange(296, device=gpu) != 3
+    assert torch.equal(dA2[0][:, :, keep], dA[0][:, :, keep]) and torch.equal(dB2[0], dB[0])
+    assert not torch.isfinite(dA2[0][0, :5, 3]).any()
+    keep = torch.arange(70, device=gpu) != 11
+    assert torch.equal(dB3[0][:, keep], dB[0][:, keep]) and not torch.isfinite(dB3[0][0, 11, :5]).any()
