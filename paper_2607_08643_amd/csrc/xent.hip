@@ -39,10 +39,12 @@ constexpr float LOG2E = 1.4426950408889634f;
 // 256-token tiles fill the compute units).
 constexpr int64_t HALF_TOKENS = 1024;
 
+constexpr int ZEROS = 4;
+
 enum { EPI_STATS, EPI_PROB, EPI_DV, EPI_DH };
 
 struct XArgs {
-    // header words: 0: tokens with a loss
+    // header words: 0: tokens with a loss; ZEROS .. + 3: 16 bytes of zeros
     int32_t *hdr, *rows, *pos;    // rows [Tp]: token of a compact row; pos [T]: compact row of a token or -1
     const uint16_t *H, *V;
     int64_t ldh, ldv, T, N, D, Tp, Dp;
@@ -123,6 +125,7 @@ __global__ __launch_bounds__(XR) void xent_pack_kernel(const XArgs a)
     const int t = threadIdx.x, sub = t / XT, tt = t % XT;
     const int64_t first = int64_t(blockIdx.x) * (XR / XT), i = first + sub;
     int64_t m = -1;
+    if (blockIdx.x == 0 && t < 4) a.hdr[ZEROS + t] = 0;
     if constexpr (ONE) {
         if (t < XR / XT) s_row[t] = -1;
         int before, all;
@@ -322,8 +325,9 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
         }
     }
     const bool full = wave < G::NI % G::NW || G::PMAX == G::PMIN;
-    // The padded k of one operand are zero (H past D, d past the tokens and
-    // words); the other's are read from where it has values.
+    // The padded k of both operands are zero: the right one's are stored (H past D, d
+    // past the tokens and words), the left one's are read from the header's zeros.
+    // (With values of V in their place, a word of -inf made 0 times -inf, a NaN.)
     const int64_t lkmax = LOGITS ? a.D : (EPI == EPI_DV ? a.Tp : kmax);
     // elements from one step to the next
     const int64_t rstep = RK ? 32 : 32 * ldr, lstep = LK ? 32 : 32 * ldl;
@@ -337,7 +341,7 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
             const int v0 = wave + G::NW * r;
             const uint16_t *p = src[r] + (v0 < G::RU ? roff : loff);
             if (past && v0 >= G::RU && 32 * int64_t(kb + u) + kof[r] >= lkmax)
-                p = LK ? src[r] - kof[r] : src[r] + (lkmax - 1 - kof[r]) * ldl;
+                p = reinterpret_cast<const uint16_t *>(a.hdr + ZEROS);
             __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4 *>(p),
                                              reinterpret_cast<uint4 *>(s_mem + slot * G::SLOT + (v0 << 10)), 16, 0, 0);
         }
