@@ -9,7 +9,8 @@
 // operations, D-deep; V is read once.
 //
 // gradient: the vocabulary in pieces of `vp` words. Per piece the logits are
-// made again and leave the tile as d in bf16 (the workspace holds one piece);
+// made again and leave the tile as d in bf16 (the workspace holds one piece; for
+// a dV of 32 bits in two bf16 parts, which its product takes one after the other);
 // two further products read them: dV's rows of the piece, and the piece's
 // contribution to dH, added in fp32 over the pieces in order.
 //
@@ -41,7 +42,8 @@ constexpr int64_t HALF_TOKENS = 1024;
 
 constexpr int ZEROS = 4;
 
-enum { EPI_STATS, EPI_PROB, EPI_DV, EPI_DH };
+// EPI_DV2: EPI_DV from both parts of d
+enum { EPI_STATS, EPI_PROB, EPI_DV, EPI_DV2, EPI_DH };
 
 struct XArgs {
     // header words: 0: tokens with a loss; ZEROS .. + 3: 16 bytes of zeros
@@ -59,7 +61,8 @@ struct XArgs {
     float *loss_out, *lse_out;
     // a piece of the vocabulary: words [v0, v0 + vp)
     int64_t v0, vp, dsp;          // dsp: row length of dS
-    uint16_t *dS;                 // [Tp][dsp]
+    uint16_t *dS;                 // [Tp][dsp]: d rounded; from column lo on, where that is not 0, what remains
+    int64_t lo;
     float *dHp;                   // [hsplit][Tp][Dp]
     int hsplit, first;
     uint16_t *dH;
@@ -235,7 +238,7 @@ struct XTiles {
 template <int EPI, int BR, int BL>
 __device__ __forceinline__ XTiles xent_tiles(const XArgs &a, int live)
 {
-    const int64_t rrows = (EPI == EPI_DV) ? a.vp : live;
+    const int64_t rrows = (EPI == EPI_DV || EPI == EPI_DV2) ? a.vp : live;
     const int64_t lrows = (EPI == EPI_STATS || EPI == EPI_PROB) ? a.vp : a.D;
     XTiles n{int((rrows + BR - 1) / BR), int((lrows + BL - 1) / BL), 1};
     if (EPI == EPI_DH) {
@@ -261,8 +264,10 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
 {
     using G = XShape<MF, NF, WM, WN>;
     constexpr bool LOGITS = EPI == EPI_STATS || EPI == EPI_PROB;
+    constexpr bool DV = EPI == EPI_DV || EPI == EPI_DV2;
+    constexpr int PARTS = (EPI == EPI_DV2) ? 2 : 1;  // of d, one after the other along k
     constexpr bool LK = LOGITS;              // left operand k contiguous
-    constexpr bool RK = EPI != EPI_DV;       // right operand k contiguous
+    constexpr bool RK = !DV;                 // right operand k contiguous
     static_assert((LK || G::LU == 16) && (RK || G::RU == 16), "256 columns where k is the row");
     constexpr int LSH = (NF == 4) ? 4 : (NF == 2 ? 3 : 2);  // log2(4 NF)
     extern __shared__ __attribute__((aligned(16))) uint4 s_mem4[];
@@ -285,14 +290,14 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
     const int bh = (rt - 8 * band < 8) ? rt - 8 * band : 8;
     const int by = 8 * band + lg % bh, bx = lg / bh;
 
-    // k: steps of 32, an even number; valid up to kmax
-    const int64_t kmax = LOGITS ? a.D : (EPI == EPI_DV ? live : (a.N - a.v0 < a.vp ? a.N - a.v0 : a.vp));
-    const int pairs = int((kmax + 63) / 64);
+    // k: steps of 32, an even number; valid up to kmax (of a part)
+    const int64_t kmax = LOGITS ? a.D : (DV ? live : (a.N - a.v0 < a.vp ? a.N - a.v0 : a.vp));
+    const int part = 2 * int((kmax + 63) / 64), pairs = PARTS * part / 2;
     const int kb = 2 * int(int64_t(pairs) * z / splits), ke = 2 * int(int64_t(pairs) * (z + 1) / splits);
     const int ku = ke - kb;
 
-    const uint16_t *L = LOGITS ? a.V + a.v0 * a.ldv : (EPI == EPI_DV ? a.Hc : a.V + a.v0 * a.ldv);
-    const int64_t ldl = LOGITS ? a.ldv : (EPI == EPI_DV ? a.Dp : a.ldv);
+    const uint16_t *L = LOGITS ? a.V + a.v0 * a.ldv : (DV ? a.Hc : a.V + a.v0 * a.ldv);
+    const int64_t ldl = LOGITS ? a.ldv : (DV ? a.Dp : a.ldv);
     const uint16_t *R = LOGITS ? a.Hc : a.dS;
     const int64_t ldr = LOGITS ? a.Dp : a.dsp;
     // rows (columns, k as row) that exist: those past them are read from the last
@@ -328,19 +333,22 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
     // The padded k of both operands are zero: the right one's are stored (H past D, d
     // past the tokens and words), the left one's are read from the header's zeros.
     // (With values of V in their place, a word of -inf made 0 times -inf, a NaN.)
-    const int64_t lkmax = LOGITS ? a.D : (EPI == EPI_DV ? a.Tp : kmax);
+    const int64_t lkmax = LOGITS ? a.D : (DV ? a.Tp : kmax);
     // elements from one step to the next
     const int64_t rstep = RK ? 32 : 32 * ldr, lstep = LK ? 32 : 32 * ldl;
     // `ends`: the step may reach past lkmax (its last two do)
     auto dma = [&](int u, int slot, bool ends) {
-        const int64_t roff = (kb + u) * rstep, loff = (kb + u) * lstep;
-        const bool past = ends && 32 * int64_t(kb + u) + 32 > lkmax;
+        // the second part of d: the same rows of H, columns of dS further on
+        const bool second = PARTS == 2 && kb + u >= part;
+        const int64_t su = kb + u - (second ? part : 0);
+        const int64_t roff = su * rstep + (second ? a.lo : 0), loff = su * lstep;
+        const bool past = ends && 32 * su + 32 > lkmax;
 #pragma unroll
         for (int r = 0; r < G::PMAX; ++r) {
             if (r >= G::PMIN && !full) continue;
             const int v0 = wave + G::NW * r;
             const uint16_t *p = src[r] + (v0 < G::RU ? roff : loff);
-            if (past && v0 >= G::RU && 32 * int64_t(kb + u) + kof[r] >= lkmax)
+            if (past && v0 >= G::RU && 32 * su + kof[r] >= lkmax)
                 p = reinterpret_cast<const uint16_t *>(a.hdr + ZEROS);
             __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4 *>(p),
                                              reinterpret_cast<uint4 *>(s_mem + slot * G::SLOT + (v0 << 10)), 16, 0, 0);
@@ -482,7 +490,12 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
             if (row < live) a.stat[int64_t(bx) * a.Tp + row] = make_float2(m, s);
         }
     } else if constexpr (EPI == EPI_PROB) {
-        // d = g (exp(z - lse) - onehot) in bf16; 0 for padded tokens and words
+        // d = g (exp(z - lse) - onehot); 0 for padded tokens and words. bf16 results
+        // take it rounded to bf16: at most 2^-9 of each value, which with the rounding
+        // of the results makes the gradients' relative error 2.2e-3 to 2.5e-3 where that
+        // rounding alone makes 1.7e-3, and a second part would double two of the three
+        // products. A dV of 32 bits is asked for to be better than that: it takes what
+        // remains as a second part (2^-18 is lost).
         const int64_t w0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * NF * g;
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
@@ -502,9 +515,22 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
                 }
             u32x4_t *q = reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w0);
 #pragma unroll
-            for (int h = 0; h < NF / 2; ++h)
-                q[h] = u32x4_t{pack_bf16x2(v[8 * h], v[8 * h + 1]), pack_bf16x2(v[8 * h + 2], v[8 * h + 3]),
-                               pack_bf16x2(v[8 * h + 4], v[8 * h + 5]), pack_bf16x2(v[8 * h + 6], v[8 * h + 7])};
+            for (int h = 0; h < NF / 2; ++h) {
+                u32x4_t hi;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) hi[e] = pack_bf16x2(v[8 * h + 2 * e], v[8 * h + 2 * e + 1]);
+                q[h] = hi;
+                if (a.lo == 0) continue;
+                u32x4_t lo;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = v[8 * h + 2 * e] - __uint_as_float(hi[e] << 16);
+                    const float y = v[8 * h + 2 * e + 1] - __uint_as_float(hi[e] & 0xffff0000u);
+                    // (nothing remains of what is no number)
+                    lo[e] = pack_bf16x2(x - x == 0.0f ? x : 0.0f, y - y == 0.0f ? y : 0.0f);
+                }
+                *reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w0 + a.lo + 8 * h) = lo;
+            }
         }
     } else if constexpr (EPI == EPI_DH) {
         // fp32 sums over the pieces, each split its own
@@ -642,7 +668,7 @@ __global__ __launch_bounds__(XT) void xent_dh_kernel(const XArgs a)
 constexpr int64_t PIECE_BYTES = int64_t(256) << 20;  // of d
 
 struct XLayout {
-    int64_t Tp, Dp, tiles, vp;
+    int64_t Tp, Dp, tiles, vp, dsp;
     int hsplit;
     size_t rows, pos, tgt, lse, g, ztgt, hc, stat, ds, dhp, total;
 };
@@ -675,7 +701,10 @@ XLayout xent_layout(bool grad, int64_t T, int64_t N, int64_t D)
         const int64_t rt = l.Tp / 256, round = 256 / std::gcd<int64_t>(256, rt);
         if (most >= round) most = most / round * round;
         l.vp = std::min(most, l.tiles) * VBLK;
-        l.ds = take(size_t(l.Tp) * size_t(l.vp) * 2);
+        // room for two parts of d: of the whole vocabulary where that fits a piece's
+        // space, of one tile of words at least
+        l.dsp = std::max<int64_t>({l.vp, 2 * VBLK, std::min<int64_t>(2 * l.vp, most * VBLK)});
+        l.ds = take(size_t(l.Tp) * size_t(l.dsp) * 2);
         // splits of dH's depth: until its launch fills the compute units
         const int64_t blocks = (l.Tp / 256) * ((D + 255) / 256);
         l.hsplit = int(std::clamp<int64_t>(256 / blocks, 1, std::max<int64_t>(1, std::min<int64_t>(l.vp / 512, 32))));
@@ -798,7 +827,7 @@ hipError_t launch_xent_grad(const XentCall &c, hipStream_t st)
     a.lse = reinterpret_cast<float *>(ws + l.lse);
     a.g = reinterpret_cast<float *>(ws + l.g);
     a.dS = reinterpret_cast<uint16_t *>(ws + l.ds);
-    a.dsp = l.vp;
+    a.dsp = l.dsp;
     a.dHp = reinterpret_cast<float *>(ws + l.dhp);
     a.hsplit = l.hsplit;
     a.dH = static_cast<uint16_t *>(c.dH);
@@ -810,14 +839,19 @@ hipError_t launch_xent_grad(const XentCall &c, hipStream_t st)
     const int64_t vb = a.dv_bf16 ? 8 : 16;
     a.dv_vec = (reinterpret_cast<uintptr_t>(c.dV) | uintptr_t(vb / 4 * c.lddv)) % vb == 0;
     a.accumulate = c.accumulate;
+    // two parts of d for a dV of 32 bits: half the words a piece, in the same space
+    const bool two = c.dV && !a.dv_bf16;
+    const int64_t vp = two ? l.dsp / 2 / VBLK * VBLK : l.vp;
+    a.lo = two ? vp : 0;
     hipError_t e = launch_rows(a, a.Tp, st);
-    for (int64_t v0 = 0; e == hipSuccess && v0 < c.N; v0 += l.vp) {
+    for (int64_t v0 = 0; e == hipSuccess && v0 < c.N; v0 += vp) {
         a.v0 = v0;
-        a.vp = std::min(l.vp, (c.N - v0 + VBLK - 1) / VBLK * VBLK);
+        a.vp = std::min(vp, (c.N - v0 + VBLK - 1) / VBLK * VBLK);
         a.first = v0 == 0;
         if ((e = launch_tokens<EPI_PROB>(a, a.vp, 1, st)) != hipSuccess) break;
         if ((e = launch_tokens<EPI_DH>(a, c.D, l.hsplit, st)) != hipSuccess) break;
-        if (c.dV) e = launch_gemm_shape<EPI_DV, 8, 4, 2, 4>(a, a.vp, c.D, 1, st);
+        if (two) e = launch_gemm_shape<EPI_DV2, 8, 4, 2, 4>(a, a.vp, c.D, 1, st);
+        else if (c.dV) e = launch_gemm_shape<EPI_DV, 8, 4, 2, 4>(a, a.vp, c.D, 1, st);
     }
     if (e != hipSuccess || c.T == 0) return e;
     hipLaunchKernelGGL(xent_dh_kernel, dim3(unsigned(c.T)), dim3(XT), 0, st, a);

@@ -1,10 +1,11 @@
-"""Cross entropy with words of -inf (masked out of the vocabulary) at any depth."""
+"""Cross entropy with words of -inf (masked out of the vocabulary) at any depth, and
+head gradients in 32 bits."""
 import pytest
 import torch
 
 import paper_2607_08643_amd as bsq
 from parity_bounds import say
-from test_gpu_xent import _check_grad, _check_loss, _inputs, _weights
+from test_gpu_xent import U32, _check_grad, _check_loss, _exact, _inputs, _weights, gamma
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +36,34 @@ def test_words_of_minus_infinity(T, D, gpu):
     assert (dV[300:600] == 0).all()
     dH[:, 0] = 0
     _check_grad(H, W, word, lse, g, dH, dV[keep])
+
+
+@pytest.mark.parametrize("T,N,D,ignore", [(1, 5000, 256, 0.0), (33, 200, 64, 0.5), (65, 777, 136, 0.0), (300, 3001, 200, 0.4),
+                                          (1030, 1500, 96, 0.0), (4000, 40003, 64, 0.1)])
+def test_head_gradients_in_32_bits(T, N, D, ignore, gpu):
+    """d enters a 32-bit dV as two bf16 parts: the first leaves at most 2^-9 of a
+    value, the second at most 2^-9 of that. Bar: 2^-17 of every |d|, d's own error
+    as in the other tests, the product's gamma over both parts, the result's
+    rounding."""
+    say(f"xent dV fp32 T={T} N={N} D={D}")
+    H, V, target = _inputs(gpu, T, N, D, ignore, seed=12)
+    g = _weights(T, 5, gpu)
+    _, lse = bsq.bsq_xent_loss(H, V, target)
+    live, h, v, z, dz, _ = _exact(H, V, target)
+    gl = g[live].double()[:, None]
+    p = (z - lse[live].double()[:, None]).exp()
+    d = p.clone()
+    d[torch.arange(len(d), device=d.device), target[live]] -= 1
+    d, ed = gl * d, gl.abs() * (p * (dz.expm1() + 2.0 ** -18) + U32 * d.abs())
+    want = d.T @ h
+    bar = (ed + (2.0 ** -17 + gamma(2 * len(d))) * d.abs()).T @ h.abs() + 1e-30
+    for before in (None, torch.randn((N, D), generator=torch.Generator().manual_seed(3)).to(gpu)):
+        dV = torch.full((N, D), 3.0, device=gpu) if before is None else before.clone()
+        dH, _ = bsq.bsq_xent_grad(H, V, target, lse, g, dV=dV, accumulate=before is not None)
+        torch.cuda.synchronize()
+        ref = want if before is None else want + before.double()
+        err = (dV.double() - ref).abs()
+        tol = bar + 2 * U32 * ref.abs()
+        say(f"  dV: worst err/tol {float((err / tol).max()):.3f}")
+        assert (err <= tol).all()
+        _check_grad(H, V, target, lse, g, dH, None)
