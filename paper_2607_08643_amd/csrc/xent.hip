@@ -806,11 +806,20 @@ hipError_t launch_xent_loss(const XentCall &c, hipStream_t st)
     a.stat = reinterpret_cast<float2 *>(static_cast<char *>(c.ws) + l.stat);
     a.loss_out = c.loss;
     a.lse_out = c.lse;
-    a.v0 = 0;
-    a.vp = l.tiles * VBLK;
     hipError_t e = launch_rows(a, c.T <= 16 ? 16 : (c.T <= 32 ? 32 : a.Tp), st);
     if (e != hipSuccess) return e;
-    if ((e = launch_tokens<EPI_STATS>(a, a.vp, 1, st)) != hipSuccess) return e;
+    // A launch holds fewer than 2^32 work items, 512 or fewer of a tile: the tiles
+    // of larger vocabularies go over several.
+    const int64_t rt = c.T <= 128 ? 1 : (c.T <= HALF_TOKENS ? (c.T + 127) / 128 : (c.T + 255) / 256);
+    const int64_t most = ((int64_t(1) << 32) - 1) / (512 * rt);
+    float2 *const stat = a.stat;
+    for (int64_t t0 = 0; t0 < l.tiles; t0 += most) {
+        a.v0 = t0 * VBLK;
+        a.vp = std::min(most, l.tiles - t0) * VBLK;
+        a.stat = stat + t0 * a.Tp;
+        if ((e = launch_tokens<EPI_STATS>(a, a.vp, 1, st)) != hipSuccess) return e;
+    }
+    a.stat = stat;
     // few tokens: a block each; else eight, whose pairs lie next to each other
     if (c.T < 512) hipLaunchKernelGGL((xent_join_kernel<1>), dim3(unsigned(c.T)), dim3(XT), 0, st, a, int(l.tiles));
     else hipLaunchKernelGGL((xent_join_kernel<8>), dim3(unsigned((c.T + 7) / 8)), dim3(XT), 0, st, a, int(l.tiles));

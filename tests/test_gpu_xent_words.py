@@ -1,5 +1,7 @@
-"""Cross entropy with words of -inf (masked out of the vocabulary) at any depth, and
-head gradients in 32 bits."""
+"""Cross entropy with words of -inf (masked out of the vocabulary) at any depth,
+head gradients in 32 bits, and vocabularies past what one launch holds."""
+import math
+
 import pytest
 import torch
 
@@ -67,3 +69,28 @@ def test_head_gradients_in_32_bits(T, N, D, ignore, gpu):
         say(f"  dV: worst err/tol {float((err / tol).max()):.3f}")
         assert (err <= tol).all()
         _check_grad(H, V, target, lse, g, dH, None)
+
+
+def test_a_vocabulary_of_more_tiles_than_a_launch_holds(gpu):
+    """2^23 + 8 tiles of 512 threads are 2^32 work items and more. Logits are 0 but for
+    four words, so lse is known: log(N - 4 + sum exp z), off by the additions of a
+    token's 2^20 tiles (each of 32 threads 2^15 of them, one rounding each: 2^-9)."""
+    T, N, D = 1024, (1 << 28) + 5, 8
+    say(f"xent loss T={T} N={N} D={D}")
+    words = [5, N // 2, N - 300, N - 1]
+    value = [19.0, 18.5, 20.0, 18.0]
+    V = torch.zeros((N, D), dtype=torch.bfloat16, device=gpu)
+    for w, x in zip(words, value):
+        V[w, 3] = x
+    H = torch.zeros((T, D), dtype=torch.bfloat16, device=gpu)
+    H[:, 3] = 1.0
+    H[1::2, 3] = 0.5
+    target = torch.tensor([words[i % 4] if i % 8 < 6 else 1000 + i for i in range(T)], device=gpu)
+    loss, lse = bsq.bsq_xent_loss(H, V, target)
+    torch.cuda.synchronize()
+    for i in range(T):
+        s = 0.5 if i % 2 else 1.0
+        want = math.log(N - 4 + sum(math.exp(s * x) for x in value))
+        z = s * value[i % 4] if i % 8 < 6 else 0.0
+        assert abs(float(lse[i]) - want) <= 2.0 ** -9 + 2.0 ** -18, i
+        assert abs(float(loss[i]) - (want - z)) <= 2.0 ** -9 + 2.0 ** -18, i
