@@ -708,8 +708,10 @@ bsq_status bsq_clip_prepare(bsq_clip_plan *plan, size_t table_bytes, const void 
                             const int64_t *sizes, const int32_t *dtypes, void *stream);
 
 /* stats (device fp32 [2]): norm and coef. A norm that is not finite gives coef
- * = 1 and ORs BSQ_DEVERR_NONFINITE into *err (device int32 or NULL). Calls that
- * share a plan must not overlap. */
+ * = 1, so that the gradients are left as they are for the caller to skip, and ORs
+ * BSQ_DEVERR_NONFINITE into *err (device int32 or NULL). One that is finite but
+ * past the range of fp32 is infinite in stats and has the coef of its fp64 value.
+ * Calls that share a plan must not overlap. */
 bsq_status bsq_grad_norm(const bsq_clip_plan *plan, float max_norm, float *stats, int32_t *err, void *stream);
 
 /* bsq_grad_norm, then out = coef g for every tensor (in place nothing is

@@ -137,15 +137,15 @@ __device__ __forceinline__ double clip_total(const ClipArgs &a, double *s)
     return __builtin_sqrt(block_sum(v, s));
 }
 
-// norm and coef; a norm that is not finite clips nothing and is reported
+// norm and coef; a norm that is not finite clips nothing and is reported. Both
+// are judged in fp64: a norm past the range of fp32 is finite, and clips.
 __device__ __forceinline__ float clip_stats(const ClipArgs &a, double norm, bool write)
 {
-    const float nf = float(norm);
-    const bool fine = nf - nf == 0.0f;
+    const bool fine = norm - norm == 0.0;
     const double q = double(a.max_norm) / (norm + 1e-6);
     const float coef = (fine && q < 1.0) ? float(q) : 1.0f;
     if (write && threadIdx.x == 0) {
-        a.stats[0] = nf;
+        a.stats[0] = float(norm);
         a.stats[1] = coef;
         if (!fine && a.err) atomicOr(a.err, BSQ_DEVERR_NONFINITE);
     }
