@@ -1016,9 +1016,13 @@ class bsq_clip_plan(ct.Structure):
 
 
 class GradPlan:
-    """The gradients of a training program (fp32 or bf16 tensors, contiguous),
-    prepared once for bsq_grad_norm and bsq_grad_clip; outs: where the clipped
-    ones go (None: in place). Holds the tensors."""
+    """The gradients of a training program (fp32 or bf16 tensors, contiguous, none
+    overlapping another), prepared once for bsq_grad_norm and bsq_grad_clip; outs:
+    where the clipped ones go (None: in place). The plan is of the memory that the
+    tensors have now, and keeps it: gradients have to stay there from step to step,
+    zeroed in place (zero_grad(set_to_none=False)). One that becomes another tensor,
+    as zero_grad() makes of it by default, needs a new plan; this one would go on
+    with the old values."""
 
     def __init__(self, tensors, outs=None, stream=None):
         tensors = list(tensors)
@@ -1039,6 +1043,8 @@ class GradPlan:
         need = ct.c_size_t(0)
         _check(lib().bsq_clip_table_bytes(count, sizes, ct.byref(need)), "bsq_clip_table_bytes")
         self.tensors, self.outs, self.device = tensors, outs, dev
+        # (a tensor object may be given other memory; the table's pointers stay good)
+        self._memory = [t.untyped_storage() for t in tensors + (outs or [])]
         with _Launch(dev, stream) as st:
             self.table = _workspace(need.value, dev)
             self._c = bsq_clip_plan(self.table.data_ptr(), count, 0)
