@@ -565,7 +565,9 @@ bsq_status bsq_train_adam(const bsq_config *cfg, const bsq_train_hparams *hp, in
  *   dA_a = sum_m u[m] x[m]^T,  dB_a = s_a sum_m dy[m] t[m]^T
  * over the tokens with a = ids[m]. Sums are fp32 in a fixed order; t and u
  * enter their second product as bf16 parts that add up to them, two for bf16
- * results (2^-16 of a value is lost), three for fp32 ones (2^-24).
+ * results (2^-16 of a value is lost), three for fp32 ones (2^-24). An entry of A, B,
+ * x or dy that is not finite can make the results of its adapter and token
+ * infinite or NaN, and no others.
  * ------------------------------------------------------------------------ */
 #define BSQ_MAX_ADAPTERS 1024
 #define BSQ_ADAPTERS_DIRECT 256

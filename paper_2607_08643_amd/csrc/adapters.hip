@@ -21,7 +21,9 @@
 // t and u are held in fp32 and enter the next product as bf16 parts: the value
 // rounded, then what remains, rounded. For bf16 results two parts (2^-16 of the
 // value is lost, and a rank block of 16 with its two parts fills one 32-deep
-// product), for fp32 results three (2^-24).
+// product), for fp32 results three (2^-24). (An infinite entry of A or B meets all
+// parts, some of them 0 or of the other sign: its results may be NaN where the
+// formula's are infinite.)
 #include <algorithm>
 #include <type_traits>
 
@@ -50,6 +52,10 @@ constexpr int PLAN_HDR = 16;
 PlanLayout plan_layout(int64_t M, int64_t n)
 {
     PlanLayout l{};
+    // Tokens of a tile: 16 leave fewer idle where adapters have few tokens each, 64
+    // read an adapter's weights less often (q, k and v of 4096 inputs at rank 16, mixed
+    // tokens of 64 adapters, apply: 768 tokens 27 us with 16, 30 with 64; 4096 tokens 63
+    // and 53; between 1024 and 2048, and with few adapters, both are within 7%)
     l.tile = (M <= 1024) ? 16 : 64;
     l.piece = std::max<int64_t>(256, (M / 16 + 63) / 64 * 64);
     l.max_tiles = std::min(M, M / l.tile + n + 1);
@@ -107,7 +113,7 @@ __device__ __forceinline__ void block_scan4(int (&v)[4], int (&all)[4], int wave
 // goes over its run again to place its tokens. No atomics: the order, and with
 // it every sum over tokens, is fixed. One compute unit issues all of it (about
 // 1 us per 1024 tokens beside 4.5 us), so what the ballots find waits in LDS and
-// up to 8192 tokens the second time is a lookup (8192 tokens of 4 adapters 12.2 us,
+// up to 8192 tokens the second time is a lookup (8192 tokens of 4 adapters 12.0 us,
 // found again 13.5).
 __global__ __launch_bounds__(64 * PLAN_WAVES) void adapters_plan_kernel(const PlanArgs a)
 {
@@ -430,7 +436,7 @@ __device__ __forceinline__ bool tile_view(const AdArgs &a, bool with_none, int (
 // with 16) and two waves along d_in. Loads are a step ahead of their products.
 // Bound by reading x, whose 64-byte pieces of many rows come at 2.0 to 2.2 TB/s
 // (2000 tokens of 25600 inputs at rank 64: 52 us; 8192 of 4096 for three projections
-// of rank 16: 31 us).
+// of rank 16: 32 us).
 // ---------------------------------------------------------------------------
 template <int VB, bool EVEN, int TG, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_shrink(const AdArgs a)
@@ -652,13 +658,13 @@ __device__ __forceinline__ void store_row(void *p, int64_t nc, const float (&v)[
 // (64-token tiles) over all of them, or every fourth 64 columns of all 16. t is
 // summed once; then per 64 columns the wave has y0 and B of the next ones in
 // flight. Bound by reading y0 and writing y (8192 tokens of 6144 columns at rank
-// 16: 54 us, 3.7 TB/s of both). Reading ahead past a block's last columns, to
+// 16: 55 us, 3.7 TB/s of both). Reading ahead past a block's last columns, to
 // spare the condition, made it 4 us slower.
 // ---------------------------------------------------------------------------
 template <int RB, bool EVEN, int TG, bool F32, bool DIRECT>
 __global__ __launch_bounds__(AT) void adapters_expand(const AdArgs a)
 {
-    constexpr int PF = (RB == 1 && !DIRECT) ? 2 : 1;  // 64-column groups in flight (DIRECT: 17 us for 64 tokens, with two 20)
+    constexpr int PF = (RB == 1 && !DIRECT) ? 2 : 1;  // 64-column groups in flight (DIRECT: 14 us for 64 tokens, with two 18)
     __shared__ int s_tok[4][16];
     TileView tv;
     if (!tile_view<DIRECT, TG>(a, true, s_tok, tv)) return;
@@ -791,7 +797,7 @@ __device__ __forceinline__ frag_t read_tr(const uint8_t *p, int four)
 // groups][rank][64 bytes], the groups swapped in ranks 8 to 15: the rows that
 // half a wave reads together fall on all banks once) and read transposed. The
 // columns are permuted on the way in (run_column). Bound by reading dx0 and
-// writing dx (8192 tokens of 4096 columns, three projections of rank 16: 43 us, 3.1
+// writing dx (8192 tokens of 4096 columns, three projections of rank 16: 42 us, 3.2
 // TB/s of both).
 // ---------------------------------------------------------------------------
 constexpr int DX_COLS = 128;
@@ -1285,7 +1291,10 @@ struct AdLayout {
     int64_t slot_floats;
 };
 
-// Rank blocks that a launch over x takes at once, of nv.
+// Rank blocks that a launch over x takes at once, of nv: threes or fours. Two,
+// three and four at once are within 9% of each other in the forward calls of 2000
+// tokens of 4096 inputs (six blocks 39, 42, 40 us; twelve 76, 70, 70). In dA fewer are
+// faster: the gradients of eight blocks take 90, 86 and 100 us, of six 73, 79 and 85.
 int blocks_at_once(int nv) { return nv <= 4 ? nv : (nv % 3 == 0 ? 3 : 4); }
 
 // Splits of d_in: until the launch has about 1024 blocks, each wave with a turn
