@@ -685,6 +685,74 @@ bsq_status bsq_xent_grad(const void *H, int64_t ldh, const void *V, int64_t ldv,
                          size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * A teacher's top logits: of every row of logits z_t over a vocabulary the K
+ * largest with their words, and lse_t = log sum_v exp(scale z_tv) over all of it.
+ * ------------------------------------------------------------------------ */
+#define BSQ_MAX_TOP 256
+
+/* Device workspace of bsq_top_logits (at most 64 MiB and a little; host only). */
+bsq_status bsq_top_workspace_bytes(int64_t T, int64_t N, size_t *bytes);
+
+/*   Z       device [T][ldz] of z_dtype (bf16 or fp32), ldz >= N, any alignment of the elements
+ *   K       1 .. BSQ_MAX_TOP
+ *   scale   > 0, finite (one over a temperature)
+ *   ids     device int32 [T][K]: words by falling logit, equal ones by rising
+ *           word. Words of -inf (masked) or NaN are not listed: where fewer than
+ *           K are left, the last entries are -1
+ *   top     device fp32 [T][K]: their logits as they are (-inf for id -1)
+ *   lse     device fp32 [T], or NULL (NaN for a row that holds one; -inf for one of -inf)
+ *   ws      device workspace, 256-byte aligned, any contents
+ * 0 <= T <= 2^20, 1 <= N < 2^31. */
+bsq_status bsq_top_logits(const void *Z, int32_t z_dtype, int64_t ldz, int64_t T, int64_t N, int32_t K, float scale,
+                          int32_t *ids, float *top, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Verification of drafted tokens (a compressed model drafts for the model that it
+ * was made from). Sequence b has n_b drafted tokens x_0 .. and one row of target
+ * logits for each and one for the token after them; p_i and q_i are the softmax
+ * of its target and draft logits over its temperature:
+ *   x_i is accepted if it and all before it have u_i q_i(x_i) < p_i(x_i);
+ *   the next token is drawn from max(p_i - q_i, 0), where x_i was the first not
+ *   accepted, from p_n where all were: the first word whose cumulative sum
+ *   exceeds r times the whole sum.
+ * Without draft logits the drafts are certain (found in the text): q_i is 1 at
+ * x_i and 0 elsewhere. At temperature 0 x_i is accepted if it is the word of the
+ * largest target logit (of equal ones the lowest), and the next token is that word;
+ * u, r and the draft logits are not used. Probabilities and sums are 64-bit.
+ * Words of -inf have probability 0. Where nothing is left of max(p_i - q_i, 0) the
+ * draw is from p_i. A target row without a probability (a NaN or +inf in it, or
+ * nothing but -inf) accepts nothing and its next token is -1; a draft row like
+ * that is not accepted either, and the draw is from p_i: both OR
+ * BSQ_DEVERR_NONFINITE into *err. Rows past the one that the next token is
+ * drawn from may hold anything.
+ * ------------------------------------------------------------------------ */
+#define BSQ_MAX_DRAFTS 64
+
+/* Device workspace of bsq_draft_verify; draft: 1 with draft logits, else 0 (host only). */
+bsq_status bsq_draft_workspace_bytes(int32_t draft, int64_t B, int64_t L, int64_t N, size_t *bytes);
+
+/*   P       device [B][L + 1][N] of p_dtype: row i of sequence b at b p_seq + i p_row
+ *           elements (strides of 0 or more); rows may lie at any alignment of the elements
+ *   Q       device [B][L][N] of q_dtype, likewise, or NULL
+ *   tokens  device int32 [B][L]; one outside the vocabulary is not accepted and ORs
+ *           BSQ_DEVERR_BAD_SET into *err
+ *   lens    device int32 [B], n_b of each (0 .. L; others are clamped and OR
+ *           BSQ_DEVERR_BAD_SET), or NULL for L. Tokens, u and rows past it may hold anything
+ *   u, r    device fp32 [B][L] and [B], in [0, 1)
+ *   temperature  device fp32 [B], or NULL for ones; negative or not finite counts as
+ *           0 and ORs BSQ_DEVERR_BAD_SET
+ *   count   device int32 [B]: accepted tokens
+ *   out     device int32 [B][L + 1]: the accepted tokens, the next one, then -1
+ *   err     device int32 or NULL
+ *   ws      device workspace, 256-byte aligned, any contents
+ * 0 <= B <= 65536, 0 <= L <= BSQ_MAX_DRAFTS, 1 <= N < 2^31. With L = 0 this draws
+ * one token of every sequence. */
+bsq_status bsq_draft_verify(const void *P, int32_t p_dtype, int64_t p_seq, int64_t p_row, const void *Q, int32_t q_dtype,
+                            int64_t q_seq, int64_t q_row, int64_t B, int64_t L, int64_t N, const int32_t *tokens,
+                            const int32_t *lens, const float *u, const float *r, const float *temperature,
+                            int32_t *count, int32_t *out, int32_t *err, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * The global norm of many gradient tensors, and their clipping:
  *   norm = sqrt(sum g^2),  coef = min(1, max_norm / (norm + 1e-6)),  out = coef g
  * with the squares summed in fp64 in a fixed order.

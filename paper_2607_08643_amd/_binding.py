@@ -25,6 +25,8 @@ MAX_LORA_RANK = 16
 MAX_GROUP = 8
 MAX_ADAPTERS = 1024
 MAX_ADAPTER_RANK = 128
+MAX_TOP = 256
+MAX_DRAFTS = 64
 GEMV_NOALLOC_SCRATCH_BYTES = 8 << 20
 
 BSQ_OK, BSQ_ERR_ARG, BSQ_ERR_SHAPE, BSQ_ERR_DTYPE, BSQ_ERR_ALIGN = 0, 1, 2, 3, 4
@@ -84,7 +86,8 @@ EXPORTS = ("bsq_version", "bsq_status_str", "bsq_config_check", "bsq_layer_sizes
            "bsq_train_workspace_bytes", "bsq_train_grad", "bsq_train_adam", "bsq_adapters_plan_bytes",
            "bsq_adapters_plan", "bsq_adapters_workspace_bytes", "bsq_adapters_apply", "bsq_adapters_grad",
            "bsq_xent_workspace_bytes", "bsq_xent_loss", "bsq_xent_grad", "bsq_clip_table_bytes", "bsq_clip_prepare",
-           "bsq_grad_norm", "bsq_grad_clip")
+           "bsq_grad_norm", "bsq_grad_clip", "bsq_top_workspace_bytes", "bsq_top_logits",
+           "bsq_draft_workspace_bytes", "bsq_draft_verify")
 
 # struct layouts above follow this version of include/bsq.h
 ABI_VERSION = 8
@@ -137,6 +140,10 @@ def lib():
     L.bsq_clip_prepare.argtypes = [P, SZ, P, P, P, P, P]
     L.bsq_grad_norm.argtypes = [P, ct.c_float, P, P, P]
     L.bsq_grad_clip.argtypes = [P, ct.c_float, P, P, P]
+    L.bsq_top_workspace_bytes.argtypes = [I64, I64, ct.POINTER(SZ)]
+    L.bsq_top_logits.argtypes = [P, I32, I64, I64, I64, I32, ct.c_float, P, P, P, P, SZ, P]
+    L.bsq_draft_workspace_bytes.argtypes = [I32, I64, I64, I64, ct.POINTER(SZ)]
+    L.bsq_draft_verify.argtypes = [P, I32, I64, I64, P, I32, I64, I64, I64, I64, I64, P, P, P, P, P, P, P, P, P, SZ, P]
     for f in EXPORTS[2:]:
         getattr(L, f).restype = I32
     if L.bsq_version() != ABI_VERSION:
@@ -1008,6 +1015,90 @@ def bsq_xent_grad(H: torch.Tensor, V: torch.Tensor, target: torch.Tensor, lse: t
                                    _ptr(dV), lddv, BSQ_BF16 if dV is None else _dtype_code(dV.dtype), int(accumulate),
                                    _ptr(err), _ptr(ws), ws.numel(), st), "bsq_xent_grad")
     return dH, dV
+
+
+# ---------------------------------------------------------------- top logits
+@functools.lru_cache(maxsize=1024)
+def bsq_top_workspace_bytes(T: int, N: int) -> int:
+    out = ct.c_size_t(0)
+    _check(lib().bsq_top_workspace_bytes(T, N, ct.byref(out)), "bsq_top_workspace_bytes")
+    return out.value
+
+
+def bsq_top_logits(Z: torch.Tensor, K: int, scale: float = 1.0, ids=None, top=None, lse=None, want_lse: bool = True,
+                   ws: torch.Tensor | None = None, stream=None):
+    """The K (1..256) largest logits of every row of Z [T, N] (bf16 or fp32):
+    (ids int32 [T, K], top fp32 [T, K], lse fp32 [T]), by falling logit, equal ones
+    by rising word; -1 and -inf past the words that are not -inf or NaN. lse: log
+    sum exp(scale z) over the whole row (None where want_lse is False)."""
+    T, N = Z.shape
+    zt = _dtype_code(Z.dtype)
+    ldz = _matrix(Z, Z.dtype, (T, N), "Z")
+    dev = _device_of((Z, ids, top, lse, ws), "bsq_top_logits")
+    need = bsq_top_workspace_bytes(T, N)
+    with _Launch(dev, stream) as st:
+        ids = torch.empty((T, K), dtype=torch.int32, device=dev) if ids is None else _need(ids, torch.int32, (T, K), "ids")
+        top = torch.empty((T, K), dtype=torch.float32, device=dev) if top is None else _need(top, torch.float32, (T, K), "top")
+        if not want_lse:
+            lse = None
+        elif lse is None:
+            lse = torch.empty(T, dtype=torch.float32, device=dev)
+        else:
+            _need(lse, torch.float32, (T,), "lse")
+        ws = ws if ws is not None else _workspace(need, dev)
+        _check(lib().bsq_top_logits(_ptr(Z), zt, ldz, T, N, K, scale, _ptr(ids), _ptr(top), _ptr(lse), _ptr(ws),
+                                    ws.numel(), st), "bsq_top_logits")
+    return ids, top, lse
+
+
+# ---------------------------------------------------------------- verification of drafted tokens
+@functools.lru_cache(maxsize=1024)
+def bsq_draft_workspace_bytes(draft: bool, B: int, L: int, N: int) -> int:
+    out = ct.c_size_t(0)
+    _check(lib().bsq_draft_workspace_bytes(int(draft), B, L, N, ct.byref(out)), "bsq_draft_workspace_bytes")
+    return out.value
+
+
+def _logit_rows(t, shape, what):
+    """Logits [B, rows, N] whose rows are contiguous: type, strides of sequences and rows."""
+    code = _dtype_code(t.dtype)
+    if t.shape != shape:
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    if shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{what}: rows must be contiguous")
+    return code, t.stride(0), t.stride(1)
+
+
+def bsq_draft_verify(target: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, r: torch.Tensor, draft=None, lens=None,
+                     temperature=None, count=None, out=None, err=None, ws: torch.Tensor | None = None, stream=None):
+    """Verify drafted tokens int32 [B, L] against the target's logits [B, L + 1, N]
+    (bf16 or fp32) with the random numbers u [B, L] and r [B] (fp32, in [0, 1)):
+    (count int32 [B], out int32 [B, L + 1]: the accepted tokens, the next one, -1).
+    draft: the logits [B, L, N] that the tokens were drawn from (None: certain
+    drafts); lens: int32 [B], drafted tokens of each sequence (None: L);
+    temperature: fp32 [B] (None: ones; 0: greedy). L = 0 draws one token each."""
+    B, L = tokens.shape
+    N = target.shape[-1]
+    pt, pseq, prow = _logit_rows(target, (B, L + 1, N), "target")
+    qt, qseq, qrow = (0, 0, 0) if draft is None else _logit_rows(draft, (B, L, N), "draft")
+    _need(tokens, torch.int32, (B, L), "tokens")
+    _need(u, torch.float32, (B, L), "u")
+    _need(r, torch.float32, (B,), "r")
+    if lens is not None:
+        _need(lens, torch.int32, (B,), "lens")
+    if temperature is not None:
+        _need(temperature, torch.float32, (B,), "temperature")
+    dev = _device_of((target, tokens, u, r, draft, lens, temperature, count, out, err, ws), "bsq_draft_verify")
+    need = bsq_draft_workspace_bytes(draft is not None, B, L, N)
+    with _Launch(dev, stream) as st:
+        count = torch.empty(B, dtype=torch.int32, device=dev) if count is None else _need(count, torch.int32, (B,), "count")
+        out = torch.empty((B, L + 1), dtype=torch.int32, device=dev) if out is None else _need(
+            out, torch.int32, (B, L + 1), "out")
+        ws = ws if ws is not None else _workspace(need, dev)
+        _check(lib().bsq_draft_verify(_ptr(target), pt, pseq, prow, _ptr(draft), qt, qseq, qrow, B, L, N, _ptr(tokens),
+                                      _ptr(lens), _ptr(u), _ptr(r), _ptr(temperature), _ptr(count), _ptr(out), _ptr(err),
+                                      _ptr(ws), ws.numel(), st), "bsq_draft_verify")
+    return count, out
 
 
 # ---------------------------------------------------------------- gradient norm and clipping

@@ -875,6 +875,121 @@ bsq_status bsq_xent_grad(const void *H, int64_t ldh, const void *V, int64_t ldv,
 }
 
 // ---------------------------------------------------------------------------
+// Top logits.
+// ---------------------------------------------------------------------------
+namespace {
+bsq_status check_top_dims(int64_t T, int64_t N)
+{
+    if (T < 0 || N < 1) return BSQ_ERR_SHAPE;
+    if (T > (int64_t(1) << 20) || N >= (int64_t(1) << 31)) return BSQ_ERR_UNSUPPORTED;
+    return BSQ_OK;
+}
+
+// positive and finite
+bool good_scale(float s) { return s > 0.0f && std::isfinite(s); }
+}  // namespace
+
+bsq_status bsq_top_workspace_bytes(int64_t T, int64_t N, size_t *bytes)
+{
+    if (!bytes) return BSQ_ERR_ARG;
+    const bsq_status s = check_top_dims(T, N);
+    if (s != BSQ_OK) return s;
+    *bytes = top_ws_bytes(T, N);
+    return BSQ_OK;
+}
+
+bsq_status bsq_top_logits(const void *Z, int32_t z_dtype, int64_t ldz, int64_t T, int64_t N, int32_t K, float scale,
+                          int32_t *ids, float *top, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    if (z_dtype != BSQ_F32 && z_dtype != BSQ_BF16) return BSQ_ERR_DTYPE;
+    const bsq_status s = check_top_dims(T, N);
+    if (s != BSQ_OK) return s;
+    if (K < 1 || K > BSQ_MAX_TOP || !good_scale(scale)) return BSQ_ERR_ARG;
+    if (!ws || (T > 0 && (!Z || !ids || !top))) return BSQ_ERR_ARG;
+    if (ldz < N) return BSQ_ERR_SHAPE;
+    if (!aligned(Z, z_dtype == BSQ_F32 ? 4 : 2) || !aligned(ids, 4) || !aligned(top, 4) || !aligned(lse, 4) ||
+        !aligned(ws, 256))
+        return BSQ_ERR_ALIGN;
+    if (ws_bytes < top_ws_bytes(T, N)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    if (T == 0) return BSQ_OK;
+    TopCall c{};
+    c.Z = Z;
+    c.z_dtype = z_dtype;
+    c.ldz = ldz;
+    c.T = T;
+    c.N = N;
+    c.K = K;
+    c.scale = scale;
+    c.ids = ids;
+    c.top = top;
+    c.lse = lse;
+    c.ws = ws;
+    return from_hip(launch_top_logits(c, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// Verification of drafted tokens.
+// ---------------------------------------------------------------------------
+namespace {
+bsq_status check_draft_dims(int64_t B, int64_t L, int64_t N)
+{
+    if (B < 0 || L < 0 || N < 1) return BSQ_ERR_SHAPE;
+    if (B > 65536 || L > BSQ_MAX_DRAFTS || N >= (int64_t(1) << 31)) return BSQ_ERR_UNSUPPORTED;
+    return BSQ_OK;
+}
+}  // namespace
+
+bsq_status bsq_draft_workspace_bytes(int32_t draft, int64_t B, int64_t L, int64_t N, size_t *bytes)
+{
+    if (!bytes || (draft != 0 && draft != 1)) return BSQ_ERR_ARG;
+    const bsq_status s = check_draft_dims(B, L, N);
+    if (s != BSQ_OK) return s;
+    *bytes = draft_ws_bytes(B, L, N, draft != 0);
+    return BSQ_OK;
+}
+
+bsq_status bsq_draft_verify(const void *P, int32_t p_dtype, int64_t p_seq, int64_t p_row, const void *Q, int32_t q_dtype,
+                            int64_t q_seq, int64_t q_row, int64_t B, int64_t L, int64_t N, const int32_t *tokens,
+                            const int32_t *lens, const float *u, const float *r, const float *temperature,
+                            int32_t *count, int32_t *out, int32_t *err, void *ws, size_t ws_bytes, void *stream)
+{
+    if (p_dtype != BSQ_F32 && p_dtype != BSQ_BF16) return BSQ_ERR_DTYPE;
+    if (Q && q_dtype != BSQ_F32 && q_dtype != BSQ_BF16) return BSQ_ERR_DTYPE;
+    const bsq_status s = check_draft_dims(B, L, N);
+    if (s != BSQ_OK) return s;
+    if (!ws || (B > 0 && (!P || !r || !count || !out)) || (B > 0 && L > 0 && (!tokens || !u))) return BSQ_ERR_ARG;
+    if (p_seq < 0 || p_row < 0 || (Q && (q_seq < 0 || q_row < 0))) return BSQ_ERR_SHAPE;
+    if (!aligned(P, p_dtype == BSQ_F32 ? 4 : 2) || (Q && !aligned(Q, q_dtype == BSQ_F32 ? 4 : 2)) || !aligned(tokens, 4) ||
+        !aligned(lens, 4) || !aligned(u, 4) || !aligned(r, 4) || !aligned(temperature, 4) || !aligned(count, 4) ||
+        !aligned(out, 4) || !aligned(err, 4) || !aligned(ws, 256))
+        return BSQ_ERR_ALIGN;
+    if (ws_bytes < draft_ws_bytes(B, L, N, Q != nullptr)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    if (B == 0) return BSQ_OK;
+    DraftCall c{};
+    c.P = P;
+    c.p_dtype = p_dtype;
+    c.pseq = p_seq;
+    c.prow = p_row;
+    c.Q = L > 0 ? Q : nullptr;
+    c.q_dtype = q_dtype;
+    c.qseq = q_seq;
+    c.qrow = q_row;
+    c.B = B;
+    c.L = L;
+    c.N = N;
+    c.tokens = tokens;
+    c.lens = lens;
+    c.u = u;
+    c.r = r;
+    c.temp = temperature;
+    c.count = count;
+    c.out = out;
+    c.err = err;
+    c.ws = ws;
+    return from_hip(launch_draft_verify(c, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
 // Gradient norm and clipping.
 // ---------------------------------------------------------------------------
 namespace {

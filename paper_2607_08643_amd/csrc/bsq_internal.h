@@ -325,6 +325,33 @@ size_t xent_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D);
 hipError_t launch_xent_loss(const XentCall &c, hipStream_t st);
 hipError_t launch_xent_grad(const XentCall &c, hipStream_t st);
 
+// The largest logits of a vocabulary's rows (top.hip).
+struct TopCall {
+    const void *Z;
+    int z_dtype;
+    int64_t ldz, T, N;
+    int K;
+    float scale;
+    int32_t *ids;
+    float *top, *lse;        // lse may be NULL
+    void *ws;
+};
+size_t top_ws_bytes(int64_t T, int64_t N);
+hipError_t launch_top_logits(const TopCall &c, hipStream_t st);
+
+// Verification of drafted tokens (draft.hip).
+struct DraftCall {
+    const void *P, *Q;       // Q may be NULL
+    int p_dtype, q_dtype;
+    int64_t B, L, N, pseq, prow, qseq, qrow;
+    const int32_t *tokens, *lens;
+    const float *u, *r, *temp;
+    int32_t *count, *out, *err;
+    void *ws;
+};
+size_t draft_ws_bytes(int64_t B, int64_t L, int64_t N, bool draft);
+hipError_t launch_draft_verify(const DraftCall &c, hipStream_t st);
+
 // Global gradient norm and clipping (clip.hip).
 int64_t clip_chunks(int64_t n);
 size_t clip_table_bytes(int64_t count, int64_t chunks);
