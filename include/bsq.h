@@ -707,6 +707,56 @@ bsq_status bsq_top_logits(const void *Z, int32_t z_dtype, int64_t ldz, int64_t T
                           int32_t *ids, float *top, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Distillation of a student, given by hidden states h_t and head weights v as for
+ * the cross entropy, from a teacher's top logits (Section III-F's recovery: the
+ * student is the compressed model, of which only adapters train):
+ *   p_k = exp(scale top_tk - norm_t),   P = sum_k p_k,
+ *   z_tv = scale h_t . v,   lse_t = log sum_v exp(z_tv),   q_v = exp(z_tv - lse_t),
+ *   loss_t = sum_k p_k (log p_k - log q_id(t,k)),
+ *   d_tv = g_t scale (P q_v - sum of p_k over id(t,k) = v),  dH = d V,  dV = d^T H.
+ * norm: the lse of the teacher's whole vocabulary (bsq_top_logits at the same scale;
+ * P is then the part that the K words hold), or NULL for that of the K words
+ * (P = 1). scale is one over a temperature; a factor of its square, where wanted,
+ * goes into g. A word that is listed twice counts twice. A negative id, or a logit
+ * of -inf, is no word; an id of N or more likewise, and ORs BSQ_DEVERR_BAD_SET into
+ * *err. A token without words has no loss: its loss, lse and row of dH are 0, and
+ * its hidden state and g are not used (they may be NaN). Roundings as for the
+ * cross entropy; the K terms of a loss are summed in 64 bits.
+ * ------------------------------------------------------------------------ */
+
+/* Device workspace of bsq_distill_loss (grad = 0), bsq_distill_grad (1); host only. */
+bsq_status bsq_distill_workspace_bytes(int32_t grad, int64_t T, int64_t N, int64_t D, int32_t K, size_t *bytes);
+
+/* Bytes of the logits that a loss can keep for its gradient: fp32, T rows of N
+ * rounded up to 256 (host only; T, N as below). */
+bsq_status bsq_distill_kept_bytes(int64_t T, int64_t N, size_t *bytes);
+
+/*   H, V    as for bsq_xent_loss
+ *   ids     device int32 [T][K], any order; top device fp32 [T][K]; 1 <= K <= BSQ_MAX_TOP
+ *   norm    device fp32 [T] or NULL
+ *   scale   > 0, finite
+ *   loss, lse  device fp32 [T]
+ *   kept    device buffer of bsq_distill_kept_bytes, 256-byte aligned, or NULL
+ *   err     device int32 or NULL
+ *   ws      device workspace, 256-byte aligned, any contents
+ * 0 <= T <= 2^20, 1 <= N < 2^31, 1 <= D <= 2^16. */
+bsq_status bsq_distill_loss(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                            const int32_t *ids, const float *top, const float *norm, int32_t K, float scale,
+                            float *loss, float *lse, void *kept, size_t kept_bytes, int32_t *err, void *ws,
+                            size_t ws_bytes, void *stream);
+
+/*   lse     device fp32 [T], as bsq_distill_loss wrote it for the same H, V, ids, top and scale
+ *   g       device fp32 [T], the gradient of each token's loss
+ *   kept    as bsq_distill_loss wrote it for the same H, V, ids, top and scale (the
+ *           logits are not made again), or NULL
+ *   dH, dV, accumulate  as for bsq_xent_grad */
+bsq_status bsq_distill_grad(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                            const int32_t *ids, const float *top, const float *norm, int32_t K, float scale,
+                            const float *lse, const float *g, const void *kept, size_t kept_bytes, void *dH,
+                            int64_t lddh, void *dV, int64_t lddv, int32_t dv_dtype, int32_t accumulate, int32_t *err,
+                            void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Verification of drafted tokens (a compressed model drafts for the model that it
  * was made from). Sequence b has n_b drafted tokens x_0 .. and one row of target
  * logits for each and one for the token after them; p_i and q_i are the softmax

@@ -17,5 +17,6 @@ from ._binding import (  # noqa: F401
     AdapterPlan, AdapterPool, GradPlan, bsq_adapter_plan, bsq_adapter_pool, bsq_adapters_apply, bsq_adapters_grad,
     bsq_adapters_plan, bsq_adapters_plan_bytes, bsq_adapters_workspace_bytes, bsq_clip_plan, bsq_grad_clip, bsq_grad_norm,
     bsq_xent_grad, bsq_xent_loss, bsq_xent_workspace_bytes,
+    bsq_distill_grad, bsq_distill_kept_bytes, bsq_distill_loss, bsq_distill_workspace_bytes,
     bsq_draft_verify, bsq_draft_workspace_bytes, bsq_top_logits, bsq_top_workspace_bytes,
 )

@@ -87,7 +87,8 @@ EXPORTS = ("bsq_version", "bsq_status_str", "bsq_config_check", "bsq_layer_sizes
            "bsq_adapters_plan", "bsq_adapters_workspace_bytes", "bsq_adapters_apply", "bsq_adapters_grad",
            "bsq_xent_workspace_bytes", "bsq_xent_loss", "bsq_xent_grad", "bsq_clip_table_bytes", "bsq_clip_prepare",
            "bsq_grad_norm", "bsq_grad_clip", "bsq_top_workspace_bytes", "bsq_top_logits",
-           "bsq_draft_workspace_bytes", "bsq_draft_verify")
+           "bsq_draft_workspace_bytes", "bsq_draft_verify", "bsq_distill_workspace_bytes", "bsq_distill_kept_bytes",
+           "bsq_distill_loss", "bsq_distill_grad")
 
 # struct layouts above follow this version of include/bsq.h
 ABI_VERSION = 8
@@ -142,6 +143,11 @@ def lib():
     L.bsq_grad_clip.argtypes = [P, ct.c_float, P, P, P]
     L.bsq_top_workspace_bytes.argtypes = [I64, I64, ct.POINTER(SZ)]
     L.bsq_top_logits.argtypes = [P, I32, I64, I64, I64, I32, ct.c_float, P, P, P, P, SZ, P]
+    L.bsq_distill_workspace_bytes.argtypes = [I32, I64, I64, I64, I32, ct.POINTER(SZ)]
+    L.bsq_distill_kept_bytes.argtypes = [I64, I64, ct.POINTER(SZ)]
+    L.bsq_distill_loss.argtypes = [P, I64, P, I64, I64, I64, I64, P, P, P, I32, ct.c_float, P, P, P, SZ, P, P, SZ, P]
+    L.bsq_distill_grad.argtypes = [P, I64, P, I64, I64, I64, I64, P, P, P, I32, ct.c_float, P, P, P, SZ, P, I64, P, I64, I32,
+                                   I32, P, P, SZ, P]
     L.bsq_draft_workspace_bytes.argtypes = [I32, I64, I64, I64, ct.POINTER(SZ)]
     L.bsq_draft_verify.argtypes = [P, I32, I64, I64, P, I32, I64, I64, I64, I64, I64, P, P, P, P, P, P, P, P, P, SZ, P]
     for f in EXPORTS[2:]:
@@ -1049,6 +1055,99 @@ def bsq_top_logits(Z: torch.Tensor, K: int, scale: float = 1.0, ids=None, top=No
         _check(lib().bsq_top_logits(_ptr(Z), zt, ldz, T, N, K, scale, _ptr(ids), _ptr(top), _ptr(lse), _ptr(ws),
                                     ws.numel(), st), "bsq_top_logits")
     return ids, top, lse
+
+
+# ---------------------------------------------------------------- distillation from top logits
+@functools.lru_cache(maxsize=1024)
+def bsq_distill_workspace_bytes(grad: bool, T: int, N: int, D: int, K: int) -> int:
+    out = ct.c_size_t(0)
+    _check(lib().bsq_distill_workspace_bytes(int(grad), T, N, D, K, ct.byref(out)), "bsq_distill_workspace_bytes")
+    return out.value
+
+
+@functools.lru_cache(maxsize=1024)
+def bsq_distill_kept_bytes(T: int, N: int) -> int:
+    out = ct.c_size_t(0)
+    _check(lib().bsq_distill_kept_bytes(T, N, ct.byref(out)), "bsq_distill_kept_bytes")
+    return out.value
+
+
+def _distill_shapes(H, V, ids, top, norm):
+    T, D = H.shape
+    ldh = _matrix(H, torch.bfloat16, (T, D), "H")
+    ldv = _matrix(V, torch.bfloat16, (V.shape[0], D), "V")
+    if ids.dim() != 2:
+        raise ValueError("ids: must be [T, K]")
+    K = ids.shape[1]
+    _need(ids, torch.int32, (T, K), "ids")
+    _need(top, torch.float32, (T, K), "top")
+    if norm is not None:
+        _need(norm, torch.float32, (T,), "norm")
+    return T, V.shape[0], D, K, ldh, ldv
+
+
+def _kept_bytes(kept):
+    if kept is None:
+        return 0
+    if kept.dtype != torch.uint8 or not kept.is_contiguous():
+        raise TypeError("kept: contiguous uint8 expected")
+    return kept.numel()
+
+
+def bsq_distill_loss(H: torch.Tensor, V: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, norm=None, scale: float = 1.0,
+                     keep: bool = False, loss=None, lse=None, kept=None, err=None, ws: torch.Tensor | None = None,
+                     stream=None):
+    """Per-token divergence of a student, given by hidden states H [T, D] under the
+    head V [N, D] (bf16), from a teacher's top logits as bsq_top_logits gives them
+    (ids int32 [T, K], top fp32 [T, K]): (loss, lse), fp32 [T]. norm: the teacher's lse at this
+    scale, fp32 [T] (None: the teacher's probabilities add up to 1 over its K words);
+    scale: one over the temperature. keep: also leave the student's logits for
+    bsq_distill_grad (fp32; in `kept`, uint8, or a new buffer): (loss, lse, kept)."""
+    T, N, D, K, ldh, ldv = _distill_shapes(H, V, ids, top, norm)
+    keep = keep or kept is not None
+    dev = _device_of((H, V, ids, top, norm, loss, lse, kept, err, ws), "bsq_distill_loss")
+    need = bsq_distill_workspace_bytes(False, T, N, D, K)
+    with _Launch(dev, stream) as st:
+        loss = torch.empty(T, dtype=torch.float32, device=dev) if loss is None else _need(loss, torch.float32, (T,), "loss")
+        lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else _need(lse, torch.float32, (T,), "lse")
+        if keep and kept is None:
+            kept = _workspace(bsq_distill_kept_bytes(T, N), dev)
+        ws = ws if ws is not None else _workspace(need, dev)
+        _check(lib().bsq_distill_loss(_ptr(H), ldh, _ptr(V), ldv, T, N, D, _ptr(ids), _ptr(top), _ptr(norm), K, scale,
+                                      _ptr(loss), _ptr(lse), _ptr(kept), _kept_bytes(kept), _ptr(err), _ptr(ws),
+                                      ws.numel(), st), "bsq_distill_loss")
+    return (loss, lse, kept) if keep else (loss, lse)
+
+
+def bsq_distill_grad(H: torch.Tensor, V: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, lse: torch.Tensor,
+                     g: torch.Tensor, norm=None, scale: float = 1.0, kept=None, head: bool = True, dH=None, dV=None,
+                     accumulate: bool = False, err=None, ws: torch.Tensor | None = None, stream=None):
+    """Gradients of sum(g * loss): (dH [T, D] bf16, dV [N, D] or None where head
+    is False). lse, kept: as bsq_distill_loss gave them for the same H, V, ids, top, norm
+    and scale (without kept the logits are made again); g: fp32 [T]. dV, accumulate:
+    as for bsq_xent_grad."""
+    T, N, D, K, ldh, ldv = _distill_shapes(H, V, ids, top, norm)
+    _need(lse, torch.float32, (T,), "lse")
+    _need(g, torch.float32, (T,), "g")
+    if accumulate and (dV is None or not head):
+        raise ValueError("bsq_distill_grad: accumulate needs dV")
+    dev = _device_of((H, V, ids, top, norm, lse, g, kept, dH, dV, err, ws), "bsq_distill_grad")
+    need = bsq_distill_workspace_bytes(True, T, N, D, K)
+    with _Launch(dev, stream) as st:
+        if dH is None:
+            dH = torch.empty((T, D), dtype=torch.bfloat16, device=dev)
+        lddh = _matrix(dH, torch.bfloat16, (T, D), "dH")
+        if not head:
+            dV = None
+        elif dV is None:
+            dV = torch.empty((N, D), dtype=torch.bfloat16, device=dev)
+        lddv = 0 if dV is None else _matrix(dV, dV.dtype, (N, D), "dV")
+        ws = ws if ws is not None else _workspace(need, dev)
+        _check(lib().bsq_distill_grad(_ptr(H), ldh, _ptr(V), ldv, T, N, D, _ptr(ids), _ptr(top), _ptr(norm), K, scale,
+                                      _ptr(lse), _ptr(g), _ptr(kept), _kept_bytes(kept), _ptr(dH), lddh, _ptr(dV), lddv,
+                                      BSQ_BF16 if dV is None else _dtype_code(dV.dtype), int(accumulate), _ptr(err),
+                                      _ptr(ws), ws.numel(), st), "bsq_distill_grad")
+    return dH, dV
 
 
 # ---------------------------------------------------------------- verification of drafted tokens

@@ -928,6 +928,114 @@ bsq_status bsq_top_logits(const void *Z, int32_t z_dtype, int64_t ldz, int64_t T
 }
 
 // ---------------------------------------------------------------------------
+// Distillation from top logits.
+// ---------------------------------------------------------------------------
+namespace {
+bsq_status check_distill(bool grad, const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N,
+                         int64_t D, const int32_t *ids, const float *top, const float *norm, int32_t K, float scale,
+                         const void *kept, size_t kept_bytes, const int32_t *err, const void *ws, size_t ws_bytes)
+{
+    const bsq_status s = check_xent_dims(T, N, D);
+    if (s != BSQ_OK) return s;
+    if (K < 1 || K > BSQ_MAX_TOP || !good_scale(scale)) return BSQ_ERR_ARG;
+    if (!V || !ws || (T > 0 && (!H || !ids || !top))) return BSQ_ERR_ARG;
+    if (ldh < D || ldv < D || ldv % 8 != 0) return BSQ_ERR_SHAPE;
+    if (!aligned(H, 2) || !aligned(V, 16) || !aligned(ids, 4) || !aligned(top, 4) || !aligned(norm, 4) ||
+        !aligned(kept, 256) || !aligned(err, 4) || !aligned(ws, 256))
+        return BSQ_ERR_ALIGN;
+    if (kept && kept_bytes < distill_kept_bytes(T, N)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    if (ws_bytes < distill_ws_bytes(grad, T, N, D, K)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    return BSQ_OK;
+}
+
+DistillCall distill_call(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                         const int32_t *ids, const float *top, const float *norm, int32_t K, float scale, void *kept,
+                         int32_t *err, void *ws)
+{
+    DistillCall c{};
+    c.x.H = H;
+    c.x.ldh = ldh;
+    c.x.V = V;
+    c.x.ldv = ldv;
+    c.x.T = T;
+    c.x.N = N;
+    c.x.D = D;
+    c.x.err = err;
+    c.x.ws = ws;
+    c.ids = ids;
+    c.top = top;
+    c.norm = norm;
+    c.K = K;
+    c.scale = scale;
+    c.kept = static_cast<float *>(kept);
+    return c;
+}
+}  // namespace
+
+bsq_status bsq_distill_workspace_bytes(int32_t grad, int64_t T, int64_t N, int64_t D, int32_t K, size_t *bytes)
+{
+    if (!bytes || (grad != 0 && grad != 1) || K < 1 || K > BSQ_MAX_TOP) return BSQ_ERR_ARG;
+    const bsq_status s = check_xent_dims(T, N, D);
+    if (s != BSQ_OK) return s;
+    *bytes = distill_ws_bytes(grad != 0, T, N, D, K);
+    return BSQ_OK;
+}
+
+bsq_status bsq_distill_kept_bytes(int64_t T, int64_t N, size_t *bytes)
+{
+    if (!bytes) return BSQ_ERR_ARG;
+    const bsq_status s = check_xent_dims(T, N, 8);
+    if (s != BSQ_OK) return s;
+    *bytes = distill_kept_bytes(T, N);
+    return BSQ_OK;
+}
+
+bsq_status bsq_distill_loss(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                            const int32_t *ids, const float *top, const float *norm, int32_t K, float scale,
+                            float *loss, float *lse, void *kept, size_t kept_bytes, int32_t *err, void *ws,
+                            size_t ws_bytes, void *stream)
+{
+    const bsq_status s = check_distill(false, H, ldh, V, ldv, T, N, D, ids, top, norm, K, scale, kept, kept_bytes, err, ws,
+                                       ws_bytes);
+    if (s != BSQ_OK) return s;
+    if (T == 0) return BSQ_OK;
+    if (!loss || !lse) return BSQ_ERR_ARG;
+    if (!aligned(loss, 4) || !aligned(lse, 4)) return BSQ_ERR_ALIGN;
+    DistillCall c = distill_call(H, ldh, V, ldv, T, N, D, ids, top, norm, K, scale, kept, err, ws);
+    c.x.loss = loss;
+    c.x.lse = lse;
+    return from_hip(launch_distill_loss(c, static_cast<hipStream_t>(stream)));
+}
+
+bsq_status bsq_distill_grad(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
+                            const int32_t *ids, const float *top, const float *norm, int32_t K, float scale,
+                            const float *lse, const float *g, const void *kept, size_t kept_bytes, void *dH,
+                            int64_t lddh, void *dV, int64_t lddv, int32_t dv_dtype, int32_t accumulate, int32_t *err,
+                            void *ws, size_t ws_bytes, void *stream)
+{
+    if (dV && dv_dtype != BSQ_F32 && dv_dtype != BSQ_BF16) return BSQ_ERR_DTYPE;
+    const bsq_status s = check_distill(true, H, ldh, V, ldv, T, N, D, ids, top, norm, K, scale, kept, kept_bytes, err, ws,
+                                       ws_bytes);
+    if (s != BSQ_OK) return s;
+    if (accumulate != 0 && accumulate != 1) return BSQ_ERR_ARG;
+    if (T > 0 && (!lse || !g || !dH)) return BSQ_ERR_ARG;
+    if (T > 0 && lddh < D) return BSQ_ERR_SHAPE;
+    if (dV && lddv < D) return BSQ_ERR_SHAPE;
+    if (!aligned(lse, 4) || !aligned(g, 4) || !aligned(dH, 2) || !aligned(dV, dv_dtype == BSQ_F32 ? 4 : 2)) return BSQ_ERR_ALIGN;
+    // (read, not written, by the gradient)
+    DistillCall c = distill_call(H, ldh, V, ldv, T, N, D, ids, top, norm, K, scale, const_cast<void *>(kept), err, ws);
+    c.x.lse_in = lse;
+    c.x.g = g;
+    c.x.dH = dH;
+    c.x.lddh = lddh;
+    c.x.dV = dV;
+    c.x.lddv = lddv;
+    c.x.dv_dtype = dv_dtype;
+    c.x.accumulate = accumulate;
+    return from_hip(launch_distill_grad(c, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
 // Verification of drafted tokens.
 // ---------------------------------------------------------------------------
 namespace {

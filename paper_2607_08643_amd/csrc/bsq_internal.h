@@ -325,6 +325,21 @@ size_t xent_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D);
 hipError_t launch_xent_loss(const XentCall &c, hipStream_t st);
 hipError_t launch_xent_grad(const XentCall &c, hipStream_t st);
 
+// Distillation from a teacher's top logits (distill.hip). x: as for the cross
+// entropy, without its target.
+struct DistillCall {
+    XentCall x;
+    const int32_t *ids;
+    const float *top, *norm;  // norm may be NULL
+    int K;
+    float scale;
+    float *kept;              // may be NULL
+};
+size_t distill_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D, int K);
+size_t distill_kept_bytes(int64_t T, int64_t N);
+hipError_t launch_distill_loss(const DistillCall &c, hipStream_t st);
+hipError_t launch_distill_grad(const DistillCall &c, hipStream_t st);
+
 // The largest logits of a vocabulary's rows (top.hip).
 struct TopCall {
     const void *Z;

@@ -1,0 +1,314 @@
+// Distillation of a student, given by hidden states H [T][D] and head weights V [N][D],
+// from a teacher's top logits a [T][K] of the words ids [T][K], at a scale s (one over the
+// temperature), and its gradient:
+//   p_k = exp(s a_k - norm)  (norm: the log of the sum over the teacher's whole vocabulary,
+//                             or over the K words),  P = sum p_k,
+//   q = softmax(s H V^T),  loss = sum_k p_k (log p_k - log q_id_k),
+//   d = g s (P q - sum of p_k at its word),  dH = d V,  dV = d^T H.
+//
+// The products are those of the cross entropy (vocab_product.h). What a token has of its
+// teacher is K words: they are sorted by word once, with the place where each 256-word
+// tile's begin, so that a tile finds the few of its own (64 of 151936 words: one in
+// ten tiles) while it holds the logits in registers. The loss is joined from the tiles'
+// statistics and these logits in 64 bits.
+//
+// Kept logits: the loss can leave its logits (fp32, compact rows) for the gradient, which
+// then makes d from them in one pass over memory and has one product less to do: 12
+// bytes a logit moved against 2 D operations.
+#include "vocab_product.h"
+
+namespace bsq {
+namespace {
+
+constexpr int KMAX = BSQ_MAX_TOP;
+static_assert(KMAX <= XT, "a thread for every word of a token");
+
+struct TeacherArgs {
+    const int32_t *ids;
+    const float *top, *norm;
+    int64_t T, N, tiles;
+    int K;
+    float scale;
+    int64_t *live;    // [T]: 0, or -1 for a token without a loss
+    int32_t *sid;     // [T][K]
+    float *sp;        // [T][K]
+    uint16_t *off;    // [T][tiles + 1]
+    float *total;     // [T]: sum of p
+    double *self;     // [T]: sum of p log p
+    int32_t *err;
+};
+
+__device__ __forceinline__ double block_sum64(double v, double *s)
+{
+    const int t = threadIdx.x;
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    __syncthreads();
+    if ((t & 63) == 0) s[t >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+    for (int w = 0; w < XT / 64; ++w) v += s[w];
+    return v;
+}
+
+// A token's words in order, their probabilities, and each tile's first. One block a token.
+__global__ __launch_bounds__(XT) void distill_teacher_kernel(const TeacherArgs a)
+{
+    __shared__ uint64_t s_key[KMAX];
+    __shared__ int32_t s_id[KMAX];
+    __shared__ double s_sum[XT / 64];
+    __shared__ float s_max[XT / 64];
+    const int t = threadIdx.x;
+    const int64_t m = blockIdx.x;
+    int32_t id = -1;
+    double x = -__builtin_inf();  // (its product with the scale is not rounded)
+    if (t < a.K) {
+        id = a.ids[m * a.K + t];
+        if (id >= a.N) {
+            if (a.err) atomicOr(a.err, BSQ_DEVERR_BAD_SET);
+            id = -1;
+        }
+        x = double(a.top[m * a.K + t]) * double(a.scale);
+        // (a word of -inf is not there: its probability is 0)
+        if (id < 0 || x == -__builtin_inf()) {
+            id = -1;
+            x = -__builtin_inf();
+        }
+    }
+    const bool there = id >= 0;
+    // absent words last, each key another
+    const uint64_t key = (uint64_t(uint32_t(there ? id : INT32_MAX)) << 16) | uint32_t(t);
+    s_key[t] = key;
+    float mx = float(x);  // what is subtracted before the exponentials: any value near the largest
+    for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+    if ((t & 63) == 0) s_max[t >> 6] = mx;
+    __syncthreads();
+    for (int w = 0; w < XT / 64; ++w) mx = fmaxf(mx, s_max[w]);
+    const double count = block_sum64(there ? 1.0 : 0.0, s_sum);
+    double logp, p;
+    if (a.norm) {
+        logp = x - double(a.norm[m]);
+    } else {
+        const double sum = block_sum64(there ? exp(x - double(mx)) : 0.0, s_sum);
+        logp = x - (double(mx) + log(sum));
+    }
+    p = there ? exp(logp) : 0.0;
+    const double total = block_sum64(p, s_sum);
+    const double self = block_sum64(there && p != 0.0 ? p * logp : 0.0, s_sum);
+    if (t < a.K) {
+        int place = 0;
+        for (int k = 0; k < a.K; ++k) place += s_key[k] < key ? 1 : 0;
+        s_id[place] = there ? id : INT32_MAX;
+        a.sid[m * a.K + place] = there ? id : INT32_MAX;
+        a.sp[m * a.K + place] = float(p);
+    }
+    if (t == 0) {
+        a.live[m] = count > 0.0 ? 0 : -1;
+        a.total[m] = float(total);
+        a.self[m] = self;
+    }
+    __syncthreads();
+    for (int64_t tile = t; tile <= a.tiles; tile += XT) {
+        const int64_t first = tile * VBLK;
+        int lo = 0, hi = a.K;  // words below `first`
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (s_id[mid] < first && s_id[mid] != INT32_MAX) lo = mid + 1;
+            else hi = mid;
+        }
+        a.off[m * (a.tiles + 1) + tile] = uint16_t(lo);
+    }
+}
+
+// A token's tiles joined, and its loss: TOK tokens a block, XT / TOK threads each over the
+// tiles and the teacher's words, joined in order.
+template <int TOK>
+__global__ __launch_bounds__(XT) void distill_join_kernel(const XArgs a, const double *self, int tiles)
+{
+    constexpr int PARTS = XT / TOK;
+    __shared__ float s_m[PARTS][TOK + 1], s_s[PARTS][TOK + 1];
+    __shared__ double s_z[PARTS][TOK + 1];
+    const int tok = threadIdx.x % TOK, part = threadIdx.x / TOK;
+    const int64_t m = int64_t(blockIdx.x) * TOK + tok;
+    const int row = m < a.T ? a.pos[m] : -1;
+    float mx = -__builtin_inff(), s = 0.0f;
+    double z = 0.0;
+    if (row >= 0) {
+#pragma unroll 4
+        for (int q = part; q < tiles; q += PARTS) {
+            const float2 v = a.stat[int64_t(q) * a.Tp + row];
+            join_stats(mx, s, v.x, v.y);
+        }
+        for (int k = part; k < a.K; k += PARTS) {
+            const float p = a.sp[m * a.K + k];
+            if (p != 0.0f) z += double(p) * double(a.zk[m * a.K + k]);
+        }
+    }
+    s_m[part][tok] = mx;
+    s_s[part][tok] = s;
+    s_z[part][tok] = z;
+#pragma unroll
+    for (int h = PARTS / 2; h > 0; h >>= 1) {
+        __syncthreads();
+        if (part < h) {
+            join_stats(mx, s, s_m[part + h][tok], s_s[part + h][tok]);
+            z += s_z[part + h][tok];
+            s_m[part][tok] = mx;
+            s_s[part][tok] = s;
+            s_z[part][tok] = z;
+        }
+    }
+    if (part != 0 || m >= a.T) return;
+    const double lse = double(mx) + log(double(s));
+    a.lse_out[m] = row >= 0 ? float(lse) : 0.0f;
+    a.loss_out[m] = row >= 0 ? float(self[m] - z + double(a.total[m]) * lse) : 0.0f;
+}
+
+// d of a piece of the vocabulary from the kept logits: eight words a thread.
+__global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blocks)
+{
+    const int live = a.hdr[0];
+    const int64_t row = blockIdx.x / blocks;
+    if (row >= (int64_t(live) + 63) / 64 * 64) return;  // (d's rows are read 64 deep by dV)
+    const int64_t w = (int64_t(blockIdx.x - row * blocks) * XT + threadIdx.x) * 8;
+    if (w >= a.vp) return;
+    u32x4_t hi{0u, 0u, 0u, 0u}, lo{0u, 0u, 0u, 0u};
+    if (row < live) {
+        const int64_t word = a.v0 + w, tok = a.rows[row];
+        const f32x4_t *zp = reinterpret_cast<const f32x4_t *>(a.Z + row * a.ldz + word);
+        const f32x4_t z[2] = {zp[0], zp[1]};
+        const float lse = a.lse[row], gg = a.g[row] * a.scale, total = a.total[tok];
+        const uint16_t *o = a.off + tok * (a.tiles + 1) + word / VBLK;
+        const int beg = o[0], end = o[1];
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = word + k < a.N ? gg * (__builtin_amdgcn_exp2f((z[k >> 2][k & 3] - lse) * LOG2E) * total) : 0.0f;
+        for (int e = beg; e < end; ++e) {
+            const int64_t q = a.sid[tok * a.K + e] - word;
+            const float p = gg * a.sp[tok * a.K + e];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] -= (q == k) ? p : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            hi[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
+            if (a.lo == 0) continue;
+            const float x = v[2 * k] - __uint_as_float(hi[k] << 16);
+            const float y = v[2 * k + 1] - __uint_as_float(hi[k] & 0xffff0000u);
+            lo[k] = pack_bf16x2(x - x == 0.0f ? x : 0.0f, y - y == 0.0f ? y : 0.0f);
+        }
+    }
+    u32x4_t *q = reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w);
+    *q = hi;
+    if (a.lo) *reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w + a.lo) = lo;
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+// The cross entropy's workspace, then what a token has of its teacher.
+struct SLayout {
+    XLayout x;
+    size_t live, sid, sp, off, total, self, zk, bytes;
+};
+
+SLayout distill_layout(bool grad, int64_t T, int64_t N, int64_t D, int K)
+{
+    SLayout l{};
+    l.x = xent_layout(grad, T, N, D);
+    size_t at = align256(l.x.total);
+    auto take = [&](size_t bytes) {
+        const size_t p = at;
+        at += align256(bytes);
+        return p;
+    };
+    const size_t t = size_t(std::max<int64_t>(T, 1));
+    l.live = take(t * 8);
+    l.sid = take(t * K * 4);
+    l.sp = take(t * K * 4);
+    l.off = take(t * size_t(l.x.tiles + 1) * 2);
+    l.total = take(t * 4);
+    l.self = take(t * 8);
+    l.zk = take(grad ? 0 : t * K * 4);
+    l.bytes = at;
+    return l;
+}
+
+// The teacher's words, and the arguments of the products.
+hipError_t launch_teacher(const DistillCall &c, const SLayout &l, XArgs &a, hipStream_t st)
+{
+    char *ws = static_cast<char *>(c.x.ws);
+    TeacherArgs h{};
+    h.ids = c.ids;
+    h.top = c.top;
+    h.norm = c.norm;
+    h.T = c.x.T;
+    h.N = c.x.N;
+    h.tiles = l.x.tiles;
+    h.K = c.K;
+    h.scale = c.scale;
+    h.live = reinterpret_cast<int64_t *>(ws + l.live);
+    h.sid = reinterpret_cast<int32_t *>(ws + l.sid);
+    h.sp = reinterpret_cast<float *>(ws + l.sp);
+    h.off = reinterpret_cast<uint16_t *>(ws + l.off);
+    h.total = reinterpret_cast<float *>(ws + l.total);
+    h.self = reinterpret_cast<double *>(ws + l.self);
+    h.err = c.x.err;
+    XentCall x = c.x;
+    x.target = h.live;
+    x.err = nullptr;
+    a = xent_args(x, l.x);
+    a.sid = h.sid;
+    a.sp = h.sp;
+    a.off = h.off;
+    a.total = h.total;
+    a.zk = reinterpret_cast<float *>(ws + l.zk);
+    a.Z = c.kept;
+    a.ldz = l.x.tiles * VBLK;
+    a.tiles = l.x.tiles;
+    a.K = c.K;
+    a.scale = c.scale;
+    if (c.x.T == 0) return hipSuccess;
+    hipLaunchKernelGGL(distill_teacher_kernel, dim3(unsigned(c.x.T)), dim3(XT), 0, st, h);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t distill_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D, int K) { return distill_layout(grad, T, N, D, K).bytes; }
+
+size_t distill_kept_bytes(int64_t T, int64_t N) { return size_t(T) * size_t((N + VBLK - 1) / VBLK * VBLK) * 4; }
+
+hipError_t launch_distill_loss(const DistillCall &c, hipStream_t st)
+{
+    const SLayout l = distill_layout(false, c.x.T, c.x.N, c.x.D, c.K);
+    XArgs a{};
+    hipError_t e = launch_teacher(c, l, a, st);
+    if (e != hipSuccess) return e;
+    char *ws = static_cast<char *>(c.x.ws);
+    a.stat = reinterpret_cast<float2 *>(ws + l.x.stat);
+    a.loss_out = c.x.loss;
+    a.lse_out = c.x.lse;
+    if ((e = launch_stats<EPI_TSTATS>(a, l.x, st)) != hipSuccess) return e;
+    const double *self = reinterpret_cast<const double *>(ws + l.self);
+    if (a.T < 512) hipLaunchKernelGGL((distill_join_kernel<1>), dim3(unsigned(a.T)), dim3(XT), 0, st, a, self, int(l.x.tiles));
+    else hipLaunchKernelGGL((distill_join_kernel<8>), dim3(unsigned((a.T + 7) / 8)), dim3(XT), 0, st, a, self, int(l.x.tiles));
+    return hipGetLastError();
+}
+
+hipError_t launch_distill_grad(const DistillCall &c, hipStream_t st)
+{
+    const SLayout l = distill_layout(true, c.x.T, c.x.N, c.x.D, c.K);
+    XArgs a{};
+    hipError_t e = launch_teacher(c, l, a, st);
+    if (e != hipSuccess) return e;
+    return launch_grad(c.x, l.x, a, st, [&](const XArgs &piece) {
+        if (!piece.Z) return launch_tokens<EPI_TPROB>(piece, piece.vp, 1, st);
+        const int64_t blocks = (piece.vp + 8 * XT - 1) / (8 * XT), rows = (piece.T + 63) / 64 * 64;
+        if (rows == 0) return hipSuccess;
+        hipLaunchKernelGGL(distill_kept_kernel, dim3(unsigned(rows * blocks)), dim3(XT), 0, st, piece, int(blocks));
+        return hipGetLastError();
+    });
+}
+
+}  // namespace bsq

@@ -116,3 +116,66 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         bsq.bsq_draft_verify(z(2, 4, 50), tokens, u, r, lens=z(3, dt=torch.int32))
     with pytest.raises(TypeError, match="temperature"):
         bsq.bsq_draft_verify(z(2, 4, 50), tokens, u, r, temperature=z(2))
+
+
+# ---------------------------------------------------------------- distillation
+@pytest.mark.parametrize("grad", [False, True])
+def test_distill_workspace(grad):
+    assert bsq.bsq_distill_workspace_bytes(grad, 0, 1, 8, 1) > 0
+    assert bsq.bsq_distill_workspace_bytes(grad, 4096, 151936, 4096, 64) > bsq.bsq_xent_workspace_bytes(grad, 4096, 151936, 4096)
+    for dims, status in (((-1, 1, 8, 1), bsq.BSQ_ERR_SHAPE), ((1, 0, 8, 1), bsq.BSQ_ERR_SHAPE), ((1, 1, 12, 1), bsq.BSQ_ERR_SHAPE),
+                         ((1, 1, 8, 0), bsq.BSQ_ERR_ARG), ((1, 1, 8, 257), bsq.BSQ_ERR_ARG),
+                         (((1 << 20) + 1, 1, 8, 1), bsq.BSQ_ERR_UNSUPPORTED), ((1, 1 << 31, 8, 1), bsq.BSQ_ERR_UNSUPPORTED)):
+        with pytest.raises(bsq.BsqError) as e:
+            bsq.bsq_distill_workspace_bytes(grad, *dims)
+        assert e.value.status == status, dims
+    assert bsq.bsq_distill_kept_bytes(10, 257) == 10 * 512 * 4 and bsq.bsq_distill_kept_bytes(0, 1) == 0
+    with pytest.raises(bsq.BsqError):
+        bsq.bsq_distill_kept_bytes(-1, 5)
+
+
+def test_distill_rejects_before_launch():
+    def call(grad, H=FAKE, ldh=64, V=FAKE, ldv=64, T=10, N=100, D=64, ids=FAKE, top=FAKE, norm=0, K=5, scale=1.0, a=FAKE,
+             b=FAKE, kept=0, kept_bytes=0, dH=FAKE, lddh=64, dV=FAKE, lddv=64, dt=1, acc=0, err=0, ws=FAKE, ws_bytes=BIG):
+        L = bsq.lib()
+        if not grad:
+            return L.bsq_distill_loss(_p(H), ldh, _p(V), ldv, T, N, D, _p(ids), _p(top), _p(norm), K, scale, _p(a), _p(b),
+                                      _p(kept), kept_bytes, _p(err), _p(ws), ws_bytes, None)
+        return L.bsq_distill_grad(_p(H), ldh, _p(V), ldv, T, N, D, _p(ids), _p(top), _p(norm), K, scale, _p(a), _p(b),
+                                  _p(kept), kept_bytes, _p(dH), lddh, _p(dV), lddv, dt, acc, _p(err), _p(ws), ws_bytes, None)
+    for g in (False, True):
+        for kw in (dict(H=0), dict(V=0), dict(ids=0), dict(top=0), dict(a=0), dict(b=0), dict(ws=0), dict(K=0), dict(K=257),
+                   dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))):
+            assert call(g, **kw) == bsq.BSQ_ERR_ARG, kw
+        for kw in (dict(T=-1), dict(N=0), dict(D=60), dict(ldh=63), dict(ldv=63), dict(ldv=68)):
+            assert call(g, **kw) == bsq.BSQ_ERR_SHAPE, kw
+        for kw in (dict(H=FAKE + 1), dict(V=FAKE + 8), dict(ids=FAKE + 2), dict(top=FAKE + 2), dict(norm=FAKE + 1),
+                   dict(a=FAKE + 2), dict(b=FAKE + 2), dict(kept=FAKE + 16, kept_bytes=BIG), dict(err=FAKE + 2), dict(ws=FAKE + 64)):
+            assert call(g, **kw) == bsq.BSQ_ERR_ALIGN, kw
+        assert call(g, ws_bytes=bsq.bsq_distill_workspace_bytes(g, 10, 100, 64, 5) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
+        assert call(g, kept=FAKE, kept_bytes=10 * 256 * 4 - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
+    assert call(True, dH=0) == bsq.BSQ_ERR_ARG
+    assert call(True, lddh=63) == bsq.BSQ_ERR_SHAPE
+    assert call(True, lddv=63) == bsq.BSQ_ERR_SHAPE
+    assert call(True, dt=5) == bsq.BSQ_ERR_DTYPE
+    assert call(True, acc=-1) == bsq.BSQ_ERR_ARG
+    assert call(True, dV=FAKE + 2, dt=0) == bsq.BSQ_ERR_ALIGN
+
+
+def test_distill_binding_refuses_wrong_shapes():
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)  # noqa: E731
+    ids, top, f = z(4, 3, dt=torch.int32), z(4, 3, dt=torch.float32), z(4, dt=torch.float32)
+    with pytest.raises(ValueError, match="GPU"):
+        bsq.bsq_distill_loss(z(4, 64), z(10, 64), ids, top)
+    with pytest.raises(TypeError, match="ids"):
+        bsq.bsq_distill_loss(z(4, 64), z(10, 64), ids.long(), top)
+    with pytest.raises(ValueError, match="K"):
+        bsq.bsq_distill_loss(z(4, 64), z(10, 64), ids[0], top)
+    with pytest.raises(ValueError, match="top"):
+        bsq.bsq_distill_loss(z(4, 64), z(10, 64), ids, top[:, :2])
+    with pytest.raises(ValueError, match="norm"):
+        bsq.bsq_distill_loss(z(4, 64), z(10, 64), ids, top, norm=top)
+    with pytest.raises(ValueError, match="accumulate"):
+        bsq.bsq_distill_grad(z(4, 64), z(10, 64), ids, top, f, f, accumulate=True)
+    with pytest.raises(TypeError, match="g"):
+        bsq.bsq_distill_grad(z(4, 64), z(10, 64), ids, top, f, f.double())
