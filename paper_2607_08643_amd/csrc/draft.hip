@@ -9,10 +9,10 @@
 // Without draft logits the drafts are certain: q_i(x_i) = 1, and x_i is taken out of p_i.
 //
 // Three launches: the largest logit and the sum of exponentials of every piece of
-// every row that is needed; the pieces' sums of max(p - q, 0) of the one row where a
-// draft was refused (every block first decides its sequence from the first launch's
-// results); the draw, one block a sequence. No atomics but an OR of error bits: a result
-// depends on the inputs alone.
+// every row that is needed; the weights of the one row that the next token is drawn from,
+// summed over runs of 512 words (every block first decides its sequence from the first
+// launch's results); the draw, a wave a sequence. No atomics but an OR of error bits: a
+// result depends on the inputs alone.
 //
 // Sums and exponentials are 64-bit: a cumulative sum over 151936 words passes a given
 // random number at the same word as the definition's only if the sum is off by much
@@ -28,10 +28,14 @@ namespace {
 
 constexpr int DT = 256;                // threads of a block
 constexpr int64_t VSTEP = 8 * DT;      // words of a vector a thread
-constexpr int64_t MAX_PIECES = 64;     // of a row: one a lane
+constexpr int64_t MOST_TURNS = 1024;   // blocks of the first launch: those that run together
+constexpr int64_t MAX_RUNS = 4096;     // of a row
+constexpr int64_t RUN = 512;           // words of a vector a lane
 constexpr int MAXL = BSQ_MAX_DRAFTS;
 constexpr double LOG2E_64 = 1.4426950408889634074;
+constexpr float MAX_TEMPERATURE = 0x1p64f;
 static_assert(MAXL <= 64, "a lane for every drafted token");
+static_assert(2 * MAXL + 1 <= DT, "a thread for every row");
 
 enum { DRAW_TARGET, DRAW_REST, DRAW_OTHERS, DRAW_LARGEST, DRAW_NONE };
 
@@ -53,13 +57,17 @@ struct Decision {
 struct DArgs {
     const void *P, *Q;
     int64_t B, N, pseq, prow, qseq, qrow;
-    int L, rows, pieces;  // rows: of a sequence, L + 1 (+ L with draft logits)
-    int64_t len;          // words of a piece
+    int L, rows;          // rows: of a sequence, L + 1 (+ L with draft logits)
+    int64_t turn, turns;  // words of a block's turn; turns of a row
+    int64_t per;          // turns of a block: those of all rows one after another
+    int64_t pieces;       // parts of a row that blocks have, at most
+    int64_t run;          // words of a run
+    int runs, parts;      // of a row; blocks that share a row's runs
     const int32_t *tokens, *lens;
     const float *u, *r, *temp;
     int32_t *count, *out, *err;
     Piece *part;          // [B][rows][pieces]
-    double *rest;         // [B][pieces]
+    double *rest;         // [B][runs]
     Decision *dec;        // [B]
 };
 
@@ -72,13 +80,13 @@ __device__ __forceinline__ int seq_len(const DArgs &a, int64_t b, bool &bad)
     return n < 0 ? 0 : (n > a.L ? a.L : n);
 }
 
-// log2(e) over the temperature; 0 for a greedy sequence. (A temperature that is negative
-// or not finite is reported and counts as 0.)
+// log2(e) over the temperature; 0 for a greedy sequence. (A temperature that is negative,
+// NaN or above 2^64 is reported and counts as 0.)
 __device__ __forceinline__ double seq_scale(const DArgs &a, int64_t b, bool &bad)
 {
     if (!a.temp) return LOG2E_64;
     const float t = a.temp[b];
-    if (!(t >= 0.0f) || t == __builtin_inff()) {
+    if (!(t >= 0.0f && t <= MAX_TEMPERATURE)) {
         bad = true;
         return 0.0;
     }
@@ -96,17 +104,6 @@ struct Rows {
     }
 };
 
-__device__ __forceinline__ float finite_ref(float m) { return m == -__builtin_inff() ? 0.0f : m; }
-
-// Two pieces' largest logit and sum joined.
-__device__ __forceinline__ void join(float &m, double &s, float m2, double s2, double c)
-{
-    const float mm = m2 > m ? m2 : m;
-    const double ref = finite_ref(mm);
-    s = s * exp2_64((m - ref) * c) + s2 * exp2_64((m2 - ref) * c);
-    m = mm;
-}
-
 // The larger of two, of equal ones the lower index.
 __device__ __forceinline__ void larger(float &m, int &arg, float m2, int arg2)
 {
@@ -116,21 +113,31 @@ __device__ __forceinline__ void larger(float &m, int &arg, float m2, int arg2)
     }
 }
 
-constexpr int NV = 4;  // vectors a thread reads together
-
-template <bool BF16>
-__device__ __forceinline__ void piece_stats(const void *row, int64_t n0, int64_t n1, double c, float &m, double &s, int &arg)
+// A thread's largest logit (greedy: and its lowest index) and sum over words [n0, n1) of
+// a row, NV vectors at a time, the next ones in flight.
+template <bool BF16, int NV>
+__device__ __forceinline__ void piece_stats(const void *row, int64_t n0, int64_t n1, double c, double reach, float &m,
+                                            double &s, int &arg)
 {
     m = -__builtin_inff();
     s = 0.0;
     arg = INT32_MAX;
-    for (int64_t base = n0 + 8 * threadIdx.x; base < n1; base += NV * VSTEP) {
-        Words8<BF16> w[NV];
+    Exp2Below e2(m, c, reach);
+    Words8<BF16> next[NV];
+    auto load = [&](int64_t base) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int64_t at = base + k * VSTEP;
-            w[k].load(row, at < n1 ? at : n1, n1);
+            next[k].load(row, at < n1 ? at : n1, n1);
         }
+    };
+    load(n0 + 8 * threadIdx.x);
+    // (the same number of turns for every thread)
+    for (int64_t base = n0 + 8 * threadIdx.x; base < n1 + 8 * threadIdx.x; base += NV * VSTEP) {
+        Words8<BF16> w[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) w[k] = next[k];
+        if (base + NV * VSTEP < n1) load(base + NV * VSTEP);
         if (c == 0.0) {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
@@ -150,30 +157,35 @@ __device__ __forceinline__ void piece_stats(const void *row, int64_t n0, int64_t
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) mx = fmaxf(mx, w[k][e]);
-        const double ref = finite_ref(mx);
         if (mx > m) {
-            s *= exp2_64((m - ref) * c);
+            e2 = Exp2Below(mx, c, reach);
+            s *= e2(m);
             m = mx;
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += exp2_64((w[k][e] - ref) * c);
+            for (int e = 0; e < 8; ++e) s += e2(w[k][e]);
     }
 }
 
-// Largest logit and sum of every piece of every row that the sequence needs.
-template <bool PB, bool QB>
+// Largest logit and sum of every row that the sequences need: the turns of all rows, in
+// equal shares; a block leaves one piece of every row that it has turns of.
+template <bool PB, bool QB, int NV>
 __global__ __launch_bounds__(DT) void draft_rows_kernel(const DArgs a)
 {
     __shared__ float s_m[DT / 64];
     __shared__ double s_s[DT / 64];
     __shared__ int s_arg[DT / 64];
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-    const int64_t items = a.B * a.rows * a.pieces;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t rr = item / a.pieces, piece = item - rr * a.pieces, b = rr / a.rows;
+    const int64_t all = a.B * a.rows * a.turns;
+    const int64_t x0 = blockIdx.x * a.per, x1 = x0 + a.per < all ? x0 + a.per : all;
+    for (int64_t x = x0; x < x1;) {
+        const int64_t rr = x / a.turns, b = rr / a.rows;
         const int j = int(rr - b * a.rows);
+        const int64_t first = x - rr * a.turns, end = x1 < (rr + 1) * a.turns ? x1 : (rr + 1) * a.turns;
+        const int64_t count = end - x;
+        x = end;
         bool bad = false;
         const int n = seq_len(a, b, bad);
         const double c = seq_scale(a, b, bad);
@@ -181,19 +193,20 @@ __global__ __launch_bounds__(DT) void draft_rows_kernel(const DArgs a)
         const int i = target ? j : j - a.L - 1;
         if (target ? i > n : (i >= n || c == 0.0)) continue;
         const Rows<PB, QB> rows(a, b, i);
-        const int64_t n0 = piece * a.len, n1 = n0 + a.len < a.N ? n0 + a.len : a.N;
+        const int64_t n0 = first * a.turn, n1 = n0 + count * a.turn < a.N ? n0 + count * a.turn : a.N;
+        const double reach = 1000.0 / c;
         float m;
         double s;
         int arg;
-        if (target) piece_stats<PB>(rows.p, n0, n1, c, m, s, arg);
-        else piece_stats<QB>(rows.q, n0, n1, c, m, s, arg);
+        if (target) piece_stats<PB, NV>(rows.p, n0, n1, c, reach, m, s, arg);
+        else piece_stats<QB, NV>(rows.q, n0, n1, c, reach, m, s, arg);
         float wm = m;
         for (int d = 32; d > 0; d >>= 1) {
             const float m2 = __shfl_xor(wm, d);
             const int arg2 = __shfl_xor(arg, d);
             larger(wm, arg, m2, arg2);
         }
-        if (c != 0.0) s *= exp2_64((m - double(finite_ref(wm))) * c);
+        if (c != 0.0) s *= Exp2Below(wm, c, reach)(m);
         for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
         if (lane == 0) {
             s_m[w] = wm;
@@ -202,36 +215,19 @@ __global__ __launch_bounds__(DT) void draft_rows_kernel(const DArgs a)
         }
         __syncthreads();
         if (t == 0) {
-            for (int k = 1; k < DT / 64; ++k) {
-                if (c != 0.0) {
-                    join(wm, s, s_m[k], s_s[k], c);
-                } else {
-                    larger(wm, arg, s_m[k], s_arg[k]);
-                    s += s_s[k];
-                }
+            float m0 = wm;
+            for (int k = 1; k < DT / 64; ++k) larger(wm, arg, s_m[k], s_arg[k]);
+            if (c != 0.0) {
+                const Exp2Below e2(wm, c, reach);
+                s *= e2(m0);
+                for (int k = 1; k < DT / 64; ++k) s += s_s[k] * e2(s_m[k]);
+            } else {
+                for (int k = 1; k < DT / 64; ++k) s += s_s[k];
             }
-            a.part[item] = Piece{s, wm, arg};
+            a.part[rr * a.pieces + (blockIdx.x - rr * a.turns / a.per)] = Piece{s, wm, arg};
         }
         __syncthreads();
     }
-}
-
-// A row's pieces joined by a wave (every lane gets the result).
-__device__ __forceinline__ void row_stats(const DArgs &a, int64_t b, int j, double c, float &m, double &s, int &arg)
-{
-    const int lane = threadIdx.x & 63;
-    const bool in = lane < a.pieces;
-    const Piece p = in ? a.part[(b * a.rows + j) * a.pieces + lane] : Piece{0.0, -__builtin_inff(), INT32_MAX};
-    m = p.top;
-    s = p.sum;
-    arg = p.arg;
-    for (int d = 32; d > 0; d >>= 1) {
-        const float m2 = __shfl_xor(m, d);
-        const int arg2 = __shfl_xor(arg, d);
-        larger(m, arg, m2, arg2);
-    }
-    if (c != 0.0) s *= exp2_64((p.top - double(finite_ref(m))) * c);
-    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
 }
 
 // Whether a row has a probability to draw from.
@@ -244,51 +240,73 @@ struct DecideShared {
     int count, bad;
 };
 
-// Which drafts are accepted, by the whole block. (Ends with a barrier.)
+// Which drafts are accepted, by the whole block: some lanes join the pieces of a row, a lane
+// of the first wave decides a token. (Ends with a barrier.)
 template <bool PB, bool QB>
-__device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, DecideShared &sh)
+__device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, int n, double c, bool bad, DecideShared &sh)
 {
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-    bool bad = false;
-    const int n = seq_len(a, b, bad);
-    const double c = seq_scale(a, b, bad);
-    for (int j = w; j < a.rows; j += DT / 64) {
-        const bool target = j <= a.L;
-        const int i = target ? j : j - a.L - 1;
-        if (target ? i > n : (i >= n || c == 0.0)) continue;
-        float m;
-        double s;
-        int arg;
-        row_stats(a, b, j, c, m, s, arg);
-        if (lane == 0) {
+    const int t = threadIdx.x;
+    // what the decisions need of the tokens, read ahead of the join
+    int x = -1;
+    float u = 0.0f, zp = 0.0f, zq = 0.0f;
+    if (t < n) {
+        x = a.tokens[b * a.L + t];
+        u = a.u[b * a.L + t];
+        if (x < 0 || x >= a.N) {
+            bad = true;
+            x = -1;
+        } else if (c != 0.0) {
+            const Rows<PB, QB> rows(a, b, t);
+            zp = word_at<PB>(rows.p, x);
+            if (a.Q) zq = word_at<QB>(rows.q, x);
+        }
+    }
+    // up to 16 lanes a row
+    int log = 0;
+    while (log < 4 && (a.rows << (log + 1)) <= DT) ++log;
+    const int j = t >> log, lanes = 1 << log, g = t & (lanes - 1);
+    const bool target = j <= a.L;
+    const int i = target ? j : j - a.L - 1;
+    const bool need = j < a.rows && (target ? i <= n : (i < n && c != 0.0));
+    {
+        const int64_t rr = b * a.rows + j;
+        const Piece *p = a.part + rr * a.pieces;
+        const int end = need ? int(((rr + 1) * a.turns - 1) / a.per - rr * a.turns / a.per + 1) : 0;
+        float m = -__builtin_inff();
+        double s = 0.0;
+        int arg = INT32_MAX;
+#pragma unroll 4
+        for (int k = g; k < end; k += lanes) larger(m, arg, p[k].top, p[k].arg);
+        for (int d = lanes >> 1; d > 0; d >>= 1) {
+            const float m2 = __shfl_xor(m, d);
+            const int arg2 = __shfl_xor(arg, d);
+            larger(m, arg, m2, arg2);
+        }
+        const Exp2Below e2(m, c);
+#pragma unroll 4
+        for (int k = g; k < end; k += lanes) s += c != 0.0 ? p[k].sum * e2(p[k].top) : p[k].sum;
+        for (int d = lanes >> 1; d > 0; d >>= 1) s += __shfl_xor(s, d);
+        if (need && g == 0) {
             sh.m[j] = m;
             sh.s[j] = s;
             if (target) sh.arg[i] = arg;
         }
     }
     __syncthreads();
-    if (w == 0) {
+    if (t < 64) {
         bool ok = false;
-        if (lane < n) {
-            const int x = a.tokens[b * a.L + lane];
-            if (x < 0 || x >= a.N) {
-                bad = true;
-            } else if (c == 0.0) {
-                ok = x == sh.arg[lane] && sh.s[lane] == 0.0;
+        if (x >= 0) {
+            if (c == 0.0) {
+                ok = x == sh.arg[t] && sh.s[t] == 0.0;
             } else {
-                const Rows<PB, QB> rows(a, b, lane);
-                const double p = exp2_64((word_at<PB>(rows.p, x) - double(finite_ref(sh.m[lane]))) * c) / sh.s[lane];
+                const double p = Exp2Below(sh.m[t], c)(zp) / sh.s[t];
                 double q = 1.0;
-                if (a.Q) {
-                    const int j = a.L + 1 + lane;
-                    q = exp2_64((word_at<QB>(rows.q, x) - double(finite_ref(sh.m[j]))) * c) / sh.s[j];
-                }
-                ok = double(a.u[b * a.L + lane]) * q < p;
+                if (a.Q) q = Exp2Below(sh.m[a.L + 1 + t], c)(zq) / sh.s[a.L + 1 + t];
+                ok = double(u) * q < p;
             }
         }
-        const uint64_t no = ~__ballot(ok);
-        const uint64_t any = __ballot(bad);
-        if (lane == 0) {
+        const uint64_t no = ~__ballot(ok), any = __ballot(bad);
+        if (t == 0) {
             const int first = no ? __builtin_ctzll(no) : 64;
             sh.count = first < n ? first : n;
             sh.bad = any != 0;
@@ -314,9 +332,8 @@ __device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, DecideShar
     } else if (!a.Q) {
         d.kind = DRAW_OTHERS;
     } else {
-        const int j = a.L + 1 + d.count;
-        d.mq = sh.m[j];
-        d.sq = sh.s[j];
+        d.mq = sh.m[a.L + 1 + d.count];
+        d.sq = sh.s[a.L + 1 + d.count];
         d.kind = good_sum(d.sq) ? DRAW_REST : DRAW_TARGET;
         if (d.kind == DRAW_TARGET) d.bits |= BSQ_DEVERR_NONFINITE;
     }
@@ -324,82 +341,72 @@ __device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, DecideShar
     return d;
 }
 
-// The weight of word i in the draw.
+// The weight of words in the draw.
 struct Weight {
-    double c, mp, mq, ip, iq;
+    Exp2Below p, q;
+    double ip, iq;
     int kind;
     int64_t token;
-    __device__ __forceinline__ Weight(const Decision &d, double scale)
-        : c(scale), mp(d.mp), mq(d.mq), ip(1.0 / d.sp), iq(1.0 / d.sq), kind(d.kind), token(d.token)
+    __device__ __forceinline__ Weight(const Decision &d, double c)
+        : p(d.mp, c), q(d.mq, c), ip(1.0 / d.sp), iq(1.0 / d.sq), kind(d.kind), token(d.token)
     {
     }
-    __device__ __forceinline__ double operator()(float zp, float zq, int64_t i) const
+
+    // of eight words from `at` on (0 past `end`), and their sum
+    template <bool PB, bool QB>
+    __device__ __forceinline__ double eight(const Rows<PB, QB> &rows, int64_t at, int64_t end, double (&v)[8]) const
     {
-        const double p = exp2_64((zp - mp) * c);
-        if (kind == DRAW_TARGET) return p;
-        if (kind == DRAW_OTHERS) return i == token ? 0.0 : p;
-        const double q = exp2_64((zq - mq) * c);
-        const double d = p * ip - q * iq;
-        return d > 0.0 ? d : 0.0;
+        Words8<PB> zp;
+        zp.load(rows.p, at < end ? at : end, end);
+        double sum = 0.0;
+        if (kind == DRAW_REST) {
+            Words8<QB> zq;
+            zq.load(rows.q, at < end ? at : end, end);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double d = p(zp[e]) * ip - q(zq[e]) * iq;
+                v[e] = d > 0.0 ? d : 0.0;
+                sum += v[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = p(zp[e]);
+                if (kind == DRAW_OTHERS && at + e == token) v[e] = 0.0;
+                sum += v[e];
+            }
+        }
+        return sum;
     }
 };
 
-__device__ __forceinline__ double block_sum64(double v, double *s)
-{
-    const int t = threadIdx.x, lane = t & 63;
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    if (lane == 0) s[t >> 6] = v;
-    __syncthreads();
-    v = 0.0;
-    for (int w = 0; w < DT / 64; ++w) v += s[w];
-    __syncthreads();
-    return v;
-}
-
-// Decisions, and the weight of every piece of the row that the next token is drawn from.
+// Decisions, and the weight of every run of the row that the next token is drawn from.
 template <bool PB, bool QB>
 __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
 {
     __shared__ DecideShared sh;
-    __shared__ double s_sum[DT / 64];
-    const int t = threadIdx.x;
-    const int64_t items = a.B * a.pieces;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t b = item / a.pieces, piece = item - b * a.pieces;
-        const Decision d = decide<PB, QB>(a, b, sh);
-        if (piece == 0 && t == 0) {
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    const uint32_t items = uint32_t(a.B) * a.parts;
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t b = item / uint32_t(a.parts), part = item - b * a.parts;
+        bool bad = false;
+        const int n = seq_len(a, b, bad);
+        const double c = seq_scale(a, b, bad);
+        const Decision d = decide<PB, QB>(a, b, n, c, bad, sh);
+        if (part == 0 && t == 0) {
             a.dec[b] = d;
             if (d.bits && a.err) atomicOr(a.err, d.bits);
         }
-        if (d.kind != DRAW_LARGEST && d.kind != DRAW_NONE) {
-            bool bad = false;
-            const Weight weight(d, seq_scale(a, b, bad));
-            const int64_t n0 = piece * a.len, n1 = n0 + a.len < a.N ? n0 + a.len : a.N;
-            const bool again = d.kind == DRAW_REST || (d.kind == DRAW_OTHERS && d.token >= n0 && d.token < n1);
-            double s = 0.0;
-            if (again) {
-                const Rows<PB, QB> rows(a, b, d.count);
-                const bool rest = d.kind == DRAW_REST;
-                for (int64_t base = n0 + 8 * t; base < n1; base += 2 * VSTEP) {
-                    Words8<PB> p[2];
-                    Words8<QB> q[2];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int64_t at = base + k * VSTEP < n1 ? base + k * VSTEP : n1;
-                        p[k].load(rows.p, at, n1);
-                        if (rest) q[k].load(rows.q, at, n1);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) s += weight(p[k][e], rest ? q[k][e] : 0.0f, base + k * VSTEP + e);
-                }
-                s = block_sum64(s, s_sum);
-            } else {
-                const Piece p = a.part[(b * a.rows + d.count) * a.pieces + piece];
-                s = p.sum * exp2_64((p.top - double(d.mp)) * weight.c);
+        if (d.kind <= DRAW_OTHERS) {
+            const Weight weight(d, c);
+            const Rows<PB, QB> rows(a, b, d.count);
+            for (int r = part * (DT / 64) + w; r < a.runs; r += a.parts * (DT / 64)) {
+                const int64_t n0 = r * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
+                double s = 0.0, v[8];
+                for (int64_t at = n0; at < n1; at += RUN) s += weight.eight(rows, at + 8 * lane, n1, v);
+                for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+                if (lane == 0) a.rest[int64_t(b) * a.runs + r] = s;
             }
-            if (t == 0) a.rest[item] = s;
         }
         __syncthreads();
     }
@@ -416,120 +423,111 @@ __device__ __forceinline__ double wave_scan(double v)
     return v;
 }
 
-// The draw and the outputs: a block a sequence.
-template <bool PB, bool QB>
-__global__ __launch_bounds__(DT) void draft_draw_kernel(const DArgs a)
+// The first lane whose cumulative sum `incl` exceeds `target` and that holds some of it;
+// the last one that holds some where roundings leave none; -1 where no lane holds any.
+__device__ __forceinline__ int crossing(double incl, double own, double target)
 {
-    __shared__ double s_sum[DT / 64], s_target, s_before;
-    __shared__ int s_piece, s_kind, s_first;
-    __shared__ unsigned s_last;
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    const uint64_t some = __ballot(own > 0.0), past = __ballot(incl > target) & some;
+    return past ? __builtin_ctzll(past) : (some ? 63 - __builtin_clzll(some) : -1);
+}
+
+// The draw and the outputs: a wave a sequence.
+template <bool PB, bool QB>
+__global__ __launch_bounds__(64) void draft_draw_kernel(const DArgs a)
+{
+    const int lane = threadIdx.x;
     const int64_t b = blockIdx.x;
     Decision d = a.dec[b];
     bool bad = false;
-    const double c = seq_scale(a, b, bad);
-    if (w == 0) {
-        // the piece where the cumulative sum passes r times the whole
-        double v = lane < a.pieces && d.kind <= DRAW_OTHERS ? a.rest[b * a.pieces + lane] : 0.0;
-        double incl = wave_scan(v), all = __shfl(incl, 63);
-        int kind = d.kind;
-        if ((kind == DRAW_REST || kind == DRAW_OTHERS) && !good_sum(all)) {
-            // nothing is left beside what was refused (p and q differ by roundings alone)
-            kind = DRAW_TARGET;
-            v = 0.0;
-            if (lane < a.pieces) {
-                const Piece p = a.part[(b * a.rows + d.count) * a.pieces + lane];
-                v = p.sum * exp2_64((p.top - double(d.mp)) * c);
-            }
-            incl = wave_scan(v);
-            all = __shfl(incl, 63);
-        }
-        const double r = a.r[b], target = r * all;
-        const uint64_t past = __ballot(incl > target), some = __ballot(v > 0.0);
-        const uint64_t in = past & some;
-        const int piece = in ? __builtin_ctzll(in) : (some ? 63 - __builtin_clzll(some) : 0);
-        const double before = __shfl(incl - v, piece);
-        if (lane == 0) {
-            s_piece = piece;
-            s_kind = kind;
-            s_target = target;
-            s_before = before;
-            s_last = 0u;
-        }
-    }
-    __syncthreads();
-    d.kind = s_kind;
+    const double c = seq_scale(a, b, bad), r = a.r[b];
     int next = -1;
     if (d.kind == DRAW_LARGEST) {
         next = d.arg;
     } else if (d.kind != DRAW_NONE) {
+        // every lane `per` runs in order
+        const int per = (a.runs + 63) / 64, r0 = lane * per, r1 = r0 + per < a.runs ? r0 + per : a.runs;
+        const double *rest = a.rest + b * a.runs;
+        double own = 0.0;
+#pragma unroll 8
+        for (int k = r0; k < r1; ++k) own += rest[k];
+        const double incl = wave_scan(own), all = __shfl(incl, 63);
+        if (!good_sum(all)) {
+            // nothing is left beside what was refused (p and q differ by roundings alone): p itself
+            d.kind = DRAW_TARGET;
+        }
         const Weight weight(d, c);
         const Rows<PB, QB> rows(a, b, d.count);
-        const bool rest = d.kind == DRAW_REST;
-        const int64_t n0 = int64_t(s_piece) * a.len, n1 = n0 + a.len < a.N ? n0 + a.len : a.N;
-        double before = s_before;
-        const double target = s_target;
-        // runs of eight words a thread, in order
-        for (int64_t base = n0; base < n1 && next < 0; base += VSTEP) {
-            const int64_t at = base + 8 * t < n1 ? base + 8 * t : n1;
-            Words8<PB> p;
-            Words8<QB> q;
-            p.load(rows.p, at, n1);
-            if (rest) q.load(rows.q, at, n1);
-            double v[8], own = 0.0;
-            int last = -1;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] = weight(p[e], rest ? q[e] : 0.0f, at + e);
-                own += v[e];
-                if (v[e] > 0.0) last = e;
-            }
-            const double scan = wave_scan(own);
-            if (lane == 63) s_sum[w] = scan;
-            if (t == 0) s_first = DT;
-            __syncthreads();
-            double at0 = before, whole = before;
-            for (int k = 0; k < DT / 64; ++k) {
-                if (k < w) at0 += s_sum[k];
-                whole += s_sum[k];
-            }
-            if (last >= 0) {
-                atomicMax(&s_last, unsigned(at + last));
-                if (at0 + scan > target) atomicMin(&s_first, t);
-            }
-            __syncthreads();
-            const int first = s_first;
-            if (first < DT) {
-                if (t == first) {
-                    double sum = at0 + (scan - own);
-                    int pick = -1;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        sum += v[e];
-                        if (pick < 0 && sum > target && v[e] > 0.0) pick = e;
-                    }
-                    s_last = unsigned(at + (pick < 0 ? last : pick));
+        int64_t n0 = 0, n1 = a.N;
+        double before = 0.0, target = 0.0;
+        if (good_sum(all)) {
+            target = r * all;
+            const int who = crossing(incl, own, target);
+            // that lane's runs
+            double sum = incl - own;
+            int run = -1;
+            double at_run = sum;
+            for (int k = r0; k < r1; ++k) {
+                const double v = rest[k];
+                if (run < 0 && v > 0.0 && sum + v > target) {
+                    run = k;
+                    at_run = sum;
                 }
-                __syncthreads();
-                next = int(s_last);
+                sum += v;
             }
-            before = whole;
-            __syncthreads();
+            if (run < 0) {  // (roundings: its last run with a weight)
+                sum = incl - own;
+                for (int k = r0; k < r1; ++k) {
+                    const double v = rest[k];
+                    if (v > 0.0) {
+                        run = k;
+                        at_run = sum;
+                    }
+                    sum += v;
+                }
+            }
+            run = __shfl(run, who);
+            before = __shfl(at_run, who);
+            n0 = run * a.run;
+            n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
+        } else {
+            double s = 0.0, v[8];
+            for (int64_t at = 0; at < a.N; at += RUN) s += weight.eight(rows, at + 8 * lane, a.N, v);
+            for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+            target = r * s;
         }
-        // (roundings: the piece's words add up to less than its sum by the first pass)
-        if (next < 0) next = int(s_last);
+        int last = -1;
+        for (int64_t at = n0; at < n1 && next < 0; at += RUN) {
+            double v[8];
+            const double mine = weight.eight(rows, at + 8 * lane, n1, v), scan = wave_scan(mine);
+            const int who = crossing(before + scan, mine, target);
+            if (who >= 0) {
+                double sum = before + (scan - mine);
+                int pick = -1, some = -1;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sum += v[e];
+                    if (v[e] > 0.0) some = e;
+                    if (pick < 0 && v[e] > 0.0 && sum > target) pick = e;
+                }
+                const int word = __shfl(pick < 0 ? some : pick, who);
+                last = int(at + 8 * who + word);
+                if (__shfl(before + scan, who) > target) next = last;
+            }
+            before += __shfl(scan, 63);
+        }
+        if (next < 0) next = last;  // (roundings: the last word with a weight)
     }
-    for (int i = t; i <= a.L; i += DT)
+    for (int i = lane; i <= a.L; i += 64)
         a.out[b * (a.L + 1) + i] = i < d.count ? a.tokens[b * a.L + i] : (i == d.count ? next : -1);
-    if (t == 0) a.count[b] = d.count;
+    if (lane == 0) a.count[b] = d.count;
 }
 
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
 struct DLayout {
-    int rows, pieces;
-    int64_t len;
+    int rows, runs, parts, vectors;  // vectors: of a turn, a thread
+    int64_t turn, turns, per, blocks, pieces, run;
     size_t part, rest, dec, total;
 };
 
@@ -537,12 +535,20 @@ DLayout draft_layout(int64_t B, int64_t L, int64_t N, bool draft)
 {
     DLayout l{};
     l.rows = int(L + 1 + (draft ? L : 0));
-    // pieces of whole steps of a block, at most one a lane
-    const int64_t steps = (N + VSTEP - 1) / VSTEP;
-    const int64_t most = NV;  // steps that a thread reads together
-    int64_t per = std::max<int64_t>((steps + MAX_PIECES - 1) / MAX_PIECES, most);
-    l.len = per * VSTEP;
-    l.pieces = int((N + l.len - 1) / l.len);
+    // Turns of four vectors a thread, of two where that leaves compute units idle, in as
+    // many equal shares as blocks run together: a block's start and joins cost it half a turn.
+    const int64_t all_rows = std::max<int64_t>(B * l.rows, 1);
+    l.vectors = all_rows * ((N + 4 * VSTEP - 1) / (4 * VSTEP)) < 512 ? 2 : 4;
+    l.turn = l.vectors * VSTEP;
+    l.turns = (N + l.turn - 1) / l.turn;
+    l.per = (all_rows * l.turns + MOST_TURNS - 1) / MOST_TURNS;
+    l.blocks = (all_rows * l.turns + l.per - 1) / l.per;
+    l.pieces = (l.turns + l.per - 1) / l.per + 1;
+    l.run = ((N + RUN - 1) / RUN + MAX_RUNS - 1) / MAX_RUNS * RUN;
+    l.runs = int((N + l.run - 1) / l.run);
+    // blocks of a row's runs: a wave one run, or as many as leaves eight blocks a compute unit
+    const int64_t most = (l.runs + DT / 64 - 1) / (DT / 64);
+    l.parts = int(std::clamp<int64_t>(2048 / std::max<int64_t>(B, 1), 1, most));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t p = at;
@@ -550,22 +556,24 @@ DLayout draft_layout(int64_t B, int64_t L, int64_t N, bool draft)
         return p;
     };
     l.part = take(size_t(B) * l.rows * l.pieces * sizeof(Piece));
-    l.rest = take(size_t(B) * l.pieces * sizeof(double));
+    l.rest = take(size_t(B) * l.runs * sizeof(double));
     l.dec = take(size_t(B) * sizeof(Decision));
     l.total = at;
     return l;
 }
 
 template <bool PB, bool QB>
-hipError_t launch_draft(const DArgs &a, hipStream_t st)
+hipError_t launch_draft(const DArgs &a, const DLayout &l, hipStream_t st)
 {
     const int64_t most = int64_t(1) << 20;  // blocks of a launch; they walk the rest
-    hipLaunchKernelGGL((draft_rows_kernel<PB, QB>), dim3(unsigned(std::min(most, a.B * a.rows * a.pieces))), dim3(DT), 0, st, a);
+    const dim3 grid{unsigned(l.blocks)};
+    if (l.vectors == 2) hipLaunchKernelGGL((draft_rows_kernel<PB, QB, 2>), grid, dim3(DT), 0, st, a);
+    else hipLaunchKernelGGL((draft_rows_kernel<PB, QB, 4>), grid, dim3(DT), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((draft_rest_kernel<PB, QB>), dim3(unsigned(std::min(most, a.B * a.pieces))), dim3(DT), 0, st, a);
+    hipLaunchKernelGGL((draft_rest_kernel<PB, QB>), dim3(unsigned(std::min(most, a.B * a.parts))), dim3(DT), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL((draft_draw_kernel<PB, QB>), dim3(unsigned(a.B)), dim3(DT), 0, st, a);
+    hipLaunchKernelGGL((draft_draw_kernel<PB, QB>), dim3(unsigned(a.B)), dim3(64), 0, st, a);
     return hipGetLastError();
 }
 
@@ -588,8 +596,13 @@ hipError_t launch_draft_verify(const DraftCall &c, hipStream_t st)
     a.qrow = c.qrow;
     a.L = int(c.L);
     a.rows = l.rows;
+    a.turn = l.turn;
+    a.turns = l.turns;
+    a.per = l.per;
     a.pieces = l.pieces;
-    a.len = l.len;
+    a.run = l.run;
+    a.runs = l.runs;
+    a.parts = l.parts;
     a.tokens = c.tokens;
     a.lens = c.lens;
     a.u = c.u;
@@ -602,8 +615,8 @@ hipError_t launch_draft_verify(const DraftCall &c, hipStream_t st)
     a.rest = reinterpret_cast<double *>(ws + l.rest);
     a.dec = reinterpret_cast<Decision *>(ws + l.dec);
     const bool pb = c.p_dtype == BSQ_BF16, qb = c.Q ? c.q_dtype == BSQ_BF16 : pb;
-    if (pb) return qb ? launch_draft<true, true>(a, st) : launch_draft<true, false>(a, st);
-    return qb ? launch_draft<false, true>(a, st) : launch_draft<false, false>(a, st);
+    if (pb) return qb ? launch_draft<true, true>(a, l, st) : launch_draft<true, false>(a, l, st);
+    return qb ? launch_draft<false, true>(a, l, st) : launch_draft<false, false>(a, l, st);
 }
 
 }  // namespace bsq

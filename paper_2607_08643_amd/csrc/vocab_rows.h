@@ -58,31 +58,52 @@ __device__ __forceinline__ float word_at(const void *row, int64_t i)
     else return static_cast<const float *>(row)[i];
 }
 
-// 2^x in 64 bits for x up to 1000; 0 below -1000 (-inf among it), NaN for NaN.
-// x = n + f, |f| <= 1/2, n by adding 1.5 2^52; 2^f by the polynomial of degree 10
-// through its Chebyshev nodes (3.2e-16 of the value), n added to the exponent. Ten fma
-// beside some six other instructions: a library exp takes about three times as many.
-__device__ __forceinline__ double exp2_64(double x)
+// 2^(d c) in 64 bits, for products from -2000 to 1000; NaN for a NaN.
+// d c = n + f, |f| <= 1/2: n by adding 1.5 2^52, f with one rounding; 2^f = 1 + f g(f), g the
+// polynomial of degree 8 through its Chebyshev nodes (3.7e-14 of the value: of a draw from
+// 151936 words one in some 10^8 is another word for it; 1 at 0). 14 instructions of 64
+// bits; a library exp takes about three times as many.
+__device__ __forceinline__ double exp2_64(double d, double c)
 {
     constexpr double SHIFT = 6755399441055744.0;
-    const double t = x + SHIFT;
-    const double f = x - (t - SHIFT);
-    double p = 0x1.e6063f7217bc6p-28;
-    p = __builtin_fma(p, f, 0x1.b675bca4eeebbp-24);
-    p = __builtin_fma(p, f, 0x1.62bfd47773353p-20);
-    p = __builtin_fma(p, f, 0x1.ffcb54062e698p-17);
-    p = __builtin_fma(p, f, 0x1.430913096fd9fp-13);
-    p = __builtin_fma(p, f, 0x1.5d87fe9d7a584p-10);
-    p = __builtin_fma(p, f, 0x1.3b2ab6fba1ddap-7);
-    p = __builtin_fma(p, f, 0x1.c6b08d703ce49p-5);
-    p = __builtin_fma(p, f, 0x1.ebfbdff82c598p-3);
-    p = __builtin_fma(p, f, 0x1.62e42fefa3a19p-1);
-    p = __builtin_fma(p, f, 1.0);
-    const uint64_t b = __builtin_bit_cast(uint64_t, p);
-    const uint32_t hi = uint32_t(b >> 32) + (uint32_t(__builtin_bit_cast(uint64_t, t)) << 20);
-    const double r = __builtin_bit_cast(double, (uint64_t(hi) << 32) | uint32_t(b));
-    return x < -1000.0 ? 0.0 : r;
+    const double t = __builtin_fma(d, c, SHIFT);
+    const double f = __builtin_fma(d, c, SHIFT - t);
+    double g = 0x1.b63880a30e9ffp-24;
+    g = __builtin_fma(g, f, 0x1.63d136366db24p-20);
+    g = __builtin_fma(g, f, 0x1.ffcb9515a8016p-17);
+    g = __builtin_fma(g, f, 0x1.4308ac85aa947p-13);
+    g = __builtin_fma(g, f, 0x1.5d87fe86fe88ep-10);
+    g = __builtin_fma(g, f, 0x1.3b2ab7181b755p-7);
+    g = __builtin_fma(g, f, 0x1.c6b08d7047e52p-5);
+    g = __builtin_fma(g, f, 0x1.ebfbdff823cedp-3);
+    g = __builtin_fma(g, f, 0x1.62e42fefa39efp-1);
+    g = __builtin_fma(g, f, 1.0);
+    return __builtin_ldexp(g, int(uint32_t(__builtin_bit_cast(uint64_t, t))));
 }
+
+// 2^((z - ref) c) of logits z up to ref, c > 0. What is more than 1000 / c below ref (-inf
+// among it) is 0; NaN for a NaN, and where ref and z are +inf. (-inf as ref counts as 0.)
+struct Exp2Below {
+    double ref, c;
+    float lowest;
+    uint32_t far;  // high word of -1500 / c: 2^-1500 is 0
+    // reach: 1000 / c
+    __device__ __forceinline__ Exp2Below(float m, double scale, double reach) : c(scale)
+    {
+        const float r = m == -__builtin_inff() ? 0.0f : m;
+        ref = double(r);
+        const float low = float(ref - reach);
+        lowest = low > -__FLT_MAX__ ? low : -__FLT_MAX__;
+        far = uint32_t(__builtin_bit_cast(uint64_t, -1.5 * reach) >> 32);
+    }
+    __device__ __forceinline__ Exp2Below(float m, double scale) : Exp2Below(m, scale, 1000.0 / scale) {}
+    __device__ __forceinline__ double operator()(float z) const
+    {
+        uint64_t d = __builtin_bit_cast(uint64_t, double(z) - ref);
+        d = (uint64_t(z < lowest ? far : uint32_t(d >> 32)) << 32) | uint32_t(d);
+        return exp2_64(__builtin_bit_cast(double, d), c);
+    }
+};
 
 }  // namespace
 }  // namespace bsq
