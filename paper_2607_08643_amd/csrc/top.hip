@@ -2,7 +2,7 @@
 // equal ones by the lower word; -inf and NaN never listed), and the log of the sum of
 // exponentials over the whole row: one reading of the logits.
 //
-// A row is cut into segments, a block each. A wave keeps, in LDS, the words that may be
+// A block reads a row, or a segment of it where there are few rows. A wave keeps, in LDS, the words that may be
 // among the K largest: those not below a bound that only rises. The bound: every lane
 // knows the largest of what it has read; if in each of the W waves that hold words at
 // least ceil(K / W) lanes have read one of b or more, at least K words are not below b.
@@ -12,26 +12,31 @@
 // full cuts it to its K largest (exactly, by the 64-bit keys of value and word), so that
 // rows in rising order or of equal values need no more room.
 //
-// A second launch joins a row's segments: keys not below a bound found the same way, each
-// placed by the number of larger ones.
+// What is left is cut to a bound found the same way; each key's place is the number of
+// larger ones. Where rows are cut into segments a second launch does that for all
+// segments of a row.
 //
-// Bound by memory for many rows, by the two launches' latency for few.
+// Bound by memory for many rows (512 rows of 151936 words in bf16: 156 MB), by latency for few.
 #include <algorithm>
+#include <type_traits>
 
 #include "vocab_rows.h"
 
 namespace bsq {
 namespace {
 
-constexpr int TT = 512;                 // threads of a block
+constexpr int TT = 1024;                // threads of a block
 constexpr int TW = TT / 64;             // its waves
 constexpr int64_t TVEC = 8 * TT;        // words of a vector a thread
-constexpr int WCAP = 512;               // keys a wave holds
-constexpr int SEG_CAP = TW * WCAP;      // keys a segment leaves
+constexpr int WCAP = 384;               // keys a wave holds
+constexpr int OWN = WCAP / 64;          // a lane
+constexpr int LIST = TW * WCAP;         // a block
+constexpr int PASSED = 16;              // lanes whose words a wave looks through in LDS
 constexpr int64_t MAX_SEGS = 64;        // of a row: one a lane
-constexpr int64_t MAX_ITEMS = 2048;     // segments in a launch (workspace: 32 KiB each)
+constexpr int64_t MAX_ITEMS = 512;      // segments in a launch: those that run together (workspace: 48 KiB each)
 constexpr float LOG2E = 1.4426950408889634f;
 static_assert(BSQ_MAX_TOP + 64 <= WCAP - 64, "a cut list has room for more");
+static_assert(LIST < 65536, "places are of 16 bits");
 
 struct TArgs {
     const void *Z;
@@ -39,11 +44,20 @@ struct TArgs {
     int segs, K;
     float scale;
     int64_t row0;             // first row of the launch
-    uint64_t *keys;           // [rows of the launch][segs][SEG_CAP]
+    uint64_t *keys;           // [rows of the launch][segs][LIST]
     int32_t *counts;          // [rows of the launch][segs]
     float2 *stat;             // [rows of the launch][segs]: largest logit, sum of exponentials against it
     int32_t *ids;
     float *top, *lse;
+};
+
+struct TShared {
+    uint64_t list[LIST];      // of the waves; then the keys that reach the bound
+    uint32_t place[LIST / 2]; // of these: the number of larger ones, two of 16 bits
+    uint64_t best[BSQ_MAX_TOP];
+    __attribute__((aligned(16))) uint32_t bound[TW];
+    int count[TW];
+    float2 stat[TW];
 };
 
 // Values in order as whole numbers (-0 as +0).
@@ -73,37 +87,39 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
-// The q-th largest of the lanes' values (0 where there are fewer above LOWEST).
+// The q-th largest of the lanes' values, cut to its upper 16 bits: a bound that may lie a
+// little below (0 where there are fewer above LOWEST).
 __device__ __forceinline__ uint32_t lanes_rank(uint32_t v, int q)
 {
     uint32_t at = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
         const uint32_t up = at | (1u << bit);
         if (__popcll(__ballot(v >= up)) >= q) at = up;
     }
     return at < LOWEST ? 0u : at;
 }
 
-// The K largest of the n (<= 512, >= K) keys of a wave's list, in no order; the
+// The K largest of the n (<= WCAP, >= K) keys of a wave's list, in no order; the
 // smallest of them is returned.
 __device__ __forceinline__ uint64_t wave_cut(uint64_t *list, int n, int K)
 {
     const int lane = threadIdx.x & 63;
-    uint64_t k[WCAP / 64];
+    uint64_t k[OWN];
 #pragma unroll
-    for (int i = 0; i < WCAP / 64; ++i) k[i] = 64 * i + lane < n ? list[64 * i + lane] : 0;
+    for (int i = 0; i < OWN; ++i) k[i] = 64 * i + lane < n ? list[64 * i + lane] : 0;
     uint64_t at = 0;
     for (int bit = 63; bit >= 0; --bit) {
         const uint64_t up = at | (uint64_t(1) << bit);
         int c = 0;
 #pragma unroll
-        for (int i = 0; i < WCAP / 64; ++i) c += __popcll(__ballot(k[i] >= up));
+        for (int i = 0; i < OWN; ++i) c += __popcll(__ballot(k[i] >= up));
         if (c >= K) at = up;
     }
     wave_sync();
     int pos = 0;
 #pragma unroll
-    for (int i = 0; i < WCAP / 64; ++i) {
+    for (int i = 0; i < OWN; ++i) {
         const uint64_t keep = __ballot(k[i] >= at);
         if (k[i] >= at) list[pos + lanes_below(keep)] = k[i];
         pos += __popcll(keep);
@@ -122,19 +138,124 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2, flo
     m = mm;
 }
 
-constexpr int CV = 2;  // vectors of a chunk
-
-template <bool BF16>
-__global__ __launch_bounds__(TT) void top_rows_kernel(const TArgs a)
+// The smallest of the waves' bounds.
+__device__ __forceinline__ uint32_t block_bound(const uint32_t *s_bound, int waves)
 {
-    __shared__ uint64_t s_list[TW][WCAP];
-    __shared__ uint32_t s_bound[TW];
-    __shared__ int s_count[TW];
-    __shared__ float2 s_stat[TW];
+    uint32_t bound = ~0u;
+#pragma unroll
+    for (int h = 0; h < TW; h += 4) {
+        const vr_u32x4_t b = *reinterpret_cast<const volatile vr_u32x4_t *>(s_bound + h);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (h + k < waves && b[k] < bound) bound = b[k];
+    }
+    return bound;
+}
+
+// Of the lanes' keys (0: none) those not below `bound`: a wave's masks, its number, and the
+// number before it and of all waves. (A barrier.)
+__device__ __forceinline__ void count_keys(const uint64_t (&own)[OWN], uint32_t bound, uint64_t (&mask)[OWN], int &before,
+                                           int &all, TShared &sh)
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        mask[i] = __ballot(own[i] != 0 && uint32_t(own[i] >> 32) >= bound);
+        count += __popcll(mask[i]);
+    }
+    if (lane == 0) sh.count[w] = count;
+    __syncthreads();
+    before = 0;
+    all = 0;
+#pragma unroll
+    for (int k = 0; k < TW; ++k) {
+        before += k < w ? sh.count[k] : 0;
+        all += sh.count[k];
+    }
+}
+
+__device__ __forceinline__ void put_keys(const uint64_t (&own)[OWN], const uint64_t (&mask)[OWN], uint64_t *out)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        if ((mask[i] >> lane) & 1) out[lanes_below(mask[i])] = own[i];
+        out += __popcll(mask[i]);
+    }
+}
+
+// The K largest of the block's keys in order into sh.best; returns their number. No two
+// keys are equal. (sh.list is written: every wave has read its own. Ends with a barrier.)
+__device__ __forceinline__ int block_cut(const uint64_t (&own)[OWN], uint32_t bound, int K, TShared &sh)
+{
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    uint64_t mask[OWN];
+    int before, m;
+    count_keys(own, bound, mask, before, m, sh);
+    put_keys(own, mask, sh.list + before);
+    for (int i = t; 2 * i < m; i += TT) sh.place[i] = 0;
+    __syncthreads();
+    // a wave compares its share of the keys with all, four a lane (one reading of LDS for
+    // four comparisons)
+    const int k0 = m * w / TW, k1 = m * (w + 1) / TW;
+    for (int i0 = 0; i0 < m; i0 += 256) {
+        uint64_t key[4];
+        uint32_t place[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) key[e] = i0 + 64 * e + lane < m ? sh.list[i0 + 64 * e + lane] : ~uint64_t(0);
+#pragma unroll 4
+        for (int k = k0; k < k1; ++k) {
+            const uint64_t other = sh.list[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) place[e] += other > key[e] ? 1u : 0u;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = i0 + 64 * e + lane;
+            if (i < m) atomicAdd(&sh.place[i >> 1], place[e] << (16 * (i & 1)));
+        }
+    }
+    __syncthreads();
+    const int keep = m < K ? m : K;
+    for (int i = t; i < m; i += TT) {
+        const int at = (sh.place[i >> 1] >> (16 * (i & 1))) & 0xffff;
+        if (at < keep) sh.best[at] = sh.list[i];
+    }
+    __syncthreads();
+    return keep;
+}
+
+__device__ __forceinline__ void write_row(const TArgs &a, int64_t row, int n, const TShared &sh)
+{
+    for (int i = threadIdx.x; i < a.K; i += TT) {
+        const uint64_t key = i < n ? sh.best[i] : 0;
+        a.ids[row * a.K + i] = i < n ? int32_t(~uint32_t(key)) : -1;
+        a.top[row * a.K + i] = i < n ? unordered(uint32_t(key >> 32)) : -__builtin_inff();
+    }
+}
+
+// (a row with +inf: its sum is against 0)
+__device__ __forceinline__ float row_lse(const TArgs &a, float m, float s)
+{
+    return (m == __builtin_inff() ? 0.0f : m * a.scale) + logf(s);
+}
+
+// WHOLE: a block a row, its results; else a segment's candidates, largest logit and sum.
+// 32 bytes a thread and turn; eight waves a SIMD hide their latency (64 registers).
+template <bool BF16, bool WHOLE>
+__global__ __launch_bounds__(TT) __attribute__((amdgpu_waves_per_eu(8, 8))) void top_rows_kernel(const TArgs a)
+{
+    constexpr int CV = BF16 ? 2 : 1;                // vectors of a chunk
+    constexpr int E = 8 * CV, AT_ONCE = 64 / E;     // words of a lane; lanes whose words a wave looks through at once
+    using Raw = std::conditional_t<BF16, uint16_t, uint32_t>;
+    __shared__ TShared sh;
+    __shared__ __attribute__((aligned(16))) Raw s_raw[TW][PASSED][E];
+    __shared__ int s_from[TW][PASSED];
     const int t = threadIdx.x, lane = t & 63;
     const int w = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int64_t r = blockIdx.x / a.segs;
-    const int seg = int(blockIdx.x - r * a.segs);
+    const int64_t r = WHOLE ? blockIdx.x : blockIdx.x / a.segs;
+    const int seg = WHOLE ? 0 : int(blockIdx.x - r * a.segs);
     const int64_t row = a.row0 + r;
     const int64_t n0 = seg * a.len, n1 = n0 + a.len < a.N ? n0 + a.len : a.N;
     const void *z = BF16 ? static_cast<const void *>(static_cast<const uint16_t *>(a.Z) + row * a.ldz)
@@ -148,23 +269,26 @@ __global__ __launch_bounds__(TT) void top_rows_kernel(const TArgs a)
     uint64_t floor_key = 0; // of the wave's list, once it was cut
     int held = 0;
     float thr = unordered(LOWEST);
-    uint64_t *list = s_list[w];
+    uint64_t *list = sh.list + w * WCAP;
 
-    Words8<BF16> next[CV];
-    auto load = [&](int64_t base) {
-#pragma unroll
-        for (int k = 0; k < CV; ++k) {
-            const int64_t at = base + k * TVEC + 8 * t;
-            next[k].load(z, at < n1 ? at : n1, n1);
-        }
-    };
-    load(n0);
     int chunk = 0;
     for (int64_t base = n0; base < n1; base += CV * TVEC, ++chunk) {
         Words8<BF16> cur[CV];
+        // (offsets of 32 bits from the chunk's first word)
+        const void *p = BF16 ? static_cast<const void *>(static_cast<const uint16_t *>(z) + base)
+                             : static_cast<const float *>(z) + base;
+        const int64_t left = n1 - base;
+        if (left >= CV * TVEC) {
 #pragma unroll
-        for (int k = 0; k < CV; ++k) cur[k] = next[k];
-        if (base + CV * TVEC < n1) load(base + CV * TVEC);
+            for (int k = 0; k < CV; ++k) cur[k].load(p, k * unsigned(TVEC) + 8u * t);
+        } else {
+            const int end = int(left);
+#pragma unroll
+            for (int k = 0; k < CV; ++k) {
+                const int at = k * int(TVEC) + 8 * t;
+                cur[k].load(p, at < end ? at : end, end);
+            }
+        }
         float mx = -__builtin_inff();
 #pragma unroll
         for (int k = 0; k < CV; ++k)
@@ -183,147 +307,87 @@ __global__ __launch_bounds__(TT) void top_rows_kernel(const TArgs a)
         // the bound
         if ((chunk & (chunk + 1)) == 0) {
             const uint32_t b = q <= 64 ? lanes_rank(ordered(m), q) : 0u;
-            if (lane == 0) s_bound[w] = b;
+            if (lane == 0) sh.bound[w] = b;
             if (chunk == 0) __syncthreads();
         }
-        uint32_t bound = ~0u;
-#pragma unroll
-        for (int k = 0; k < TW; ++k) {
-            const uint32_t b = reinterpret_cast<volatile uint32_t *>(s_bound)[k];
-            if (k < waves && b < bound) bound = b;
-        }
+        const uint32_t bound = block_bound(sh.bound, waves);
         if (bound > LOWEST) {
             const float f = unordered(bound);
             thr = f > thr ? f : thr;
         }
-        if (__ballot(mx >= thr) == 0) continue;
-        uint32_t pass = 0;
+        // lanes that hold a word not below it leave theirs in LDS, where the wave looks through them
+        for (uint64_t some = __ballot(mx >= thr); some != 0;) {
+            const bool in = (some >> lane) & 1;
+            const int rank = lanes_below(some), n = __popcll(some) < PASSED ? __popcll(some) : PASSED;
+            if (in && rank < PASSED) {
+                constexpr int QUADS = int(sizeof(cur[0].raw) / 16);
 #pragma unroll
-        for (int k = 0; k < CV; ++k)
+                for (int k = 0; k < CV; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pass |= (cur[k][e] >= thr) ? 1u << (8 * k + e) : 0u;
-        while (__ballot(pass != 0)) {
-            const int e = pass ? __builtin_ctz(pass) : 0;
-            float v = cur[0][0];
-#pragma unroll
-            for (int k = 0; k < CV; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v = (e == 8 * k + i) ? cur[k][i] : v;
-            const uint64_t key = key_of(v, uint32_t(base + (e >> 3) * TVEC + 8 * t + (e & 7)));
-            const bool put = pass != 0 && key > floor_key;
-            pass &= pass - 1;
-            const uint64_t mask = __ballot(put);
-            if (put) list[held + lanes_below(mask)] = key;
-            held += __popcll(mask);
-            if (held > WCAP - 64) {
-                wave_sync();
-                floor_key = wave_cut(list, held, a.K);
-                held = a.K;
-                const float f = unordered(uint32_t(floor_key >> 32));
-                thr = f > thr ? f : thr;
+                    for (int h = 0; h < QUADS; ++h)
+                        reinterpret_cast<vr_u32x4_t *>(s_raw[w][rank])[k * QUADS + h] = cur[k].raw[h];
+                s_from[w][rank] = lane;
             }
+            some = __ballot(in && rank >= PASSED);
+            wave_sync();
+            for (int j = 0; j < n; j += AT_ONCE) {
+                const int from = j + lane / E, e = lane % E;
+                const bool there = from < n;
+                const Raw raw = s_raw[w][there ? from : 0][e];
+                const float v = BF16 ? bf16_to_f32(uint16_t(raw)) : __uint_as_float(raw);
+                const uint32_t word = uint32_t(base) + (e >> 3) * unsigned(TVEC) + 8u * (64 * w + s_from[w][there ? from : 0]) + (e & 7);
+                const uint64_t key = key_of(v, word);
+                const bool put = there && v >= thr && key > floor_key;
+                const uint64_t mask = __ballot(put);
+                if (put) list[held + lanes_below(mask)] = key;
+                held += __popcll(mask);
+                if (held > WCAP - 64) {
+                    wave_sync();
+                    floor_key = wave_cut(list, held, a.K);
+                    held = a.K;
+                    const float f = unordered(uint32_t(floor_key >> 32));
+                    thr = f > thr ? f : thr;
+                }
+            }
+            wave_sync();
         }
     }
-    // what is left at the bound of the whole segment, and its largest and sum
+    // what is left at the bound of all words, and their largest and sum
     {
         const uint32_t b = q <= 64 ? lanes_rank(ordered(m), q) : 0u;
-        if (lane == 0) s_bound[w] = b;
+        if (lane == 0) sh.bound[w] = b;
     }
     for (int d = 32; d > 0; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d), c);
-    wave_sync();
-    __syncthreads();
-    uint32_t bound = ~0u;
+    if (lane == 0) sh.stat[w] = make_float2(m, s);
+    uint64_t own[OWN];
 #pragma unroll
-    for (int k = 0; k < TW; ++k)
-        if (k < waves && s_bound[k] < bound) bound = s_bound[k];
-    int kept = 0;
-    for (int i = 0; i < held; i += 64) {
-        const uint64_t key = i + lane < held ? list[i + lane] : 0;
-        kept += __popcll(__ballot(key != 0 && uint32_t(key >> 32) >= bound));
-    }
-    if (lane == 0) {
-        s_count[w] = kept;
-        s_stat[w] = make_float2(m, s);
-    }
+    for (int i = 0; i < OWN; ++i) own[i] = 64 * i + lane < held ? list[64 * i + lane] : 0;
     __syncthreads();
-    int at = 0, all = 0;
-    for (int k = 0; k < TW; ++k) {
-        at += k < w ? s_count[k] : 0;
-        all += s_count[k];
-    }
-    const int64_t item = blockIdx.x;
-    uint64_t *out = a.keys + item * SEG_CAP + at;
-    for (int i = 0; i < held; i += 64) {
-        const uint64_t key = i + lane < held ? list[i + lane] : 0;
-        const bool keep = key != 0 && uint32_t(key >> 32) >= bound;
-        const uint64_t mask = __ballot(keep);
-        if (keep) out[lanes_below(mask)] = key;
-        out += __popcll(mask);
-    }
-    if (t == 0) {
-        for (int k = 1; k < TW; ++k) join(m, s, s_stat[k].x, s_stat[k].y, c);
-        a.counts[item] = all;
-        a.stat[item] = make_float2(m, s);
+    const uint32_t bound = block_bound(sh.bound, waves);
+    if (t == 0)
+        for (int k = 1; k < TW; ++k) join(m, s, sh.stat[k].x, sh.stat[k].y, c);
+    if constexpr (WHOLE) {
+        if (t == 0 && a.lse) a.lse[row] = row_lse(a, m, s);
+        write_row(a, row, block_cut(own, bound, a.K, sh), sh);
+    } else {
+        uint64_t mask[OWN];
+        int before, all;
+        count_keys(own, bound, mask, before, all, sh);
+        const int64_t item = blockIdx.x;
+        put_keys(own, mask, a.keys + item * LIST + before);
+        if (t == 0) {
+            a.counts[item] = all;
+            a.stat[item] = make_float2(m, s);
+        }
     }
 }
 
-// ---------------------------------------------------------------------------
-// A row's segments joined. Keys go through LDS in batches; each batch is cut to
-// the K largest, sorted.
-// ---------------------------------------------------------------------------
-constexpr int JCAP = 4096;
-
-// s_keys[0 .. n) -> its min(n, K) largest in order, at the front; returns their number.
-// s_rank: room for as many. By the whole block, ends with a barrier.
-__device__ __forceinline__ int block_cut(uint64_t *s_keys, uint64_t *s_rank, int n, int K, uint32_t *s_bound, int *s_n)
-{
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-    const int keep = n < K ? n : K;
-    // a bound that at least K keys reach, as in the first launch
-    const int q = (K + TW - 1) / TW;
-    uint64_t own[JCAP / TT];
-    uint32_t best = 0;
-#pragma unroll
-    for (int i = 0; i < JCAP / TT; ++i) {
-        own[i] = i * TT + t < n ? s_keys[i * TT + t] : 0;
-        const uint32_t v = uint32_t(own[i] >> 32);
-        best = v > best ? v : best;
-    }
-    const uint32_t b = lanes_rank(best, q);
-    if (lane == 0) s_bound[w] = b;
-    if (t == 0) *s_n = 0;
-    __syncthreads();
-    uint32_t bound = ~0u;
-#pragma unroll
-    for (int k = 0; k < TW; ++k) bound = s_bound[k] < bound ? s_bound[k] : bound;
-#pragma unroll
-    for (int i = 0; i < JCAP / TT; ++i) {
-        const bool in = own[i] != 0 && uint32_t(own[i] >> 32) >= bound;
-        const uint64_t mask = __ballot(in);
-        int at = 0;
-        if (lane == 0 && mask) at = atomicAdd(s_n, __popcll(mask));
-        at = __shfl(at, 0);
-        if (in) s_rank[at + lanes_below(mask)] = own[i];
-    }
-    __syncthreads();
-    const int m = *s_n;
-    // every key's place is the number of larger ones (no two are equal)
-    for (int i = t; i < m; i += TT) {
-        const uint64_t key = s_rank[i];
-        int place = 0;
-        for (int k = 0; k < m; ++k) place += s_rank[k] > key ? 1 : 0;
-        if (place < keep) s_keys[place] = key;
-    }
-    __syncthreads();
-    return keep;
-}
-
+// A row's segments joined, in batches of as many keys as a block holds.
 __global__ __launch_bounds__(TT) void top_join_kernel(const TArgs a)
 {
-    __shared__ uint64_t s_keys[JCAP], s_rank[JCAP];
-    __shared__ uint32_t s_bound[TW];
-    __shared__ int s_n, s_off[MAX_SEGS + 1];
-    const int t = threadIdx.x, lane = t & 63;
+    __shared__ TShared sh;
+    __shared__ int s_off[MAX_SEGS + 1];
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
     const int64_t r = blockIdx.x, row = a.row0 + r;
     if (t < 64) {
         int end = lane < a.segs ? a.counts[r * a.segs + lane] : 0;
@@ -334,40 +398,52 @@ __global__ __launch_bounds__(TT) void top_join_kernel(const TArgs a)
         s_off[lane + 1] = end;
         if (lane == 0) s_off[0] = 0;
     }
-    __syncthreads();
-    const int all = s_off[a.segs];
-    int n = 0;
-    for (int done = 0; done < all;) {
-        if (n == JCAP) {
-            __syncthreads();
-            n = block_cut(s_keys, s_rank, n, a.K, s_bound, &s_n);
-        }
-        const int take = all - done < JCAP - n ? all - done : JCAP - n;
-        for (int i = t; i < take; i += TT) {
-            int g = 0;  // the segment of key done + i
-#pragma unroll
-            for (int h = 32; h > 0; h >>= 1)
-                if (g + h < a.segs && s_off[g + h] <= done + i) g += h;
-            s_keys[n + i] = a.keys[(r * a.segs + g) * SEG_CAP + (done + i - s_off[g])];
-        }
-        n += take;
-        done += take;
-    }
-    __syncthreads();
-    n = block_cut(s_keys, s_rank, n, a.K, s_bound, &s_n);
-    for (int i = t; i < a.K; i += TT) {
-        const uint64_t key = i < n ? s_keys[i] : 0;
-        a.ids[row * a.K + i] = i < n ? int32_t(~uint32_t(key)) : -1;
-        a.top[row * a.K + i] = i < n ? unordered(uint32_t(key >> 32)) : -__builtin_inff();
-    }
-    if (a.lse && t < 64) {
+    if (t >= 64 && t < 128 && a.lse) {
         const float c = a.scale * LOG2E;
         const float2 v = lane < a.segs ? a.stat[r * a.segs + lane] : make_float2(-__builtin_inff(), 0.0f);
         float m = v.x, s = v.y;
         for (int d = 32; d > 0; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d), c);
-        // (a row with +inf: its sum is against 0)
-        if (t == 0) a.lse[row] = (m == __builtin_inff() ? 0.0f : m * a.scale) + logf(s);
+        if (lane == 0) a.lse[row] = row_lse(a, m, s);
     }
+    __syncthreads();
+    const int all = s_off[a.segs];
+    int n = 0;
+    for (int done = 0; done < all || done == 0;) {
+        // what is kept, then as many more: a wave a segment
+        if (t < n) sh.list[t] = sh.best[t];
+        const int take = LIST - n;
+        for (int g = w; g < a.segs; g += TW) {
+            const int first = s_off[g], count = s_off[g + 1] - first;
+            const uint64_t *src = a.keys + (r * a.segs + g) * LIST;
+            for (int i0 = 0; i0 < count; i0 += WCAP) {
+                uint64_t v[OWN];
+#pragma unroll
+                for (int e = 0; e < OWN; ++e) v[e] = i0 + 64 * e + lane < count ? src[i0 + 64 * e + lane] : 0;
+#pragma unroll
+                for (int e = 0; e < OWN; ++e) {
+                    const int at = first + i0 + 64 * e + lane - done;
+                    if (v[e] != 0 && at >= 0 && at < take) sh.list[n + at] = v[e];
+                }
+            }
+        }
+        __syncthreads();
+        const int batch = n + (all - done < take ? all - done : take);
+        done += take;
+        uint64_t own[OWN];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            own[i] = i * TT + t < batch ? sh.list[i * TT + t] : 0;
+            const uint32_t v = uint32_t(own[i] >> 32);
+            top = v > top ? v : top;
+        }
+        // a bound that at least K of them reach
+        const uint32_t b = lanes_rank(top, (a.K + TW - 1) / TW);
+        if (lane == 0) sh.bound[w] = b;
+        __syncthreads();
+        n = block_cut(own, block_bound(sh.bound, TW), a.K, sh);
+    }
+    write_row(a, row, n, sh);
 }
 
 // ---------------------------------------------------------------------------
@@ -382,23 +458,41 @@ struct TLayout {
 TLayout top_layout(int64_t T, int64_t N)
 {
     TLayout l{};
-    // segments until the launch fills the compute units (four blocks each)
-    const int64_t unit = CV * TVEC, steps = (N + unit - 1) / unit;
+    // segments of whole chunks until the launch fills the compute units (two blocks each)
+    const int64_t steps = (N + TVEC - 1) / TVEC;
     const int64_t want = std::clamp<int64_t>(MAX_ITEMS / std::max<int64_t>(T, 1), 1, std::min(MAX_SEGS, steps));
-    l.len = (steps + want - 1) / want * unit;
+    l.len = (steps + want - 1) / want * TVEC;
     l.segs = int((N + l.len - 1) / l.len);
-    l.rows = std::min<int64_t>(std::max<int64_t>(T, 1), MAX_ITEMS / l.segs);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t p = at;
         at += align256(bytes);
         return p;
     };
-    l.keys = take(size_t(l.rows) * l.segs * SEG_CAP * 8);
-    l.counts = take(size_t(l.rows) * l.segs * 4);
-    l.stat = take(size_t(l.rows) * l.segs * 8);
-    l.total = at;
+    l.rows = std::max<int64_t>(T, 1);
+    if (l.segs > 1) {
+        l.rows = std::min<int64_t>(l.rows, MAX_ITEMS / l.segs);
+        l.keys = take(size_t(l.rows) * l.segs * LIST * 8);
+        l.counts = take(size_t(l.rows) * l.segs * 4);
+        l.stat = take(size_t(l.rows) * l.segs * 8);
+    }
+    l.total = std::max<size_t>(at, 256);
     return l;
+}
+
+template <bool BF16>
+hipError_t launch_rows(const TArgs &a, int64_t rows, hipStream_t st)
+{
+    const dim3 grid(unsigned(rows * a.segs));
+    if (a.segs == 1) {
+        hipLaunchKernelGGL((top_rows_kernel<BF16, true>), grid, dim3(TT), 0, st, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((top_rows_kernel<BF16, false>), grid, dim3(TT), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(top_join_kernel, dim3(unsigned(rows)), dim3(TT), 0, st, a);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -428,12 +522,7 @@ hipError_t launch_top_logits(const TopCall &c, hipStream_t st)
     for (int64_t r0 = 0; e == hipSuccess && r0 < c.T; r0 += l.rows) {
         const int64_t rows = std::min(l.rows, c.T - r0);
         a.row0 = r0;
-        const dim3 grid(unsigned(rows * l.segs));
-        if (c.z_dtype == BSQ_BF16) hipLaunchKernelGGL((top_rows_kernel<true>), grid, dim3(TT), 0, st, a);
-        else hipLaunchKernelGGL((top_rows_kernel<false>), grid, dim3(TT), 0, st, a);
-        if ((e = hipGetLastError()) != hipSuccess) break;
-        hipLaunchKernelGGL(top_join_kernel, dim3(unsigned(rows)), dim3(TT), 0, st, a);
-        e = hipGetLastError();
+        e = c.z_dtype == BSQ_BF16 ? launch_rows<true>(a, rows, st) : launch_rows<false>(a, rows, st);
     }
     return e;
 }

@@ -18,17 +18,25 @@ template <bool BF16>
 struct Words8 {
     vr_u32x4_t raw[BF16 ? 1 : 2];
 
-    // words [at, at + 8) of `row`; those from `end` on are -inf
-    __device__ __forceinline__ void load(const void *row, int64_t at, int64_t end)
+    // words [at, at + 8) of `row`
+    template <typename Int>
+    __device__ __forceinline__ void load(const void *row, Int at)
+    {
+        if constexpr (BF16) {
+            raw[0] = *reinterpret_cast<const vr_bf16x8_raw_t *>(static_cast<const uint16_t *>(row) + at);
+        } else {
+            const vr_f32x4_raw_t *p = reinterpret_cast<const vr_f32x4_raw_t *>(static_cast<const float *>(row) + at);
+            raw[0] = p[0];
+            raw[1] = p[1];
+        }
+    }
+
+    // likewise; those from `end` on are -inf
+    template <typename Int>
+    __device__ __forceinline__ void load(const void *row, Int at, Int end)
     {
         if (at + 8 <= end) {
-            if constexpr (BF16) {
-                raw[0] = *reinterpret_cast<const vr_bf16x8_raw_t *>(static_cast<const uint16_t *>(row) + at);
-            } else {
-                const vr_f32x4_raw_t *p = reinterpret_cast<const vr_f32x4_raw_t *>(static_cast<const float *>(row) + at);
-                raw[0] = p[0];
-                raw[1] = p[1];
-            }
+            load(row, at);
             return;
         }
 #pragma unroll
