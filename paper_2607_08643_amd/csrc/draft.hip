@@ -200,14 +200,11 @@ __global__ __launch_bounds__(DT) void draft_rows_kernel(const DArgs a)
         int arg;
         if (target) piece_stats<PB, NV>(rows.p, n0, n1, c, reach, m, s, arg);
         else piece_stats<QB, NV>(rows.q, n0, n1, c, reach, m, s, arg);
-        float wm = m;
-        for (int d = 32; d > 0; d >>= 1) {
-            const float m2 = __shfl_xor(wm, d);
-            const int arg2 = __shfl_xor(arg, d);
-            larger(wm, arg, m2, arg2);
-        }
+        float wm = wave_max(m);
+        // (the lowest index among the lanes that hold the largest)
+        if (c == 0.0) arg = lane_value(wave_scan(m == wm ? arg : INT32_MAX, INT32_MAX, [](int x, int y) { return x < y ? x : y; }), 63);
         if (c != 0.0) s *= Exp2Below(wm, c, reach)(m);
-        for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+        s = wave_sum(s);
         if (lane == 0) {
             s_m[w] = wm;
             s_s[w] = s;
@@ -404,7 +401,7 @@ __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
                 const int64_t n0 = r * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
                 double s = 0.0, v[8];
                 for (int64_t at = n0; at < n1; at += RUN) s += weight.eight(rows, at + 8 * lane, n1, v);
-                for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+                s = wave_sum(s);
                 if (lane == 0) a.rest[int64_t(b) * a.runs + r] = s;
             }
         }
@@ -412,15 +409,9 @@ __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
     }
 }
 
-// Inclusive sums over a wave.
-__device__ __forceinline__ double wave_scan(double v)
+__device__ __forceinline__ double sum_scan(double v)
 {
-    const int lane = threadIdx.x & 63;
-    for (int d = 1; d < 64; d <<= 1) {
-        const double o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
+    return wave_scan(v, 0.0, [](double x, double y) { return x + y; });
 }
 
 // The first lane whose cumulative sum `incl` exceeds `target` and that holds some of it;
@@ -450,7 +441,7 @@ __global__ __launch_bounds__(64) void draft_draw_kernel(const DArgs a)
         double own = 0.0;
 #pragma unroll 8
         for (int k = r0; k < r1; ++k) own += rest[k];
-        const double incl = wave_scan(own), all = __shfl(incl, 63);
+        const double incl = sum_scan(own), all = lane_value(incl, 63);
         if (!good_sum(all)) {
             // nothing is left beside what was refused (p and q differ by roundings alone): p itself
             d.kind = DRAW_TARGET;
@@ -485,20 +476,19 @@ __global__ __launch_bounds__(64) void draft_draw_kernel(const DArgs a)
                     sum += v;
                 }
             }
-            run = __shfl(run, who);
-            before = __shfl(at_run, who);
+            run = lane_value(run, who);
+            before = lane_value(at_run, who);
             n0 = run * a.run;
             n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
         } else {
             double s = 0.0, v[8];
             for (int64_t at = 0; at < a.N; at += RUN) s += weight.eight(rows, at + 8 * lane, a.N, v);
-            for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
-            target = r * s;
+            target = r * wave_sum(s);
         }
         int last = -1;
         for (int64_t at = n0; at < n1 && next < 0; at += RUN) {
             double v[8];
-            const double mine = weight.eight(rows, at + 8 * lane, n1, v), scan = wave_scan(mine);
+            const double mine = weight.eight(rows, at + 8 * lane, n1, v), scan = sum_scan(mine);
             const int who = crossing(before + scan, mine, target);
             if (who >= 0) {
                 double sum = before + (scan - mine);
@@ -509,11 +499,11 @@ __global__ __launch_bounds__(64) void draft_draw_kernel(const DArgs a)
                     if (v[e] > 0.0) some = e;
                     if (pick < 0 && v[e] > 0.0 && sum > target) pick = e;
                 }
-                const int word = __shfl(pick < 0 ? some : pick, who);
+                const int word = lane_value(pick < 0 ? some : pick, who);
                 last = int(at + 8 * who + word);
-                if (__shfl(before + scan, who) > target) next = last;
+                if (lane_value(before + scan, who) > target) next = last;
             }
-            before += __shfl(scan, 63);
+            before += lane_value(scan, 63);
         }
         if (next < 0) next = last;  // (roundings: the last word with a weight)
     }

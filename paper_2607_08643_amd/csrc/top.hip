@@ -32,6 +32,8 @@ constexpr int WCAP = 384;               // keys a wave holds
 constexpr int OWN = WCAP / 64;          // a lane
 constexpr int LIST = TW * WCAP;         // a block
 constexpr int PASSED = 16;              // lanes whose words a wave looks through in LDS
+constexpr int BINS = 256;               // of values, four a lane
+constexpr int FEW = 1024;               // keys that are put in order by counting
 constexpr int64_t MAX_SEGS = 64;        // of a row: one a lane
 constexpr int64_t MAX_ITEMS = 512;      // segments in a launch: those that run together (workspace: 48 KiB each)
 constexpr float LOG2E = 1.4426950408889634f;
@@ -56,8 +58,9 @@ struct TShared {
     uint32_t place[LIST / 2]; // of these: the number of larger ones, two of 16 bits
     uint64_t best[BSQ_MAX_TOP];
     __attribute__((aligned(16))) uint32_t bound[TW];
-    int count[TW];
-    float2 stat[TW];
+    __attribute__((aligned(16))) uint32_t bins[BINS];  // 0 before a cut
+    int count[2][TW];
+    float2 stat[TW];          // of the waves (a cut reads their largest)
 };
 
 // Values in order as whole numbers (-0 as +0).
@@ -130,48 +133,55 @@ __device__ __forceinline__ uint64_t wave_cut(uint64_t *list, int n, int K)
 
 __device__ __forceinline__ float finite_ref(float m) { return m == -__builtin_inff() ? 0.0f : m; }
 
-// Largest value and sum of exponentials against it, joined with another pair.
-__device__ __forceinline__ void join(float &m, float &s, float m2, float s2, float c)
+// The lanes' largest values and sums of exponentials against them, joined. (Sums beside
+// an infinite largest value are against 0.)
+__device__ __forceinline__ void wave_join(float &m, float &s, float c)
 {
-    const float mm = m2 > m ? m2 : m, ref = (mm == __builtin_inff()) ? 0.0f : finite_ref(mm);
-    s = s * __builtin_amdgcn_exp2f((m - ref) * c) + s2 * __builtin_amdgcn_exp2f((m2 - ref) * c);
+    const float mm = wave_max(m), ref = (mm == __builtin_inff()) ? 0.0f : finite_ref(mm);
+    s = wave_sum(s * __builtin_amdgcn_exp2f((m - ref) * c));
     m = mm;
 }
 
-// The smallest of the waves' bounds.
-__device__ __forceinline__ uint32_t block_bound(const uint32_t *s_bound, int waves)
+// The smallest of the waves' bounds (those without words leave the largest).
+__device__ __forceinline__ uint32_t block_bound(const uint32_t *s_bound)
 {
     uint32_t bound = ~0u;
 #pragma unroll
     for (int h = 0; h < TW; h += 4) {
         const vr_u32x4_t b = *reinterpret_cast<const volatile vr_u32x4_t *>(s_bound + h);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (h + k < waves && b[k] < bound) bound = b[k];
+        for (int k = 0; k < 4; ++k) bound = b[k] < bound ? b[k] : bound;
     }
     return bound;
 }
 
-// Of the lanes' keys (0: none) those not below `bound`: a wave's masks, its number, and the
-// number before it and of all waves. (A barrier.)
-__device__ __forceinline__ void count_keys(const uint64_t (&own)[OWN], uint32_t bound, uint64_t (&mask)[OWN], int &before,
-                                           int &all, TShared &sh)
+// A wave's bound: what q lanes reach.
+__device__ __forceinline__ uint32_t wave_bound(uint32_t best, int q, bool words)
+{
+    return !words ? ~0u : (q <= 64 ? lanes_rank(best, q) : 0u);
+}
+
+// Of the lanes' keys (0: none) those of `least` or more: a wave's masks, and their number
+// before the wave's and of all waves. (A barrier; calls take turns with `slot`.)
+__device__ __forceinline__ void count_keys(const uint64_t (&own)[OWN], uint64_t least, uint64_t (&mask)[OWN], int &before,
+                                           int &all, int slot, TShared &sh)
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     int count = 0;
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
-        mask[i] = __ballot(own[i] != 0 && uint32_t(own[i] >> 32) >= bound);
+        mask[i] = __ballot(own[i] != 0 && own[i] >= least);
         count += __popcll(mask[i]);
     }
-    if (lane == 0) sh.count[w] = count;
+    if (lane == 0) sh.count[slot][w] = count;
     __syncthreads();
     before = 0;
     all = 0;
 #pragma unroll
     for (int k = 0; k < TW; ++k) {
-        before += k < w ? sh.count[k] : 0;
-        all += sh.count[k];
+        const int n = sh.count[slot][k];
+        before += k < w ? n : 0;
+        all += n;
     }
 }
 
@@ -185,14 +195,61 @@ __device__ __forceinline__ void put_keys(const uint64_t (&own)[OWN], const uint6
     }
 }
 
+// A bound nearer to the K-th largest: the values from `bound` to the largest in 256 bins, the
+// lowest bin that the K largest reach. (A barrier.)
+__device__ __forceinline__ uint32_t bin_bound(const uint64_t (&own)[OWN], uint32_t bound, int K, TShared &sh)
+{
+    const int lane = threadIdx.x & 63;
+    float most = -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < TW; ++k) most = fmaxf(most, sh.stat[k].x);
+    const uint32_t last = ordered(most), range = last > bound ? last - bound : 0;
+    const int shift = range < BINS ? 0 : 24 - __builtin_clz(range);
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const uint32_t v = uint32_t(own[i] >> 32);
+        if (own[i] != 0 && v >= bound) atomicAdd(&sh.bins[(v - bound) >> shift], 1u);
+    }
+    __syncthreads();
+    // lane 0 has the upper four bins
+    const int first = BINS - 4 - 4 * lane;
+    const vr_u32x4_t n = *reinterpret_cast<const vr_u32x4_t *>(sh.bins + first);
+    const int own_n = int(n[0] + n[1] + n[2] + n[3]);
+    const int upto = wave_scan(own_n, 0, [](int x, int y) { return x + y; });
+    const uint64_t reach = __ballot(upto >= K);
+    if (reach == 0) return bound;
+    int bin = 0, sum = upto - own_n;
+#pragma unroll
+    for (int k = 3; k >= 0; --k) {
+        if (sum < K) bin = first + k;
+        sum += int(n[k]);
+    }
+    bin = lane_value(bin, __builtin_ctzll(reach));
+    return bound + (uint32_t(bin) << shift);
+}
+
 // The K largest of the block's keys in order into sh.best; returns their number. No two
-// keys are equal. (sh.list is written: every wave has read its own. Ends with a barrier.)
+// keys are equal; at least min(K, all) are not below `bound`. (sh.list is written: every wave
+// has read its own. Ends with a barrier.)
 __device__ __forceinline__ int block_cut(const uint64_t (&own)[OWN], uint32_t bound, int K, TShared &sh)
 {
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
-    uint64_t mask[OWN];
+    uint64_t least = uint64_t(bin_bound(own, bound, K, sh)) << 32, mask[OWN];
     int before, m;
-    count_keys(own, bound, mask, before, m, sh);
+    count_keys(own, least, mask, before, m, 0, sh);
+    if (m > FEW) {
+        // many equal values: the K-th largest key, bit by bit
+        least = 0;
+        int slot = 1;
+        for (int bit = 63; bit >= 0; --bit) {
+            const uint64_t up = least | (uint64_t(1) << bit);
+            int n;
+            count_keys(own, up, mask, before, n, slot, sh);
+            slot ^= 1;
+            if (n >= K) least = up;
+        }
+        count_keys(own, least, mask, before, m, slot, sh);
+    }
     put_keys(own, mask, sh.list + before);
     for (int i = t; 2 * i < m; i += TT) sh.place[i] = 0;
     __syncthreads();
@@ -271,29 +328,39 @@ __global__ __launch_bounds__(TT) __attribute__((amdgpu_waves_per_eu(8, 8))) void
     float thr = unordered(LOWEST);
     uint64_t *list = sh.list + w * WCAP;
 
-    int chunk = 0;
-    for (int64_t base = n0; base < n1; base += CV * TVEC, ++chunk) {
-        Words8<BF16> cur[CV];
+    Words8<BF16> next[CV];  // the next chunk's, in flight
+    auto load = [&](int64_t base) {
         // (offsets of 32 bits from the chunk's first word)
         const void *p = BF16 ? static_cast<const void *>(static_cast<const uint16_t *>(z) + base)
                              : static_cast<const float *>(z) + base;
         const int64_t left = n1 - base;
         if (left >= CV * TVEC) {
 #pragma unroll
-            for (int k = 0; k < CV; ++k) cur[k].load(p, k * unsigned(TVEC) + 8u * t);
+            for (int k = 0; k < CV; ++k) next[k].load(p, k * unsigned(TVEC) + 8u * t);
         } else {
             const int end = int(left);
 #pragma unroll
             for (int k = 0; k < CV; ++k) {
                 const int at = k * int(TVEC) + 8 * t;
-                cur[k].load(p, at < end ? at : end, end);
+                next[k].load(p, at < end ? at : end, end);
             }
         }
+    };
+    load(n0);
+    int chunk = 0;
+    for (int64_t base = n0; base < n1; base += CV * TVEC, ++chunk) {
+        Words8<BF16> cur[CV];
+#pragma unroll
+        for (int k = 0; k < CV; ++k) cur[k] = next[k];
+        if (base + CV * TVEC < n1) load(base + CV * TVEC);
         float mx = -__builtin_inff();
 #pragma unroll
         for (int k = 0; k < CV; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) mx = fmaxf(mx, cur[k][e]);
+        // (taken apart again for the sum: kept, the words would take twice the registers)
+#pragma unroll
+        for (int k = 0; k < CV; ++k) asm volatile("" : "+v"(cur[k].raw[0]));
         // the sum, against the largest that the thread has read
         const float mm = mx > m ? mx : m, ref = (mm == __builtin_inff()) ? 0.0f : finite_ref(mm);
         if (mx > m) {
@@ -306,11 +373,11 @@ __global__ __launch_bounds__(TT) __attribute__((amdgpu_waves_per_eu(8, 8))) void
             for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f((cur[k][e] - ref) * c);
         // the bound
         if ((chunk & (chunk + 1)) == 0) {
-            const uint32_t b = q <= 64 ? lanes_rank(ordered(m), q) : 0u;
+            const uint32_t b = wave_bound(ordered(m), q, w < waves);
             if (lane == 0) sh.bound[w] = b;
             if (chunk == 0) __syncthreads();
         }
-        const uint32_t bound = block_bound(sh.bound, waves);
+        const uint32_t bound = block_bound(sh.bound);
         if (bound > LOWEST) {
             const float f = unordered(bound);
             thr = f > thr ? f : thr;
@@ -353,26 +420,30 @@ __global__ __launch_bounds__(TT) __attribute__((amdgpu_waves_per_eu(8, 8))) void
         }
     }
     // what is left at the bound of all words, and their largest and sum
-    {
-        const uint32_t b = q <= 64 ? lanes_rank(ordered(m), q) : 0u;
+    if (chunk > 1) {
+        const uint32_t b = wave_bound(ordered(m), q, w < waves);
         if (lane == 0) sh.bound[w] = b;
     }
-    for (int d = 32; d > 0; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d), c);
+    wave_join(m, s, c);
     if (lane == 0) sh.stat[w] = make_float2(m, s);
+    if (t < BINS) sh.bins[t] = 0;
     uint64_t own[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i) own[i] = 64 * i + lane < held ? list[64 * i + lane] : 0;
     __syncthreads();
-    const uint32_t bound = block_bound(sh.bound, waves);
-    if (t == 0)
-        for (int k = 1; k < TW; ++k) join(m, s, sh.stat[k].x, sh.stat[k].y, c);
+    const uint32_t bound = block_bound(sh.bound);
+    if (w == 0) {
+        m = lane < TW ? sh.stat[lane].x : -__builtin_inff();
+        s = lane < TW ? sh.stat[lane].y : 0.0f;
+        wave_join(m, s, c);
+    }
     if constexpr (WHOLE) {
         if (t == 0 && a.lse) a.lse[row] = row_lse(a, m, s);
         write_row(a, row, block_cut(own, bound, a.K, sh), sh);
     } else {
         uint64_t mask[OWN];
         int before, all;
-        count_keys(own, bound, mask, before, all, sh);
+        count_keys(own, uint64_t(bound) << 32, mask, before, all, 0, sh);
         const int64_t item = blockIdx.x;
         put_keys(own, mask, a.keys + item * LIST + before);
         if (t == 0) {
@@ -390,19 +461,15 @@ __global__ __launch_bounds__(TT) void top_join_kernel(const TArgs a)
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
     const int64_t r = blockIdx.x, row = a.row0 + r;
     if (t < 64) {
-        int end = lane < a.segs ? a.counts[r * a.segs + lane] : 0;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(end, d);
-            if (lane >= d) end += o;
-        }
-        s_off[lane + 1] = end;
+        const int count = lane < a.segs ? a.counts[r * a.segs + lane] : 0;
+        s_off[lane + 1] = wave_scan(count, 0, [](int x, int y) { return x + y; });
         if (lane == 0) s_off[0] = 0;
     }
     if (t >= 64 && t < 128 && a.lse) {
         const float c = a.scale * LOG2E;
         const float2 v = lane < a.segs ? a.stat[r * a.segs + lane] : make_float2(-__builtin_inff(), 0.0f);
         float m = v.x, s = v.y;
-        for (int d = 32; d > 0; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d), c);
+        wave_join(m, s, c);
         if (lane == 0) a.lse[row] = row_lse(a, m, s);
     }
     __syncthreads();
@@ -437,11 +504,16 @@ __global__ __launch_bounds__(TT) void top_join_kernel(const TArgs a)
             const uint32_t v = uint32_t(own[i] >> 32);
             top = v > top ? v : top;
         }
-        // a bound that at least K of them reach
+        // a bound that at least K of them reach, and the waves' largest
         const uint32_t b = lanes_rank(top, (a.K + TW - 1) / TW);
-        if (lane == 0) sh.bound[w] = b;
+        top = lane_value(wave_scan(top, 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }), 63);
+        if (lane == 0) {
+            sh.bound[w] = b;
+            sh.stat[w].x = top ? unordered(top) : -__builtin_inff();
+        }
+        if (t < BINS) sh.bins[t] = 0;
         __syncthreads();
-        n = block_cut(own, block_bound(sh.bound, TW), a.K, sh);
+        n = block_cut(own, block_bound(sh.bound), a.K, sh);
     }
     write_row(a, row, n, sh);
 }

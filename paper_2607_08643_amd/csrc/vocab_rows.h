@@ -113,5 +113,58 @@ struct Exp2Below {
     }
 };
 
+// Inclusive scans of a wave by data-parallel moves (rows of 16 lanes, then a row's last
+// lane into the next row, lane 31 into the upper half): lane 63 ends with all of it. A few
+// cycles a step, where a shuffle through LDS takes some hundred.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T moved(T v, T none)
+{
+    if constexpr (sizeof(T) == 8) {
+        const uint64_t a = __builtin_bit_cast(uint64_t, v), o = __builtin_bit_cast(uint64_t, none);
+        const uint32_t lo = __builtin_amdgcn_update_dpp(int(uint32_t(o)), int(uint32_t(a)), CTRL, ROWS, 0xf, false);
+        const uint32_t hi = __builtin_amdgcn_update_dpp(int(uint32_t(o >> 32)), int(uint32_t(a >> 32)), CTRL, ROWS, 0xf, false);
+        return __builtin_bit_cast(T, (uint64_t(hi) << 32) | lo);
+    } else {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL,
+                                                                 ROWS, 0xf, false));
+    }
+}
+
+template <typename T, typename Op>
+__device__ __forceinline__ T wave_scan(T v, T none, Op op)
+{
+    v = op(moved<0x111, 0xf>(v, none), v);  // from 1, 2, 4 and 8 lanes below in the row
+    v = op(moved<0x112, 0xf>(v, none), v);
+    v = op(moved<0x114, 0xf>(v, none), v);
+    v = op(moved<0x118, 0xf>(v, none), v);
+    v = op(moved<0x142, 0xa>(v, none), v);  // lane 15 of a row into rows 1 and 3
+    v = op(moved<0x143, 0xc>(v, none), v);  // lane 31 into rows 2 and 3
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ T lane_value(T v, int lane)
+{
+    if constexpr (sizeof(T) == 8) {
+        const uint64_t a = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = __builtin_amdgcn_readlane(int(uint32_t(a)), lane), hi = __builtin_amdgcn_readlane(int(uint32_t(a >> 32)), lane);
+        return __builtin_bit_cast(T, (uint64_t(hi) << 32) | lo);
+    } else {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v)
+{
+    return lane_value(wave_scan(v, T(0), [](T a, T b) { return a + b; }), 63);
+}
+
+// (NaN counts as nothing)
+__device__ __forceinline__ float wave_max(float v)
+{
+    return lane_value(wave_scan(v, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); }), 63);
+}
+
 }  // namespace
 }  // namespace bsq
