@@ -144,7 +144,7 @@ def lib():
     L.bsq_top_workspace_bytes.argtypes = [I64, I64, ct.POINTER(SZ)]
     L.bsq_top_logits.argtypes = [P, I32, I64, I64, I64, I32, ct.c_float, P, P, P, P, SZ, P]
     L.bsq_distill_workspace_bytes.argtypes = [I32, I64, I64, I64, I32, ct.POINTER(SZ)]
-    L.bsq_distill_kept_bytes.argtypes = [I64, I64, ct.POINTER(SZ)]
+    L.bsq_distill_kept_bytes.argtypes = [I64, I64, I64, I32, ct.POINTER(SZ)]
     L.bsq_distill_loss.argtypes = [P, I64, P, I64, I64, I64, I64, P, P, P, I32, ct.c_float, P, P, P, SZ, P, P, SZ, P]
     L.bsq_distill_grad.argtypes = [P, I64, P, I64, I64, I64, I64, P, P, P, I32, ct.c_float, P, P, P, SZ, P, I64, P, I64, I32,
                                    I32, P, P, SZ, P]
@@ -1066,9 +1066,9 @@ def bsq_distill_workspace_bytes(grad: bool, T: int, N: int, D: int, K: int) -> i
 
 
 @functools.lru_cache(maxsize=1024)
-def bsq_distill_kept_bytes(T: int, N: int) -> int:
+def bsq_distill_kept_bytes(T: int, N: int, D: int, K: int) -> int:
     out = ct.c_size_t(0)
-    _check(lib().bsq_distill_kept_bytes(T, N, ct.byref(out)), "bsq_distill_kept_bytes")
+    _check(lib().bsq_distill_kept_bytes(T, N, D, K, ct.byref(out)), "bsq_distill_kept_bytes")
     return out.value
 
 
@@ -1111,7 +1111,7 @@ def bsq_distill_loss(H: torch.Tensor, V: torch.Tensor, ids: torch.Tensor, top: t
         loss = torch.empty(T, dtype=torch.float32, device=dev) if loss is None else _need(loss, torch.float32, (T,), "loss")
         lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else _need(lse, torch.float32, (T,), "lse")
         if keep and kept is None:
-            kept = _workspace(bsq_distill_kept_bytes(T, N), dev)
+            kept = _workspace(bsq_distill_kept_bytes(T, N, D, K), dev)
         ws = ws if ws is not None else _workspace(need, dev)
         _check(lib().bsq_distill_loss(_ptr(H), ldh, _ptr(V), ldv, T, N, D, _ptr(ids), _ptr(top), _ptr(norm), K, scale,
                                       _ptr(loss), _ptr(lse), _ptr(kept), _kept_bytes(kept), _ptr(err), _ptr(ws),

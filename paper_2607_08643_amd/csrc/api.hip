@@ -943,7 +943,7 @@ bsq_status check_distill(bool grad, const void *H, int64_t ldh, const void *V, i
     if (!aligned(H, 2) || !aligned(V, 16) || !aligned(ids, 4) || !aligned(top, 4) || !aligned(norm, 4) ||
         !aligned(kept, 256) || !aligned(err, 4) || !aligned(ws, 256))
         return BSQ_ERR_ALIGN;
-    if (kept && kept_bytes < distill_kept_bytes(T, N)) return BSQ_ERR_BUFFER_TOO_SMALL;
+    if (kept && kept_bytes < distill_kept_bytes(T, N, D, K)) return BSQ_ERR_BUFFER_TOO_SMALL;
     if (ws_bytes < distill_ws_bytes(grad, T, N, D, K)) return BSQ_ERR_BUFFER_TOO_SMALL;
     return BSQ_OK;
 }
@@ -967,7 +967,7 @@ DistillCall distill_call(const void *H, int64_t ldh, const void *V, int64_t ldv,
     c.norm = norm;
     c.K = K;
     c.scale = scale;
-    c.kept = static_cast<float *>(kept);
+    c.kept = kept;
     return c;
 }
 }  // namespace
@@ -981,12 +981,12 @@ bsq_status bsq_distill_workspace_bytes(int32_t grad, int64_t T, int64_t N, int64
     return BSQ_OK;
 }
 
-bsq_status bsq_distill_kept_bytes(int64_t T, int64_t N, size_t *bytes)
+bsq_status bsq_distill_kept_bytes(int64_t T, int64_t N, int64_t D, int32_t K, size_t *bytes)
 {
-    if (!bytes) return BSQ_ERR_ARG;
-    const bsq_status s = check_xent_dims(T, N, 8);
+    if (!bytes || K < 1 || K > BSQ_MAX_TOP) return BSQ_ERR_ARG;
+    const bsq_status s = check_xent_dims(T, N, D);
     if (s != BSQ_OK) return s;
-    *bytes = distill_kept_bytes(T, N);
+    *bytes = distill_kept_bytes(T, N, D, K);
     return BSQ_OK;
 }
 

@@ -333,10 +333,10 @@ struct DistillCall {
     const float *top, *norm;  // norm may be NULL
     int K;
     float scale;
-    float *kept;              // may be NULL
+    void *kept;               // may be NULL
 };
 size_t distill_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D, int K);
-size_t distill_kept_bytes(int64_t T, int64_t N);
+size_t distill_kept_bytes(int64_t T, int64_t N, int64_t D, int K);
 hipError_t launch_distill_loss(const DistillCall &c, hipStream_t st);
 hipError_t launch_distill_grad(const DistillCall &c, hipStream_t st);
 

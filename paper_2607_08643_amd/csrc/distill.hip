@@ -12,9 +12,9 @@
 // ten tiles) while it holds the logits in registers. The loss is joined from the tiles'
 // statistics and these logits in 64 bits.
 //
-// Kept logits: the loss can leave its logits (fp32, compact rows) for the gradient, which
-// then makes d from them in one pass over memory and has one product less to do: 12
-// bytes a logit moved against 2 D operations.
+// Kept logits: the loss can leave its logits (fp32, compact rows) and what it found of
+// tokens and teacher for the gradient, which then makes d in one pass over memory and has
+// one product less to do: 10 bytes a logit moved against 2 D operations.
 #include "vocab_product.h"
 
 namespace bsq {
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blo
         const int64_t word = a.v0 + w, tok = a.rows[row];
         const f32x4_t *zp = reinterpret_cast<const f32x4_t *>(a.Z + row * a.ldz + word);
         const f32x4_t z[2] = {zp[0], zp[1]};
-        const float lse = a.lse[row], gg = a.g[row] * a.scale, total = a.total[tok];
+        const float lse = a.lse_in[tok], gg = a.g_in[tok] * a.scale, total = a.total[tok];
         const uint16_t *o = a.off + tok * (a.tiles + 1) + word / VBLK;
         const int beg = o[0], end = o[1];
         float v[8];
@@ -206,17 +206,20 @@ __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blo
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
-// The cross entropy's workspace, then what a token has of its teacher.
+// What the products need of tokens and teacher: compact rows, then a token's words and
+// their tiles. It lies in the workspace, or first in what a loss keeps for its gradient.
 struct SLayout {
     XLayout x;
-    size_t live, sid, sp, off, total, self, zk, bytes;
+    size_t live, sid, sp, off, total, base_bytes;
+    size_t logits, kept_bytes;          // kept: after the base
+    size_t self, zk, ws_bytes;
 };
 
 SLayout distill_layout(bool grad, int64_t T, int64_t N, int64_t D, int K)
 {
     SLayout l{};
     l.x = xent_layout(grad, T, N, D);
-    size_t at = align256(l.x.total);
+    size_t at = align256(l.x.compact);
     auto take = [&](size_t bytes) {
         const size_t p = at;
         at += align256(bytes);
@@ -228,16 +231,24 @@ SLayout distill_layout(bool grad, int64_t T, int64_t N, int64_t D, int K)
     l.sp = take(t * K * 4);
     l.off = take(t * size_t(l.x.tiles + 1) * 2);
     l.total = take(t * 4);
+    l.base_bytes = at;
+    l.logits = at;
+    l.kept_bytes = at + align256(size_t(T) * size_t(l.x.tiles) * VBLK * 4);
+    // workspace: the cross entropy's (its first part is the compact rows), the rest of the base
+    at = align256(l.x.total) + (l.base_bytes - align256(l.x.compact));
     l.self = take(t * 8);
     l.zk = take(grad ? 0 : t * K * 4);
-    l.bytes = at;
+    l.ws_bytes = at;
     return l;
 }
 
-// The teacher's words, and the arguments of the products.
-hipError_t launch_teacher(const DistillCall &c, const SLayout &l, XArgs &a, hipStream_t st)
+// The arguments of the products and, `make`, the teacher's words.
+hipError_t launch_teacher(const DistillCall &c, const SLayout &l, bool make, XArgs &a, hipStream_t st)
 {
     char *ws = static_cast<char *>(c.x.ws);
+    // (in the workspace the rest of the base follows the cross entropy's part)
+    char *base = c.kept ? static_cast<char *>(c.kept) : ws;
+    char *words = c.kept ? base : ws + (align256(l.x.total) - align256(l.x.compact));
     TeacherArgs h{};
     h.ids = c.ids;
     h.top = c.top;
@@ -247,43 +258,43 @@ hipError_t launch_teacher(const DistillCall &c, const SLayout &l, XArgs &a, hipS
     h.tiles = l.x.tiles;
     h.K = c.K;
     h.scale = c.scale;
-    h.live = reinterpret_cast<int64_t *>(ws + l.live);
-    h.sid = reinterpret_cast<int32_t *>(ws + l.sid);
-    h.sp = reinterpret_cast<float *>(ws + l.sp);
-    h.off = reinterpret_cast<uint16_t *>(ws + l.off);
-    h.total = reinterpret_cast<float *>(ws + l.total);
+    h.live = reinterpret_cast<int64_t *>(words + l.live);
+    h.sid = reinterpret_cast<int32_t *>(words + l.sid);
+    h.sp = reinterpret_cast<float *>(words + l.sp);
+    h.off = reinterpret_cast<uint16_t *>(words + l.off);
+    h.total = reinterpret_cast<float *>(words + l.total);
     h.self = reinterpret_cast<double *>(ws + l.self);
     h.err = c.x.err;
     XentCall x = c.x;
     x.target = h.live;
     x.err = nullptr;
-    a = xent_args(x, l.x);
+    a = xent_args(x, l.x, base);
     a.sid = h.sid;
     a.sp = h.sp;
     a.off = h.off;
     a.total = h.total;
     a.zk = reinterpret_cast<float *>(ws + l.zk);
-    a.Z = c.kept;
+    a.Z = c.kept ? reinterpret_cast<float *>(base + l.logits) : nullptr;
     a.ldz = l.x.tiles * VBLK;
     a.tiles = l.x.tiles;
     a.K = c.K;
     a.scale = c.scale;
-    if (c.x.T == 0) return hipSuccess;
+    if (!make || c.x.T == 0) return hipSuccess;
     hipLaunchKernelGGL(distill_teacher_kernel, dim3(unsigned(c.x.T)), dim3(XT), 0, st, h);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t distill_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D, int K) { return distill_layout(grad, T, N, D, K).bytes; }
+size_t distill_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D, int K) { return distill_layout(grad, T, N, D, K).ws_bytes; }
 
-size_t distill_kept_bytes(int64_t T, int64_t N) { return size_t(T) * size_t((N + VBLK - 1) / VBLK * VBLK) * 4; }
+size_t distill_kept_bytes(int64_t T, int64_t N, int64_t D, int K) { return distill_layout(false, T, N, D, K).kept_bytes; }
 
 hipError_t launch_distill_loss(const DistillCall &c, hipStream_t st)
 {
     const SLayout l = distill_layout(false, c.x.T, c.x.N, c.x.D, c.K);
     XArgs a{};
-    hipError_t e = launch_teacher(c, l, a, st);
+    hipError_t e = launch_teacher(c, l, true, a, st);
     if (e != hipSuccess) return e;
     char *ws = static_cast<char *>(c.x.ws);
     a.stat = reinterpret_cast<float2 *>(ws + l.x.stat);
@@ -296,13 +307,17 @@ hipError_t launch_distill_loss(const DistillCall &c, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_distill_grad(const DistillCall &c, hipStream_t st)
+hipError_t launch_distill_grad(const DistillCall &call, hipStream_t st)
 {
+    // (nothing was kept of no tokens)
+    DistillCall c = call;
+    if (c.x.T == 0) c.kept = nullptr;
     const SLayout l = distill_layout(true, c.x.T, c.x.N, c.x.D, c.K);
+    const bool kept = c.kept != nullptr;
     XArgs a{};
-    hipError_t e = launch_teacher(c, l, a, st);
+    const hipError_t e = launch_teacher(c, l, !kept, a, st);
     if (e != hipSuccess) return e;
-    return launch_grad(c.x, l.x, a, st, [&](const XArgs &piece) {
+    return launch_grad(c.x, l.x, a, kept, st, [&](const XArgs &piece) {
         if (!piece.Z) return launch_tokens<EPI_TPROB>(piece, piece.vp, 1, st);
         const int64_t blocks = (piece.vp + 8 * XT - 1) / (8 * XT), rows = (piece.T + 63) / 64 * 64;
         if (rows == 0) return hipSuccess;

@@ -460,25 +460,48 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
 #pragma unroll
             for (int j = 0; j < NF; ++j) acc[i][j] *= a.scale;
     }
+    // Visits them, two of every row at a time so that their loads are in flight together
+    // (the first tiles hold ten or more words of a row): f(the row's values, word, its place
+    // in the lists, i).
+    auto teacher_words = [&](auto f) {
+        int most = 0;
+#pragma unroll
+        for (int i = 0; i < MF; ++i) most = e_end[i] - e_beg[i] > most ? e_end[i] - e_beg[i] : most;
+        for (int e0 = 0; e0 < most; e0 += 2) {
+            int32_t word[MF][2];
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int e = e_beg[i] + e0 + k;
+                    word[i][k] = e < e_end[i] ? a.sid[int64_t(e_tok[i]) * a.K + e] : -1;
+                }
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (word[i][k] >= 0) f(acc[i], word[i][k], int64_t(e_tok[i]) * a.K + e_beg[i] + e0 + k, i);
+        }
+    };
     if constexpr (epi_stats(EPI)) {
         // per token: the largest of the tile's logits, the sum against it
         lds_barrier();
         float *s_max = reinterpret_cast<float *>(s_mem), *s_sum = s_max + WN * G::BR;
         const int64_t w0 = a.v0 + int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * NF * g;
+        if constexpr (TEACHER)
+            teacher_words([&](const f32x4_t(&v)[NF], int32_t word, int64_t at, int) {
+                const int64_t q = word - w0;
+                if (q < 0 || q >= 4 * NF) return;
+                float z = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 4 * NF; ++k) z = (q == k) ? v[k >> 2][k & 3] : z;
+                a.zk[at] = z;
+            });
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
             const int64_t row = rbeg + 16 * i;
             const int tg = (!TEACHER && row < a.Tp) ? a.tgt[row] : -1;
             if constexpr (TEACHER) {
-                const int64_t at = int64_t(e_tok[i]) * a.K;
-                for (int e = e_beg[i]; e < e_end[i]; ++e) {
-                    const int64_t q = a.sid[at + e] - w0;
-                    if (q < 0 || q >= 4 * NF) continue;
-                    float z = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < 4 * NF; ++k) z = (q == k) ? acc[i][k >> 2][k & 3] : z;
-                    a.zk[at + e] = z;
-                }
                 if (a.Z && row < live) {
                     f32x4_t *z = reinterpret_cast<f32x4_t *>(a.Z + row * a.ldz + w0);
 #pragma unroll
@@ -531,15 +554,16 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
         // products. A dV of 32 bits is asked for to be better than that: it takes what
         // remains as a second part (2^-18 is lost).
         const int64_t w0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * NF * g;
+        float gs[MF];
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
             const int64_t row = rbeg + 16 * i;
             const bool in = row < live;
             const int64_t tg = TEACHER ? -1 : int64_t(a.tgt[row]) - a.v0;
-            const float lse = a.lse[row], gg = TEACHER ? a.g[row] * a.scale : a.g[row];
+            const float lse = a.lse[row];
             float total = 1.0f;
+            gs[i] = TEACHER ? a.g[row] * a.scale : a.g[row];
             if constexpr (TEACHER) total = in ? a.total[e_tok[i]] : 0.0f;
-            float v[4 * NF];
 #pragma unroll
             for (int j = 0; j < NF; ++j)
 #pragma unroll
@@ -548,17 +572,24 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
                     float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * LOG2E);
                     if constexpr (TEACHER) p *= total;
                     else if (w == tg) p -= 1.0f;
-                    v[4 * j + r] = (in && a.v0 + w < a.N) ? gg * p : 0.0f;
+                    acc[i][j][r] = (in && a.v0 + w < a.N) ? gs[i] * p : 0.0f;
                 }
-            if constexpr (TEACHER) {
-                const int64_t at = int64_t(e_tok[i]) * a.K;
-                for (int e = e_beg[i]; e < e_end[i]; ++e) {
-                    const int64_t q = a.sid[at + e] - a.v0 - w0;
-                    const float p = gg * a.sp[at + e];
+        }
+        if constexpr (TEACHER) {
+            teacher_words([&](f32x4_t(&v)[NF], int32_t word, int64_t at, int i) {
+                const int64_t q = word - a.v0 - w0;
+                if (q < 0 || q >= 4 * NF) return;
+                const float p = gs[i] * a.sp[at];
 #pragma unroll
-                    for (int k = 0; k < 4 * NF; ++k) v[k] -= (q == k) ? p : 0.0f;
-                }
-            }
+                for (int k = 0; k < 4 * NF; ++k) v[k >> 2][k & 3] -= (q == k) ? p : 0.0f;
+            });
+        }
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int64_t row = rbeg + 16 * i;
+            float v[4 * NF];
+#pragma unroll
+            for (int k = 0; k < 4 * NF; ++k) v[k] = acc[i][k >> 2][k & 3];
             u32x4_t *q = reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w0);
 #pragma unroll
             for (int h = 0; h < NF / 2; ++h) {
@@ -682,6 +713,7 @@ struct XLayout {
     int64_t Tp, Dp, tiles, vp, dsp;
     int hsplit;
     size_t rows, pos, tgt, lse, g, ztgt, hc, stat, ds, dhp, total;
+    size_t compact;  // bytes of the compact rows, which lie first
 };
 
 XLayout xent_layout(bool grad, int64_t T, int64_t N, int64_t D)
@@ -700,6 +732,7 @@ XLayout xent_layout(bool grad, int64_t T, int64_t N, int64_t D)
     l.pos = take(size_t(std::max<int64_t>(T, 1)) * 4);
     l.tgt = take(size_t(l.Tp) * 4);
     l.hc = take(size_t(l.Tp) * size_t(l.Dp) * 2);
+    l.compact = at;
     if (!grad) {
         l.ztgt = take(size_t(l.Tp) * 4);
         l.stat = take(size_t(l.tiles) * size_t(l.Tp) * 8);
@@ -767,9 +800,10 @@ hipError_t launch_tokens(const XArgs &a, int64_t left, int splits, hipStream_t s
     return launch_gemm_shape<EPI, 8, 4, 2, 4>(a, a.T, left, splits, st);
 }
 
-XArgs xent_args(const XentCall &c, const XLayout &l)
+// base: what the compact rows (header, rows, pos, tgt, Hc) are offsets from
+XArgs xent_args(const XentCall &c, const XLayout &l, void *base)
 {
-    char *ws = static_cast<char *>(c.ws);
+    char *ws = static_cast<char *>(base);
     XArgs a{};
     a.hdr = reinterpret_cast<int32_t *>(ws);
     a.rows = reinterpret_cast<int32_t *>(ws + l.rows);
@@ -809,7 +843,8 @@ hipError_t launch_rows(const XArgs &a, int64_t rows, hipStream_t st)
 template <int EPI>
 hipError_t launch_stats(XArgs &a, const XLayout &l, hipStream_t st)
 {
-    hipError_t e = launch_rows(a, a.T <= 16 ? 16 : (a.T <= 32 ? 32 : a.Tp), st);
+    // (kept rows are read 64 deep by dV)
+    hipError_t e = launch_rows(a, a.T <= 16 && !a.Z ? 16 : (a.T <= 32 && !a.Z ? 32 : a.Tp), st);
     if (e != hipSuccess) return e;
     // A launch holds fewer than 2^32 work items, 512 or fewer of a tile: the tiles
     // of larger vocabularies go over several.
@@ -827,9 +862,9 @@ hipError_t launch_stats(XArgs &a, const XLayout &l, hipStream_t st)
 }
 
 // The gradient of the rows that have a loss, piece by piece of the vocabulary; make_d: the
-// launch that leaves a piece's d.
+// launch that leaves a piece's d. compact: the compact rows are there already.
 template <typename MakeD>
-hipError_t launch_grad(const XentCall &c, const XLayout &l, XArgs a, hipStream_t st, MakeD make_d)
+hipError_t launch_grad(const XentCall &c, const XLayout &l, XArgs a, bool compact, hipStream_t st, MakeD make_d)
 {
     char *ws = static_cast<char *>(c.ws);
     a.lse_in = c.lse_in;
@@ -853,7 +888,7 @@ hipError_t launch_grad(const XentCall &c, const XLayout &l, XArgs a, hipStream_t
     const bool two = c.dV && !a.dv_bf16;
     const int64_t vp = two ? l.dsp / 2 / VBLK * VBLK : l.vp;
     a.lo = two ? vp : 0;
-    hipError_t e = launch_rows(a, a.Tp, st);
+    hipError_t e = compact ? hipSuccess : launch_rows(a, a.Tp, st);
     for (int64_t v0 = 0; e == hipSuccess && v0 < c.N; v0 += vp) {
         a.v0 = v0;
         a.vp = std::min(vp, (c.N - v0 + VBLK - 1) / VBLK * VBLK);

@@ -70,7 +70,7 @@ size_t xent_ws_bytes(bool grad, int64_t T, int64_t N, int64_t D) { return xent_l
 hipError_t launch_xent_loss(const XentCall &c, hipStream_t st)
 {
     const XLayout l = xent_layout(false, c.T, c.N, c.D);
-    XArgs a = xent_args(c, l);
+    XArgs a = xent_args(c, l, c.ws);
     a.ztgt = reinterpret_cast<float *>(static_cast<char *>(c.ws) + l.ztgt);
     a.stat = reinterpret_cast<float2 *>(static_cast<char *>(c.ws) + l.stat);
     a.loss_out = c.loss;
@@ -86,8 +86,8 @@ hipError_t launch_xent_loss(const XentCall &c, hipStream_t st)
 hipError_t launch_xent_grad(const XentCall &c, hipStream_t st)
 {
     const XLayout l = xent_layout(true, c.T, c.N, c.D);
-    const XArgs a = xent_args(c, l);
-    return launch_grad(c, l, a, st, [&](const XArgs &piece) { return launch_tokens<EPI_PROB>(piece, piece.vp, 1, st); });
+    const XArgs a = xent_args(c, l, c.ws);
+    return launch_grad(c, l, a, false, st, [&](const XArgs &piece) { return launch_tokens<EPI_PROB>(piece, piece.vp, 1, st); });
 }
 
 }  // namespace bsq

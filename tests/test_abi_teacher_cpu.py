@@ -129,9 +129,10 @@ def test_distill_workspace(grad):
         with pytest.raises(bsq.BsqError) as e:
             bsq.bsq_distill_workspace_bytes(grad, *dims)
         assert e.value.status == status, dims
-    assert bsq.bsq_distill_kept_bytes(10, 257) == 10 * 512 * 4 and bsq.bsq_distill_kept_bytes(0, 1) == 0
-    with pytest.raises(bsq.BsqError):
-        bsq.bsq_distill_kept_bytes(-1, 5)
+    assert 10 * 512 * 4 < bsq.bsq_distill_kept_bytes(10, 257, 64, 5) < bsq.bsq_distill_kept_bytes(300, 257, 64, 5)
+    for dims in ((-1, 5, 8, 1), (1, 0, 8, 1), (1, 1, 8, 0)):
+        with pytest.raises(bsq.BsqError):
+            bsq.bsq_distill_kept_bytes(*dims)
 
 
 def test_distill_rejects_before_launch():
@@ -153,7 +154,7 @@ def test_distill_rejects_before_launch():
                    dict(a=FAKE + 2), dict(b=FAKE + 2), dict(kept=FAKE + 16, kept_bytes=BIG), dict(err=FAKE + 2), dict(ws=FAKE + 64)):
             assert call(g, **kw) == bsq.BSQ_ERR_ALIGN, kw
         assert call(g, ws_bytes=bsq.bsq_distill_workspace_bytes(g, 10, 100, 64, 5) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
-        assert call(g, kept=FAKE, kept_bytes=10 * 256 * 4 - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
+        assert call(g, kept=FAKE, kept_bytes=bsq.bsq_distill_kept_bytes(10, 100, 64, 5) - 1) == bsq.BSQ_ERR_BUFFER_TOO_SMALL
     assert call(True, dH=0) == bsq.BSQ_ERR_ARG
     assert call(True, lddh=63) == bsq.BSQ_ERR_SHAPE
     assert call(True, lddv=63) == bsq.BSQ_ERR_SHAPE
