@@ -727,8 +727,8 @@ bsq_status bsq_top_logits(const void *Z, int32_t z_dtype, int64_t ldz, int64_t T
 /* Device workspace of bsq_distill_loss (grad = 0), bsq_distill_grad (1); host only. */
 bsq_status bsq_distill_workspace_bytes(int32_t grad, int64_t T, int64_t N, int64_t D, int32_t K, size_t *bytes);
 
-/* Bytes of what a loss can keep for its gradient: 4 for each of T rows of N rounded up
- * to 256 words, and some for each token (host only). */
+/* Bytes of what a loss can keep for its gradient: 2 for each of T rows of N rounded up
+ * to 256 words, 4 more for each 64 words, and some for each token (host only). */
 bsq_status bsq_distill_kept_bytes(int64_t T, int64_t N, int64_t D, int32_t K, size_t *bytes);
 
 /*   H, V    as for bsq_xent_loss
@@ -748,7 +748,8 @@ bsq_status bsq_distill_loss(const void *H, int64_t ldh, const void *V, int64_t l
 /*   lse     device fp32 [T], as bsq_distill_loss wrote it for the same H, V, ids, top and scale
  *   g       device fp32 [T], the gradient of each token's loss
  *   kept    as bsq_distill_loss wrote it for the same H, V, ids, top, norm and scale, or
- *           NULL. With it the logits are not made again, and of those V alone is read
+ *           NULL. With it the logits are not made again, but for a dV of 32 bits: the
+ *           probabilities are then those kept, off by 2^-11 of each
  *   dH, dV, accumulate  as for bsq_xent_grad */
 bsq_status bsq_distill_grad(const void *H, int64_t ldh, const void *V, int64_t ldv, int64_t T, int64_t N, int64_t D,
                             const int32_t *ids, const float *top, const float *norm, int32_t K, float scale,

@@ -1102,7 +1102,7 @@ def bsq_distill_loss(H: torch.Tensor, V: torch.Tensor, ids: torch.Tensor, top: t
     (ids int32 [T, K], top fp32 [T, K]): (loss, lse), fp32 [T]. norm: the teacher's lse at this
     scale, fp32 [T] (None: the teacher's probabilities add up to 1 over its K words);
     scale: one over the temperature. keep: also leave the student's logits for
-    bsq_distill_grad (fp32; in `kept`, uint8, or a new buffer): (loss, lse, kept)."""
+    bsq_distill_grad (16 bits each; in `kept`, uint8, or a new buffer): (loss, lse, kept)."""
     T, N, D, K, ldh, ldv = _distill_shapes(H, V, ids, top, norm)
     keep = keep or kept is not None
     dev = _device_of((H, V, ids, top, norm, loss, lse, kept, err, ws), "bsq_distill_loss")

@@ -12,9 +12,11 @@
 // ten tiles) while it holds the logits in registers. The loss is joined from the tiles'
 // statistics and these logits in 64 bits.
 //
-// Kept logits: the loss can leave its logits (fp32, compact rows) and what it found of
-// tokens and teacher for the gradient, which then makes d in one pass over memory and has
-// one product less to do: 10 bytes a logit moved against 2 D operations.
+// What is kept: the loss can leave the exponentials of its logits, 16 bits each, and what
+// it found of tokens and teacher for the gradient, which then makes d in one pass over
+// memory and has one product less to do: 6 bytes a logit moved against 2 D operations. (d
+// is rounded to bf16 all the same, 2^-9, beside which 2^-11 adds nothing to speak of; for a
+// dV of 32 bits the logits are made again.)
 #include "vocab_product.h"
 
 namespace bsq {
@@ -163,7 +165,8 @@ __global__ __launch_bounds__(XT) void distill_join_kernel(const XArgs a, const d
     a.loss_out[m] = row >= 0 ? float(self[m] - z + double(a.total[m]) * lse) : 0.0f;
 }
 
-// d of a piece of the vocabulary from the kept logits: eight words a thread.
+// d of a piece of the vocabulary from what the loss kept: eight words a thread. The teacher's
+// words, where P q and p may nearly cancel, are made from their logits in 32 bits.
 __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blocks)
 {
     const int live = a.hdr[0];
@@ -171,36 +174,36 @@ __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blo
     if (row >= (int64_t(live) + 63) / 64 * 64) return;  // (d's rows are read 64 deep by dV)
     const int64_t w = (int64_t(blockIdx.x - row * blocks) * XT + threadIdx.x) * 8;
     if (w >= a.vp) return;
-    u32x4_t hi{0u, 0u, 0u, 0u}, lo{0u, 0u, 0u, 0u};
+    u32x4_t d{0u, 0u, 0u, 0u};
     if (row < live) {
         const int64_t word = a.v0 + w, tok = a.rows[row];
-        const f32x4_t *zp = reinterpret_cast<const f32x4_t *>(a.Z + row * a.ldz + word);
-        const f32x4_t z[2] = {zp[0], zp[1]};
+        const u32x4_t code = *reinterpret_cast<const u32x4_t *>(a.kept + row * a.ldk + word);
+        const float m = a.kept_max[row * (a.ldk / 64) + word / 64];
         const float lse = a.lse_in[tok], gg = a.g_in[tok] * a.scale, total = a.total[tok];
         const uint16_t *o = a.off + tok * (a.tiles + 1) + word / VBLK;
         const int beg = o[0], end = o[1];
+        const float f = m == -__builtin_inff() && lse == lse ? 0.0f : gg * (__builtin_amdgcn_exp2f((m - lse) * LOG2E) * total);
         float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            v[k] = word + k < a.N ? gg * (__builtin_amdgcn_exp2f((z[k >> 2][k & 3] - lse) * LOG2E) * total) : 0.0f;
+            v[k] = word + k < a.N ? f * kept_value((k & 1) ? code[k >> 1] >> 16 : code[k >> 1] & 0xffffu) : 0.0f;
+        int32_t last = -1;
         for (int e = beg; e < end; ++e) {
-            const int64_t q = a.sid[tok * a.K + e] - word;
-            const float p = gg * a.sp[tok * a.K + e];
+            const int64_t at = tok * a.K + e;
+            const int32_t id = a.sid[at];
+            const int64_t q = id - word;
+            if (q >= 0 && q < 8) {
+                const float p = gg * a.sp[at];
+                const float pq = gg * (__builtin_amdgcn_exp2f((a.zk[at] - lse) * LOG2E) * total);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] -= (q == k) ? p : 0.0f;
+                for (int k = 0; k < 8; ++k) v[k] = q == k ? (id == last ? v[k] : pq) - p : v[k];
+            }
+            last = id;
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            hi[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
-            if (a.lo == 0) continue;
-            const float x = v[2 * k] - __uint_as_float(hi[k] << 16);
-            const float y = v[2 * k + 1] - __uint_as_float(hi[k] & 0xffff0000u);
-            lo[k] = pack_bf16x2(x - x == 0.0f ? x : 0.0f, y - y == 0.0f ? y : 0.0f);
-        }
+        for (int k = 0; k < 4; ++k) d[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
     }
-    u32x4_t *q = reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w);
-    *q = hi;
-    if (a.lo) *reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w + a.lo) = lo;
+    *reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w) = d;
 }
 
 // ---------------------------------------------------------------------------
@@ -210,9 +213,9 @@ __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blo
 // their tiles. It lies in the workspace, or first in what a loss keeps for its gradient.
 struct SLayout {
     XLayout x;
-    size_t live, sid, sp, off, total, base_bytes;
-    size_t logits, kept_bytes;          // kept: after the base
-    size_t self, zk, ws_bytes;
+    size_t live, sid, sp, off, total, zk, base_bytes;
+    size_t codes, maxima, kept_bytes;   // kept: after the base
+    size_t self, ws_bytes;
 };
 
 SLayout distill_layout(bool grad, int64_t T, int64_t N, int64_t D, int K)
@@ -231,13 +234,14 @@ SLayout distill_layout(bool grad, int64_t T, int64_t N, int64_t D, int K)
     l.sp = take(t * K * 4);
     l.off = take(t * size_t(l.x.tiles + 1) * 2);
     l.total = take(t * 4);
+    l.zk = take(t * K * 4);
     l.base_bytes = at;
-    l.logits = at;
-    l.kept_bytes = at + align256(size_t(T) * size_t(l.x.tiles) * VBLK * 4);
+    l.codes = take(size_t(T) * size_t(l.x.tiles) * VBLK * 2);
+    l.maxima = take(size_t(T) * size_t(l.x.tiles) * (VBLK / 64) * 4);
+    l.kept_bytes = at;
     // workspace: the cross entropy's (its first part is the compact rows), the rest of the base
     at = align256(l.x.total) + (l.base_bytes - align256(l.x.compact));
     l.self = take(t * 8);
-    l.zk = take(grad ? 0 : t * K * 4);
     l.ws_bytes = at;
     return l;
 }
@@ -273,9 +277,10 @@ hipError_t launch_teacher(const DistillCall &c, const SLayout &l, bool make, XAr
     a.sp = h.sp;
     a.off = h.off;
     a.total = h.total;
-    a.zk = reinterpret_cast<float *>(ws + l.zk);
-    a.Z = c.kept ? reinterpret_cast<float *>(base + l.logits) : nullptr;
-    a.ldz = l.x.tiles * VBLK;
+    a.zk = reinterpret_cast<float *>(words + l.zk);
+    a.kept = c.kept ? reinterpret_cast<uint16_t *>(base + l.codes) : nullptr;
+    a.kept_max = c.kept ? reinterpret_cast<float *>(base + l.maxima) : nullptr;
+    a.ldk = l.x.tiles * VBLK;
     a.tiles = l.x.tiles;
     a.K = c.K;
     a.scale = c.scale;
@@ -309,16 +314,16 @@ hipError_t launch_distill_loss(const DistillCall &c, hipStream_t st)
 
 hipError_t launch_distill_grad(const DistillCall &call, hipStream_t st)
 {
-    // (nothing was kept of no tokens)
+    // (nothing was kept of no tokens; 16 bits are too few for d in two parts)
     DistillCall c = call;
-    if (c.x.T == 0) c.kept = nullptr;
+    if (c.x.T == 0 || (c.x.dV && c.x.dv_dtype == BSQ_F32)) c.kept = nullptr;
     const SLayout l = distill_layout(true, c.x.T, c.x.N, c.x.D, c.K);
     const bool kept = c.kept != nullptr;
     XArgs a{};
     const hipError_t e = launch_teacher(c, l, !kept, a, st);
     if (e != hipSuccess) return e;
     return launch_grad(c.x, l.x, a, kept, st, [&](const XArgs &piece) {
-        if (!piece.Z) return launch_tokens<EPI_TPROB>(piece, piece.vp, 1, st);
+        if (!kept) return launch_tokens<EPI_TPROB>(piece, piece.vp, 1, st);
         const int64_t blocks = (piece.vp + 8 * XT - 1) / (8 * XT), rows = (piece.T + 63) / 64 * 64;
         if (rows == 0) return hipSuccess;
         hipLaunchKernelGGL(distill_kept_kernel, dim3(unsigned(rows * blocks)), dim3(XT), 0, st, piece, int(blocks));

@@ -64,8 +64,11 @@ struct XArgs {
     const uint16_t *off;          // [T][tiles of the vocabulary + 1]
     const float *total;           // [T]: sum of the probabilities
     float *zk;                    // [T][K]: the student's logits of these words, scaled
-    float *Z;                     // [compact rows][ldz]: its logits as they are kept, scaled, or NULL
-    int64_t ldz, tiles;
+    // what is kept of the student's logits, or NULL: exponentials against the largest of
+    // each 64 words, in 16 bits, and those largest
+    uint16_t *kept;               // [compact rows][ldk]
+    float *kept_max;              // [compact rows][ldk / 64]
+    int64_t ldk, tiles;
     int K;
     float scale;
 };
@@ -227,6 +230,19 @@ __device__ __forceinline__ void join_stats(float &m, float &s, float m2, float s
     const float ref = (mm == -__builtin_inff()) ? 0.0f : mm;
     s = s * __builtin_amdgcn_exp2f((m - ref) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - ref) * LOG2E);
     m = mm;
+}
+
+// An exponential from 0 to 1 in 16 bits: six of exponent, ten of fraction (off by at most
+// 2^-11 of it; 0 below 2^-62). Made into a gradient that is rounded to bf16 (2^-9) it adds
+// 1/32 to that rounding's square.
+__device__ __forceinline__ uint32_t kept_code(float e)
+{
+    const int c = (int(__float_as_uint(e)) - 0x20000000 + 0x1000) >> 13;
+    return uint32_t(c < 0 ? 0 : (c > 0xffff ? 0xffff : c));
+}
+__device__ __forceinline__ float kept_value(uint32_t code)
+{
+    return code ? __uint_as_float((code << 13) + 0x20000000u) : 0.0f;
 }
 
 // Tiles of a product over `live` tokens, and splits of dH's depth: until the
@@ -501,13 +517,6 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
         for (int i = 0; i < MF; ++i) {
             const int64_t row = rbeg + 16 * i;
             const int tg = (!TEACHER && row < a.Tp) ? a.tgt[row] : -1;
-            if constexpr (TEACHER) {
-                if (a.Z && row < live) {
-                    f32x4_t *z = reinterpret_cast<f32x4_t *>(a.Z + row * a.ldz + w0);
-#pragma unroll
-                    for (int j = 0; j < NF; ++j) z[j] = acc[i][j];
-                }
-            }
             float m = -__builtin_inff();
             bool nan = false;
 #pragma unroll
@@ -527,12 +536,30 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
 #pragma unroll
             for (int j = 0; j < NF; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (w0 + 4 * j + r < a.N) s += __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * LOG2E);
+                for (int r = 0; r < 4; ++r) {
+                    const float e = __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * LOG2E);
+                    if (w0 + 4 * j + r < a.N) s += e;
+                    if constexpr (TEACHER) acc[i][j][r] = e;
+                }
             if (nan) s = __builtin_nanf("");
+            const float own = m;
             // join the four lanes of the token
 #pragma unroll
             for (int d = 16; d < 64; d <<= 1) join_stats(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+            if constexpr (TEACHER && NF == 4) {
+                if (a.kept && row < live) {
+                    const float f = own == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((own - m) * LOG2E);
+                    u32x4_t code[2];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        code[k >> 2][k & 3] = kept_code(acc[i][k >> 1][2 * (k & 1)] * f) |
+                                              kept_code(acc[i][k >> 1][2 * (k & 1) + 1] * f) << 16;
+                    u32x4_t *q = reinterpret_cast<u32x4_t *>(a.kept + row * a.ldk + w0);
+                    q[0] = code[0];
+                    q[1] = code[1];
+                    if (g == 0) a.kept_max[row * (a.ldk / 64) + w0 / 64] = m;
+                }
+            }
             if (g == 0) {
                 s_max[wn * G::BR + 16 * (wm * MF + i) + r16] = m;
                 s_sum[wn * G::BR + 16 * (wm * MF + i) + r16] = s;
@@ -844,7 +871,7 @@ template <int EPI>
 hipError_t launch_stats(XArgs &a, const XLayout &l, hipStream_t st)
 {
     // (kept rows are read 64 deep by dV)
-    hipError_t e = launch_rows(a, a.T <= 16 && !a.Z ? 16 : (a.T <= 32 && !a.Z ? 32 : a.Tp), st);
+    hipError_t e = launch_rows(a, a.T <= 16 && !a.kept ? 16 : (a.T <= 32 && !a.kept ? 32 : a.Tp), st);
     if (e != hipSuccess) return e;
     // A launch holds fewer than 2^32 work items, 512 or fewer of a tile: the tiles
     // of larger vocabularies go over several.
