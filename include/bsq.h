@@ -790,8 +790,8 @@ bsq_status bsq_draft_workspace_bytes(int32_t draft, int64_t B, int64_t L, int64_
  *   lens    device int32 [B], n_b of each (0 .. L; others are clamped and OR
  *           BSQ_DEVERR_BAD_SET), or NULL for L. Tokens, u and rows past it may hold anything
  *   u, r    device fp32 [B][L] and [B], in [0, 1)
- *   temperature  device fp32 [B], or NULL for ones; one that is negative, NaN or above
- *           2^64 counts as 0 and ORs BSQ_DEVERR_BAD_SET
+ *   temperature  device fp32 [B], or NULL for ones; one below 2^-64 counts as 0, and one
+ *           that is negative, NaN or above 2^64 too, which ORs BSQ_DEVERR_BAD_SET
  *   count   device int32 [B]: accepted tokens
  *   out     device int32 [B][L + 1]: the accepted tokens, the next one, then -1
  *   err     device int32 or NULL

@@ -8,17 +8,23 @@
 //   times the whole.
 // Without draft logits the drafts are certain: q_i(x_i) = 1, and x_i is taken out of p_i.
 //
-// Three launches: the largest logit and the sum of exponentials of every piece of
-// every row that is needed; the weights of the one row that the next token is drawn from,
-// summed over runs of 512 words (every block first decides its sequence from the first
-// launch's results); the draw, a wave a sequence. No atomics but an OR of error bits: a
-// result depends on the inputs alone.
+// Three launches: the largest logit and the sum of exponentials of every row that is
+// needed; the weights of the one row that the next token is drawn from, summed over runs of
+// 512 words (every block first decides its sequence from the first launch's results); the
+// draw, a wave a sequence. No atomics but an OR of error bits: a result depends on the
+// inputs alone.
 //
-// Sums and exponentials are 64-bit: a cumulative sum over 151936 words passes a given
-// random number at the same word as the definition's only if the sum is off by much
-// less than one word's share, and with exponentials of 32 bits one draw in some 200
-// would be another word. The rows are read once from memory and, of one or two rows a
-// sequence, once again from the caches.
+// Results are those of 64-bit sums. A cumulative sum over 151936 words passes a given
+// random number at the same word as the definition's only if it is off by much less than
+// one word's share; with exponentials of 32 bits one draw in some 200 would be another
+// word. Exponentials of 64 bits cost some 125 cycles a wave, four times what a word
+// costs to read, so the rows that only decide are summed in 32 (3e-5 of a ratio covers
+// every rounding), and where u q lies so near to p that this does not settle it the block
+// sums the two rows again in 64. max(p - q, 0) of the drawn row needs both rows' sums
+// before it can be formed: the second launch instead splits p and q into the words where p
+// is larger, by the first launch's sums, and their rests; the draw puts them together with
+// the exact sums. A word on the wrong side counts for less than 1e-5 of itself, and where
+// so little is left that this would matter the draw forms the weights anew.
 #include <algorithm>
 
 #include "vocab_rows.h"
@@ -28,24 +34,33 @@ namespace {
 
 constexpr int DT = 256;                // threads of a block
 constexpr int64_t VSTEP = 8 * DT;      // words of a vector a thread
-constexpr int64_t MOST_TURNS = 1024;   // blocks of the first launch: those that run together
+constexpr int64_t MOST_TURNS = 2048;   // blocks of the first launch: those that run together
 constexpr int64_t MAX_RUNS = 4096;     // of a row
 constexpr int64_t RUN = 512;           // words of a vector a lane
 constexpr int MAXL = BSQ_MAX_DRAFTS;
 constexpr double LOG2E_64 = 1.4426950408889634074;
-constexpr float MAX_TEMPERATURE = 0x1p64f;
+constexpr float MAX_TEMPERATURE = 0x1p64f, MIN_TEMPERATURE = 0x1p-64f;
+constexpr double UNSURE = 0x1p-15;     // of p: what the first launch's sums leave open, twice over
+constexpr double LITTLE = 0x1p-8;      // of the whole: max(p - q, 0) is formed word by word
 static_assert(MAXL <= 64, "a lane for every drafted token");
 static_assert(2 * MAXL + 1 <= DT, "a thread for every row");
 
 enum { DRAW_TARGET, DRAW_REST, DRAW_OTHERS, DRAW_LARGEST, DRAW_NONE };
 
 struct Piece {
-    double sum;   // of exponentials against `top` (greedy rows: 0, or NaN where a logit is)
+    double sum;   // of 32-bit exponentials against `top` (greedy rows: 0, or NaN where a logit is)
     float top;
     int32_t arg;  // greedy rows: lowest index of the largest
 };
 
-// What a sequence's drafts came to: `kind` of draw, the rows' largest logits and sums.
+// Of a run of the row that is drawn from: its words' exponentials (without the refused token
+// of a certain draft) and the draft row's, and of both those of the words where p > q.
+struct Run {
+    double p, q, above_p, above_q;
+};
+
+// What a sequence's drafts came to: `kind` of draw, the rows' largest logits and sums (those
+// of the first launch).
 struct Decision {
     int32_t count, kind;
     float mp, mq;
@@ -67,7 +82,7 @@ struct DArgs {
     const float *u, *r, *temp;
     int32_t *count, *out, *err;
     Piece *part;          // [B][rows][pieces]
-    double *rest;         // [B][runs]
+    Run *rest;            // [B][runs]
     Decision *dec;        // [B]
 };
 
@@ -80,8 +95,8 @@ __device__ __forceinline__ int seq_len(const DArgs &a, int64_t b, bool &bad)
     return n < 0 ? 0 : (n > a.L ? a.L : n);
 }
 
-// log2(e) over the temperature; 0 for a greedy sequence. (A temperature that is negative,
-// NaN or above 2^64 is reported and counts as 0.)
+// log2(e) over the temperature; 0 for a greedy sequence, one below 2^-64 among them. (A
+// temperature that is negative, NaN or above 2^64 is reported and counts as 0.)
 __device__ __forceinline__ double seq_scale(const DArgs &a, int64_t b, bool &bad)
 {
     if (!a.temp) return LOG2E_64;
@@ -90,7 +105,7 @@ __device__ __forceinline__ double seq_scale(const DArgs &a, int64_t b, bool &bad
         bad = true;
         return 0.0;
     }
-    return t == 0.0f ? 0.0 : LOG2E_64 / double(t);
+    return t < MIN_TEMPERATURE ? 0.0 : LOG2E_64 / double(t);
 }
 
 template <bool PB, bool QB>
@@ -116,13 +131,11 @@ __device__ __forceinline__ void larger(float &m, int &arg, float m2, int arg2)
 // A thread's largest logit (greedy: and its lowest index) and sum over words [n0, n1) of
 // a row, NV vectors at a time, the next ones in flight.
 template <bool BF16, int NV>
-__device__ __forceinline__ void piece_stats(const void *row, int64_t n0, int64_t n1, double c, double reach, float &m,
-                                            double &s, int &arg)
+__device__ __forceinline__ void piece_stats(const void *row, int64_t n0, int64_t n1, float c, float &m, double &s, int &arg)
 {
     m = -__builtin_inff();
     s = 0.0;
     arg = INT32_MAX;
-    Exp2Below e2(m, c, reach);
     Words8<BF16> next[NV];
     auto load = [&](int64_t base) {
 #pragma unroll
@@ -138,7 +151,7 @@ __device__ __forceinline__ void piece_stats(const void *row, int64_t n0, int64_t
 #pragma unroll
         for (int k = 0; k < NV; ++k) w[k] = next[k];
         if (base + NV * VSTEP < n1) load(base + NV * VSTEP);
-        if (c == 0.0) {
+        if (c == 0.0f) {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -157,15 +170,22 @@ __device__ __forceinline__ void piece_stats(const void *row, int64_t n0, int64_t
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) mx = fmaxf(mx, w[k][e]);
-        if (mx > m) {
-            e2 = Exp2Below(mx, c, reach);
-            s *= e2(m);
-            m = mx;
-        }
+        // (taken apart again for the sum: kept, the words would take twice the registers)
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += e2(w[k][e]);
+            for (int h = 0; h < int(sizeof(w[0].raw) / 16); ++h) asm volatile("" : "+v"(w[k].raw[h]));
+        const float ref = mx == -__builtin_inff() ? 0.0f : mx;
+        if (mx > m) {
+            s *= double(__builtin_amdgcn_exp2f((m - ref) * c));
+            m = mx;
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f((w[k][e] - ref) * c);
+        s += double(sum);
     }
 }
 
@@ -198,8 +218,8 @@ __global__ __launch_bounds__(DT) void draft_rows_kernel(const DArgs a)
         float m;
         double s;
         int arg;
-        if (target) piece_stats<PB, NV>(rows.p, n0, n1, c, reach, m, s, arg);
-        else piece_stats<QB, NV>(rows.q, n0, n1, c, reach, m, s, arg);
+        if (target) piece_stats<PB, NV>(rows.p, n0, n1, float(c), m, s, arg);
+        else piece_stats<QB, NV>(rows.q, n0, n1, float(c), m, s, arg);
         float wm = wave_max(m);
         // (the lowest index among the lanes that hold the largest)
         if (c == 0.0) arg = lane_value(wave_scan(m == wm ? arg : INT32_MAX, INT32_MAX, [](int x, int y) { return x < y ? x : y; }), 63);
@@ -234,13 +254,37 @@ struct DecideShared {
     float m[2 * MAXL + 1];
     double s[2 * MAXL + 1];
     int arg[MAXL + 1];
-    int count, bad;
+    double sum[DT / 64];
+    int count, bad, ask;
 };
+
+// Sum of exponentials of a whole row in 64 bits, by the block. (Two barriers.)
+template <bool BF16>
+__device__ __forceinline__ double row_sum(const void *row, int64_t N, float m, double c, double reach, double *s_sum)
+{
+    const int t = threadIdx.x;
+    const Exp2Below e2(m, c, reach);
+    double s = 0.0;
+    for (int64_t at = 8 * t; at < N; at += VSTEP) {
+        Words8<BF16> w;
+        w.load(row, at, N);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += e2(w[e]);
+    }
+    s = wave_sum(s);
+    if ((t & 63) == 0) s_sum[t >> 6] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int w = 0; w < DT / 64; ++w) s += s_sum[w];
+    __syncthreads();
+    return s;
+}
 
 // Which drafts are accepted, by the whole block: some lanes join the pieces of a row, a lane
 // of the first wave decides a token. (Ends with a barrier.)
 template <bool PB, bool QB>
-__device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, int n, double c, bool bad, DecideShared &sh)
+__device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, int n, double c, double reach, bool bad,
+                                           DecideShared &sh)
 {
     const int t = threadIdx.x;
     // what the decisions need of the tokens, read ahead of the join
@@ -279,7 +323,7 @@ __device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, int n, dou
             const int arg2 = __shfl_xor(arg, d);
             larger(m, arg, m2, arg2);
         }
-        const Exp2Below e2(m, c);
+        const Exp2Below e2(m, c, reach);
 #pragma unroll 4
         for (int k = g; k < end; k += lanes) s += c != 0.0 ? p[k].sum * e2(p[k].top) : p[k].sum;
         for (int d = lanes >> 1; d > 0; d >>= 1) s += __shfl_xor(s, d);
@@ -290,26 +334,42 @@ __device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, int n, dou
         }
     }
     __syncthreads();
-    if (t < 64) {
-        bool ok = false;
-        if (x >= 0) {
-            if (c == 0.0) {
-                ok = x == sh.arg[t] && sh.s[t] == 0.0;
-            } else {
-                const double p = Exp2Below(sh.m[t], c)(zp) / sh.s[t];
-                double q = 1.0;
-                if (a.Q) q = Exp2Below(sh.m[a.L + 1 + t], c)(zq) / sh.s[a.L + 1 + t];
-                ok = double(u) * q < p;
-            }
-        }
-        const uint64_t no = ~__ballot(ok), any = __ballot(bad);
-        if (t == 0) {
-            const int first = no ? __builtin_ctzll(no) : 64;
-            sh.count = first < n ? first : n;
-            sh.bad = any != 0;
+    bool ok = false, unsure = false;
+    const int jq = a.L + 1 + t;
+    if (x >= 0) {
+        if (c == 0.0) {
+            ok = x == sh.arg[t] && sh.s[t] == 0.0;
+        } else {
+            const double p = Exp2Below(sh.m[t], c, reach)(zp) / sh.s[t];
+            const double q = a.Q ? Exp2Below(sh.m[jq], c, reach)(zq) / sh.s[jq] : 1.0;
+            ok = double(u) * q < p;
+            unsure = p > 0.0 && __builtin_fabs(double(u) * q - p) <= UNSURE * p;
         }
     }
-    __syncthreads();
+    for (;;) {
+        if (t < 64) {
+            const uint64_t stop = ~__ballot(ok && !unsure), any = __ballot(bad), open = __ballot(unsure);
+            if (t == 0) {
+                const int first = stop ? __builtin_ctzll(stop) : 64;
+                sh.count = first < n ? first : n;
+                sh.ask = first < n && ((open >> first) & 1);
+                sh.bad = any != 0;
+            }
+        }
+        __syncthreads();
+        if (!sh.ask) break;
+        // by the rows' sums in 64 bits
+        const int k = sh.count;
+        const Rows<PB, QB> rows(a, b, k);
+        const double sp = row_sum<PB>(rows.p, a.N, sh.m[k], c, reach, sh.sum);
+        const double sq = a.Q ? row_sum<QB>(rows.q, a.N, sh.m[a.L + 1 + k], c, reach, sh.sum) : 1.0;
+        if (t == k) {
+            const double p = Exp2Below(sh.m[t], c, reach)(zp) / sp;
+            const double q = a.Q ? Exp2Below(sh.m[jq], c, reach)(zq) / sq : 1.0;
+            ok = double(u) * q < p;
+            unsure = false;
+        }
+    }
     Decision d;
     d.count = sh.count;
     d.mp = sh.m[d.count];
@@ -338,42 +398,33 @@ __device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, int n, dou
     return d;
 }
 
-// The weight of words in the draw.
-struct Weight {
+// Exponentials of the row that is drawn from, and of the draft's where `rest` is asked for.
+template <bool PB, bool QB>
+struct Drawn {
+    Rows<PB, QB> rows;
     Exp2Below p, q;
-    double ip, iq;
-    int kind;
-    int64_t token;
-    __device__ __forceinline__ Weight(const Decision &d, double c)
-        : p(d.mp, c), q(d.mq, c), ip(1.0 / d.sp), iq(1.0 / d.sq), kind(d.kind), token(d.token)
+    int64_t out;  // the word that is left out, or -1
+    __device__ __forceinline__ Drawn(const DArgs &a, int64_t b, const Decision &d, double c, double reach)
+        : rows(a, b, d.count), p(d.mp, c, reach), q(d.mq, c, reach), out(d.kind == DRAW_OTHERS ? d.token : -1)
     {
     }
-
-    // of eight words from `at` on (0 past `end`), and their sum
-    template <bool PB, bool QB>
-    __device__ __forceinline__ double eight(const Rows<PB, QB> &rows, int64_t at, int64_t end, double (&v)[8]) const
+    // eight words from `at` on (-inf past `end`)
+    __device__ __forceinline__ void read(int64_t at, int64_t end, bool rest, Words8<PB> &zp, Words8<QB> &zq) const
+    {
+        zp.load(rows.p, at < end ? at : end, end);
+        if (rest) zq.load(rows.q, at < end ? at : end, end);
+    }
+    __device__ __forceinline__ void eight(int64_t at, int64_t end, bool rest, double (&ep)[8], double (&eq)[8]) const
     {
         Words8<PB> zp;
-        zp.load(rows.p, at < end ? at : end, end);
-        double sum = 0.0;
-        if (kind == DRAW_REST) {
-            Words8<QB> zq;
-            zq.load(rows.q, at < end ? at : end, end);
+        Words8<QB> zq;
+        read(at, end, rest, zp, zq);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const double d = p(zp[e]) * ip - q(zq[e]) * iq;
-                v[e] = d > 0.0 ? d : 0.0;
-                sum += v[e];
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] = p(zp[e]);
-                if (kind == DRAW_OTHERS && at + e == token) v[e] = 0.0;
-                sum += v[e];
-            }
+        for (int e = 0; e < 8; ++e) {
+            ep[e] = p(zp[e]);
+            if (at + e == out) ep[e] = 0.0;
+            eq[e] = rest ? q(zq[e]) : 0.0;
         }
-        return sum;
     }
 };
 
@@ -389,19 +440,52 @@ __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
         bool bad = false;
         const int n = seq_len(a, b, bad);
         const double c = seq_scale(a, b, bad);
-        const Decision d = decide<PB, QB>(a, b, n, c, bad, sh);
+        const double reach = 1000.0 / c;
+        const Decision d = decide<PB, QB>(a, b, n, c, reach, bad, sh);
         if (part == 0 && t == 0) {
             a.dec[b] = d;
             if (d.bits && a.err) atomicOr(a.err, d.bits);
         }
         if (d.kind <= DRAW_OTHERS) {
-            const Weight weight(d, c);
-            const Rows<PB, QB> rows(a, b, d.count);
-            for (int r = part * (DT / 64) + w; r < a.runs; r += a.parts * (DT / 64)) {
-                const int64_t n0 = r * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
-                double s = 0.0, v[8];
-                for (int64_t at = n0; at < n1; at += RUN) s += weight.eight(rows, at + 8 * lane, n1, v);
-                s = wave_sum(s);
+            const Drawn<PB, QB> drawn(a, b, d, c, reach);
+            const bool rest = d.kind == DRAW_REST;
+            const double ratio = d.sp / d.sq;  // p > q where ep > eq ratio
+            // (vectors of a wave: the next one is in flight)
+            Words8<PB> zp;
+            Words8<QB> zq;
+            const int step = a.parts * (DT / 64);
+            int r = part * (DT / 64) + w;
+            auto read = [&](int run, int64_t at) {
+                const int64_t n0 = run * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
+                drawn.read(n0 + at + 8 * lane, n1, rest, zp, zq);
+            };
+            if (r < a.runs) read(r, 0);
+            for (; r < a.runs; r += step) {
+                const int64_t n0 = r * a.run;
+                Run s{0.0, 0.0, 0.0, 0.0};
+                for (int64_t at = 0; at < a.run; at += RUN) {
+                    const Words8<PB> wp = zp;
+                    const Words8<QB> wq = zq;
+                    if (at + RUN < a.run) read(r, at + RUN);
+                    else if (r + step < a.runs) read(r + step, 0);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const double ep = n0 + at + 8 * lane + e == drawn.out ? 0.0 : drawn.p(wp[e]);
+                        s.p += ep;
+                        if (!rest) continue;
+                        const double eq = drawn.q(wq[e]);
+                        const bool above = ep > eq * ratio;
+                        s.q += eq;
+                        s.above_p += above ? ep : 0.0;
+                        s.above_q += above ? eq : 0.0;
+                    }
+                }
+                s.p = wave_sum(s.p);
+                if (rest) {
+                    s.q = wave_sum(s.q);
+                    s.above_p = wave_sum(s.above_p);
+                    s.above_q = wave_sum(s.above_q);
+                }
                 if (lane == 0) a.rest[int64_t(b) * a.runs + r] = s;
             }
         }
@@ -437,75 +521,113 @@ __global__ __launch_bounds__(64) void draft_draw_kernel(const DArgs a)
     } else if (d.kind != DRAW_NONE) {
         // every lane `per` runs in order
         const int per = (a.runs + 63) / 64, r0 = lane * per, r1 = r0 + per < a.runs ? r0 + per : a.runs;
-        const double *rest = a.rest + b * a.runs;
-        double own = 0.0;
-#pragma unroll 8
-        for (int k = r0; k < r1; ++k) own += rest[k];
-        const double incl = sum_scan(own), all = lane_value(incl, 63);
-        if (!good_sum(all)) {
-            // nothing is left beside what was refused (p and q differ by roundings alone): p itself
-            d.kind = DRAW_TARGET;
-        }
-        const Weight weight(d, c);
-        const Rows<PB, QB> rows(a, b, d.count);
-        int64_t n0 = 0, n1 = a.N;
-        double before = 0.0, target = 0.0;
-        if (good_sum(all)) {
-            target = r * all;
-            const int who = crossing(incl, own, target);
-            // that lane's runs
-            double sum = incl - own;
-            int run = -1;
-            double at_run = sum;
+        Run *runs = a.rest + b * a.runs;
+        double ip = 1.0, iq = 0.0;  // a word's weight: ep ip - eq iq, where that is more than 0
+        bool rest = d.kind == DRAW_REST;
+        const Drawn<PB, QB> drawn(a, b, d, c, 1000.0 / c);
+        if (rest) {
+            double sp = 0.0, sq = 0.0;
+#pragma unroll 4
             for (int k = r0; k < r1; ++k) {
-                const double v = rest[k];
-                if (run < 0 && v > 0.0 && sum + v > target) {
-                    run = k;
-                    at_run = sum;
-                }
-                sum += v;
+                sp += runs[k].p;
+                sq += runs[k].q;
             }
-            if (run < 0) {  // (roundings: its last run with a weight)
-                sum = incl - own;
-                for (int k = r0; k < r1; ++k) {
-                    const double v = rest[k];
-                    if (v > 0.0) {
+            ip = 1.0 / wave_sum(sp);
+            iq = 1.0 / wave_sum(sq);
+        }
+        auto weight = [&](double ep, double eq) {
+            const double v = ep * ip - eq * iq;
+            return v > 0.0 ? v : 0.0;
+        };
+        auto run_weight = [&](int k) { return rest ? weight(runs[k].above_p, runs[k].above_q) : runs[k].p; };
+        auto lane_weight = [&]() {
+            double v = 0.0;
+#pragma unroll 4
+            for (int k = r0; k < r1; ++k) v += run_weight(k);
+            return v;
+        };
+        double own = lane_weight(), incl = sum_scan(own), all = lane_value(incl, 63);
+        if (rest && !(all > LITTLE)) {
+            // word by word; each lane keeps the weights of its own runs
+            for (int k = 0; k < a.runs; ++k) {
+                const int64_t n0 = k * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
+                double s = 0.0;
+                for (int64_t at = n0; at < n1; at += RUN) {
+                    double ep[8], eq[8];
+                    drawn.eight(at + 8 * lane, n1, true, ep, eq);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s += weight(ep[e], eq[e]);
+                }
+                s = wave_sum(s);
+                if (k >= r0 && k < r1) {
+                    runs[k].above_p = s / ip;
+                    runs[k].above_q = 0.0;
+                }
+            }
+            own = lane_weight();
+            incl = sum_scan(own);
+            all = lane_value(incl, 63);
+            if (!good_sum(all)) {
+                // nothing is left beside what was refused (p and q differ by roundings alone): p itself
+                rest = false;
+                ip = 1.0;
+                iq = 0.0;
+                own = lane_weight();
+                incl = sum_scan(own);
+                all = lane_value(incl, 63);
+            }
+        }
+        if (!good_sum(all)) {
+            next = d.token;  // (the refused token is all that p holds)
+        } else {
+            const double target = r * all;
+            const int who = crossing(incl, own, target);
+            // that lane's first run past it (roundings: its last run with a weight)
+            double sum = incl - own, at_run = sum, at_last = sum;
+            int run = -1, some = r0;
+            for (int k = r0; k < r1; ++k) {
+                const double v = run_weight(k);
+                if (v > 0.0) {
+                    some = k;
+                    at_last = sum;
+                    if (run < 0 && sum + v > target) {
                         run = k;
                         at_run = sum;
                     }
-                    sum += v;
                 }
+                sum += v;
             }
-            run = lane_value(run, who);
-            before = lane_value(at_run, who);
-            n0 = run * a.run;
-            n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
-        } else {
-            double s = 0.0, v[8];
-            for (int64_t at = 0; at < a.N; at += RUN) s += weight.eight(rows, at + 8 * lane, a.N, v);
-            target = r * wave_sum(s);
-        }
-        int last = -1;
-        for (int64_t at = n0; at < n1 && next < 0; at += RUN) {
-            double v[8];
-            const double mine = weight.eight(rows, at + 8 * lane, n1, v), scan = sum_scan(mine);
-            const int who = crossing(before + scan, mine, target);
-            if (who >= 0) {
-                double sum = before + (scan - mine);
-                int pick = -1, some = -1;
+            double before = lane_value(run < 0 ? at_last : at_run, who);
+            run = lane_value(run < 0 ? some : run, who);
+            const int64_t n0 = run * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
+            int last = -1;
+            for (int64_t at = n0; at < n1 && next < 0; at += RUN) {
+                double ep[8], eq[8], mine = 0.0;
+                drawn.eight(at + 8 * lane, n1, rest, ep, eq);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    sum += v[e];
-                    if (v[e] > 0.0) some = e;
-                    if (pick < 0 && v[e] > 0.0 && sum > target) pick = e;
+                    ep[e] = weight(ep[e], eq[e]);
+                    mine += ep[e];
                 }
-                const int word = lane_value(pick < 0 ? some : pick, who);
-                last = int(at + 8 * who + word);
-                if (lane_value(before + scan, who) > target) next = last;
+                const double scan = sum_scan(mine);
+                const int who = crossing(before + scan, mine, target);
+                if (who >= 0) {
+                    double upto = before + (scan - mine);
+                    int pick = -1, some = -1;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        upto += ep[e];
+                        if (ep[e] > 0.0) some = e;
+                        if (pick < 0 && ep[e] > 0.0 && upto > target) pick = e;
+                    }
+                    const int word = lane_value(pick < 0 ? some : pick, who);
+                    last = int(at + 8 * who + word);
+                    if (lane_value(before + scan, who) > target) next = last;
+                }
+                before += lane_value(scan, 63);
             }
-            before += lane_value(scan, 63);
+            if (next < 0) next = last;  // (roundings: the last word with a weight)
         }
-        if (next < 0) next = last;  // (roundings: the last word with a weight)
     }
     for (int i = lane; i <= a.L; i += 64)
         a.out[b * (a.L + 1) + i] = i < d.count ? a.tokens[b * a.L + i] : (i == d.count ? next : -1);
@@ -536,9 +658,9 @@ DLayout draft_layout(int64_t B, int64_t L, int64_t N, bool draft)
     l.pieces = (l.turns + l.per - 1) / l.per + 1;
     l.run = ((N + RUN - 1) / RUN + MAX_RUNS - 1) / MAX_RUNS * RUN;
     l.runs = int((N + l.run - 1) / l.run);
-    // blocks of a row's runs: a wave one run, or as many as leaves eight blocks a compute unit
+    // blocks of a row's runs: a wave one run, or as many as leaves three blocks a compute unit
     const int64_t most = (l.runs + DT / 64 - 1) / (DT / 64);
-    l.parts = int(std::clamp<int64_t>(2048 / std::max<int64_t>(B, 1), 1, most));
+    l.parts = int(std::clamp<int64_t>(768 / std::max<int64_t>(B, 1), 1, most));
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t p = at;
@@ -546,7 +668,7 @@ DLayout draft_layout(int64_t B, int64_t L, int64_t N, bool draft)
         return p;
     };
     l.part = take(size_t(B) * l.rows * l.pieces * sizeof(Piece));
-    l.rest = take(size_t(B) * l.runs * sizeof(double));
+    l.rest = take(size_t(B) * l.runs * sizeof(Run));
     l.dec = take(size_t(B) * sizeof(Decision));
     l.total = at;
     return l;
@@ -602,7 +724,7 @@ hipError_t launch_draft_verify(const DraftCall &c, hipStream_t st)
     a.out = c.out;
     a.err = c.err;
     a.part = reinterpret_cast<Piece *>(ws + l.part);
-    a.rest = reinterpret_cast<double *>(ws + l.rest);
+    a.rest = reinterpret_cast<Run *>(ws + l.rest);
     a.dec = reinterpret_cast<Decision *>(ws + l.dec);
     const bool pb = c.p_dtype == BSQ_BF16, qb = c.Q ? c.q_dtype == BSQ_BF16 : pb;
     if (pb) return qb ? launch_draft<true, true>(a, l, st) : launch_draft<true, false>(a, l, st);

@@ -1,7 +1,7 @@
 """Verification of drafted tokens (bsq_draft_verify) against the definition in 64
 bits, one sequence and one token after another. Results are whole numbers and have to
-be equal: both sides sum in 64 bits, so a draw on a vocabulary of N words differs only
-where a random number lies within some 1e-14 of a border of the cumulative sum."""
+be equal: both are those of 64-bit sums, so a draw on a vocabulary of N words differs
+only where a random number lies within some 1e-13 of a border of the cumulative sum."""
 import pytest
 import torch
 
@@ -144,6 +144,50 @@ def test_random_numbers_on_borders(gpu):
     count, out = bsq.bsq_draft_verify(target, tokens, torch.full_like(u, last), r, target[:, :1].clone())
     torch.cuda.synchronize()
     assert (count == 1).all()
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_random_numbers_next_to_the_ratio(dt, gpu):
+    """u is p / q rounded to 32 bits, and its neighbours: 32-bit sums do not settle any of these."""
+    target, tokens, u, r, draft, lens, temp = _case(gpu, 12, 4, 5003, dt, dt, near=0.4, seed=13)
+    for given in (draft, None):
+        for b in range(12):
+            for i in range(4):
+                x, tau = int(tokens[b, i]), float(temp[b])
+                p = _law(target[b, i].cpu(), tau)[x]
+                q = _law(draft[b, i].cpu(), tau)[x] if given is not None else torch.tensor(1.0)
+                u[b, i] = min(float(p / q), 1 - 2.0 ** -24)
+        for side in (0.0, 1.0, -1.0):
+            v = torch.nextafter(u, torch.full_like(u, side * 2)) if side else u
+            v = v.clamp(0, 1 - 2.0 ** -24)
+            _check(_reference(target, tokens, v, r, given, lens, temp),
+                   bsq.bsq_draft_verify(target, tokens, v, r, given, lens=lens, temperature=temp))
+
+
+@pytest.mark.parametrize("near", [1e-5, 1e-3, 2e-2])
+def test_little_left_of_the_target(near, gpu):
+    """Drafts so near to the target that max(p - q, 0) is a small part of p, and refused all the same."""
+    target, tokens, u, r, draft, lens, temp = _case(gpu, 40, 2, 4001, torch.float32, torch.float32, near=near, seed=14)
+    parts = []
+    for b in range(40):
+        for i in range(2):
+            x, tau = int(tokens[b, i]), float(temp[b])
+            p, q = _law(target[b, i].cpu(), tau), _law(draft[b, i].cpu(), tau)
+            u[b, i] = 1 - 2.0 ** -24 if p[x] < q[x] else 0.0
+            parts.append(float((p - q).clamp_min(0).sum()))
+    want = _reference(target, tokens, u, r, draft, lens, temp)
+    say(f"  near={near}: max(p - q, 0) is {min(parts):.1e} to {max(parts):.1e}; accepted {int(want[0].sum())} of {int(lens.sum())}")
+    assert (want[0] < lens.cpu()).any()
+    _check(want, bsq.bsq_draft_verify(target, tokens, u, r, draft, lens=lens, temperature=temp))
+
+
+@pytest.mark.parametrize("tau", [1e-30, 1e-6, 0.01, 50.0, 1e10])
+def test_temperatures_of_any_size(tau, gpu):
+    target, tokens, u, r, draft, lens, _ = _case(gpu, 16, 3, 3000, masked=0.3, seed=15)
+    temp = torch.full((16,), tau, device=gpu)
+    want_temp = temp if tau > 2.0 ** -64 else torch.zeros_like(temp)  # (smaller ones count as 0)
+    _check(_reference(target, tokens, u, r, draft, lens, want_temp),
+           bsq.bsq_draft_verify(target, tokens, u, r, draft, lens=lens, temperature=temp))
 
 
 def test_outputs_follow_the_target(gpu):
