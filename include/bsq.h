@@ -690,7 +690,7 @@ bsq_status bsq_xent_grad(const void *H, int64_t ldh, const void *V, int64_t ldv,
  * ------------------------------------------------------------------------ */
 #define BSQ_MAX_TOP 256
 
-/* Device workspace of bsq_top_logits (at most 64 MiB and a little; host only). */
+/* Device workspace of bsq_top_logits (at most 13 MiB; host only). */
 bsq_status bsq_top_workspace_bytes(int64_t T, int64_t N, size_t *bytes);
 
 /*   Z       device [T][ldz] of z_dtype (bf16 or fp32), ldz >= N, any alignment of the elements

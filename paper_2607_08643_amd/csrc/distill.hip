@@ -18,6 +18,7 @@
 // is rounded to bf16 all the same, 2^-9, beside which 2^-11 adds nothing to speak of; for a
 // dV of 32 bits the logits are made again.)
 #include "vocab_product.h"
+#include "vocab_rows.h"
 
 namespace bsq {
 namespace {
@@ -43,7 +44,7 @@ struct TeacherArgs {
 __device__ __forceinline__ double block_sum64(double v, double *s)
 {
     const int t = threadIdx.x;
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    v = wave_sum(v);
     __syncthreads();
     if ((t & 63) == 0) s[t >> 6] = v;
     __syncthreads();
@@ -81,11 +82,10 @@ __global__ __launch_bounds__(XT) void distill_teacher_kernel(const TeacherArgs a
     const uint64_t key = (uint64_t(uint32_t(there ? id : INT32_MAX)) << 16) | uint32_t(t);
     s_key[t] = key;
     float mx = float(x);  // what is subtracted before the exponentials: any value near the largest
-    for (int d = 32; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+    mx = wave_max(mx);
     if ((t & 63) == 0) s_max[t >> 6] = mx;
-    __syncthreads();
+    const bool live = __syncthreads_or(there);
     for (int w = 0; w < XT / 64; ++w) mx = fmaxf(mx, s_max[w]);
-    const double count = block_sum64(there ? 1.0 : 0.0, s_sum);
     double logp, p;
     if (a.norm) {
         logp = x - double(a.norm[m]);
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(XT) void distill_teacher_kernel(const TeacherArgs a
         a.sp[m * a.K + place] = float(p);
     }
     if (t == 0) {
-        a.live[m] = count > 0.0 ? 0 : -1;
+        a.live[m] = live ? 0 : -1;
         a.total[m] = float(total);
         a.self[m] = self;
     }
@@ -165,45 +165,72 @@ __global__ __launch_bounds__(XT) void distill_join_kernel(const XArgs a, const d
     a.loss_out[m] = row >= 0 ? float(self[m] - z + double(a.total[m]) * lse) : 0.0f;
 }
 
-// d of a piece of the vocabulary from what the loss kept: eight words a thread. The teacher's
-// words, where P q and p may nearly cancel, are made from their logits in 32 bits.
+// d of a piece of the vocabulary from what the loss kept: a block has KV runs of eight words
+// a thread of a row, all in flight at once (4096 tokens of 32768 words: 99 us, 5.5 TB/s;
+// with one run 119). The teacher's words, where P q and p may nearly cancel, are made from
+// their logits in 32 bits.
+constexpr int KV = 4;
+
 __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blocks)
 {
     const int live = a.hdr[0];
     const int64_t row = blockIdx.x / blocks;
     if (row >= (int64_t(live) + 63) / 64 * 64) return;  // (d's rows are read 64 deep by dV)
-    const int64_t w = (int64_t(blockIdx.x - row * blocks) * XT + threadIdx.x) * 8;
-    if (w >= a.vp) return;
-    u32x4_t d{0u, 0u, 0u, 0u};
-    if (row < live) {
-        const int64_t word = a.v0 + w, tok = a.rows[row];
-        const u32x4_t code = *reinterpret_cast<const u32x4_t *>(a.kept + row * a.ldk + word);
-        const float m = a.kept_max[row * (a.ldk / 64) + word / 64];
-        const float lse = a.lse_in[tok], gg = a.g_in[tok] * a.scale, total = a.total[tok];
+    const int64_t w0 = int64_t(blockIdx.x - row * blocks) * (8 * XT * KV) + 8 * threadIdx.x;
+    uint16_t *dS = a.dS + row * a.dsp;
+    if (row >= live) {
+#pragma unroll
+        for (int j = 0; j < KV; ++j)
+            if (w0 + 8 * XT * j < a.vp) *reinterpret_cast<u32x4_t *>(dS + w0 + 8 * XT * j) = u32x4_t{0u, 0u, 0u, 0u};
+        return;
+    }
+    const int64_t tok = a.rows[row];
+    const float lse = a.lse_in[tok], gg = a.g_in[tok] * a.scale, total = a.total[tok];
+    u32x4_t code[KV];
+    float f[KV];
+    int beg[KV], end[KV];
+#pragma unroll
+    for (int j = 0; j < KV; ++j) {
+        const int64_t w = w0 + 8 * XT * j, word = a.v0 + (w < a.vp ? w : 0);
+        code[j] = *reinterpret_cast<const u32x4_t *>(a.kept + row * a.ldk + word);
+        f[j] = a.kept_max[row * (a.ldk / 64) + word / 64];
         const uint16_t *o = a.off + tok * (a.tiles + 1) + word / VBLK;
-        const int beg = o[0], end = o[1];
-        const float f = m == -__builtin_inff() && lse == lse ? 0.0f : gg * (__builtin_amdgcn_exp2f((m - lse) * LOG2E) * total);
+        beg[j] = o[0];
+        end[j] = o[1];
+    }
+#pragma unroll
+    for (int j = 0; j < KV; ++j) {
+        const int64_t w = w0 + 8 * XT * j, word = a.v0 + w;
+        if (w >= a.vp) break;
+        // (a group of -inf is 0, but for a row that is NaN)
+        const float q = f[j] == -__builtin_inff() && lse == lse ? 0.0f : gg * (__builtin_amdgcn_exp2f((f[j] - lse) * LOG2E) * total);
         float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            v[k] = word + k < a.N ? f * kept_value((k & 1) ? code[k >> 1] >> 16 : code[k >> 1] & 0xffffu) : 0.0f;
+            v[k] = word + k < a.N ? q * kept_value((k & 1) ? code[j][k >> 1] >> 16 : code[j][k >> 1] & 0xffffu) : 0.0f;
         int32_t last = -1;
-        for (int e = beg; e < end; ++e) {
-            const int64_t at = tok * a.K + e;
-            const int32_t id = a.sid[at];
-            const int64_t q = id - word;
-            if (q >= 0 && q < 8) {
-                const float p = gg * a.sp[at];
-                const float pq = gg * (__builtin_amdgcn_exp2f((a.zk[at] - lse) * LOG2E) * total);
+        for (int e0 = beg[j]; e0 < end[j]; e0 += 4) {
+            int32_t id[4];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = q == k ? (id == last ? v[k] : pq) - p : v[k];
+            for (int h = 0; h < 4; ++h) id[h] = e0 + h < end[j] ? a.sid[tok * a.K + e0 + h] : -1;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const int64_t at = tok * a.K + e0 + h, place = id[h] - word;
+                if (id[h] >= 0 && place >= 0 && place < 8) {
+                    const float p = gg * a.sp[at];
+                    const float pq = gg * (__builtin_amdgcn_exp2f((a.zk[at] - lse) * LOG2E) * total);
+                    // (a word listed again: its probability is in already)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = place == k ? (id[h] == last ? v[k] : pq) - p : v[k];
+                }
+                last = id[h];
             }
-            last = id;
         }
+        u32x4_t d;
 #pragma unroll
         for (int k = 0; k < 4; ++k) d[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
+        *reinterpret_cast<u32x4_t *>(dS + w) = d;
     }
-    *reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w) = d;
 }
 
 // ---------------------------------------------------------------------------
@@ -215,7 +242,8 @@ struct SLayout {
     XLayout x;
     size_t live, sid, sp, off, total, zk, base_bytes;
     size_t codes, maxima, kept_bytes;   // kept: after the base
-    size_t self, ws_bytes;
+    size_t self, stat, ws_bytes;
+    int narrow;
 };
 
 SLayout distill_layout(bool grad, int64_t T, int64_t N, int64_t D, int K)
@@ -242,6 +270,10 @@ SLayout distill_layout(bool grad, int64_t T, int64_t N, int64_t D, int K)
     // workspace: the cross entropy's (its first part is the compact rows), the rest of the base
     at = align256(l.x.total) + (l.base_bytes - align256(l.x.compact));
     l.self = take(t * 8);
+    // tiles of 128 words where 256 leave compute units idle (37 tokens of 32003 words, 1000
+    // inputs: the loss's product 25 us with 126 tiles, 19 with 251)
+    l.narrow = !grad && T <= 128 && l.x.tiles < 256;
+    l.stat = l.narrow ? take(size_t(2 * l.x.tiles) * size_t(l.x.Tp) * 8) : l.x.stat;
     l.ws_bytes = at;
     return l;
 }
@@ -283,6 +315,7 @@ hipError_t launch_teacher(const DistillCall &c, const SLayout &l, bool make, XAr
     a.ldk = l.x.tiles * VBLK;
     a.tiles = l.x.tiles;
     a.K = c.K;
+    a.narrow = l.narrow;
     a.scale = c.scale;
     if (!make || c.x.T == 0) return hipSuccess;
     hipLaunchKernelGGL(distill_teacher_kernel, dim3(unsigned(c.x.T)), dim3(XT), 0, st, h);
@@ -302,13 +335,14 @@ hipError_t launch_distill_loss(const DistillCall &c, hipStream_t st)
     hipError_t e = launch_teacher(c, l, true, a, st);
     if (e != hipSuccess) return e;
     char *ws = static_cast<char *>(c.x.ws);
-    a.stat = reinterpret_cast<float2 *>(ws + l.x.stat);
+    a.stat = reinterpret_cast<float2 *>(ws + l.stat);
     a.loss_out = c.x.loss;
     a.lse_out = c.x.lse;
     if ((e = launch_stats<EPI_TSTATS>(a, l.x, st)) != hipSuccess) return e;
     const double *self = reinterpret_cast<const double *>(ws + l.self);
-    if (a.T < 512) hipLaunchKernelGGL((distill_join_kernel<1>), dim3(unsigned(a.T)), dim3(XT), 0, st, a, self, int(l.x.tiles));
-    else hipLaunchKernelGGL((distill_join_kernel<8>), dim3(unsigned((a.T + 7) / 8)), dim3(XT), 0, st, a, self, int(l.x.tiles));
+    const int tiles = int(l.x.tiles << l.narrow);
+    if (a.T < 512) hipLaunchKernelGGL((distill_join_kernel<1>), dim3(unsigned(a.T)), dim3(XT), 0, st, a, self, tiles);
+    else hipLaunchKernelGGL((distill_join_kernel<8>), dim3(unsigned((a.T + 7) / 8)), dim3(XT), 0, st, a, self, tiles);
     return hipGetLastError();
 }
 
@@ -324,7 +358,7 @@ hipError_t launch_distill_grad(const DistillCall &call, hipStream_t st)
     if (e != hipSuccess) return e;
     return launch_grad(c.x, l.x, a, kept, st, [&](const XArgs &piece) {
         if (!kept) return launch_tokens<EPI_TPROB>(piece, piece.vp, 1, st);
-        const int64_t blocks = (piece.vp + 8 * XT - 1) / (8 * XT), rows = (piece.T + 63) / 64 * 64;
+        const int64_t blocks = (piece.vp + 8 * XT * KV - 1) / (8 * XT * KV), rows = (piece.T + 63) / 64 * 64;
         if (rows == 0) return hipSuccess;
         hipLaunchKernelGGL(distill_kept_kernel, dim3(unsigned(rows * blocks)), dim3(XT), 0, st, piece, int(blocks));
         return hipGetLastError();

@@ -35,7 +35,7 @@ constexpr int PASSED = 16;              // lanes whose words a wave looks throug
 constexpr int BINS = 256;               // of values, four a lane
 constexpr int FEW = 1024;               // keys that are put in order by counting
 constexpr int64_t MAX_SEGS = 64;        // of a row: one a lane
-constexpr int64_t MAX_ITEMS = 512;      // segments in a launch: those that run together (workspace: 48 KiB each)
+constexpr int64_t MAX_ITEMS = 256;      // segments in a launch, where rows are cut (workspace: 48 KiB each)
 constexpr float LOG2E = 1.4426950408889634f;
 static_assert(BSQ_MAX_TOP + 64 <= WCAP - 64, "a cut list has room for more");
 static_assert(LIST < 65536, "places are of 16 bits");
@@ -58,9 +58,10 @@ struct TShared {
     uint32_t place[LIST / 2]; // of these: the number of larger ones, two of 16 bits
     uint64_t best[BSQ_MAX_TOP];
     __attribute__((aligned(16))) uint32_t bound[TW];
-    __attribute__((aligned(16))) uint32_t bins[BINS];  // 0 before a cut
+    __attribute__((aligned(16))) uint32_t bins[BINS];
+    uint32_t low[TW];         // before a cut: the waves' smallest key, its value; their largest in stat; bins of 0
     int count[2][TW];
-    float2 stat[TW];          // of the waves (a cut reads their largest)
+    float2 stat[TW];          // of the waves
 };
 
 // Values in order as whole numbers (-0 as +0).
@@ -195,14 +196,34 @@ __device__ __forceinline__ void put_keys(const uint64_t (&own)[OWN], const uint6
     }
 }
 
-// A bound nearer to the K-th largest: the values from `bound` to the largest in 256 bins, the
-// lowest bin that the K largest reach. (A barrier.)
+// Before a cut and a barrier: what it needs to know of the wave's keys.
+__device__ __forceinline__ void prepare_cut(const uint64_t (&own)[OWN], TShared &sh)
+{
+    const int t = threadIdx.x;
+    uint32_t low = ~0u;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const uint32_t v = own[i] != 0 ? uint32_t(own[i] >> 32) : ~0u;
+        low = v < low ? v : low;
+    }
+    low = lane_value(wave_scan(low, ~0u, [](uint32_t x, uint32_t y) { return x < y ? x : y; }), 63);
+    if ((t & 63) == 0) sh.low[t >> 6] = low;
+    if (t < BINS) sh.bins[t] = 0;
+}
+
+// A bound nearer to the K-th largest: the values from `bound` (or the smallest) to the largest
+// in 256 bins, the lowest bin that the K largest reach. (A barrier.)
 __device__ __forceinline__ uint32_t bin_bound(const uint64_t (&own)[OWN], uint32_t bound, int K, TShared &sh)
 {
     const int lane = threadIdx.x & 63;
     float most = -__builtin_inff();
+    uint32_t low = ~0u;
 #pragma unroll
-    for (int k = 0; k < TW; ++k) most = fmaxf(most, sh.stat[k].x);
+    for (int k = 0; k < TW; ++k) {
+        most = fmaxf(most, sh.stat[k].x);
+        low = sh.low[k] < low ? sh.low[k] : low;
+    }
+    bound = low > bound ? low : bound;
     const uint32_t last = ordered(most), range = last > bound ? last - bound : 0;
     const int shift = range < BINS ? 0 : 24 - __builtin_clz(range);
 #pragma unroll
@@ -426,10 +447,10 @@ __global__ __launch_bounds__(TT) __attribute__((amdgpu_waves_per_eu(8, 8))) void
     }
     wave_join(m, s, c);
     if (lane == 0) sh.stat[w] = make_float2(m, s);
-    if (t < BINS) sh.bins[t] = 0;
     uint64_t own[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i) own[i] = 64 * i + lane < held ? list[64 * i + lane] : 0;
+    if constexpr (WHOLE) prepare_cut(own, sh);
     __syncthreads();
     const uint32_t bound = block_bound(sh.bound);
     if (w == 0) {
@@ -504,14 +525,15 @@ __global__ __launch_bounds__(TT) void top_join_kernel(const TArgs a)
             const uint32_t v = uint32_t(own[i] >> 32);
             top = v > top ? v : top;
         }
-        // a bound that at least K of them reach, and the waves' largest
-        const uint32_t b = lanes_rank(top, (a.K + TW - 1) / TW);
+        // a bound that at least K of them reach, from the waves with a key a lane, and the waves' largest
+        const int full = batch / 64 < TW ? batch / 64 : TW;
+        const uint32_t b = w < full || full == 0 ? wave_bound(top, full ? (a.K + full - 1) / full : 65, true) : ~0u;
         top = lane_value(wave_scan(top, 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }), 63);
         if (lane == 0) {
             sh.bound[w] = b;
             sh.stat[w].x = top ? unordered(top) : -__builtin_inff();
         }
-        if (t < BINS) sh.bins[t] = 0;
+        prepare_cut(own, sh);
         __syncthreads();
         n = block_cut(own, block_bound(sh.bound), a.K, sh);
     }
@@ -530,10 +552,16 @@ struct TLayout {
 TLayout top_layout(int64_t T, int64_t N)
 {
     TLayout l{};
-    // segments of whole chunks until the launch fills the compute units (two blocks each)
-    const int64_t steps = (N + TVEC - 1) / TVEC;
-    const int64_t want = std::clamp<int64_t>(MAX_ITEMS / std::max<int64_t>(T, 1), 1, std::min(MAX_SEGS, steps));
-    l.len = (steps + want - 1) / want * TVEC;
+    // A row is cut where it is long and rows are few: into segments of 16384 words or more, up
+    // to a block for every compute unit; ten segments at most while they are short (the
+    // second launch costs 6 us and what they leave). Whole against cut, us, bf16, K = 64: 8
+    // rows of 151936 words 22.6 against 14.4 (ten), 100 rows 23.0 against 21.4 (two), 200
+    // rows 23.9 against 29.6 (two), 64 rows of 32003 words 11.6 against 14.3.
+    constexpr int64_t UNIT = 16384;
+    const int64_t units = (N + UNIT - 1) / UNIT;
+    int64_t want = std::min({MAX_ITEMS / std::max<int64_t>(T, 1), std::max<int64_t>(10, units / 8), MAX_SEGS, units});
+    if (want < 1 || units <= 4) want = 1;
+    l.len = (units + want - 1) / want * UNIT;
     l.segs = int((N + l.len - 1) / l.len);
     size_t at = 0;
     auto take = [&](size_t bytes) {

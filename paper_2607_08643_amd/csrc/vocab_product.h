@@ -69,7 +69,7 @@ struct XArgs {
     uint16_t *kept;               // [compact rows][ldk]
     float *kept_max;              // [compact rows][ldk / 64]
     int64_t ldk, tiles;
-    int K;
+    int K, narrow;                // narrow: tiles of 128 words (up to 128 tokens)
     float scale;
 };
 
@@ -462,7 +462,7 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
     // The teacher's words of a row's token that lie in this tile.
     int e_tok[MF], e_beg[MF], e_end[MF];
     if constexpr (TEACHER) {
-        const int64_t tile = a.v0 / VBLK + bx;
+        const int64_t tile = (a.v0 + int64_t(bx) * G::BL) / VBLK;
 #pragma unroll
         for (int i = 0; i < MF; ++i) e_tok[i] = rbeg + 16 * i < live ? a.rows[rbeg + 16 * i] : -1;
 #pragma unroll
@@ -476,26 +476,27 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
 #pragma unroll
             for (int j = 0; j < NF; ++j) acc[i][j] *= a.scale;
     }
-    // Visits them, two of every row at a time so that their loads are in flight together
+    // Visits them, some of every row at a time so that their loads are in flight together
     // (the first tiles hold ten or more words of a row): f(the row's values, word, its place
     // in the lists, i).
     auto teacher_words = [&](auto f) {
+        constexpr int AT_ONCE = MF > 4 ? 2 : 4;
         int most = 0;
 #pragma unroll
         for (int i = 0; i < MF; ++i) most = e_end[i] - e_beg[i] > most ? e_end[i] - e_beg[i] : most;
-        for (int e0 = 0; e0 < most; e0 += 2) {
-            int32_t word[MF][2];
+        for (int e0 = 0; e0 < most; e0 += AT_ONCE) {
+            int32_t word[MF][AT_ONCE];
 #pragma unroll
             for (int i = 0; i < MF; ++i)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
+                for (int k = 0; k < AT_ONCE; ++k) {
                     const int e = e_beg[i] + e0 + k;
                     word[i][k] = e < e_end[i] ? a.sid[int64_t(e_tok[i]) * a.K + e] : -1;
                 }
 #pragma unroll
             for (int i = 0; i < MF; ++i)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < AT_ONCE; ++k)
                     if (word[i][k] >= 0) f(acc[i], word[i][k], int64_t(e_tok[i]) * a.K + e_beg[i] + e0 + k, i);
         }
     };
@@ -814,6 +815,13 @@ hipError_t launch_gemm_shape(const XArgs &a, int64_t right, int64_t left, int sp
 template <int EPI>
 hipError_t launch_tokens(const XArgs &a, int64_t left, int splits, hipStream_t st)
 {
+    if constexpr (EPI == EPI_TSTATS) {
+        if (a.narrow) {
+            if (a.T <= 32) return launch_gemm_shape<EPI, 1, 4, 2, 2>(a, a.T, left, splits, st);
+            if (a.T <= 64) return launch_gemm_shape<EPI, 2, 4, 2, 2>(a, a.T, left, splits, st);
+            return launch_gemm_shape<EPI, 4, 4, 2, 2>(a, a.T, left, splits, st);
+        }
+    }
     if constexpr (epi_stats(EPI)) {
         if (a.T <= 16) return launch_gemm_shape<EPI, 1, 4, 1, 4>(a, a.T, left, splits, st);
         if (a.T <= 32) return launch_gemm_shape<EPI, 1, 4, 2, 4>(a, a.T, left, splits, st);
@@ -871,7 +879,7 @@ template <int EPI>
 hipError_t launch_stats(XArgs &a, const XLayout &l, hipStream_t st)
 {
     // (kept rows are read 64 deep by dV)
-    hipError_t e = launch_rows(a, a.T <= 16 && !a.kept ? 16 : (a.T <= 32 && !a.kept ? 32 : a.Tp), st);
+    hipError_t e = launch_rows(a, a.T <= 16 && !a.kept && !a.narrow ? 16 : (a.T <= 32 && !a.kept ? 32 : a.Tp), st);
     if (e != hipSuccess) return e;
     // A launch holds fewer than 2^32 work items, 512 or fewer of a tile: the tiles
     // of larger vocabularies go over several.
