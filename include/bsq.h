@@ -721,7 +721,8 @@ bsq_status bsq_top_logits(const void *Z, int32_t z_dtype, int64_t ldz, int64_t T
  * of -inf, is no word; an id of N or more likewise, and ORs BSQ_DEVERR_BAD_SET into
  * *err. A token without words has no loss: its loss, lse and row of dH are 0, and
  * its hidden state and g are not used (they may be NaN). Roundings as for the
- * cross entropy; the K terms of a loss are summed in 64 bits.
+ * cross entropy, but that up to 128 tokens both products take d in two bf16 parts;
+ * the K terms of a loss are summed in 64 bits.
  * ------------------------------------------------------------------------ */
 
 /* Device workspace of bsq_distill_loss (grad = 0), bsq_distill_grad (1); host only. */

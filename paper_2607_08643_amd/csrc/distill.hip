@@ -180,8 +180,11 @@ __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blo
     uint16_t *dS = a.dS + row * a.dsp;
     if (row >= live) {
 #pragma unroll
-        for (int j = 0; j < KV; ++j)
-            if (w0 + 8 * XT * j < a.vp) *reinterpret_cast<u32x4_t *>(dS + w0 + 8 * XT * j) = u32x4_t{0u, 0u, 0u, 0u};
+        for (int j = 0; j < KV; ++j) {
+            if (w0 + 8 * XT * j >= a.vp) break;
+            *reinterpret_cast<u32x4_t *>(dS + w0 + 8 * XT * j) = u32x4_t{0u, 0u, 0u, 0u};
+            if (a.lo) *reinterpret_cast<u32x4_t *>(dS + w0 + 8 * XT * j + a.lo) = u32x4_t{0u, 0u, 0u, 0u};
+        }
         return;
     }
     const int64_t tok = a.rows[row];
@@ -230,6 +233,14 @@ __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blo
 #pragma unroll
         for (int k = 0; k < 4; ++k) d[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
         *reinterpret_cast<u32x4_t *>(dS + w) = d;
+        if (a.lo == 0) continue;
+        u32x4_t rest;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float x = v[2 * k] - __uint_as_float(d[k] << 16), y = v[2 * k + 1] - __uint_as_float(d[k] & 0xffff0000u);
+            rest[k] = pack_bf16x2(x - x == 0.0f ? x : 0.0f, y - y == 0.0f ? y : 0.0f);
+        }
+        *reinterpret_cast<u32x4_t *>(dS + w + a.lo) = rest;
     }
 }
 
@@ -356,13 +367,16 @@ hipError_t launch_distill_grad(const DistillCall &call, hipStream_t st)
     XArgs a{};
     const hipError_t e = launch_teacher(c, l, !kept, a, st);
     if (e != hipSuccess) return e;
-    return launch_grad(c.x, l.x, a, kept, st, [&](const XArgs &piece) {
+    auto make_d = [&](const XArgs &piece) {
         if (!kept) return launch_tokens<EPI_TPROB>(piece, piece.vp, 1, st);
         const int64_t blocks = (piece.vp + 8 * XT * KV - 1) / (8 * XT * KV), rows = (piece.T + 63) / 64 * 64;
         if (rows == 0) return hipSuccess;
         hipLaunchKernelGGL(distill_kept_kernel, dim3(unsigned(rows * blocks)), dim3(XT), 0, st, piece, int(blocks));
         return hipGetLastError();
-    });
+    };
+    // Where tokens are few the rounding of d to bf16 does not average out over them, and the
+    // products read and write the head either way: they take d in two parts.
+    return c.x.T <= FEW_TOKENS ? launch_grad<true>(c.x, l.x, a, kept, st, make_d) : launch_grad<false>(c.x, l.x, a, kept, st, make_d);
 }
 
 }  // namespace bsq

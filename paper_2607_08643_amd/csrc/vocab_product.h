@@ -27,8 +27,9 @@ constexpr int64_t HALF_TOKENS = 1024;
 
 constexpr int ZEROS = 4;
 
-// EPI_DV2: EPI_DV from both parts of d; EPI_TSTATS, EPI_TPROB: with a teacher's words
-enum { EPI_STATS, EPI_PROB, EPI_DV, EPI_DV2, EPI_DH, EPI_TSTATS, EPI_TPROB };
+// EPI_DV2: EPI_DV from both parts of d; EPI_TSTATS, EPI_TPROB: with a teacher's words;
+// EPI_DH2: EPI_DH of few tokens, the second parts of d as rows of their own
+enum { EPI_STATS, EPI_PROB, EPI_DV, EPI_DV2, EPI_DH, EPI_TSTATS, EPI_TPROB, EPI_DH2 };
 constexpr bool epi_stats(int e) { return e == EPI_STATS || e == EPI_TSTATS; }
 constexpr bool epi_prob(int e) { return e == EPI_PROB || e == EPI_TPROB; }
 constexpr bool epi_logits(int e) { return epi_stats(e) || epi_prob(e); }
@@ -53,6 +54,7 @@ struct XArgs {
     int64_t lo;
     float *dHp;                   // [hsplit][Tp][Dp]
     int hsplit, first;
+    int second;                   // (EPI_DH2, else 0) the row from which the second parts are taken
     uint16_t *dH;
     void *dV;
     int64_t lddh, lddv;
@@ -254,10 +256,10 @@ struct XTiles {
 template <int EPI, int BR, int BL>
 __device__ __forceinline__ XTiles xent_tiles(const XArgs &a, int live)
 {
-    const int64_t rrows = (EPI == EPI_DV || EPI == EPI_DV2) ? a.vp : live;
+    const int64_t rrows = (EPI == EPI_DV || EPI == EPI_DV2) ? a.vp : (EPI == EPI_DH2 ? a.second + live : live);
     const int64_t lrows = epi_logits(EPI) ? a.vp : a.D;
     XTiles n{int((rrows + BR - 1) / BR), int((lrows + BL - 1) / BL), 1};
-    if (EPI == EPI_DH) {
+    if (EPI == EPI_DH || EPI == EPI_DH2) {
         const int fill = n.rt > 0 ? 256 / (n.rt * n.lt) : 1;
         n.splits = fill < 1 ? 1 : (fill < a.hsplit ? fill : a.hsplit);
     }
@@ -337,6 +339,7 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
             int64_t at = tile0 + row;
             if (!right && at >= lend) at = lend - 1;
             src[r] = mat + at * ld + kof[r];
+            if (EPI == EPI_DH2 && right && at >= a.second) src[r] = mat + (at - a.second) * ld + a.lo + kof[r];
         } else {
             const int blk = u >> 2, key = (lane >> 2) & 7, chunk = lane & 3;
             const int k = 16 * (blk >> 1) + 8 * (key >> 2) + 4 * (blk & 1) + (key & 3);
@@ -637,14 +640,14 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
                 *reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w0 + a.lo + 8 * h) = lo;
             }
         }
-    } else if constexpr (EPI == EPI_DH) {
+    } else if constexpr (EPI == EPI_DH || EPI == EPI_DH2) {
         // fp32 sums over the pieces, each split its own
         float *o = a.dHp + int64_t(z) * a.Tp * a.Dp;
         const int64_t c0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * g;
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
             const int64_t row = rbeg + 16 * i;
-            if (row >= live) continue;
+            if ((EPI == EPI_DH2 && row >= a.second ? row - a.second : row) >= live) continue;
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
                 const int64_t c = c0 + 16 * j;
@@ -710,19 +713,29 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     else xent_tile<EPI, 8, 4, 2, 4>(a, live);
 }
 
-// dH rows from the sums (0 for tokens without a loss). One block per token.
+// dH rows from the sums (0 for tokens without a loss). One block per token. FEW: of both
+// parts of d.
+template <bool FEW>
 __global__ __launch_bounds__(XT) void xent_dh_kernel(const XArgs a)
 {
     const int64_t m = blockIdx.x;
     const int row = a.pos[m], live = a.hdr[0];
-    const bool half = a.T <= 128 || (a.T <= HALF_TOKENS && xent_half_tiles<EPI_DH>(a, live));
-    const int splits = half ? xent_tiles<EPI_DH, 128, 256>(a, live).splits : xent_tiles<EPI_DH, 256, 256>(a, live).splits;
+    int splits;
+    if constexpr (FEW) {
+        splits = xent_tiles<EPI_DH2, 256, 256>(a, live).splits;  // (one tile of tokens, of 128 or 256 rows)
+    } else {
+        const bool half = a.T <= 128 || (a.T <= HALF_TOKENS && xent_half_tiles<EPI_DH>(a, live));
+        splits = half ? xent_tiles<EPI_DH, 128, 256>(a, live).splits : xent_tiles<EPI_DH, 256, 256>(a, live).splits;
+    }
     for (int64_t c = 4 * threadIdx.x; c < a.D; c += 4 * XT) {
         f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         if (row >= 0) {
             const float *q = a.dHp + int64_t(row) * a.Dp + c;
 #pragma unroll 8
-            for (int z = 0; z < splits; ++z) v += *reinterpret_cast<const f32x4_t *>(q + int64_t(z) * a.Tp * a.Dp);
+            for (int z = 0; z < splits; ++z) {
+                v += *reinterpret_cast<const f32x4_t *>(q + int64_t(z) * a.Tp * a.Dp);
+                if constexpr (FEW) v += *reinterpret_cast<const f32x4_t *>(q + (int64_t(z) * a.Tp + a.second) * a.Dp);
+            }
         }
         uint16_t *o = a.dH + m * a.lddh + c;
         if (a.dh_vec) *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
@@ -897,8 +910,11 @@ hipError_t launch_stats(XArgs &a, const XLayout &l, hipStream_t st)
 }
 
 // The gradient of the rows that have a loss, piece by piece of the vocabulary; make_d: the
-// launch that leaves a piece's d. compact: the compact rows are there already.
-template <typename MakeD>
+// launch that leaves a piece's d. compact: the compact rows are there already. FEW: up to
+// FEW_TOKENS tokens, with d in two parts for both products.
+constexpr int64_t FEW_TOKENS = 128;
+
+template <bool FEW, typename MakeD>
 hipError_t launch_grad(const XentCall &c, const XLayout &l, XArgs a, bool compact, hipStream_t st, MakeD make_d)
 {
     char *ws = static_cast<char *>(c.ws);
@@ -919,8 +935,9 @@ hipError_t launch_grad(const XentCall &c, const XLayout &l, XArgs a, bool compac
     const int64_t vb = a.dv_bf16 ? 8 : 16;
     a.dv_vec = (reinterpret_cast<uintptr_t>(c.dV) | uintptr_t(vb / 4 * c.lddv)) % vb == 0;
     a.accumulate = c.accumulate;
-    // two parts of d for a dV of 32 bits: half the words a piece, in the same space
-    const bool two = c.dV && !a.dv_bf16;
+    // two parts of d, for a dV of 32 bits or few tokens: half the words a piece, in the same space
+    const bool two = FEW || (c.dV && !a.dv_bf16);
+    a.second = FEW ? (c.T <= 64 ? 64 : 128) : 0;
     const int64_t vp = two ? l.dsp / 2 / VBLK * VBLK : l.vp;
     a.lo = two ? vp : 0;
     hipError_t e = compact ? hipSuccess : launch_rows(a, a.Tp, st);
@@ -929,12 +946,16 @@ hipError_t launch_grad(const XentCall &c, const XLayout &l, XArgs a, bool compac
         a.vp = std::min(vp, (c.N - v0 + VBLK - 1) / VBLK * VBLK);
         a.first = v0 == 0;
         if ((e = make_d(a)) != hipSuccess) break;
-        if ((e = launch_tokens<EPI_DH>(a, c.D, l.hsplit, st)) != hipSuccess) break;
-        if (two) e = launch_gemm_shape<EPI_DV2, 8, 4, 2, 4>(a, a.vp, c.D, 1, st);
+        if constexpr (FEW)
+            e = c.T <= 64 ? launch_gemm_shape<EPI_DH2, 4, 4, 2, 4>(a, 128, c.D, l.hsplit, st)
+                          : launch_gemm_shape<EPI_DH2, 8, 4, 2, 4>(a, 256, c.D, l.hsplit, st);
+        else e = launch_tokens<EPI_DH>(a, c.D, l.hsplit, st);
+        if (e != hipSuccess) break;
+        if (c.dV && two) e = launch_gemm_shape<EPI_DV2, 8, 4, 2, 4>(a, a.vp, c.D, 1, st);
         else if (c.dV) e = launch_gemm_shape<EPI_DV, 8, 4, 2, 4>(a, a.vp, c.D, 1, st);
     }
     if (e != hipSuccess || c.T == 0) return e;
-    hipLaunchKernelGGL(xent_dh_kernel, dim3(unsigned(c.T)), dim3(XT), 0, st, a);
+    hipLaunchKernelGGL((xent_dh_kernel<FEW>), dim3(unsigned(c.T)), dim3(XT), 0, st, a);
     return hipGetLastError();
 }
 

@@ -87,7 +87,7 @@ hipError_t launch_xent_grad(const XentCall &c, hipStream_t st)
 {
     const XLayout l = xent_layout(true, c.T, c.N, c.D);
     const XArgs a = xent_args(c, l, c.ws);
-    return launch_grad(c, l, a, false, st, [&](const XArgs &piece) { return launch_tokens<EPI_PROB>(piece, piece.vp, 1, st); });
+    return launch_grad<false>(c, l, a, false, st, [&](const XArgs &piece) { return launch_tokens<EPI_PROB>(piece, piece.vp, 1, st); });
 }
 
 }  // namespace bsq

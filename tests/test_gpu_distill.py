@@ -11,7 +11,8 @@ roundings of 2^-24 of its two terms (and by 2^-11 of P q from kept exponentials,
 the teacher's words), then rounded to bf16: an error uniform on half an ulp
 (at most 2^-8 |d|), whose sum over independent terms exceeds 3.78 * 2^-8 * sqrt(sum of
 squares) with probability under 1e-9; then the second product's gamma and the
-rounding of the result.
+rounding of the result. A dV of 32 bits, and up to 128 tokens all results, take d in
+two bf16 parts: 2^-9 of 2^-9 of a value is left, at most 2^-17.
 """
 import pytest
 import torch
@@ -106,16 +107,19 @@ def _check_grad(c, lse, dH, dV, before=None, kept=False):
     if kept:
         ed += torch.where(t > 0, 0.0, 2.0 ** -11 * d.abs())
     want = d @ v
-    tol = SUBGAUSS * U16 * (d.square() @ v.square()).sqrt() + (ed + gamma(v.shape[0]) * d.abs()) @ v.abs() + U16 * want.abs() + 1e-30
+    two = len(c.g) <= 128  # d in two bf16 parts
+    tol = (ed + (2.0 ** -17 if two else 0) * d.abs() + gamma(2 * v.shape[0]) * d.abs()) @ v.abs() + U16 * want.abs() + 1e-30
+    if not two:
+        tol += SUBGAUSS * U16 * (d.square() @ v.square()).sqrt()
     err = (dH[c.live].double() - want).abs()
     say(f"  dH: worst err/tol {float((err / tol).max()) if err.numel() else 0:.3f}")
     assert (err <= tol * 1.01).all()
     if dV is None:
         return
     want = d.T @ h
-    if dV.dtype == torch.bfloat16:
+    if dV.dtype == torch.bfloat16 and not two:
         tol = SUBGAUSS * U16 * (d.square().T @ h.square()).sqrt() + (ed + gamma(len(d)) * d.abs()).T @ h.abs() + 1e-30
-    else:  # d in two bf16 parts, as the cross entropy's
+    else:
         tol = (ed + (2.0 ** -17 + gamma(2 * len(d))) * d.abs()).T @ h.abs() + 1e-30
     if before is not None:
         want = want + before.double()
