@@ -695,7 +695,7 @@ bsq_status bsq_top_workspace_bytes(int64_t T, int64_t N, size_t *bytes);
 
 /*   Z       device [T][ldz] of z_dtype (bf16 or fp32), ldz >= N, any alignment of the elements
  *   K       1 .. BSQ_MAX_TOP
- *   scale   > 0, finite (one over a temperature)
+ *   scale   one over a temperature, 2^-64 .. 2^64
  *   ids     device int32 [T][K]: words by falling logit, equal ones by rising
  *           word. Words of -inf (masked) or NaN are not listed: where fewer than
  *           K are left, the last entries are -1
@@ -735,7 +735,7 @@ bsq_status bsq_distill_kept_bytes(int64_t T, int64_t N, int64_t D, int32_t K, si
 /*   H, V    as for bsq_xent_loss
  *   ids     device int32 [T][K], any order; top device fp32 [T][K]; 1 <= K <= BSQ_MAX_TOP
  *   norm    device fp32 [T] or NULL
- *   scale   > 0, finite
+ *   scale   2^-64 .. 2^64
  *   loss, lse  device fp32 [T]
  *   kept    device buffer of bsq_distill_kept_bytes, 256-byte aligned, or NULL
  *   err     device int32 or NULL

@@ -885,8 +885,8 @@ bsq_status check_top_dims(int64_t T, int64_t N)
     return BSQ_OK;
 }
 
-// positive and finite
-bool good_scale(float s) { return s > 0.0f && std::isfinite(s); }
+// (far from where its products with logits overflow or vanish)
+bool good_scale(float s) { return s >= 0x1p-64f && s <= 0x1p64f; }
 }  // namespace
 
 bsq_status bsq_top_workspace_bytes(int64_t T, int64_t N, size_t *bytes)

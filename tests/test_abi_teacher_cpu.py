@@ -38,7 +38,7 @@ def test_top_rejects_before_launch():
     assert call(T=(1 << 20) + 1) == bsq.BSQ_ERR_UNSUPPORTED
     for K in (0, -1, 257):
         assert call(K=K) == bsq.BSQ_ERR_ARG
-    for s in (0.0, -1.0, float("inf"), float("nan")):
+    for s in (0.0, -1.0, float("inf"), float("nan"), 2.0 ** -65, 2.0 ** 65):
         assert call(scale=s) == bsq.BSQ_ERR_ARG
     for kw in (dict(Z=0), dict(ids=0), dict(top=0), dict(ws=0)):
         assert call(**kw) == bsq.BSQ_ERR_ARG
@@ -146,7 +146,7 @@ def test_distill_rejects_before_launch():
                                   _p(kept), kept_bytes, _p(dH), lddh, _p(dV), lddv, dt, acc, _p(err), _p(ws), ws_bytes, None)
     for g in (False, True):
         for kw in (dict(H=0), dict(V=0), dict(ids=0), dict(top=0), dict(a=0), dict(b=0), dict(ws=0), dict(K=0), dict(K=257),
-                   dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))):
+                   dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=2.0 ** -65), dict(scale=2.0 ** 65)):
             assert call(g, **kw) == bsq.BSQ_ERR_ARG, kw
         for kw in (dict(T=-1), dict(N=0), dict(D=60), dict(ldh=63), dict(ldv=63), dict(ldv=68)):
             assert call(g, **kw) == bsq.BSQ_ERR_SHAPE, kw

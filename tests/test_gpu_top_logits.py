@@ -119,6 +119,11 @@ def test_nan_and_infinities(dtype, gpu):
     _check(Z, 40, scale=0.5)
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -64, 1e-3, 30.0, 2.0 ** 64])
+def test_scales_of_any_size(scale, gpu):
+    _check(_rows(gpu, 5, 9001, torch.float32, seed=6), 12, scale=scale)
+
+
 def test_no_lse_and_given_outputs(gpu):
     Z = _rows(gpu, 20, 3001, torch.bfloat16)
     ids, top, lse = bsq.bsq_top_logits(Z, 10, want_lse=False)
