@@ -229,18 +229,7 @@ __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blo
                 last = id[h];
             }
         }
-        u32x4_t d;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) d[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
-        *reinterpret_cast<u32x4_t *>(dS + w) = d;
-        if (a.lo == 0) continue;
-        u32x4_t rest;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float x = v[2 * k] - __uint_as_float(d[k] << 16), y = v[2 * k + 1] - __uint_as_float(d[k] & 0xffff0000u);
-            rest[k] = pack_bf16x2(x - x == 0.0f ? x : 0.0f, y - y == 0.0f ? y : 0.0f);
-        }
-        *reinterpret_cast<u32x4_t *>(dS + w + a.lo) = rest;
+        put_d(dS + w, v, a.lo);
     }
 }
 

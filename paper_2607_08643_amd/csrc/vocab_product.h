@@ -247,6 +247,24 @@ __device__ __forceinline__ float kept_value(uint32_t code)
     return code ? __uint_as_float((code << 13) + 0x20000000u) : 0.0f;
 }
 
+// Eight values of d in bf16 and, where lo is not 0, what remains of them that much further
+// on (nothing remains of what is no number).
+__device__ __forceinline__ void put_d(uint16_t *q, const float (&v)[8], int64_t lo)
+{
+    u32x4_t d;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) d[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
+    *reinterpret_cast<u32x4_t *>(q) = d;
+    if (lo == 0) return;
+    u32x4_t rest;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float x = v[2 * k] - __uint_as_float(d[k] << 16), y = v[2 * k + 1] - __uint_as_float(d[k] & 0xffff0000u);
+        rest[k] = pack_bf16x2(x - x == 0.0f ? x : 0.0f, y - y == 0.0f ? y : 0.0f);
+    }
+    *reinterpret_cast<u32x4_t *>(q + lo) = rest;
+}
+
 // Tiles of a product over `live` tokens, and splits of dH's depth: until the
 // launch fills the compute units.
 struct XTiles {
@@ -483,7 +501,7 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
     // (the first tiles hold ten or more words of a row): f(the row's values, word, its place
     // in the lists, i).
     auto teacher_words = [&](auto f) {
-        constexpr int AT_ONCE = MF > 4 ? 2 : 4;
+        constexpr int AT_ONCE = MF <= 4 ? 4 : (EPI == EPI_TPROB ? 1 : 2);
         int most = 0;
 #pragma unroll
         for (int i = 0; i < MF; ++i) most = e_end[i] - e_beg[i] > most ? e_end[i] - e_beg[i] : most;
@@ -577,7 +595,7 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
             const int64_t row = int64_t(by) * G::BR + q;
             if (row < live) a.stat[int64_t(bx) * a.Tp + row] = make_float2(m, s);
         }
-    } else if constexpr (epi_prob(EPI)) {
+    } else if constexpr (EPI == EPI_PROB) {
         // d = g (exp(z - lse) - onehot); 0 for padded tokens and words. bf16 results
         // take it rounded to bf16: at most 2^-9 of each value, which with the rounding
         // of the results makes the gradients' relative error 2.2e-3 to 2.5e-3 where that
@@ -585,42 +603,22 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
         // products. A dV of 32 bits is asked for to be better than that: it takes what
         // remains as a second part (2^-18 is lost).
         const int64_t w0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * NF * g;
-        float gs[MF];
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
             const int64_t row = rbeg + 16 * i;
             const bool in = row < live;
-            const int64_t tg = TEACHER ? -1 : int64_t(a.tgt[row]) - a.v0;
-            const float lse = a.lse[row];
-            float total = 1.0f;
-            gs[i] = TEACHER ? a.g[row] * a.scale : a.g[row];
-            if constexpr (TEACHER) total = in ? a.total[e_tok[i]] : 0.0f;
+            const int64_t tg = int64_t(a.tgt[row]) - a.v0;
+            const float lse = a.lse[row] , gg = a.g[row];
+            float v[4 * NF];
 #pragma unroll
             for (int j = 0; j < NF; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int64_t w = w0 + 4 * j + r;
                     float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * LOG2E);
-                    if constexpr (TEACHER) p *= total;
-                    else if (w == tg) p -= 1.0f;
-                    acc[i][j][r] = (in && a.v0 + w < a.N) ? gs[i] * p : 0.0f;
+                    if (w == tg) p -= 1.0f;
+                    v[4 * j + r] = (in && a.v0 + w < a.N) ? gg * p : 0.0f;
                 }
-        }
-        if constexpr (TEACHER) {
-            teacher_words([&](f32x4_t(&v)[NF], int32_t word, int64_t at, int i) {
-                const int64_t q = word - a.v0 - w0;
-                if (q < 0 || q >= 4 * NF) return;
-                const float p = gs[i] * a.sp[at];
-#pragma unroll
-                for (int k = 0; k < 4 * NF; ++k) v[k >> 2][k & 3] -= (q == k) ? p : 0.0f;
-            });
-        }
-#pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            const int64_t row = rbeg + 16 * i;
-            float v[4 * NF];
-#pragma unroll
-            for (int k = 0; k < 4 * NF; ++k) v[k] = acc[i][k >> 2][k & 3];
             u32x4_t *q = reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w0);
 #pragma unroll
             for (int h = 0; h < NF / 2; ++h) {
@@ -640,6 +638,40 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
                 *reinterpret_cast<u32x4_t *>(a.dS + row * a.dsp + w0 + a.lo + 8 * h) = lo;
             }
         }
+    } else if constexpr (EPI == EPI_TPROB) {
+        // d = g scale (P exp(z - lse) - the teacher's words), likewise
+        const int64_t w0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * NF * g;
+        float gs[MF];
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int64_t row = rbeg + 16 * i;
+            const bool in = row < live;
+            const float lse = a.lse[row], total = in ? a.total[e_tok[i]] : 0.0f;
+            gs[i] = a.g[row] * a.scale;
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = total * __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * LOG2E);
+                    acc[i][j][r] = (in && a.v0 + w0 + 4 * j + r < a.N) ? gs[i] * p : 0.0f;
+                }
+        }
+        teacher_words([&](f32x4_t(&v)[NF], int32_t word, int64_t at, int i) {
+            const int64_t q = word - a.v0 - w0;
+            if (q < 0 || q >= 4 * NF) return;
+            const float p = gs[i] * a.sp[at];
+#pragma unroll
+            for (int k = 0; k < 4 * NF; ++k) v[k >> 2][k & 3] -= (q == k) ? p : 0.0f;
+        });
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int h = 0; h < NF / 2; ++h) {
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = acc[i][2 * h + (k >> 2)][k & 3];
+                put_d(a.dS + (rbeg + 16 * i) * a.dsp + w0 + 8 * h, v, a.lo);
+            }
     } else if constexpr (EPI == EPI_DH || EPI == EPI_DH2) {
         // fp32 sums over the pieces, each split its own
         float *o = a.dHp + int64_t(z) * a.Tp * a.Dp;
