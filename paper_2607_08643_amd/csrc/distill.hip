@@ -17,6 +17,11 @@
 // memory and has one product less to do: 6 bytes a logit moved against 2 D operations. (d
 // is rounded to bf16 all the same, 2^-9, beside which 2^-11 adds nothing to speak of; for a
 // dV of 32 bits the logits are made again.)
+//
+// Bound by the matrix cores from some hundred tokens on: 4096 tokens of 151936 words, 4096
+// inputs: logits with what is kept of them 4.5 ms (1.14 PFLOP/s), d 0.44 (5.6 TB/s), dH 3.7
+// (1.38), dV 4.1 (1.24); the teacher's words 17 us. 37 tokens of 32003 words, 1000 inputs:
+// the logits 18 us (one reading of V, 3.6 TB/s), three short launches 14.
 #include "vocab_product.h"
 #include "vocab_rows.h"
 

@@ -25,6 +25,10 @@
 // is larger, by the first launch's sums, and their rests; the draw puts them together with
 // the exact sums. A word on the wrong side counts for less than 1e-5 of itself, and where
 // so little is left that this would matter the draw forms the weights anew.
+//
+// 64 sequences of four drafts, 151936 words in bf16: rows 39 us (175 MB, 4.5 TB/s), the
+// drawn rows 35 (64-bit exponentials: two a word), draws 7. One sequence: 6, 9 and 6, each
+// a chain of a few dependent loads.
 #include <algorithm>
 
 #include "vocab_rows.h"
@@ -40,7 +44,11 @@ constexpr int64_t RUN = 512;           // words of a vector a lane
 constexpr int MAXL = BSQ_MAX_DRAFTS;
 constexpr double LOG2E_64 = 1.4426950408889634074;
 constexpr float MAX_TEMPERATURE = 0x1p64f, MIN_TEMPERATURE = 0x1p-64f;
-constexpr double UNSURE = 0x1p-15;     // of p: what the first launch's sums leave open, twice over
+// Of p, what the first launch's sums leave open. A term's exponent is rounded three times
+// (2^-24 of it each; its mean under the softmax is at most log2 N < 31), the exponential by
+// 2^-22, a thread's 32 terms by 2^-19, what a larger logit rescales by 2^-22 a time: 1e-5 of
+// a sum, 2e-5 of the ratio of two.
+constexpr double UNSURE = 0x1p-15;
 constexpr double LITTLE = 0x1p-8;      // of the whole: max(p - q, 0) is formed word by word
 static_assert(MAXL <= 64, "a lane for every drafted token");
 static_assert(2 * MAXL + 1 <= DT, "a thread for every row");

