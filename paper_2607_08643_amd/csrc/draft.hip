@@ -16,9 +16,10 @@
 //
 // Results are those of 64-bit sums. A cumulative sum over 151936 words passes a given
 // random number at the same word as the definition's only if it is off by much less than
-// one word's share; with exponentials of 32 bits one draw in some 200 would be another
-// word. Exponentials of 64 bits cost some 125 cycles a wave, four times what a word
-// costs to read, so the rows that only decide are summed in 32 (3e-5 of a ratio covers
+// one word's share; with exponentials of 32 bits (some 3e-8 of the sum off) one draw
+// in some 200 would be another word. Exponentials of 64 bits bound the reading (all
+// rows of 64 sequences 78 us, in 32 bits 39), so the rows that only decide are summed
+// in 32 (3e-5 of a ratio covers
 // every rounding), and where u q lies so near to p that this does not settle it the block
 // sums the two rows again in 64. max(p - q, 0) of the drawn row needs both rows' sums
 // before it can be formed: the second launch instead splits p and q into the words where p

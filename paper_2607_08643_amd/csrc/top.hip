@@ -16,9 +16,10 @@
 // larger ones. Where rows are cut into segments a second launch does that for all
 // segments of a row.
 //
-// 512 rows of 151936 words in bf16, K = 64: 42 us (156 MB, 3.7 TB/s), of which reading alone
-// takes 26, the exponentials 6, the words that pass the bound some 6, the cut 4. Few
-// rows take two launches of 7 us, chains of a few dependent steps.
+// 512 rows of 151936 words in bf16, K = 64: 42 us (156 MB, 3.7 TB/s). With parts left
+// out of a run of 44: reading and the bound alone 26, all but the exponentials 38, all but
+// the last cut 39, without words that pass (and so nothing to cut) 33. Few rows take two
+// launches of 7 to 8 us, chains of a few dependent steps.
 #include <algorithm>
 #include <type_traits>
 
