@@ -35,7 +35,7 @@ static_assert(KMAX <= XT, "a thread for every word of a token");
 struct TeacherArgs {
     const int32_t *ids;
     const float *top, *norm;
-    int64_t T, N, tiles;
+    int64_t N, tiles;
     int K;
     float scale;
     int64_t *live;    // [T]: 0, or -1 for a token without a loss
@@ -299,7 +299,6 @@ hipError_t launch_teacher(const DistillCall &c, const SLayout &l, bool make, XAr
     h.ids = c.ids;
     h.top = c.top;
     h.norm = c.norm;
-    h.T = c.x.T;
     h.N = c.x.N;
     h.tiles = l.x.tiles;
     h.K = c.K;

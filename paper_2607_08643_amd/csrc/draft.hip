@@ -16,16 +16,16 @@
 //
 // Results are those of 64-bit sums. A cumulative sum over 151936 words passes a given
 // random number at the same word as the definition's only if it is off by much less than
-// one word's share; with exponentials of 32 bits (some 3e-8 of the sum off) one draw
-// in some 200 would be another word. Exponentials of 64 bits bound the reading (all
-// rows of 64 sequences 78 us, in 32 bits 39), so the rows that only decide are summed
-// in 32 (3e-5 of a ratio covers
-// every rounding), and where u q lies so near to p that this does not settle it the block
-// sums the two rows again in 64. max(p - q, 0) of the drawn row needs both rows' sums
-// before it can be formed: the second launch instead splits p and q into the words where p
-// is larger, by the first launch's sums, and their rests; the draw puts them together with
-// the exact sums. A word on the wrong side counts for less than 1e-5 of itself, and where
-// so little is left that this would matter the draw forms the weights anew.
+// one word's share; with exponentials of 32 bits (some 3e-8 of the sum off) one draw in
+// some 200 would be another word. Exponentials of 64 bits bound the reading (all rows of 64
+// sequences 78 us, in 32 bits 39), so the rows that only decide are summed in 32 (3e-5 of a
+// ratio covers every rounding), and where u q lies so near to p that this does not settle
+// it the block sums the two rows again in 64. max(p - q, 0) of the drawn row needs both
+// rows' sums before it can be formed: the second launch instead splits p and q into the
+// words where p is larger, by the first launch's sums, and their rests; the draw puts them
+// together with the exact sums. A word on the wrong side counts for less than 1e-5 of
+// itself, and where so little is left that this would matter the draw forms the weights
+// anew.
 //
 // 64 sequences of four drafts, 151936 words in bf16: rows 39 us (175 MB, 4.5 TB/s), the
 // drawn rows 35 (64-bit exponentials: two a word), draws 7. One sequence: 6, 9 and 6, each
@@ -443,62 +443,58 @@ __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
 {
     __shared__ DecideShared sh;
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-    const uint32_t items = uint32_t(a.B) * a.parts;
-    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t b = item / uint32_t(a.parts), part = item - b * a.parts;
-        bool bad = false;
-        const int n = seq_len(a, b, bad);
-        const double c = seq_scale(a, b, bad);
-        const double reach = 1000.0 / c;
-        const Decision d = decide<PB, QB>(a, b, n, c, reach, bad, sh);
-        if (part == 0 && t == 0) {
-            a.dec[b] = d;
-            if (d.bits && a.err) atomicOr(a.err, d.bits);
-        }
-        if (d.kind <= DRAW_OTHERS) {
-            const Drawn<PB, QB> drawn(a, b, d, c, reach);
-            const bool rest = d.kind == DRAW_REST;
-            const double ratio = d.sp / d.sq;  // p > q where ep > eq ratio
-            // (vectors of a wave: the next one is in flight)
-            Words8<PB> zp;
-            Words8<QB> zq;
-            const int step = a.parts * (DT / 64);
-            int r = part * (DT / 64) + w;
-            auto read = [&](int run, int64_t at) {
-                const int64_t n0 = run * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
-                drawn.read(n0 + at + 8 * lane, n1, rest, zp, zq);
-            };
-            if (r < a.runs) read(r, 0);
-            for (; r < a.runs; r += step) {
-                const int64_t n0 = r * a.run;
-                Run s{0.0, 0.0, 0.0, 0.0};
-                for (int64_t at = 0; at < a.run; at += RUN) {
-                    const Words8<PB> wp = zp;
-                    const Words8<QB> wq = zq;
-                    if (at + RUN < a.run) read(r, at + RUN);
-                    else if (r + step < a.runs) read(r + step, 0);
+    const uint32_t b = blockIdx.x / uint32_t(a.parts), part = blockIdx.x - b * a.parts;
+    bool bad = false;
+    const int n = seq_len(a, b, bad);
+    const double c = seq_scale(a, b, bad);
+    const double reach = 1000.0 / c;
+    const Decision d = decide<PB, QB>(a, b, n, c, reach, bad, sh);
+    if (part == 0 && t == 0) {
+        a.dec[b] = d;
+        if (d.bits && a.err) atomicOr(a.err, d.bits);
+    }
+    if (d.kind <= DRAW_OTHERS) {
+        const Drawn<PB, QB> drawn(a, b, d, c, reach);
+        const bool rest = d.kind == DRAW_REST;
+        const double ratio = d.sp / d.sq;  // p > q where ep > eq ratio
+        // (vectors of a wave: the next one is in flight)
+        Words8<PB> zp;
+        Words8<QB> zq;
+        const int step = a.parts * (DT / 64);
+        int r = part * (DT / 64) + w;
+        auto read = [&](int run, int64_t at) {
+            const int64_t n0 = run * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
+            drawn.read(n0 + at + 8 * lane, n1, rest, zp, zq);
+        };
+        if (r < a.runs) read(r, 0);
+        for (; r < a.runs; r += step) {
+            const int64_t n0 = r * a.run;
+            Run s{0.0, 0.0, 0.0, 0.0};
+            for (int64_t at = 0; at < a.run; at += RUN) {
+                const Words8<PB> wp = zp;
+                const Words8<QB> wq = zq;
+                if (at + RUN < a.run) read(r, at + RUN);
+                else if (r + step < a.runs) read(r + step, 0);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const double ep = n0 + at + 8 * lane + e == drawn.out ? 0.0 : drawn.p(wp[e]);
-                        s.p += ep;
-                        if (!rest) continue;
-                        const double eq = drawn.q(wq[e]);
-                        const bool above = ep > eq * ratio;
-                        s.q += eq;
-                        s.above_p += above ? ep : 0.0;
-                        s.above_q += above ? eq : 0.0;
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const double ep = n0 + at + 8 * lane + e == drawn.out ? 0.0 : drawn.p(wp[e]);
+                    s.p += ep;
+                    if (!rest) continue;
+                    const double eq = drawn.q(wq[e]);
+                    const bool above = ep > eq * ratio;
+                    s.q += eq;
+                    s.above_p += above ? ep : 0.0;
+                    s.above_q += above ? eq : 0.0;
                 }
-                s.p = wave_sum(s.p);
-                if (rest) {
-                    s.q = wave_sum(s.q);
-                    s.above_p = wave_sum(s.above_p);
-                    s.above_q = wave_sum(s.above_q);
-                }
-                if (lane == 0) a.rest[int64_t(b) * a.runs + r] = s;
             }
+            s.p = wave_sum(s.p);
+            if (rest) {
+                s.q = wave_sum(s.q);
+                s.above_p = wave_sum(s.above_p);
+                s.above_q = wave_sum(s.above_q);
+            }
+            if (lane == 0) a.rest[int64_t(b) * a.runs + r] = s;
         }
-        __syncthreads();
     }
 }
 
@@ -686,13 +682,12 @@ DLayout draft_layout(int64_t B, int64_t L, int64_t N, bool draft)
 template <bool PB, bool QB>
 hipError_t launch_draft(const DArgs &a, const DLayout &l, hipStream_t st)
 {
-    const int64_t most = int64_t(1) << 20;  // blocks of a launch; they walk the rest
     const dim3 grid{unsigned(l.blocks)};
     if (l.vectors == 2) hipLaunchKernelGGL((draft_rows_kernel<PB, QB, 2>), grid, dim3(DT), 0, st, a);
     else hipLaunchKernelGGL((draft_rows_kernel<PB, QB, 4>), grid, dim3(DT), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((draft_rest_kernel<PB, QB>), dim3(unsigned(std::min(most, a.B * a.parts))), dim3(DT), 0, st, a);
+    hipLaunchKernelGGL((draft_rest_kernel<PB, QB>), dim3(unsigned(a.B * a.parts)), dim3(DT), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL((draft_draw_kernel<PB, QB>), dim3(unsigned(a.B)), dim3(64), 0, st, a);
     return hipGetLastError();

@@ -45,7 +45,7 @@ static_assert(LIST < 65536, "places are of 16 bits");
 
 struct TArgs {
     const void *Z;
-    int64_t ldz, T, N, len;   // len: words of a segment
+    int64_t ldz, N, len;   // len: words of a segment
     int segs, K;
     float scale;
     int64_t row0;             // first row of the launch
@@ -609,7 +609,6 @@ hipError_t launch_top_logits(const TopCall &c, hipStream_t st)
     TArgs a{};
     a.Z = c.Z;
     a.ldz = c.ldz;
-    a.T = c.T;
     a.N = c.N;
     a.len = l.len;
     a.segs = l.segs;

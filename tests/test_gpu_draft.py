@@ -326,3 +326,45 @@ def test_another_stream_and_a_captured_call(gpu):
         torch.cuda.synchronize()
         for h, w, x in zip(held, want, again):
             assert torch.equal(h, w) and torch.equal(x, w)
+
+
+def test_the_largest_batch(gpu):
+    say("draft B=65536 L=1 N=2")
+    g = torch.Generator().manual_seed(3)
+    B = 65536
+    target, u, r = torch.randn((B, 2, 2), generator=g), torch.rand((B, 1), generator=g), torch.rand(B, generator=g)
+    tokens = torch.randint(0, 2, (B, 1), generator=g).int()
+    p = target.double().softmax(2)
+    kept = u[:, 0].double() < p[:, 0].gather(1, tokens.long())[:, 0]
+    # refused: the other word is all that is left
+    after = torch.where(p[:, 1, 0] > r.double(), 0, 1)
+    want = torch.stack([torch.where(kept, tokens[:, 0], 1 - tokens[:, 0]), torch.where(kept, after, -1)], 1).int()
+    _check((kept.int(), want), bsq.bsq_draft_verify(target.to(gpu), tokens.to(gpu), u.to(gpu), r.to(gpu)))
+
+
+def test_rows_that_sequences_share(gpu):
+    say("draft rows of stride 0")
+    target, tokens, u, r, draft, lens, temp = _case(gpu, 6, 3, 1001)
+    one, two = target[:1].expand(6, 4, 1001), draft[:, :1].expand(6, 3, 1001)
+    _check(_reference(one, tokens, u, r, two, lens, temp),
+           bsq.bsq_draft_verify(one, tokens, u, r, two, lens=lens, temperature=temp))
+
+
+def test_two_streams_at_once(gpu):
+    say("draft and top logits on two streams")
+    target, tokens, u, r, draft, lens, temp = _case(gpu, 5, 4, 32003)
+    want = _reference(target, tokens, u, r, draft)
+    ids, top, lse = bsq.bsq_top_logits(target[:, 0], 40)
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        with torch.cuda.stream(one):
+            verified = bsq.bsq_draft_verify(target, tokens, u, r, draft)
+        with torch.cuda.stream(two):
+            listed = bsq.bsq_top_logits(target[:, 0], 40)
+        got.append((verified, listed))
+    torch.cuda.synchronize()
+    for verified, listed in got:
+        _check(want, verified)
+        assert all(torch.equal(x, y) for x, y in zip(listed, (ids, top, lse)))
