@@ -19,7 +19,7 @@
 // dV of 32 bits the logits are made again.)
 //
 // Bound by the matrix cores from some hundred tokens on: 4096 tokens of 151936 words, 4096
-// inputs: logits with what is kept of them 4.7 ms (1.08 PFLOP/s), d 0.44 (5.6 TB/s), dH 4.0
+// inputs: logits with what is kept of them 4.55 ms (1.12 PFLOP/s), d 0.44 (5.6 TB/s), dH 4.0
 // (1.27), dV 4.5 (1.14), as a profiler sees them (the step 4% longer than without); the
 // teacher's words 18 to 21 us. 37 tokens of 32003 words, 1000 inputs:
 // the logits 18 to 19 us (one reading of V, 3.4 to 3.6 TB/s), three short launches 14.

@@ -492,10 +492,12 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
             e_beg[i] = e_tok[i] < 0 ? 0 : o[0];
             e_end[i] = e_tok[i] < 0 ? 0 : o[1];
         }
+        if constexpr (EPI == EPI_TPROB) {
 #pragma unroll
-        for (int i = 0; i < MF; ++i)
+            for (int i = 0; i < MF; ++i)
 #pragma unroll
-            for (int j = 0; j < NF; ++j) acc[i][j] *= a.scale;
+                for (int j = 0; j < NF; ++j) acc[i][j] *= a.scale;
+        }
     }
     // Visits them, some of every row at a time so that their loads are in flight together
     // (the first tiles hold ten or more words of a row): f(the row's values, word, its place
@@ -533,58 +535,104 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
                 float z = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 4 * NF; ++k) z = (q == k) ? v[k >> 2][k & 3] : z;
-                a.zk[at] = z;
+                a.zk[at] = z * a.scale;
             });
+        if constexpr (TEACHER) {
+            // Logits are scaled with the difference from the largest of the token's four
+            // lanes, which is found first: no sum is rescaled, and what is kept is there. Words
+            // past the vocabulary, in its last tile alone, are -inf; a NaN reaches the sum by
+            // its exponential. (2000 tokens of 151936 words, 4096 inputs: 2196 us against 2252
+            // with each lane's own largest and checks of every word, 2156 with neither maximum
+            // nor exponentials; 4096 tokens with what is kept 4414, 4522 and, with nothing kept
+            // either, 4084.)
+            if (a.v0 + int64_t(bx + 1) * G::BL > a.N) {
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            const int64_t row = rbeg + 16 * i;
-            const int tg = (!TEACHER && row < a.Tp) ? a.tgt[row] : -1;
-            float m = -__builtin_inff();
-            bool nan = false;
+                for (int j = 0; j < NF; ++j)
 #pragma unroll
-            for (int j = 0; j < NF; ++j)
+                    for (int r = 0; r < 4; ++r)
+                        if (w0 + 4 * j + r >= a.N) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t w = w0 + 4 * j + r;
-                    if (w >= a.N) continue;
-                    const float z = acc[i][j][r];
-                    if (!TEACHER && w == tg) a.ztgt[row] = z;
-                    nan |= !(z == z);
-                    m = z > m ? z : m;
+                            for (int i = 0; i < MF; ++i) acc[i][j][r] = -__builtin_inff();
+                        }
+            }
+            const float c = a.scale * LOG2E;
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                const int64_t row = rbeg + 16 * i;
+                float m = -__builtin_inff();
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[i][j][r]);
+#pragma unroll
+                for (int d = 16; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+                // (a finite value: where all are -inf the sum is 0)
+                const float ref = (m == -__builtin_inff()) ? 0.0f : m;
+                float s = 0.0f;
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        acc[i][j][r] = __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * c);
+                        s += acc[i][j][r];
+                    }
+#pragma unroll
+                for (int d = 16; d < 64; d <<= 1) s += __shfl_xor(s, d);
+                m *= a.scale;
+                if constexpr (NF == 4) {
+                    if (a.kept && row < live) {
+                        u32x4_t code[2];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            code[k >> 2][k & 3] = kept_code(acc[i][k >> 1][2 * (k & 1)]) |
+                                                  kept_code(acc[i][k >> 1][2 * (k & 1) + 1]) << 16;
+                        u32x4_t *q = reinterpret_cast<u32x4_t *>(a.kept + row * a.ldk + w0);
+                        q[0] = code[0];
+                        q[1] = code[1];
+                        if (g == 0) a.kept_max[row * (a.ldk / 64) + w0 / 64] = m;
+                    }
                 }
-            float s = 0.0f;
-            // against a finite value: a lane whose words are all -inf (or absent) adds 0
-            const float ref = (m == -__builtin_inff()) ? 0.0f : m;
-#pragma unroll
-            for (int j = 0; j < NF; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * LOG2E);
-                    if (w0 + 4 * j + r < a.N) s += e;
-                    if constexpr (TEACHER) acc[i][j][r] = e;
-                }
-            if (nan) s = __builtin_nanf("");
-            const float own = m;
-            // join the four lanes of the token
-#pragma unroll
-            for (int d = 16; d < 64; d <<= 1) join_stats(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
-            if constexpr (TEACHER && NF == 4) {
-                if (a.kept && row < live) {
-                    const float f = own == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((own - m) * LOG2E);
-                    u32x4_t code[2];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        code[k >> 2][k & 3] = kept_code(acc[i][k >> 1][2 * (k & 1)] * f) |
-                                              kept_code(acc[i][k >> 1][2 * (k & 1) + 1] * f) << 16;
-                    u32x4_t *q = reinterpret_cast<u32x4_t *>(a.kept + row * a.ldk + w0);
-                    q[0] = code[0];
-                    q[1] = code[1];
-                    if (g == 0) a.kept_max[row * (a.ldk / 64) + w0 / 64] = m;
+                if (g == 0) {
+                    s_max[wn * G::BR + 16 * (wm * MF + i) + r16] = m;
+                    s_sum[wn * G::BR + 16 * (wm * MF + i) + r16] = s;
                 }
             }
-            if (g == 0) {
-                s_max[wn * G::BR + 16 * (wm * MF + i) + r16] = m;
-                s_sum[wn * G::BR + 16 * (wm * MF + i) + r16] = s;
+        } else {
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                const int64_t row = rbeg + 16 * i;
+                const int tg = (row < a.Tp) ? a.tgt[row] : -1;
+                float m = -__builtin_inff();
+                bool nan = false;
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int64_t w = w0 + 4 * j + r;
+                        if (w >= a.N) continue;
+                        const float z = acc[i][j][r];
+                        if (w == tg) a.ztgt[row] = z;
+                        nan |= !(z == z);
+                        m = z > m ? z : m;
+                    }
+                float s = 0.0f;
+                // against a finite value: a lane whose words are all -inf (or absent) adds 0
+                const float ref = (m == -__builtin_inff()) ? 0.0f : m;
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float e = __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * LOG2E);
+                        if (w0 + 4 * j + r < a.N) s += e;
+                    }
+                if (nan) s = __builtin_nanf("");
+                // join the four lanes of the token
+#pragma unroll
+                for (int d = 16; d < 64; d <<= 1) join_stats(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+                if (g == 0) {
+                    s_max[wn * G::BR + 16 * (wm * MF + i) + r16] = m;
+                    s_sum[wn * G::BR + 16 * (wm * MF + i) + r16] = s;
+                }
             }
         }
         __syncthreads();
