@@ -154,12 +154,13 @@ __device__ __forceinline__ void piece_stats(const void *row, int64_t n0, int64_t
         }
     };
     load(n0 + 8 * threadIdx.x);
-    // (the same number of turns for every thread)
-    for (int64_t base = n0 + 8 * threadIdx.x; base < n1 + 8 * threadIdx.x; base += NV * VSTEP) {
+    // Every thread has the same turns: one whose words of the last lie past n1 has -inf there.
+    for (int64_t turn = n0; turn < n1; turn += NV * VSTEP) {
+        const int64_t base = turn + 8 * threadIdx.x;
         Words8<BF16> w[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) w[k] = next[k];
-        if (base + NV * VSTEP < n1) load(base + NV * VSTEP);
+        if (turn + NV * VSTEP < n1) load(base + NV * VSTEP);
         if (c == 0.0f) {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
