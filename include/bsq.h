@@ -716,8 +716,10 @@ bsq_status bsq_top_logits(const void *Z, int32_t z_dtype, int64_t ldz, int64_t T
  *   d_tv = g_t scale (P q_v - sum of p_k over id(t,k) = v),  dH = d V,  dV = d^T H.
  * norm: the lse of the teacher's whole vocabulary (bsq_top_logits at the same scale;
  * P is then the part that the K words hold), or NULL for that of the K words
- * (P = 1). scale is one over a temperature; a factor of its square, where wanted,
- * goes into g. A word that is listed twice counts twice. A negative id, or a logit
+ * (P = 1). norm is of 32 bits: its rounding changes every p by a factor of up to
+ * exp(2^-24 |norm|), so that products of scale and logits beyond some thousands want
+ * NULL. scale is one over a temperature; a factor of its square, where wanted, goes
+ * into g. A word that is listed twice counts twice. A negative id, or a logit
  * of -inf, is no word; an id of N or more likewise, and ORs BSQ_DEVERR_BAD_SET into
  * *err. A token without words has no loss: its loss, lse and row of dH are 0, and
  * its hidden state and g are not used (they may be NaN). Roundings as for the

@@ -64,8 +64,7 @@ __global__ __launch_bounds__(XT) void distill_teacher_kernel(const TeacherArgs a
 {
     __shared__ uint64_t s_key[KMAX];
     __shared__ int32_t s_id[KMAX];
-    __shared__ double s_sum[XT / 64];
-    __shared__ float s_max[XT / 64];
+    __shared__ double s_sum[XT / 64], s_max[XT / 64];
     const int t = threadIdx.x;
     const int64_t m = blockIdx.x;
     int32_t id = -1;
@@ -87,17 +86,18 @@ __global__ __launch_bounds__(XT) void distill_teacher_kernel(const TeacherArgs a
     // absent words last, each key another
     const uint64_t key = (uint64_t(uint32_t(there ? id : INT32_MAX)) << 16) | uint32_t(t);
     s_key[t] = key;
-    float mx = float(x);  // what is subtracted before the exponentials: any value near the largest
-    mx = wave_max(mx);
+    // The largest in 64 bits, so that its exponential is 1: rounded to 32 it is some 2^-24 of
+    // itself off, which leaves exp's range from products of 10^10 on. (A NaN counts as nothing.)
+    double mx = lane_value(wave_scan(x, -__builtin_inf(), [](double a, double b) { return fmax(a, b); }), 63);
     if ((t & 63) == 0) s_max[t >> 6] = mx;
     const bool live = __syncthreads_or(there);
-    for (int w = 0; w < XT / 64; ++w) mx = fmaxf(mx, s_max[w]);
+    for (int w = 0; w < XT / 64; ++w) mx = fmax(mx, s_max[w]);
     double logp, p;
     if (a.norm) {
         logp = x - double(a.norm[m]);
     } else {
-        const double sum = block_sum64(there ? exp(x - double(mx)) : 0.0, s_sum);
-        logp = x - (double(mx) + log(sum));
+        const double sum = block_sum64(there ? exp(x - mx) : 0.0, s_sum);
+        logp = (x - mx) - log(sum);
     }
     p = there ? exp(logp) : 0.0;
     const double total = block_sum64(p, s_sum);
