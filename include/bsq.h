@@ -772,7 +772,8 @@ bsq_status bsq_distill_grad(const void *H, int64_t ldh, const void *V, int64_t l
  * Without draft logits the drafts are certain (found in the text): q_i is 1 at
  * x_i and 0 elsewhere. At temperature 0 x_i is accepted if it is the word of the
  * largest target logit (of equal ones the lowest), and the next token is that word;
- * u, r and the draft logits are not used. Probabilities and sums are 64-bit.
+ * u, r and the draft logits are not used. Results are those of probabilities and sums
+ * in 64 bits, with exponentials to 4e-14 of themselves.
  * Words of -inf have probability 0. Where nothing is left of max(p_i - q_i, 0) the
  * draw is from p_i. A target row without a probability (a NaN or +inf in it, or
  * nothing but -inf) accepts nothing and its next token is -1; a draft row like

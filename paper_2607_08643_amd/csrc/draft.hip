@@ -22,14 +22,17 @@
 // ratio covers every rounding), and where u q lies so near to p that this does not settle
 // it the block sums the two rows again in 64. max(p - q, 0) of the drawn row needs both
 // rows' sums before it can be formed: the second launch instead splits p and q into the
-// words where p is larger, by the first launch's sums, and their rests; the draw puts them
-// together with the exact sums. A word on the wrong side counts for less than 1e-5 of
-// itself, and where so little is left that this would matter the draw forms the weights
-// anew.
+// words where p is larger, by the first launch's sums, and their rests, and marks the runs
+// that hold a word where p / q lies within 2^-20 of 1. The draw puts them together with the
+// exact sums, which are by now known to say how far off the first ones were (up to 5e-7 in
+// rows of many shapes): where that is less than 2^-20 only the marked runs can hold a word on
+// the wrong side, and their weights are formed anew, word by word; else those of all.
 //
 // 64 sequences of four drafts, 151936 words in bf16: rows 39 us (175 MB, 4.5 TB/s), the
-// drawn rows 35 (64-bit exponentials: two a word), draws 7. One sequence: 6, 9 and 6, each
-// a chain of a few dependent loads.
+// drawn rows 36 (64-bit exponentials: two a word), draws 8. One sequence: 6, 9 and 6, each
+// a chain of a few dependent loads. Where all runs are weighed anew (drafts in bf16 that
+// are the target's but for some words) the draws take some 350 more: a wave reads both
+// rows.
 #include <algorithm>
 
 #include "vocab_rows.h"
@@ -40,7 +43,7 @@ namespace {
 constexpr int DT = 256;                // threads of a block
 constexpr int64_t VSTEP = 8 * DT;      // words of a vector a thread
 constexpr int64_t MOST_TURNS = 2048;   // blocks of the first launch: those that run together
-constexpr int64_t MAX_RUNS = 4096;     // of a row
+constexpr int64_t MAX_RUNS = 4096;     // of a row: 64 a lane
 constexpr int64_t RUN = 512;           // words of a vector a lane
 constexpr int MAXL = BSQ_MAX_DRAFTS;
 constexpr double LOG2E_64 = 1.4426950408889634074;
@@ -50,7 +53,10 @@ constexpr float MAX_TEMPERATURE = 0x1p64f, MIN_TEMPERATURE = 0x1p-64f;
 // 2^-22, a thread's 32 terms by 2^-19, what a larger logit rescales by 2^-22 a time: 1e-5 of
 // a sum, 2e-5 of the ratio of two.
 constexpr double UNSURE = 0x1p-15;
-constexpr double LITTLE = 0x1p-8;      // of the whole: max(p - q, 0) is formed word by word
+// Of p, how near q has to be for the first launch's sums to leave open which is larger: 2^-20.
+// (Few words are: of drafts with noise of 0.6 in their logits one in 10^6.)
+constexpr int CLOSE_BITS = 20;
+constexpr double CLOSE = 0x1p-20;
 static_assert(MAXL <= 64, "a lane for every drafted token");
 static_assert(2 * MAXL + 1 <= DT, "a thread for every row");
 
@@ -63,9 +69,11 @@ struct Piece {
 };
 
 // Of a run of the row that is drawn from: its words' exponentials (without the refused token
-// of a certain draft) and the draft row's, and of both those of the words where p > q.
+// of a certain draft) and the draft row's, and of both those of the words where p > q by the
+// first launch's sums; close: whether it has words where those leave this open.
 struct Run {
     double p, q, above_p, above_q;
+    int32_t close, pad;
 };
 
 // What a sequence's drafts came to: `kind` of draw, the rows' largest logits and sums (those
@@ -438,6 +446,8 @@ struct Drawn {
     }
 };
 
+__device__ __forceinline__ int32_t high_word(double v) { return int32_t(__builtin_bit_cast(uint64_t, v) >> 32); }
+
 // Decisions, and the weight of every run of the row that the next token is drawn from.
 template <bool PB, bool QB>
 __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
@@ -470,7 +480,8 @@ __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
         if (r < a.runs) read(r, 0);
         for (; r < a.runs; r += step) {
             const int64_t n0 = r * a.run;
-            Run s{0.0, 0.0, 0.0, 0.0};
+            Run s{0.0, 0.0, 0.0, 0.0, 0, 0};
+            int32_t closest = 0;  // how far the high word of ep - eq ratio is below that of ep
             for (int64_t at = 0; at < a.run; at += RUN) {
                 const Words8<PB> wp = zp;
                 const Words8<QB> wq = zq;
@@ -482,7 +493,11 @@ __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
                     s.p += ep;
                     if (!rest) continue;
                     const double eq = drawn.q(wq[e]);
-                    const bool above = ep > eq * ratio;
+                    // (by the high words: exponent and 20 bits. Equal ones count as above and are
+                    // close, those of 0 add nothing and are not)
+                    const int32_t more = high_word(__builtin_fma(-eq, ratio, ep)), below = high_word(ep) - (more & 0x7fffffff);
+                    const bool above = more >= 0;
+                    closest = below > closest ? below : closest;
                     s.q += eq;
                     s.above_p += above ? ep : 0.0;
                     s.above_q += above ? eq : 0.0;
@@ -493,6 +508,7 @@ __global__ __launch_bounds__(DT) void draft_rest_kernel(const DArgs a)
                 s.q = wave_sum(s.q);
                 s.above_p = wave_sum(s.above_p);
                 s.above_q = wave_sum(s.above_q);
+                s.close = __ballot(closest > (CLOSE_BITS << 20)) != 0;
             }
             if (lane == 0) a.rest[int64_t(b) * a.runs + r] = s;
         }
@@ -531,15 +547,20 @@ __global__ __launch_bounds__(64) void draft_draw_kernel(const DArgs a)
         double ip = 1.0, iq = 0.0;  // a word's weight: ep ip - eq iq, where that is more than 0
         bool rest = d.kind == DRAW_REST;
         const Drawn<PB, QB> drawn(a, b, d, c, 1000.0 / c);
+        uint64_t open = 0;  // the lane's runs that may hold a word on the wrong side
         if (rest) {
             double sp = 0.0, sq = 0.0;
 #pragma unroll 4
             for (int k = r0; k < r1; ++k) {
                 sp += runs[k].p;
                 sq += runs[k].q;
+                open |= uint64_t(runs[k].close) << (k - r0);
             }
             ip = 1.0 / wave_sum(sp);
             iq = 1.0 / wave_sum(sq);
+            // (2^-10 of it for the roundings of this comparison and of the marks)
+            if (!(__builtin_fabs(d.sp / d.sq * ip / iq - 1.0) < CLOSE * (1.0 - 0x1p-10)))
+                open = r0 < r1 ? ~uint64_t(0) >> (64 - (r1 - r0)) : 0;
         }
         auto weight = [&](double ep, double eq) {
             const double v = ep * ip - eq * iq;
@@ -552,36 +573,33 @@ __global__ __launch_bounds__(64) void draft_draw_kernel(const DArgs a)
             for (int k = r0; k < r1; ++k) v += run_weight(k);
             return v;
         };
-        double own = lane_weight(), incl = sum_scan(own), all = lane_value(incl, 63);
-        if (rest && !(all > LITTLE)) {
-            // word by word; each lane keeps the weights of its own runs
-            for (int k = 0; k < a.runs; ++k) {
-                const int64_t n0 = k * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
-                double s = 0.0;
-                for (int64_t at = n0; at < n1; at += RUN) {
-                    double ep[8], eq[8];
-                    drawn.eight(at + 8 * lane, n1, true, ep, eq);
+        // their weights word by word; the lane that has the run keeps it
+        for (uint64_t some; (some = __ballot(open != 0)) != 0;) {
+            const int who = __builtin_ctzll(some), run = lane_value(r0 + (open ? __builtin_ctzll(open) : 0), who);
+            const int64_t n0 = run * a.run, n1 = n0 + a.run < a.N ? n0 + a.run : a.N;
+            double s = 0.0;
+            for (int64_t at = n0; at < n1; at += RUN) {
+                double ep[8], eq[8];
+                drawn.eight(at + 8 * lane, n1, true, ep, eq);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s += weight(ep[e], eq[e]);
-                }
-                s = wave_sum(s);
-                if (k >= r0 && k < r1) {
-                    runs[k].above_p = s / ip;
-                    runs[k].above_q = 0.0;
-                }
+                for (int e = 0; e < 8; ++e) s += weight(ep[e], eq[e]);
             }
+            s = wave_sum(s);
+            if (lane == who) {
+                runs[run].above_p = s / ip;
+                runs[run].above_q = 0.0;
+                open &= open - 1;
+            }
+        }
+        double own = lane_weight(), incl = sum_scan(own), all = lane_value(incl, 63);
+        if (rest && !good_sum(all)) {
+            // nothing is left beside what was refused: p itself
+            rest = false;
+            ip = 1.0;
+            iq = 0.0;
             own = lane_weight();
             incl = sum_scan(own);
             all = lane_value(incl, 63);
-            if (!good_sum(all)) {
-                // nothing is left beside what was refused (p and q differ by roundings alone): p itself
-                rest = false;
-                ip = 1.0;
-                iq = 0.0;
-                own = lane_weight();
-                incl = sum_scan(own);
-                all = lane_value(incl, 63);
-            }
         }
         if (!good_sum(all)) {
             next = d.token;  // (the refused token is all that p holds)
