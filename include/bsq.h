@@ -778,8 +778,9 @@ bsq_status bsq_distill_grad(const void *H, int64_t ldh, const void *V, int64_t l
  * draw is from p_i. A target row without a probability (a NaN or +inf in it, or
  * nothing but -inf) accepts nothing and its next token is -1; a draft row like
  * that is not accepted either, and the draw is from p_i: both OR
- * BSQ_DEVERR_NONFINITE into *err. Rows past the one that the next token is
- * drawn from may hold anything.
+ * BSQ_DEVERR_NONFINITE into *err. At temperature 0 +inf is a largest logit like
+ * another; a NaN, or nothing but -inf, leaves the row without a word there too.
+ * Rows past the one that the next token is drawn from may hold anything.
  * ------------------------------------------------------------------------ */
 #define BSQ_MAX_DRAFTS 64
 
