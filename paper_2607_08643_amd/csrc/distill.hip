@@ -365,6 +365,11 @@ hipError_t launch_distill_grad(const DistillCall &call, hipStream_t st)
     XArgs a{};
     const hipError_t e = launch_teacher(c, l, !kept, a, st);
     if (e != hipSuccess) return e;
+    // (with what is kept nothing before the gradient's last launch looks at the ids)
+    if (kept && c.x.err) {
+        a.given = c.ids;
+        a.err = c.x.err;
+    }
     auto make_d = [&](const XArgs &piece) {
         if (!kept) return launch_tokens<EPI_TPROB>(piece, piece.vp, 1, st);
         const int64_t blocks = (piece.vp + 8 * XT * KV - 1) / (8 * XT * KV), rows = (piece.T + 63) / 64 * 64;

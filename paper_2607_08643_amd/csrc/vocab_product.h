@@ -73,6 +73,9 @@ struct XArgs {
     int64_t ldk, tiles;
     int K, narrow;                // narrow: tiles of 128 words (up to 128 tokens)
     float scale;
+    // [T][K]: a teacher's words as they were given, where the gradient has yet to report
+    // those past the vocabulary; else NULL
+    const int32_t *given;
 };
 
 // ---------------------------------------------------------------------------
@@ -800,6 +803,7 @@ __global__ __launch_bounds__(XT) void xent_dh_kernel(const XArgs a)
 {
     const int64_t m = blockIdx.x;
     const int row = a.pos[m], live = a.hdr[0];
+    if (a.given && int(threadIdx.x) < a.K && a.given[m * a.K + threadIdx.x] >= a.N) atomicOr(a.err, BSQ_DEVERR_BAD_SET);
     int splits;
     if constexpr (FEW) {
         splits = xent_tiles<EPI_DH2, 256, 256>(a, live).splits;  // (one tile of tokens, of 128 or 256 rows)
