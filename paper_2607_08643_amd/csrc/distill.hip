@@ -222,8 +222,8 @@ __global__ __launch_bounds__(XT) void distill_kept_kernel(const XArgs a, int blo
     for (int j = 0; j < KV; ++j) {
         const int64_t w = w0 + 8 * XT * j, word = a.v0 + w;
         if (w >= a.vp) break;
-        // (a group of -inf is 0, but for a row that is NaN)
-        const float q = f[j] == -__builtin_inff() && lse == lse ? 0.0f : gg * (__builtin_amdgcn_exp2f((f[j] - lse) * LOG2E) * total);
+        // (a group of -inf is 0, but for a row without a softmax: lse is NaN, or -inf itself)
+        const float q = f[j] == -__builtin_inff() && lse > -__builtin_inff() ? 0.0f : gg * (__builtin_amdgcn_exp2f((f[j] - lse) * LOG2E) * total);
         float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k)
