@@ -50,9 +50,10 @@ constexpr double LOG2E_64 = 1.4426950408889634074;
 constexpr float MAX_TEMPERATURE = 0x1p64f, MIN_TEMPERATURE = 0x1p-64f;
 // Of p, what the first launch's sums leave open. A term's exponent is rounded three times
 // (2^-24 of it each; its mean under the softmax is at most log2 N < 31), the exponential by
-// 2^-22, a thread's 32 terms by 2^-19, what a larger logit rescales by 2^-22 a time: 1e-5 of
-// a sum, 2e-5 of the ratio of two.
-constexpr double UNSURE = 0x1p-15;
+// 2^-22, a thread's 32 terms by 2^-19: 8e-6 of a sum, 1.6e-5 of the ratio of two. And in every
+// turn that a block has of a row a larger logit may rescale what came before, by an exponential
+// that is 2^-22 off.
+constexpr double UNSURE = 0x1p-15, UNSURE_TURN = 0x1p-21;
 // Of p, how near q has to be for the first launch's sums to leave open which is larger: 2^-20.
 // (Few words are: of drafts with noise of 0.6 in their logits one in 10^6.)
 constexpr int CLOSE_BITS = 20;
@@ -93,6 +94,7 @@ struct DArgs {
     int64_t turn, turns;  // words of a block's turn; turns of a row
     int64_t per;          // turns of a block: those of all rows one after another
     int64_t pieces;       // parts of a row that blocks have, at most
+    double unsure;        // of p: what their sums leave open
     int64_t run;          // words of a run
     int runs, parts;      // of a row; blocks that share a row's runs
     const int32_t *tokens, *lens;
@@ -361,7 +363,7 @@ __device__ __forceinline__ Decision decide(const DArgs &a, int64_t b, int n, dou
             const double p = Exp2Below(sh.m[t], c, reach)(zp) / sh.s[t];
             const double q = a.Q ? Exp2Below(sh.m[jq], c, reach)(zq) / sh.s[jq] : 1.0;
             ok = double(u) * q < p;
-            unsure = p > 0.0 && __builtin_fabs(double(u) * q - p) <= UNSURE * p;
+            unsure = p > 0.0 && __builtin_fabs(double(u) * q - p) <= a.unsure * p;
         }
     }
     for (;;) {
@@ -735,6 +737,7 @@ hipError_t launch_draft_verify(const DraftCall &c, hipStream_t st)
     a.turns = l.turns;
     a.per = l.per;
     a.pieces = l.pieces;
+    a.unsure = UNSURE + UNSURE_TURN * double(std::min(l.per, l.turns));
     a.run = l.run;
     a.runs = l.runs;
     a.parts = l.parts;

@@ -62,3 +62,20 @@ def test_many_long_rows_match_the_definition(B, L, N, dt, gpu):
     for given in (draft, None):
         _check(_reference(target, tokens, u, r, given, lens, temp),
                bsq.bsq_draft_verify(target, tokens, u, r, given, lens=lens, temperature=temp))
+
+
+@pytest.mark.parametrize("rise", [1e-6, 1e-3, 20.0])
+def test_rows_that_rise_over_many_turns(rise, gpu):
+    """Rows whose every turn has a larger logit than those before, in blocks of 64 turns: random numbers next to
+    the probability, further and further off."""
+    say(f"draft rows that rise by {rise}")
+    B, L, N = 512, 1, 1 << 20
+    z = (torch.arange(N, dtype=torch.float64) / N * rise).float()
+    target = z.to(gpu).expand(B, L + 1, N)
+    token = torch.randint(0, N, (B, L), generator=torch.Generator().manual_seed(3))
+    p = (z.double() - torch.logsumexp(z.double(), 0)).exp()
+    off = torch.tensor([s * 2.0 ** -k for k in range(10, 23) for s in (1, -1)])
+    u = (p[token[:, 0]] * (1 + off.repeat(B)[:B])).float()
+    count, _ = bsq.bsq_draft_verify(target, token.int().to(gpu), u[:, None].to(gpu), torch.zeros(B, device=gpu))
+    torch.cuda.synchronize()
+    assert torch.equal(count.cpu() > 0, u.double() < p[token[:, 0]])
