@@ -652,8 +652,8 @@ bsq_status bsq_adapters_grad(const bsq_adapter_plan *plan, int32_t n_proj, const
  *   z_tv = h_t . v,  lse_t = log sum_v exp(z_tv),  loss_t = lse_t - z_t,target
  *   d_tv = g_t (exp(z_tv - lse_t) - [v = target_t]),  dH = d V,  dV = d^T H
  * (perplexity of a compressed model; the loss of adapter training). Logits and
- * sums are fp32; d enters the products of bf16 results rounded to bf16 (2^-9 of
- * each value), that of a 32-bit dV as two bf16 parts (2^-18; twice that product's
+ * sums are fp32; d enters the products of bf16 results rounded to bf16 (at most 2^-8
+ * of each value), that of a 32-bit dV as two bf16 parts (2^-17; twice that product's
  * time). A token with a negative target has no loss: its loss, lse and
  * row of dH are 0, and its hidden state is not used (it may be NaN). A target
  * of N or more counts as negative and ORs BSQ_DEVERR_BAD_SET into *err.

@@ -1101,8 +1101,9 @@ def bsq_distill_loss(H: torch.Tensor, V: torch.Tensor, ids: torch.Tensor, top: t
     head V [N, D] (bf16), from a teacher's top logits as bsq_top_logits gives them
     (ids int32 [T, K], top fp32 [T, K]): (loss, lse), fp32 [T]. norm: the teacher's lse at this
     scale, fp32 [T] (None: the teacher's probabilities add up to 1 over its K words);
-    scale: one over the temperature. keep: also leave the student's logits for
-    bsq_distill_grad (16 bits each; in `kept`, uint8, or a new buffer): (loss, lse, kept)."""
+    scale: one over the temperature. keep: also leave the exponentials of the student's
+    logits for bsq_distill_grad (16 bits each; in `kept`, uint8, or a new buffer):
+    (loss, lse, kept)."""
     T, N, D, K, ldh, ldv = _distill_shapes(H, V, ids, top, norm)
     keep = keep or kept is not None
     dev = _device_of((H, V, ids, top, norm, loss, lse, kept, err, ws), "bsq_distill_loss")

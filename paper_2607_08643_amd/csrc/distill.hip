@@ -15,8 +15,8 @@
 // What is kept: the loss can leave the exponentials of its logits, 16 bits each, and what
 // it found of tokens and teacher for the gradient, which then makes d in one pass over
 // memory and has one product less to do: 6 bytes a logit moved against 2 D operations. (d
-// is rounded to bf16 all the same, 2^-9, beside which 2^-11 adds nothing to speak of; for a
-// dV of 32 bits the logits are made again.)
+// is rounded to bf16 all the same, by up to 2^-8, beside which 2^-11 adds nothing to speak
+// of; for a dV of 32 bits the logits are made again.)
 //
 // Bound by the matrix cores from some hundred tokens on: 4096 tokens of 151936 words, 4096
 // inputs: logits with what is kept of them 4.55 ms (1.12 PFLOP/s), d 0.44 (5.6 TB/s), dH 4.0

@@ -558,8 +558,11 @@ TLayout top_layout(int64_t T, int64_t N)
     // A row is cut where it is long and rows are few: into segments of 16384 words or more, up
     // to a block for every compute unit; ten segments at most while they are short (the
     // second launch costs 6 us and what they leave). Whole against cut, us, bf16, K = 64: 8
-    // rows of 151936 words 22.6 against 14.4 (ten), 100 rows 23.0 against 21.4 (two), 200
-    // rows 23.9 against 29.6 (two), 64 rows of 32003 words 11.6 against 14.3.
+    // rows of 151936 words 22.8 against 16.1 (ten), 100 rows 23.2 against 21.4 (two), 200
+    // rows 23.9 against 29.6 (two); 8 rows of 262144 words 30.9 against 17.2 (ten), 100 rows
+    // 31.6 against 26.3; 8 rows of 100352 words 18.8 against 16.2 (seven), 100 rows 18.9 against
+    // 19.8 (two). Up to four units, whole: 64 rows of 64000 words 14.9 against 16.1 (in fp32
+    // 16.8 against 16.3), of 32003 words 13.3 against 16.1.
     constexpr int64_t UNIT = 16384;
     const int64_t units = (N + UNIT - 1) / UNIT;
     int64_t want = std::min({MAX_ITEMS / std::max<int64_t>(T, 1), std::max<int64_t>(10, units / 8), MAX_SEGS, units});

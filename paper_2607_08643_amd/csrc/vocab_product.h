@@ -238,8 +238,8 @@ __device__ __forceinline__ void join_stats(float &m, float &s, float m2, float s
 }
 
 // An exponential from 0 to 1 in 16 bits: six of exponent, ten of fraction (off by at most
-// 2^-11 of it; 0 below 2^-62). Made into a gradient that is rounded to bf16 (2^-9) it adds
-// 1/32 to that rounding's square.
+// 2^-11 of it; 0 up to 2^-63). Made into a gradient that is rounded to bf16 (by up to 2^-8) it
+// adds 1/64 to that rounding's square.
 __device__ __forceinline__ uint32_t kept_code(float e)
 {
     const int c = (int(__float_as_uint(e)) - 0x20000000 + 0x1000) >> 13;
@@ -648,11 +648,11 @@ __device__ __forceinline__ void xent_tile(const XArgs &a, int live)
         }
     } else if constexpr (EPI == EPI_PROB) {
         // d = g (exp(z - lse) - onehot); 0 for padded tokens and words. bf16 results
-        // take it rounded to bf16: at most 2^-9 of each value, which with the rounding
+        // take it rounded to bf16: at most 2^-8 of each value, which with the rounding
         // of the results makes the gradients' relative error 2.2e-3 to 2.5e-3 where that
         // rounding alone makes 1.7e-3, and a second part would double two of the three
         // products. A dV of 32 bits is asked for to be better than that: it takes what
-        // remains as a second part (2^-18 is lost).
+        // remains as a second part (2^-17 is lost at most).
         const int64_t w0 = int64_t(bx) * G::BL + 16 * (wn * NF) + 4 * NF * g;
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
