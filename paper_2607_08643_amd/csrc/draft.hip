@@ -25,11 +25,11 @@
 // words where p is larger, by the first launch's sums, and their rests, and marks the runs
 // that hold a word where p / q lies within 2^-20 of 1. The draw puts them together with the
 // exact sums, which are by now known to say how far off the first ones were (up to 5e-7 in
-// rows of many shapes): where that is less than 2^-20 only the marked runs can hold a word on
+// 2600 rows of many shapes): where that is less than 2^-20 only the marked runs can hold a word on
 // the wrong side, and their weights are formed anew, word by word; else those of all.
 //
 // 64 sequences of four drafts, 151936 words in bf16: rows 39 us (175 MB, 4.5 TB/s), the
-// drawn rows 36 (64-bit exponentials: two a word), draws 8. One sequence: 6, 9 and 6, each
+// drawn rows 35 to 36 (64-bit exponentials: two a word), draws 7 to 8. One sequence: 6, 9 and 6, each
 // a chain of a few dependent loads. Where all runs are weighed anew (drafts in bf16 that
 // are the target's but for some words) the draws take some 350 more: a wave reads both
 // rows.
